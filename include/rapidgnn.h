@@ -425,6 +425,60 @@ rg_status rg_prefetcher_release(rg_prefetcher *p, void *consumer_stream);
 rg_status rg_prefetcher_depth(const rg_prefetcher *p, uint32_t *staged_not_acquired, uint32_t *held);
 void rg_prefetcher_destroy(rg_prefetcher *p);
 
+/* ------------------------------------------------------------------------
+ * Operators of the training step behind the gathered blocks (Sec. 4 par. (8):
+ * the trainer's forward and backward pass and its optimiser).  They take and
+ * leave plain device memory, keep nothing between calls, allocate nothing and
+ * do not wait: every call only enqueues kernels on `stream` and may be
+ * recorded into a graph.  Where a call needs scratch the caller gives it a
+ * workspace of the size that the matching *_workspace call names; its contents
+ * before and after do not matter, and calls that share one must be ordered.
+ * Strides are bytes between the starts of consecutive rows, multiples of the
+ * element size; an output's is at least its row's bytes, so that the padded
+ * rows of rg_gather_batch are taken as they are, and bytes between rows are left
+ * untouched.  Arithmetic and sums are in 32 bits and more whatever the type; a
+ * result is rounded once, to nearest even.  The same call gives the same bits.
+ * RG_EINVAL: a null pointer, an unknown type, a stride or address that does not
+ * suit the type; RG_ERANGE: a size beyond what is said here, or too small a
+ * workspace.  Nothing is written then. */
+#define RG_F32   0u
+#define RG_BF16  1u
+#define RG_F16   2u
+
+/*
+ * rg_layer_norm -- of every row x of n_cols elements
+ *     mean = sum x / n_cols,  rstd = 1 / sqrt(sum (x - mean)^2 / n_cols + eps),
+ *     y = (x - mean) * rstd * weight + bias.
+ *
+ *   type         of x and y
+ *   weight, bias dev, [n_cols] of weight_type (RG_F32, or the same as `type`); NULL: all ones, all zeros
+ *   eps          >= 0
+ *   y            dev; may be x itself, with the same stride
+ *   mean, rstd   dev, float [n_rows], what the backward pass takes; may be NULL
+ * n_rows may be 0; 1 <= n_cols < 2^31, n_rows < 2^40.
+ */
+rg_status rg_layer_norm(const void *x, uint64_t x_stride, uint64_t n_rows, uint64_t n_cols, uint32_t type,
+                        const void *weight, const void *bias, uint32_t weight_type, float eps,
+                        void *y, uint64_t y_stride, float *mean, float *rstd, void *stream);
+
+/*
+ * rg_layer_norm_backward -- from dy, with xhat = (x - mean) * rstd and q = dy * weight:
+ *     dx = rstd * (q - sum q / n_cols - xhat * sum (q * xhat) / n_cols)   (sums over the row),
+ *     dweight = sum over the rows of dy * xhat,  dbias = sum over the rows of dy.
+ *
+ *   mean, rstd   as rg_layer_norm left them
+ *   dx           dev, of `type`, or NULL where x is data and no gradient is wanted; may be dy itself, with the same stride
+ *   dweight, dbias  dev, [n_cols] of weight_type; each may be NULL
+ *   workspace    dev, 16-byte aligned, as many bytes as rg_layer_norm_workspace says; may be NULL where neither
+ *                dweight nor dbias is wanted
+ * With no rows dweight and dbias are zero.
+ */
+rg_status rg_layer_norm_workspace(uint64_t n_rows, uint64_t n_cols, uint32_t type, uint64_t *bytes);
+rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, const void *x, uint64_t x_stride, uint64_t n_rows, uint64_t n_cols,
+                                 uint32_t type, const void *weight, uint32_t weight_type, const float *mean, const float *rstd,
+                                 void *dx, uint64_t dx_stride, void *dweight, void *dbias,
+                                 void *workspace, uint64_t workspace_bytes, void *stream);
+
 /* Timing aid for benchmarks: sums, since the last reset, the device time spent
  * in the named kernel group when profiling is enabled (HIP events around each
  * launch on the launch stream; adds a little latency).  Groups: 0 sampler

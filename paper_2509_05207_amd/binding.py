@@ -26,7 +26,8 @@ EXPORTS = ("rg_last_error", "rg_graph_validate", "rg_build_schedule", "rg_schedu
            "rg_prefetcher_create", "rg_prefetcher_fill", "rg_prefetcher_acquire", "rg_prefetcher_release",
            "rg_prefetcher_depth", "rg_prefetcher_destroy", "rg_schedule_build_blocks", "rg_schedule_block",
            "rg_classify_batch", "rg_build_schedule_with", "rg_gather_batches",
-           "rg_schedule_save", "rg_schedule_load", "rg_gather_batch_noalloc", "rg_schedule_seeds", "rg_schedule_load_range")
+           "rg_schedule_save", "rg_schedule_load", "rg_gather_batch_noalloc", "rg_schedule_seeds", "rg_schedule_load_range",
+           "rg_layer_norm", "rg_layer_norm_workspace", "rg_layer_norm_backward")
 
 
 class RgError(RuntimeError):
@@ -115,6 +116,11 @@ def lib():
         L.rg_prefetcher_release.argtypes = [vp, vp]
         L.rg_prefetcher_depth.argtypes = [vp, P(u32), P(u32)]
         L.rg_prefetcher_destroy.argtypes = [vp]; L.rg_prefetcher_destroy.restype = None
+        L.rg_layer_norm.argtypes = [vp, u64, u64, u64, u32, vp, vp, u32, C.c_float, vp, u64, vp, vp, vp]
+        L.rg_layer_norm_workspace.argtypes = [u64, u64, u32, P(u64)]
+        L.rg_layer_norm_backward.argtypes = [vp, u64, vp, u64, u64, u64, u32, vp, u32, vp, vp, vp, u64, vp, vp, vp, u64, vp]
+        for name in ("rg_layer_norm", "rg_layer_norm_workspace", "rg_layer_norm_backward"):
+            getattr(L, name).restype = C.c_int32
         for name in ("rg_graph_validate", "rg_build_schedule", "rg_schedule_info", "rg_schedule_frontier", "rg_schedule_samples",
                      "rg_build_cache", "rg_cache_view", "rg_gather_batch", "rg_profile_read",
                      "rg_cache_pair_create", "rg_cache_pair_begin_next", "rg_cache_pair_swap",
@@ -488,6 +494,84 @@ def rg_prefetcher_depth(p):
     a, h = C.c_uint32(), C.c_uint32()
     _check(lib().rg_prefetcher_depth(p.h, C.byref(a), C.byref(h)))
     return a.value, h.value
+
+
+# ---------------------------------------------------------------- operators of the training step behind the gathered blocks
+RG_F32, RG_BF16, RG_F16 = 0, 1, 2
+_ELEMENT = {torch.float32: RG_F32, torch.bfloat16: RG_BF16, torch.float16: RG_F16}
+
+
+def _rows(name, t, shape=None, dtype=None):
+    """(pointer, stride in bytes) of a device matrix whose rows are contiguous."""
+    assert t.is_cuda and t.dim() == 2, f"{name}: expected a device matrix"
+    assert shape is None or tuple(t.shape) == tuple(shape), f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}"
+    assert t.dtype in _ELEMENT and (dtype is None or t.dtype == dtype), f"{name}: got {t.dtype}"
+    assert t.shape[1] <= 1 or t.stride(1) == 1, f"{name}: the elements of a row have to be contiguous"
+    return C.c_void_p(t.data_ptr()), t.stride(0) * t.element_size()
+
+
+def _vector(name, t, n, dtype):
+    if t is None:
+        return None
+    assert t.is_cuda and t.shape == (n,) and (n <= 1 or t.stride(0) == 1) and t.dtype == dtype, f"{name}: expected {n} contiguous {dtype} on the device"
+    return C.c_void_p(t.data_ptr())
+
+
+def _used_on(stream, *made):
+    """Tensors made here on the current stream are handed to work on `stream`."""
+    if stream is None:
+        return
+    stream = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+    if stream == torch.cuda.current_stream():
+        return
+    stream.wait_stream(torch.cuda.current_stream())              # what had their memory before may still be queued there
+    for t in made:
+        if t is not None:
+            t.record_stream(stream)
+
+
+def rg_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
+    """(y, mean, rstd) of the rows of `x` (device matrix; rows may be padded).  out: where y goes (x itself: in place)."""
+    n, d = x.shape
+    xp, xs = _rows("x", x)
+    y = torch.empty((n, d), dtype=x.dtype, device=x.device) if out is None else out
+    yp, ys = _rows("out", y, (n, d), x.dtype)
+    wt = (weight if weight is not None else bias if bias is not None else x).dtype
+    stats = torch.empty((2, n), dtype=torch.float32, device=x.device)
+    _used_on(stream, y if out is None else None, stats)
+    _check(lib().rg_layer_norm(xp, xs, n, d, _ELEMENT[x.dtype], _vector("weight", weight, d, wt), _vector("bias", bias, d, wt), _ELEMENT[wt],
+                               eps, yp, ys, stats.data_ptr(), stats.data_ptr() + 4 * n, _stream_ptr(stream)))
+    return y, stats[0], stats[1]
+
+
+def rg_layer_norm_workspace(n_rows, n_cols, dtype):
+    """Bytes of scratch that the backward pass takes."""
+    b = C.c_uint64()
+    _check(lib().rg_layer_norm_workspace(int(n_rows), int(n_cols), _ELEMENT[dtype], C.byref(b)))
+    return b.value
+
+
+def rg_layer_norm_backward(dy, x, weight, mean, rstd, want_dx=True, want_dweight=True, want_dbias=True, out=None, workspace=None, stream=None):
+    """(dx, dweight, dbias); None for what is not wanted.  weight None: all ones (the gradients of weight and bias are then fp32).
+    out: where dx goes (dy itself: in place); workspace: a device tensor of rg_layer_norm_workspace bytes, made here if None."""
+    n, d = x.shape
+    xp, xs = _rows("x", x)
+    gp, gs = _rows("dy", dy, (n, d), x.dtype)
+    wt = weight.dtype if weight is not None else torch.float32
+    dx = (torch.empty((n, d), dtype=x.dtype, device=x.device) if out is None else out) if want_dx else None
+    op, os_ = _rows("out", dx, (n, d), x.dtype) if want_dx else (None, 0)
+    dw = torch.empty(d, dtype=wt, device=x.device) if want_dweight else None
+    db = torch.empty(d, dtype=wt, device=x.device) if want_dbias else None
+    made = workspace is None and (want_dweight or want_dbias)
+    if made:
+        workspace = torch.empty(max(rg_layer_norm_workspace(n, d, x.dtype), 1), dtype=torch.uint8, device=x.device)
+    _used_on(stream, dx if out is None else None, dw, db, workspace if made else None)
+    _check(lib().rg_layer_norm_backward(gp, gs, xp, xs, n, d, _ELEMENT[x.dtype], _vector("weight", weight, d, wt), _ELEMENT[wt],
+                                        _vector("mean", mean, n, torch.float32), _vector("rstd", rstd, n, torch.float32), op, os_,
+                                        dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None,
+                                        _dev_ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                        _stream_ptr(stream)))
+    return dx, dw, db
 
 
 def rg_trim_memory():

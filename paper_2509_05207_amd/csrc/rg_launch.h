@@ -94,4 +94,35 @@ inline bool blocks_by_ranks(uint64_t n_nodes, uint32_t L, uint64_t beta, uint64_
     return edges * n_nodes >= least * (L + 1) * beta;
 }
 
+// ---------------------------------------------------------------- layer norm
+constexpr int NORM_ELEMENTS = 32;        // of a row in a lane's registers, at most
+struct NormShape {
+    int pack;                            // elements of an access: 16 bytes, or single elements where a row has fewer
+    int lanes;                           // of a row: 8 to 64, or a workgroup of 256 or 1,024; 0: the row is longer than that
+    int packs;                           // of a lane
+    uint32_t grid;                       // workgroups; their waves, or they, take rows by turns
+    uint32_t n_partial;                  // partial sums of every column that the backward pass leaves
+    uint32_t column_grid;                // workgroups over the columns of long rows
+};
+inline NormShape norm_shape(int64_t n_rows, int64_t n_cols, int element_bytes, int n_cu, bool backward)
+{
+    NormShape s{};
+    const int v = 16 / element_bytes;
+    s.pack = n_cols < v ? 1 : v;
+    const int64_t need = (n_cols + s.pack - 1) / s.pack;
+    // The backward pass holds five values to an element, which workgroups of 1,024 threads have registers for at half as many.
+    const int64_t wide = 1024 * (int64_t)std::min(4, (backward ? NORM_ELEMENTS / 2 : NORM_ELEMENTS) / s.pack);
+    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : need <= 256 ? 64 : need <= 1024 ? 256 : need <= wide ? 1024 : 0;
+    const int64_t most = (int64_t)n_cu * (s.lanes == 1024 || s.lanes == 0 ? 2 : 8);
+    const int64_t groups = s.lanes == 0 || s.lanes > 64 ? 1 : 256 / s.lanes;
+    s.packs = s.lanes ? (int)((need + s.lanes - 1) / s.lanes) : 0;
+    s.grid = (uint32_t)std::max<int64_t>(1, std::min(most, (n_rows + groups - 1) / groups));
+    s.n_partial = n_rows ? s.grid : 0;
+    if (s.lanes == 0) {
+        s.column_grid = (uint32_t)((n_cols + 256 * v - 1) / (256 * v));
+        s.n_partial = (uint32_t)std::min<int64_t>(n_rows, std::max<int64_t>(1, (int64_t)n_cu * 4 / s.column_grid));
+    }
+    return s;
+}
+
 }  // namespace rg
