@@ -479,6 +479,47 @@ rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, const void 
                                  void *dx, uint64_t dx_stride, void *dweight, void *dbias,
                                  void *workspace, uint64_t workspace_bytes, void *stream);
 
+/*
+ * rg_orthogonalize -- the nearest thing to an orthogonal matrix that a few
+ * products make of a matrix G: with X = G / (|G| + eps) (Frobenius norm; of
+ * the two sides the narrower one first), `steps` times
+ *     A = X X^T,   X <- a X + (b A + c A^2) X,   a, b, c = 3.4445, -4.7750, 2.0315,
+ * which takes every singular value in (0, 1] to about one (Newton-Schulz).
+ * rg_muon_step -- one step of the Muon optimiser on weight matrices W:
+ *     M' = momentum * M + G,   U = G + momentum * M' (nesterov) or M',
+ *     W' = W - lr * (weight_decay * W + sqrt(max(1, rows / cols)) * orthogonalized(U)).
+ *
+ * All matrices of a model go in one call: what is small is bound by launches,
+ * of which there are 2 + 3 * steps for every RG_UPDATES_PER_LAUNCH matrices of a size class.
+ *
+ *   u        host, [n]: the matrices (the arrays on the device)
+ *   type     of grad, weight and out; momenta are fp32
+ *   steps    1 to RG_MAX_STEPS
+ *   workspace  dev, 256-byte aligned, as many bytes as rg_update_workspace says for the same u
+ * The state X is fp32 throughout.  Products take it rounded to 16 bits for the
+ * 16-bit types (the result is off by 3e-3 and less, 2-norm), in two such parts, 22 bits, for
+ * RG_F32 and where the narrower side is 32 or less.  A matrix with an infinity or a NaN comes out
+ * all NaN.  rows and cols up to RG_MAX_SIDE; matrices without elements are passed over.
+ * Outputs may be the inputs that they replace, with the same stride; other
+ * overlaps, also between matrices, are not allowed.
+ */
+#define RG_MAX_SIDE             32768u
+#define RG_MAX_STEPS            32u
+#define RG_UPDATES_PER_LAUNCH   12u
+typedef struct rg_update {
+    const void *grad;          uint64_t grad_stride;           /* G */
+    const void *weight;        uint64_t weight_stride;         /* W  (rg_muon_step) */
+    const float *momentum;     uint64_t momentum_stride;       /* M  (rg_muon_step) */
+    float *momentum_out;       uint64_t momentum_out_stride;   /* M' (rg_muon_step); may be momentum */
+    void *out;                 uint64_t out_stride;            /* W', may be weight; rg_orthogonalize: the result, may be grad */
+    uint32_t rows, cols;
+} rg_update;
+rg_status rg_update_workspace(const rg_update *u, uint32_t n, uint32_t type, uint64_t *bytes);
+rg_status rg_orthogonalize(const rg_update *u, uint32_t n, uint32_t type, uint32_t steps, float eps,
+                           void *workspace, uint64_t workspace_bytes, void *stream);
+rg_status rg_muon_step(const rg_update *u, uint32_t n, uint32_t type, float lr, float weight_decay, float momentum, int nesterov,
+                       uint32_t steps, float eps, void *workspace, uint64_t workspace_bytes, void *stream);
+
 /* Timing aid for benchmarks: sums, since the last reset, the device time spent
  * in the named kernel group when profiling is enabled (HIP events around each
  * launch on the launch stream; adds a little latency).  Groups: 0 sampler

@@ -27,7 +27,8 @@ EXPORTS = ("rg_last_error", "rg_graph_validate", "rg_build_schedule", "rg_schedu
            "rg_prefetcher_depth", "rg_prefetcher_destroy", "rg_schedule_build_blocks", "rg_schedule_block",
            "rg_classify_batch", "rg_build_schedule_with", "rg_gather_batches",
            "rg_schedule_save", "rg_schedule_load", "rg_gather_batch_noalloc", "rg_schedule_seeds", "rg_schedule_load_range",
-           "rg_layer_norm", "rg_layer_norm_workspace", "rg_layer_norm_backward")
+           "rg_layer_norm", "rg_layer_norm_workspace", "rg_layer_norm_backward",
+           "rg_update_workspace", "rg_orthogonalize", "rg_muon_step")
 
 
 class RgError(RuntimeError):
@@ -47,6 +48,12 @@ class rg_features(C.Structure):
 
 class rg_gather_stats(C.Structure):
     _fields_ = [("n_rows", C.c_uint64), ("n_local", C.c_uint64), ("n_hit", C.c_uint64), ("n_miss", C.c_uint64)]
+
+
+class rg_update(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("grad_stride", C.c_uint64), ("weight", C.c_void_p), ("weight_stride", C.c_uint64),
+                ("momentum", C.c_void_p), ("momentum_stride", C.c_uint64), ("momentum_out", C.c_void_p), ("momentum_out_stride", C.c_uint64),
+                ("out", C.c_void_p), ("out_stride", C.c_uint64), ("rows", C.c_uint32), ("cols", C.c_uint32)]
 
 
 ALLOC_FN = C.CFUNCTYPE(C.c_void_p, C.c_uint64, C.c_int, C.c_void_p)
@@ -119,7 +126,10 @@ def lib():
         L.rg_layer_norm.argtypes = [vp, u64, u64, u64, u32, vp, vp, u32, C.c_float, vp, u64, vp, vp, vp]
         L.rg_layer_norm_workspace.argtypes = [u64, u64, u32, P(u64)]
         L.rg_layer_norm_backward.argtypes = [vp, u64, vp, u64, u64, u64, u32, vp, u32, vp, vp, vp, u64, vp, vp, vp, u64, vp]
-        for name in ("rg_layer_norm", "rg_layer_norm_workspace", "rg_layer_norm_backward"):
+        L.rg_update_workspace.argtypes = [P(rg_update), u32, u32, P(u64)]
+        L.rg_orthogonalize.argtypes = [P(rg_update), u32, u32, u32, C.c_float, vp, u64, vp]
+        L.rg_muon_step.argtypes = [P(rg_update), u32, u32, C.c_float, C.c_float, C.c_float, C.c_int, u32, C.c_float, vp, u64, vp]
+        for name in ("rg_layer_norm", "rg_layer_norm_workspace", "rg_layer_norm_backward", "rg_update_workspace", "rg_orthogonalize", "rg_muon_step"):
             getattr(L, name).restype = C.c_int32
         for name in ("rg_graph_validate", "rg_build_schedule", "rg_schedule_info", "rg_schedule_frontier", "rg_schedule_samples",
                      "rg_build_cache", "rg_cache_view", "rg_gather_batch", "rg_profile_read",
@@ -572,6 +582,63 @@ def rg_layer_norm_backward(dy, x, weight, mean, rstd, want_dx=True, want_dweight
                                         _dev_ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
                                         _stream_ptr(stream)))
     return dx, dw, db
+
+
+RG_MAX_SIDE, RG_MAX_STEPS, RG_UPDATES_PER_LAUNCH = 32768, 32, 12
+
+
+def _updates(grads, outs, weights=None, momenta=None, out_momenta=None):
+    """The host array of rg_update over lists of device matrices, and their type."""
+    assert len(grads) == len(outs) and all(x is None or len(x) == len(grads) for x in (weights, momenta, out_momenta)), "lists of one length are expected"
+    u = (rg_update * max(len(grads), 1))()
+    dt = grads[0].dtype if grads else torch.float32
+    for k, (e, g, o) in enumerate(zip(u, grads, outs)):
+        e.rows, e.cols = g.shape
+        e.grad, e.grad_stride = _rows("grad", g, None, dt)
+        e.out, e.out_stride = _rows("out", o, g.shape, dt)
+        if weights is not None:
+            e.weight, e.weight_stride = _rows("weight", weights[k], g.shape, dt)
+            e.momentum, e.momentum_stride = _rows("momentum", momenta[k], g.shape, torch.float32)
+            e.momentum_out, e.momentum_out_stride = _rows("momentum", out_momenta[k], g.shape, torch.float32)
+    return u, _ELEMENT[dt]
+
+
+def _update_scratch(u, n, t, workspace, stream):
+    if workspace is None:
+        b = C.c_uint64()
+        _check(lib().rg_update_workspace(u, n, t, C.byref(b)))
+        workspace = torch.empty(max(b.value, 1), dtype=torch.uint8, device="cuda")
+        _used_on(stream, workspace)
+    return _dev_ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def rg_update_workspace(matrices):
+    """Bytes of scratch for an update of these matrices in one call."""
+    u, t = _updates(matrices, matrices)
+    b = C.c_uint64()
+    _check(lib().rg_update_workspace(u, len(matrices), t, C.byref(b)))
+    return b.value
+
+
+def rg_orthogonalize(grads, steps=5, eps=1e-7, out=None, workspace=None, stream=None):
+    """The orthogonalised form of every device matrix of the list.  out: a list of where they go (the matrices themselves: in place)."""
+    made = out is None
+    out = [torch.empty(g.shape, dtype=g.dtype, device=g.device) for g in grads] if made else out
+    u, t = _updates(grads, out)
+    p, b = _update_scratch(u, len(grads), t, workspace, stream)
+    _used_on(stream, *(out if made else ()))
+    _check(lib().rg_orthogonalize(u, len(grads), t, int(steps), eps, p, b, _stream_ptr(stream)))
+    return out
+
+
+def rg_muon_step(weights, grads, momenta, lr, weight_decay=0.0, momentum=0.95, nesterov=True, steps=5, eps=1e-7, out_weights=None, out_momenta=None,
+                 workspace=None, stream=None):
+    """One optimiser step on lists of device matrices; momenta are fp32.  In place, unless out_weights / out_momenta say where the new ones go."""
+    out_weights = weights if out_weights is None else out_weights
+    out_momenta = momenta if out_momenta is None else out_momenta
+    u, t = _updates(grads, out_weights, weights, momenta, out_momenta)
+    p, b = _update_scratch(u, len(grads), t, workspace, stream)
+    _check(lib().rg_muon_step(u, len(grads), t, lr, weight_decay, momentum, 1 if nesterov else 0, int(steps), eps, p, b, _stream_ptr(stream)))
 
 
 def rg_trim_memory():

@@ -125,4 +125,16 @@ inline NormShape norm_shape(int64_t n_rows, int64_t n_cols, int element_bytes, i
     return s;
 }
 
+// ---------------------------------------------------------------- orthogonalised updates
+constexpr int UPDATE_TILE = 128, UPDATE_TILE_SMALL = 64;          // of the products
+enum UpdateClass { UPDATE_NARROW, UPDATE_SMALL, UPDATE_LARGE };
+inline int tile_of(UpdateClass c) { return c == UPDATE_LARGE ? UPDATE_TILE : UPDATE_TILE_SMALL; }
+// Tiles of 128 where they fill the chip; matrices of fewer of them take tiles of 64.  Narrow ones of 16-bit types have their operands in two parts.
+inline UpdateClass update_class(uint64_t rows, uint64_t cols, bool wide_type)
+{
+    const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);
+    if (!wide_type && n <= 32) return UPDATE_NARROW;
+    return ((n + 127) / 128) * ((m + 127) / 128) >= 128 ? UPDATE_LARGE : UPDATE_SMALL;
+}
+
 }  // namespace rg

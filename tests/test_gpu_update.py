@@ -1,0 +1,274 @@
+"""Orthogonalised updates and the optimiser step through the C ABI, against the definition in 64 bits.
+
+Tolerances, relative in the 2-norm.  The steps amplify what is off in the directions of small singular values by up to
+3.4445^steps; what is rounded is known (rg_update.hip):
+  fp32           operands of 22 bits, products accumulated in fp32 over n terms: u = 2^-22 on every operand, sqrt(n) 2^-24 on sums.  An
+                 error in X of relative size u (of the largest singular value) is amplified 485 times in five steps at worst: 485 * 2^-22
+                 = 1.2e-4 for matrices without rank; 1e-5 for those whose singular values lie within a factor of a hundred (a hundredth
+                 grows 3.4^4 = 140 times to order one, where the sizes meet)
+  16-bit types   the state is fp32, A and P and the copy of X in P X are rounded to 11 bits: every step P X is off by 3 u |P||X| in norm, u = 2^-12 and
+                 random in sign, so that the last steps, where |P| <= 2.9, leave 2.9 * 1.7 * 2^-12 = 1.2e-3 a step, 4e-3 over all; and the result's own
+                 rounding, 2^-9 / sqrt(3) (bf16) or 2^-12 / sqrt(3) (fp16)
+"""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+A, B, CC = 3.4445, -4.7750, 2.0315
+BOUND = {torch.float32: 1e-5, torch.bfloat16: 5e-3, torch.float16: 4e-3}
+
+
+@pytest.fixture(scope="module")
+def rg():
+    from paper_2509_05207_amd import binding
+    binding.lib()
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return binding
+
+
+def definition(g, steps=5, eps=1e-7):
+    x = g.double().cpu()
+    tall = x.shape[0] > x.shape[1]
+    x = x.t() if tall else x
+    x = x / (x.norm() + eps)
+    for _ in range(steps):
+        s = x @ x.t()
+        x = A * x + (B * s + CC * s @ s) @ x
+    return (x.t() if tall else x).cuda()
+
+
+def made(rows, cols, dtype, seed, kind="noise"):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def rand(*size):
+        return torch.randn(size, generator=g, device="cuda", dtype=torch.float64)
+    if kind == "noise":
+        t = rand(rows, cols)
+    elif kind == "sizes":               # rows of different sizes, as weights of different activations have
+        t = rand(rows, cols) * torch.exp(rand(1, cols) * 0.7)
+    elif kind == "low":                 # of rank 3 and little noise
+        t = rand(rows, 3) @ rand(3, cols) + 0.02 * rand(rows, cols)
+    return (0.01 * t).to(dtype)
+
+
+def off(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+SHAPES = [(1, 1), (1, 7), (9, 1), (2, 3), (16, 16), (47, 256), (41, 512), (63, 65), (64, 64), (65, 63), (100, 47), (128, 129), (256, 602), (602, 256), (333, 1000), (1111, 130), (517, 515),
+          (1, 5000), (5000, 2), (60, 9001)]
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("dtype", list(BOUND))
+@pytest.mark.parametrize("kind", ["noise", "sizes"])
+def test_orthogonalize(rg, rows, cols, dtype, kind):
+    g = made(rows, cols, dtype, rows * 7 + cols, kind)
+    out, = rg.rg_orthogonalize([g])
+    assert out.shape == g.shape and out.dtype == dtype
+    assert off(out, definition(g)) <= BOUND[dtype]
+
+
+@pytest.mark.parametrize("rows,cols", [(2048, 1030), (1500, 1500), (1025, 4000), (2047, 2177)])
+@pytest.mark.parametrize("dtype", list(BOUND))
+def test_large(rg, rows, cols, dtype):
+    """Matrices that fill the chip with the larger tiles."""
+    g = made(rows, cols, dtype, rows + cols, "sizes")
+    assert off(rg.rg_orthogonalize([g])[0], definition(g)) <= BOUND[dtype]
+
+
+@pytest.mark.parametrize("dtype", list(BOUND))
+@pytest.mark.parametrize("rows,cols", [(64, 200), (300, 250), (1300, 1400)])
+def test_little_rank(rg, dtype, rows, cols):
+    """Singular values a thousand times apart."""
+    g = made(rows, cols, dtype, 3, "low")
+    assert off(rg.rg_orthogonalize([g])[0], definition(g)) <= (1.2e-4 if dtype == torch.float32 else BOUND[dtype])
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 7, 32])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_steps(rg, steps, dtype):
+    """Singular values of one or less stay below 1.21 however many steps there are; beyond five they move about one another, and what is off with them."""
+    g = made(90, 200, dtype, 4)
+    s = 3.5 if steps > 5 else 1.0
+    assert off(rg.rg_orthogonalize([g], steps=steps)[0], definition(g, steps)) <= BOUND[dtype] * s
+
+
+def test_singular_values_come_to_about_one(rg):
+    out, = rg.rg_orthogonalize([made(200, 300, torch.float32, 5)])
+    s = torch.linalg.svdvals(out.double().cpu())
+    assert float(s.min()) > 0.6 and float(s.max()) < 1.25
+
+
+@pytest.mark.parametrize("dtype", list(BOUND))
+def test_many_matrices_in_one_call(rg, dtype):
+    """More than a launch takes, of both size classes, some without elements: each as it comes out alone, to the bit."""
+    shapes = [(40 + 9 * k, 30 + 17 * k) for k in range(15)] + [(0, 5), (1400, 1500), (7, 0), (1600, 1300), (3, 3)]
+    gs = [made(r, c, dtype, k) for k, (r, c) in enumerate(shapes)]
+    outs = rg.rg_orthogonalize(gs)
+    for g, o in zip(gs, outs):
+        assert o.shape == g.shape
+        if g.numel():
+            assert torch.equal(o, rg.rg_orthogonalize([g])[0])
+    assert rg.rg_orthogonalize([]) == []
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("size", [1e-30, 1e-20, 1e-4, 1e10, 1e25, 3e36])
+def test_sizes(rg, dtype, size):
+    """The norm is summed in 64 bits: neither small nor large gradients leave the range (eps then decides how small is nothing)."""
+    g = (made(70, 90, torch.float64, 6) * size).to(dtype)
+    got, = rg.rg_orthogonalize([g], eps=0.0)
+    assert off(got, definition(g, eps=0.0)) <= BOUND[dtype]
+    got, = rg.rg_orthogonalize([g], eps=1e-7)
+    want = definition(g, eps=1e-7)
+    assert off(got, want) <= BOUND[dtype] + (0 if float(want.norm()) > 1e-20 else 1.0)
+
+
+def test_zeros_and_what_is_no_number(rg):
+    z = torch.zeros((50, 60), device="cuda")
+    assert bool((rg.rg_orthogonalize([z])[0] == 0).all())
+    assert bool(rg.rg_orthogonalize([z], eps=0.0)[0].isnan().all())             # 0 / 0
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        for dtype in BOUND:
+            a, b = made(50, 60, dtype, 7), made(70, 40, dtype, 8)
+            want = rg.rg_orthogonalize([b])[0]
+            a[17, 5] = bad
+            x, y = rg.rg_orthogonalize([a, b])
+            assert bool(x.isnan().all()) and torch.equal(y, want)              # and no other matrix
+
+
+@pytest.mark.parametrize("dtype", list(BOUND))
+def test_sparse_rows_and_columns(rg, dtype):
+    """Matrices of one element, of empty rows and columns: entries of X up to one, where the products' scale has to hold."""
+    g = torch.zeros((80, 100), dtype=dtype, device="cuda")
+    g[3, 4] = 2.5
+    assert off(rg.rg_orthogonalize([g])[0], definition(g)) <= BOUND[dtype]
+    g = made(80, 100, dtype, 9)
+    g[10:40] = 0
+    g[:, 50:60] = 0
+    got = rg.rg_orthogonalize([g])[0]
+    assert off(got, definition(g)) <= BOUND[dtype]
+    assert bool((got[10:40] == 0).all()) and bool((got[:, 50:60] == 0).all())
+
+
+def step_definition(w, g, m, lr, wd, mu, nesterov, steps=5, eps=1e-7):
+    m2 = mu * m.double() + g.double()
+    o = definition(g.double() + mu * m2 if nesterov else m2, steps, eps)
+    return w.double() * (1 - lr * wd) - lr * math.sqrt(max(1.0, w.shape[0] / w.shape[1])) * o, m2
+
+
+@pytest.mark.parametrize("dtype", list(BOUND))
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("rows,cols", [(47, 256), (300, 100), (1400, 1300)])
+def test_muon_step(rg, dtype, nesterov, rows, cols):
+    w, g = made(rows, cols, dtype, 10), made(rows, cols, dtype, 11, "sizes")
+    m = made(rows, cols, torch.float32, 12) * 4
+    want_w, want_m = step_definition(w, g, m, 0.03, 0.1, 0.9, nesterov)
+    w2, m2 = torch.empty_like(w), torch.empty_like(m)
+    before = [t.clone() for t in (w, g, m)]
+    rg.rg_muon_step([w], [g], [m], lr=0.03, weight_decay=0.1, momentum=0.9, nesterov=nesterov, out_weights=[w2], out_momenta=[m2])
+    assert all(torch.equal(a, b) for a, b in zip(before, (w, g, m)))
+    assert off(m2, want_m) <= 2.0 ** -23
+    change = want_w - w.double()
+    rounding = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -9, torch.float16: 2.0 ** -12}[dtype] * float(want_w.norm())
+    assert float((w2.double() - want_w).norm()) <= BOUND[dtype] * float(change.norm()) + rounding
+    rg.rg_muon_step([w], [g], [m], lr=0.03, weight_decay=0.1, momentum=0.9, nesterov=nesterov)          # in place
+    assert torch.equal(w, w2) and torch.equal(m, m2)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_strides(rg, dtype):
+    """Matrices inside larger ones, rows at any phase; what lies between rows stays."""
+    for rows, cols in ((33, 70), (150, 61), (1300, 1301)):
+        g = made(rows, cols, dtype, 13)
+        buf = torch.full((rows, cols + 3), 2.0, dtype=dtype, device="cuda")
+        buf[:, 1:cols + 1] = g
+        whole = torch.full((rows, cols + 5), 3.0, dtype=dtype, device="cuda")
+        rg.rg_orthogonalize([buf[:, 1:cols + 1]], out=[whole[:, 2:cols + 2]])
+        assert torch.equal(whole[:, 2:cols + 2], rg.rg_orthogonalize([g])[0])
+        assert bool((whole[:, :2] == 3).all()) and bool((whole[:, cols + 2:] == 3).all())
+    g = made(1, 80, dtype, 14).expand(50, 80)                                   # one row fifty times
+    assert off(rg.rg_orthogonalize([g])[0], definition(g)) <= (1.2e-4 if dtype == torch.float32 else BOUND[dtype])
+
+
+def test_in_place_on_another_stream_and_again(rg):
+    gs = [made(100, 130, torch.float32, 15), made(1400, 1400, torch.float32, 16)]
+    want = rg.rg_orthogonalize(gs)
+    for a, b in zip(want, rg.rg_orthogonalize(gs)):
+        assert torch.equal(a, b)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = rg.rg_orthogonalize(gs, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    rg.rg_orthogonalize(gs, out=gs)
+    assert all(torch.equal(a, b) for a, b in zip(want, gs))
+
+
+def test_recorded_into_a_graph(rg):
+    w, g, m = [made(60, 90, torch.float32, 17)], [made(60, 90, torch.float32, 18)], [made(60, 90, torch.float32, 19)]
+    w2, m2 = [torch.empty_like(w[0])], [torch.empty_like(m[0])]
+    ws = torch.empty(rg.rg_update_workspace(g), dtype=torch.uint8, device="cuda")
+
+    def step():
+        rg.rg_muon_step(w, g, m, lr=0.1, out_weights=w2, out_momenta=m2, workspace=ws)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        g[0].copy_(made(60, 90, torch.float32, 30 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = w2[0].clone(), m2[0].clone()
+        step()
+        assert torch.equal(got[0], w2[0]) and torch.equal(got[1], m2[0])
+
+
+def test_refusals(rg):
+    L = rg.lib()
+    g = torch.zeros((8, 16), device="cuda")
+    out = torch.full((8, 16), 5.0, device="cuda")
+    ws = torch.empty(rg.rg_update_workspace([g]), dtype=torch.uint8, device="cuda")
+
+    def update(**kw):
+        u = (rg.rg_update * 1)()
+        e = u[0]
+        e.rows, e.cols = 8, 16
+        e.grad = e.weight = e.momentum = g.data_ptr()
+        e.momentum_out = e.out = out.data_ptr()
+        for k in ("grad", "weight", "momentum", "momentum_out", "out"):
+            setattr(e, k + "_stride", 64)
+        for k, v in kw.items():
+            setattr(e, k, v)
+        return u
+
+    def orth(u=None, n=1, t=0, steps=5, eps=1e-7, p=ws.data_ptr(), b=ws.numel(), **kw):
+        return L.rg_orthogonalize(update(**kw) if u is None else u, n, t, steps, eps, p, b, None)
+
+    def muon(lr=0.1, wd=0.0, mu=0.9, steps=5, eps=1e-7, p=ws.data_ptr(), b=ws.numel(), **kw):
+        return L.rg_muon_step(update(**kw), 1, 0, lr, wd, mu, 1, steps, eps, p, b, None)
+    size = C.c_uint64()
+    nan, inf = float("nan"), float("inf")
+    for status, calls in ((rg.RG_EINVAL, [
+            lambda: orth(t=3), lambda: L.rg_orthogonalize(None, 1, 0, 5, 1e-7, ws.data_ptr(), ws.numel(), None), lambda: orth(steps=0), lambda: orth(steps=33), lambda: orth(eps=-1.0),
+            lambda: orth(eps=nan), lambda: orth(eps=inf), lambda: orth(grad=None), lambda: orth(out=None), lambda: orth(grad=g.data_ptr() + 2), lambda: orth(grad_stride=66),
+            lambda: orth(out_stride=60), lambda: orth(p=None), lambda: orth(p=ws.data_ptr() + 16), lambda: muon(weight=None), lambda: muon(momentum=None), lambda: muon(momentum_out=None),
+            lambda: muon(momentum_stride=2), lambda: muon(momentum_out_stride=32), lambda: muon(lr=nan), lambda: muon(wd=inf), lambda: muon(mu=nan),
+            lambda: L.rg_update_workspace(update(), 1, 0, None), lambda: L.rg_update_workspace(update(), 1, 5, C.byref(size))]),
+        (rg.RG_ERANGE, [lambda: orth(b=ws.numel() - 1), lambda: orth(rows=32769), lambda: orth(cols=2 ** 31), lambda: orth(grad_stride=2 ** 41), lambda: muon(rows=40000),
+                        lambda: L.rg_update_workspace(update(cols=40000), 1, 0, C.byref(size))])):
+        for k, call in enumerate(calls):
+            assert call() == status and L.rg_last_error(), (status, k)
+    torch.cuda.synchronize()
+    assert bool((out == 5).all())
+    assert orth(rows=0, grad=None, p=None, b=0) == rg.RG_OK                     # nothing to do
+    for bad in (lambda: rg.rg_orthogonalize([g.t()]), lambda: rg.rg_orthogonalize([g, g.bfloat16()]), lambda: rg.rg_orthogonalize([g], out=[out[:4]]), lambda: rg.rg_orthogonalize([g.double()]),
+                lambda: rg.rg_orthogonalize([g.cpu()]), lambda: rg.rg_muon_step([g], [g], [g.half()], lr=0.1), lambda: rg.rg_muon_step([g], [g], [], lr=0.1)):
+        with pytest.raises((AssertionError, KeyError)):
+            bad()
