@@ -126,15 +126,41 @@ inline NormShape norm_shape(int64_t n_rows, int64_t n_cols, int element_bytes, i
 }
 
 // ---------------------------------------------------------------- orthogonalised updates
-constexpr int UPDATE_TILE = 128, UPDATE_TILE_SMALL = 64;          // of the products
-enum UpdateClass { UPDATE_NARROW, UPDATE_SMALL, UPDATE_LARGE };
-inline int tile_of(UpdateClass c) { return c == UPDATE_LARGE ? UPDATE_TILE : UPDATE_TILE_SMALL; }
-// Tiles of 128 where they fill the chip; matrices of fewer of them take tiles of 64.  Narrow ones of 16-bit types have their operands in two parts.
+constexpr int UPDATE_PAD = 64;            // sides are padded to multiples of this: the least tile, and the step along K
+inline uint64_t half_tiles(uint64_t n, uint64_t tile)
+{
+    const uint64_t t = (n + tile - 1) / tile;
+    return t * (t + 1) / 2;
+}
+inline uint64_t whole_tiles(uint64_t n, uint64_t m, uint64_t tile) { return (n + tile - 1) / tile * ((m + tile - 1) / tile); }
+constexpr int UPDATE_TILE_SHARED = 65;    // names a tile of 64 whose waves are four times as many
+inline int tile_side(int tile) { return tile == UPDATE_TILE_SHARED ? 64 : tile; }
+// What a matrix' products are made of.  It goes by the matrix alone, so that its result does not depend on what else is in the call: sums along K
+// are taken in one order by all tiles but the shared ones.
+//   NARROW   16-bit types, 32 or less of the narrower side: operands in two parts all the same (see rg_update.hip)
+//   SHARED   no more tiles of 64 than the chip has compute units: waves share them
+//   HALF     so it is with the symmetric products alone
+enum UpdateClass { UPDATE_NARROW, UPDATE_SHARED, UPDATE_HALF, UPDATE_FULL };
 inline UpdateClass update_class(uint64_t rows, uint64_t cols, bool wide_type)
 {
     const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);
     if (!wide_type && n <= 32) return UPDATE_NARROW;
-    return ((n + 127) / 128) * ((m + 127) / 128) >= 128 ? UPDATE_LARGE : UPDATE_SMALL;
+    return whole_tiles(n, m, 64) <= 256 ? UPDATE_SHARED : half_tiles(n, 64) <= 256 ? UPDATE_HALF : UPDATE_FULL;
+}
+// Of the other tiles the one whose launch is done first: so many tiles to the fullest compute unit, each at what it takes of one that is full (us a step of 64 along K, measured
+// on products of 1024 to 4096 a side), but no less than a tile that has the unit to itself.
+template <typename F> inline int update_tile(F &&tiles, int n_cu, bool split)
+{
+    struct Cost { int tile; double full, alone; };
+    static constexpr Cost ONE[] = {{64, 0.20, 0.27}, {128, 0.47, 0.53}, {192, 0.95, 0.95}, {256, 1.6, 1.4}};
+    static constexpr Cost TWO[] = {{64, 0.40, 0.45}, {128, 0.95, 1.0}, {192, 1.9, 1.9}, {256, 3.2, 3.2}};
+    int best = 64;
+    double least = 0;
+    for (const Cost &c : split ? TWO : ONE) {
+        const double t = std::max(c.alone, c.full * (double)((tiles(c.tile) + n_cu - 1) / n_cu));
+        if (least == 0 || t < least) { least = t; best = c.tile; }
+    }
+    return best;
 }
 
 }  // namespace rg

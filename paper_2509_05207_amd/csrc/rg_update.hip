@@ -21,7 +21,9 @@
 #include "rg_elements.h"
 #include "rg_launch.h"
 
+#include <atomic>
 #include <cmath>
+#include <type_traits>
 
 namespace rg {
 
@@ -29,11 +31,11 @@ namespace {
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float SCALE = 16384.f, UNSCALE = 1.f / 16384.f;             // of the fp16 operands
-constexpr int SUM_BLOCKS = 256;                                       // partial sums of squares of a matrix, at most
+constexpr int SUM_BLOCKS = 1024;                                      // partial sums of squares of a matrix, at most
 
 typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef f16 f16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // An operand: the fp16 numbers nearest to its values, and (fp32 matrices) those nearest to what they leave.
 struct Operand { f16 *hi, *lo; };
@@ -74,28 +76,52 @@ template <typename T> __device__ __forceinline__ const T *row_at(const void *p, 
 template <typename T> __device__ __forceinline__ T *row_at(void *p, uint64_t stride, int64_t r) { return reinterpret_cast<T *>(static_cast<uint8_t *>(p) + (uint64_t)r * stride); }
 
 // ---------------------------------------------------------------- momentum, sum of squares
+constexpr int PACK = 8;
+
+// Elements [c, c + PACK) of a row of cols, what lies beyond it zero.
+template <typename T> __device__ __forceinline__ void load_part(const T *row, uint32_t c, uint32_t cols, float (&v)[PACK])
+{
+    if (c + PACK <= cols) {
+        load_pack(row + c, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < PACK; ++e) v[e] = c + e < cols ? (float)row[c + e] : 0.f;
+    }
+}
+
+// The update that a step orthogonalises, out of the gradient and (muon) the new momentum.
+__device__ __forceinline__ float update_of(const Group &g, float grad, float next) { return g.nesterov ? grad + g.momentum * next : next; }
+
 template <typename T>
 __global__ void __launch_bounds__(256) update_sums_kernel(Group g)
 {
     const Matrix &m = g.mat[matrix_of<&Matrix::sum_first>(g, blockIdx.x)];
     const uint32_t block = blockIdx.x - m.sum_first;
-    uint32_t tx = 256;
-    while (tx > 1 && tx / 2 >= m.u.cols) tx /= 2;                       // threads along a row
-    const uint32_t ty = 256 / tx;
+    const uint32_t cols = m.u.cols, packs = (cols + PACK - 1) / PACK, all = m.u.rows * packs;
     double s = 0.0;
-    for (uint32_t r = block * ty + threadIdx.x / tx; r < m.u.rows; r += m.sum_blocks * ty) {
-        const T *grad = row_at<T>(m.u.grad, m.u.grad_stride, r);
-        const float *mom = row_at<float>(m.u.momentum, m.u.momentum_stride, r);
-        float *mom_out = row_at<float>(m.u.momentum_out, m.u.momentum_out_stride, r);
-        for (uint32_t c = threadIdx.x % tx; c < m.u.cols; c += tx) {
-            float v = (float)grad[c];
-            if (g.muon) {
-                const float next = g.momentum * mom[c] + v;
-                mom_out[c] = next;
-                v = g.nesterov ? v + g.momentum * next : next;
+    for (uint32_t p = block * 256 + threadIdx.x; p < all; p += m.sum_blocks * 256) {
+        const uint32_t r = p / packs, c = (p - r * packs) * PACK;
+        float v[PACK];
+        load_part(row_at<T>(m.u.grad, m.u.grad_stride, r), c, cols, v);
+        if (g.muon) {
+            float next[PACK];
+            load_part(row_at<float>(m.u.momentum, m.u.momentum_stride, r), c, cols, next);
+            float *out = row_at<float>(m.u.momentum_out, m.u.momentum_out_stride, r) + c;
+#pragma unroll
+            for (int e = 0; e < PACK; ++e) {
+                next[e] = g.momentum * next[e] + v[e];
+                v[e] = update_of(g, v[e], next[e]);
             }
-            s += (double)v * (double)v;
+            if (c + PACK <= cols) {
+                store_pack(out, next);
+            } else {
+#pragma unroll
+                for (int e = 0; e < PACK; ++e)
+                    if (c + e < cols) out[e] = next[e];
+            }
         }
+#pragma unroll
+        for (int e = 0; e < PACK; ++e) s += (double)v[e] * (double)v[e];
     }
     __shared__ double part[4];
     for (int k = 1; k < 64; k <<= 1) s += __shfl_xor(s, k);
@@ -105,11 +131,18 @@ __global__ void __launch_bounds__(256) update_sums_kernel(Group g)
 }
 
 // ---------------------------------------------------------------- X in the layouts of the products
-__device__ __forceinline__ void put(const Operand &o, uint64_t at, float v, bool split)
+// PACK consecutive numbers of an operand.
+template <bool SPLIT> __device__ __forceinline__ void put8(const Operand &o, uint64_t at, const float (&v)[PACK])
 {
-    const f16 h = (f16)v;
-    o.hi[at] = h;
-    if (split) o.lo[at] = (f16)(v - (float)h);
+    f16x8 h;
+#pragma unroll
+    for (int e = 0; e < PACK; ++e) h[e] = (f16)v[e];
+    *reinterpret_cast<f16x8 *>(o.hi + at) = h;
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int e = 0; e < PACK; ++e) h[e] = (f16)(v[e] - (float)h[e]);
+        *reinterpret_cast<f16x8 *>(o.lo + at) = h;
+    }
 }
 
 // A workgroup takes 64 x 64 elements of the padded X.
@@ -120,143 +153,263 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
     const uint32_t tile = blockIdx.x - m.tile_first;
     __shared__ double part[4];
     __shared__ float block[64][65];
-    double s = threadIdx.x < m.sum_blocks ? m.sums[threadIdx.x] : 0.0;
-    for (int k = 1; k < 64; k <<= 1) s += __shfl_xor(s, k);
+    // G is read along its rows: along X's rows, or, where X is G's transpose, along its columns.  What is read does not wait for the norm.
+    const int32_t across = m.m_pad / 64;
+    const int32_t i0 = (int32_t)(tile / across) * 64, j0 = (int32_t)(tile % across) * 64;
+    const int32_t k = (int32_t)threadIdx.x >> 3, c = ((int32_t)threadIdx.x & 7) * PACK;
+    float v[2][PACK];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int32_t row = (m.tall ? j0 : i0) + k + 32 * h, col = (m.tall ? i0 : j0) + c;
+        if (row < (int32_t)m.u.rows) {
+            load_part(row_at<T>(m.u.grad, m.u.grad_stride, row), col, m.u.cols, v[h]);
+            if (g.muon) {
+                float next[PACK];
+                load_part(row_at<float>(m.u.momentum_out, m.u.momentum_out_stride, row), col, m.u.cols, next);
+#pragma unroll
+                for (int e = 0; e < PACK; ++e) v[h][e] = update_of(g, v[h][e], next[e]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < PACK; ++e) v[h][e] = 0.f;
+        }
+    }
+    double s = 0.0;
+    for (uint32_t p = threadIdx.x; p < m.sum_blocks; p += 256) s += m.sums[p];
+    for (int q = 1; q < 64; q <<= 1) s += __shfl_xor(s, q);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
     __syncthreads();
     const double norm = sqrt(part[0] + part[1] + part[2] + part[3]);
-    int e = 0;
-    if (norm > 0.0 && norm < INFINITY) (void)frexp(norm, &e);
+    int e2 = 0;
+    if (norm > 0.0 && norm < INFINITY) (void)frexp(norm, &e2);
     if (tile == 0 && threadIdx.x == 0) {
-        const double f = ldexp(1.0, e) / (norm + (double)g.eps);
+        const double f = ldexp(1.0, e2) / (norm + (double)g.eps);
         *m.factor = norm == 0.0 && g.eps > 0.f ? 0.f : norm < INFINITY ? (float)f : NAN;
     }
-    const int32_t across = m.m_pad / 64;
-    const int32_t i0 = (int32_t)(tile / across) * 64, j0 = (int32_t)(tile % across) * 64;
-    const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // G is read along its rows: along X's rows, or, where X is G's transpose, along its columns
-    for (int32_t k = wave; k < 64; k += 4) {
-        const int32_t r = (m.tall ? j0 : i0) + k, c = (m.tall ? i0 : j0) + lane;
-        float v = 0.f;
-        if (r < (int32_t)m.u.rows && c < (int32_t)m.u.cols) {
-            v = (float)row_at<T>(m.u.grad, m.u.grad_stride, r)[c];
-            if (g.muon) {
-                const float next = row_at<float>(m.u.momentum_out, m.u.momentum_out_stride, r)[c];
-                v = g.nesterov ? v + g.momentum * next : next;
-            }
-            v = ldexpf(v, -e);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < PACK; ++e) {
+            const float x = ldexpf(v[h][e], -e2);
+            if (m.tall) block[c + e][k + 32 * h] = x; else block[k + 32 * h][c + e] = x;
         }
-        if (m.tall) block[lane][k] = v; else block[k][lane] = v;
-    }
     __syncthreads();
-    for (int32_t k = wave; k < 64; k += 4) {
-        const uint64_t row = (uint64_t)(i0 + k) * m.m_pad + j0 + lane, column = (uint64_t)(j0 + k) * m.n_pad + i0 + lane;
-        const float v = block[k][lane];
-        m.x[row] = v;
-        put(m.xr, row, v * SCALE, SPLIT);
-        put(m.xt[0], column, block[lane][k] * SCALE, SPLIT);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int32_t line = k + 32 * h;
+        float x[PACK];
+#pragma unroll
+        for (int e = 0; e < PACK; ++e) x[e] = block[line][c + e];
+        const uint64_t row = (uint64_t)(i0 + line) * m.m_pad + j0 + c;
+        *reinterpret_cast<f32x4 *>(m.x + row) = f32x4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4 *>(m.x + row + 4) = f32x4{x[4], x[5], x[6], x[7]};
+#pragma unroll
+        for (int e = 0; e < PACK; ++e) x[e] *= SCALE;
+        put8<SPLIT>(m.xr, row, x);
+#pragma unroll
+        for (int e = 0; e < PACK; ++e) x[e] = block[c + e][line] * SCALE;
+        put8<SPLIT>(m.xt[0], (uint64_t)(j0 + line) * m.n_pad + i0 + c, x);
     }
 }
 
 // ---------------------------------------------------------------- products
-// C = L R^T of a tile of TILE x TILE by four waves: both operands run along K contiguously, K a multiple of 64.  Steps of DEPTH along K pass through LDS,
-// two of them there: one is multiplied while the other arrives, written into LDS by the loads themselves.  A row of a step is 16-byte chunks,
-// stored in an order that depends on the row, so that the lanes of a read (32 rows, one chunk of each) spread over the banks.
-template <int TILE, bool SPLIT>
+// C = L R^T of a tile of TM x TN by WM x WN waves of BI x BJ blocks of 16 x 16; both operands run along K contiguously, K a multiple of 64.  Steps of
+// DEPTH along K pass through LDS, STAGES of them there: one is multiplied while the others arrive, written into LDS by the loads
+// themselves.  A row of a step is 16-byte chunks, stored in an order that depends on the row, so that the 16 lanes that LDS serves at a time (16 rows, one
+// chunk of each) fall on all banks once.
+//
+// What bounds a step is the sum of what LDS takes in, what the waves read from it and the matrix operations: all waves stand at the same
+// point of a step.  Larger tiles read less for the same products (16 bits, 4096 x 4096, K = 4096, us: tiles of 64 188, 128 128, 192 130, 256 104 to 120; the
+// library's product 112); smaller ones fill the chip with less work, where a third stage hides the way from memory (2048 x 2048, K = 2048, tiles of 128: 27 with two stages, 21).
+//
+// Where there are no more tiles than compute units a wave alone on its vector unit waits for LDS most of a step.  KG > 1: KG waves share a block, each with
+// its own slices of a step; their sums meet in LDS at the end, and each finishes one block of the wave's BI x BJ.
+template <int WM, int WN, int BI, int BJ, int DEPTH_, int STAGES_, bool SPLIT_, int KG = 1>
 struct Product {
-    static constexpr int DEPTH = SPLIT ? 32 : 64;
-    static constexpr int CHUNKS = DEPTH / 8;
-    static constexpr int PARTS = SPLIT ? 2 : 1;
-    static constexpr int PART = TILE * DEPTH;                    // elements of one part of one operand's step
-    static constexpr int STAGE = 2 * PARTS * PART;
-    static constexpr int LDS_BYTES = 2 * STAGE * 2;
-    static constexpr int BLOCKS = TILE / 64;                     // blocks of 32 x 32 of a wave, either way
-    static constexpr int LOADS = TILE * CHUNKS / 256;            // of a thread, to a part
-    static_assert(TILE * CHUNKS % 256 == 0, "");
+    static constexpr bool SPLIT = SPLIT_;
+    static constexpr int DEPTH = DEPTH_, STAGES = STAGES_;
+    static constexpr int THREADS = WM * WN * KG * 64, TM = WM * BI * 16, TN = WN * BJ * 16;
+    static_assert(TM == TN, "the lower half of a symmetric product is made of square tiles");
+    static constexpr int TILE = TM, CHUNKS = DEPTH / 8, PARTS = SPLIT ? 2 : 1;
+    static constexpr int ROWS = (TM + TN) * PARTS;               // of a step: L's hi, L's lo, R's hi, R's lo
+    static constexpr int STAGE = ROWS * DEPTH;                   // elements
+    static constexpr int LDS_BYTES = STAGES * STAGE * 2;
+    static constexpr int SIDE_LOADS = TILE * CHUNKS / THREADS;   // of a thread, to a part of a step
+    static constexpr int LOADS = 2 * PARTS * SIDE_LOADS;
+    static_assert(TILE * CHUNKS % THREADS == 0 && LDS_BYTES <= 160 * 1024, "");
+    static constexpr int SLICES = DEPTH / 32 / KG;               // of a wave; what one matrix operation takes along K each
+    static_assert(DEPTH == SLICES * KG * 32 && (KG == 1 || (KG == BI * BJ && WM * WN * KG * KG * 1024 <= LDS_BYTES)), "");
+    typedef f32x4 Acc[BI][BJ];
 
-    static __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ ((DEPTH == 64 ? row >> 1 : row >> 2) & (CHUNKS - 1)); }
+    static __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ (DEPTH >= 128 ? row & 15 : DEPTH == 64 ? (row >> 1) & 7 : (row >> 2) & 3); }
 
-    static __device__ __forceinline__ void load(const f16 *const (&src)[2 * PARTS], uint64_t ld, int32_t k0, f16 *stage)
-    {
+    // Rows from first on of the operand, of which it has n_rows (a multiple of 16; what a tile has beyond is read from the last row and not used).
+    struct Side { Operand o; int32_t first, n_rows; };
+
+    // Where a thread's loads of a step come from: a base of each part, and 32-bit offsets that the parts of a side share (sides are RG_MAX_SIDE at
+    // most, an operand 2 GiB).
+    struct Source {
+        const uint8_t *base[2 * PARTS];
+        uint32_t offset[2][SIDE_LOADS];
+        uint32_t along[KG > 1 ? SIDE_LOADS : 1], most;             // KG > 1, where a step can leave K: the bytes along K apart, and the last chunk's
+        __device__ __forceinline__ void load(int32_t k0, f16 *stage) const
+        {
 #pragma unroll
-        for (int p = 0; p < 2 * PARTS; ++p)
+            for (int p = 0; p < 2 * PARTS; ++p) {
+                const auto *from = (const __attribute__((address_space(1))) uint8_t *)(base[p] + (KG > 1 ? 0 : 2 * (int64_t)k0));
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int q = i * 256 + (int)threadIdx.x, row = q / CHUNKS, chunk = slot_of(row, q % CHUNKS);
-                const f16 *from = src[p] + (uint64_t)row * ld + k0 + chunk * 8;
-                f16 *to = stage + p * PART + (i * 256 + (int)(threadIdx.x & ~63u)) * 8;
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+                for (int i = 0; i < SIDE_LOADS; ++i) {
+                    f16 *to = stage + p * TILE * DEPTH + (i * THREADS + (int)(threadIdx.x & ~63u)) * 8;
+                    const uint32_t at = KG > 1 ? offset[p / PARTS][i] + min(along[KG > 1 ? i : 0] + 2u * (uint32_t)k0, most) : offset[p / PARTS][i];
+                    __builtin_amdgcn_global_load_lds(from + at, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+                }
             }
+        }
+    };
+
+    // Waits until all but the newest N of this wave's loads have arrived, and then for every wave to be there.  __syncthreads would wait for all of the
+    // loads: this is the barrier alone, and what was read from LDS before has been used before.  The fences keep the compiler to the order and cost no instruction.
+    template <int N> static __device__ __forceinline__ void arrive()
+    {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));             // vmcnt N, lgkmcnt 0
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_sched_barrier(0);
     }
 
-    static __device__ __forceinline__ f16x8 fragment(const f16 *part, int row, int chunk) { return *reinterpret_cast<const f16x8 *>(part + row * DEPTH + slot_of(row, chunk) * 8); }
-
-    // Every load into LDS of this wave has arrived, and then of every wave.  (A barrier by itself waits for LDS operations, not for
-    // loads from global memory; the builtin's bits leave the other counters alone.)
-    static __device__ __forceinline__ void arrive()
+    static __device__ __forceinline__ void run(const Side &L, const Side &R, int32_t K, f16 *lds, Acc &acc)
     {
-        __builtin_amdgcn_s_waitcnt(0x0F70);
-        __syncthreads();
-    }
-
-    // src: the tile's first rows of L (hi, lo) and of R
-    static __device__ __forceinline__ void run(const f16 *const (&src)[2 * PARTS], uint64_t ld, int32_t K, f16 *lds, f32x16 (&acc)[BLOCKS][BLOCKS])
-    {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const int l0 = (wave >> 1) * (TILE / 2) + (lane & 31), r0 = (wave & 1) * (TILE / 2) + (lane & 31), half = lane >> 5;
+        const int lane = threadIdx.x & 63, group = (threadIdx.x >> 6) / (WM * WN), wave = (threadIdx.x >> 6) % (WM * WN);
+        Source src;
+        src.base[0] = reinterpret_cast<const uint8_t *>(L.o.hi);
+        src.base[PARTS] = reinterpret_cast<const uint8_t *>(R.o.hi);
+        if constexpr (SPLIT) {
+            src.base[1] = reinterpret_cast<const uint8_t *>(L.o.lo);
+            src.base[3] = reinterpret_cast<const uint8_t *>(R.o.lo);
+        }
+        src.most = (uint32_t)K * 2u - 16u;
 #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i)
+        for (int i = 0; i < SIDE_LOADS; ++i) {
+            const int q = i * THREADS + (int)threadIdx.x, row = q / CHUNKS;
+            const uint32_t at = (uint32_t)slot_of(row, q % CHUNKS) * 16u;
+            if constexpr (KG > 1) src.along[i] = at;
+            src.offset[0][i] = (uint32_t)min(L.first + row, L.n_rows - 1) * (uint32_t)K * 2u + (KG > 1 ? 0 : at);
+            src.offset[1][i] = (uint32_t)min(R.first + row, R.n_rows - 1) * (uint32_t)K * 2u + (KG > 1 ? 0 : at);
+        }
 #pragma unroll
-            for (int j = 0; j < BLOCKS; ++j)
+        for (int i = 0; i < BI; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-        load(src, ld, 0, lds);
-        arrive();
+            for (int j = 0; j < BJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int row_l = (wave / WN) * BI * 16 + (lane & 15), row_r = TILE * PARTS + (wave % WN) * BJ * 16 + (lane & 15);
+        // Fragments of a step in the order they are read and used: of each slice the hi parts, then the lo parts.
+        constexpr int GROUPS = SLICES * PARTS;
+        f16x8 l[GROUPS][BI], r[GROUPS][BJ];
+        const auto read = [&](const f16 *stage, int g) {
+            const int s = group * SLICES + g / PARTS, p = g % PARTS;
+            const int slot = slot_of(lane & 15, s * 4 + (lane >> 4)) * 8;                  // the rows of a block begin at multiples of 16
+#pragma unroll
+            for (int i = 0; i < BI; ++i) l[g][i] = *reinterpret_cast<const f16x8 *>(stage + (row_l + p * TILE + i * 16) * DEPTH + slot);
+#pragma unroll
+            for (int j = 0; j < BJ; ++j) r[g][j] = *reinterpret_cast<const f16x8 *>(stage + (row_r + p * TILE + j * 16) * DEPTH + slot);
+        };
+        const auto multiply = [&](const f16x8 (&x)[BI], const f16x8 (&y)[BJ]) {
+#pragma unroll
+            for (int i = 0; i < BI; ++i)
+#pragma unroll
+                for (int j = 0; j < BJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], acc[i][j], 0, 0, 0);
+        };
+        // The loads that are not waited for belong to the steps behind the next; behind the last step the last one is loaded again, into a stage of
+        // its own, so that their number stays the same.
+        const int32_t last = (K - 1) / DEPTH * DEPTH;
+#pragma unroll
+        for (int q = 0; q < STAGES - 1; ++q) src.load(min(q * DEPTH, last), lds + q * STAGE);
         int now = 0;
-        for (int32_t k0 = 0; k0 < K; k0 += DEPTH, now ^= 1) {
+        for (int32_t k0 = 0; k0 < K; k0 += DEPTH) {
+            arrive<(STAGES - 2) * LOADS>();
             const f16 *stage = lds + now * STAGE;
-            f16x8 l[PARTS][BLOCKS][DEPTH / 16], r[PARTS][BLOCKS][DEPTH / 16];
+            f16 *freed = lds + (now == 0 ? STAGES - 1 : now - 1) * STAGE;                  // no wave reads it any more since the barrier
+            read(stage, 0);
 #pragma unroll
-            for (int s = 0; s < DEPTH / 16; ++s)
+            for (int g = 0; g < GROUPS; ++g) {
+                // What was read is there, what comes next goes out, and the products run meanwhile.  (The wait is explicit because the compiler, with loads into
+                // LDS under way, would wait for the next reads too.)
+                __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));
+                __builtin_amdgcn_sched_barrier(0);
+                if (g + 1 < GROUPS) read(stage, g + 1);
+                if (g == 0) src.load(min(k0 + (STAGES - 1) * DEPTH, last), freed);
+                __builtin_amdgcn_sched_barrier(0);
+                if (KG > 1 && k0 + (group * SLICES + g / PARTS) * 32 >= K) continue;       // K is a multiple of 64, a slice inside or outside as a whole
+                if (SPLIT && g % 2 == 1) {
+                    multiply(l[g], r[g - 1]);
+                    multiply(l[g - 1], r[g]);
+                } else {
+                    multiply(l[g], r[g]);
+                }
+            }
+            now = now == STAGES - 1 ? 0 : now + 1;
+        }
+        arrive<0>();                                               // a workgroup's LDS is not left with loads under way
+        if constexpr (KG > 1) {
+            f32x4 *sums = reinterpret_cast<f32x4 *>(lds) + lane;   // [group][wave][block][lane]
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p)
+            for (int b = 0; b < KG; ++b) sums[((group * WM * WN + wave) * KG + b) * 64] = acc[b / BJ][b % BJ];
+            __syncthreads();
+            acc[0][0] = sums[(wave * KG + group) * 64];
 #pragma unroll
-                    for (int i = 0; i < BLOCKS; ++i) {
-                        l[p][i][s] = fragment(stage + p * PART, l0 + i * 32, s * 2 + half);
-                        r[p][i][s] = fragment(stage + (PARTS + p) * PART, r0 + i * 32, s * 2 + half);
-                    }
-            // The next step's loads go out behind these reads (of the other stage, which no wave reads any more since the last barrier).
-            if (k0 + DEPTH < K) load(src, ld, k0 + DEPTH, lds + (now ^ 1) * STAGE);
-#pragma unroll
-            for (int s = 0; s < DEPTH / 16; ++s)
-#pragma unroll
-                for (int i = 0; i < BLOCKS; ++i)
-#pragma unroll
-                    for (int j = 0; j < BLOCKS; ++j) {
-                        if constexpr (SPLIT) {
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[1][i][s], r[0][j][s], acc[i][j], 0, 0, 0);
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[0][i][s], r[1][j][s], acc[i][j], 0, 0, 0);
-                        }
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[0][i][s], r[0][j][s], acc[i][j], 0, 0, 0);
-                    }
-            __builtin_amdgcn_sched_barrier(0);                   // the wait stays behind the products
-            arrive();
+            for (int q = 1; q < KG; ++q) acc[0][0] += sums[((q * WM * WN + wave) * KG + group) * 64];
         }
     }
 
-    // body(row, column of the tile, value) for the elements of this lane: four consecutive rows of a column at a time
-    template <typename F> static __device__ __forceinline__ void each(const f32x16 (&acc)[BLOCKS][BLOCKS], F &&body)
+    // body(row, column of the tile, values): four consecutive rows of a column at a time
+    template <typename F> static __device__ __forceinline__ void each(const Acc &acc, F &&body)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, group = (threadIdx.x >> 6) / (WM * WN), wave = (threadIdx.x >> 6) % (WM * WN);
+        if constexpr (KG > 1) {
+            float v[4] = {acc[0][0][0], acc[0][0][1], acc[0][0][2], acc[0][0][3]};
+            body((wave / WN) * BI * 16 + group / BJ * 16 + (lane >> 4) * 4, (wave % WN) * BJ * 16 + group % BJ * 16 + (lane & 15), v);
+            return;
+        }
 #pragma unroll
-        for (int i = 0; i < BLOCKS; ++i)
+        for (int i = 0; i < BI; ++i)
 #pragma unroll
-            for (int j = 0; j < BLOCKS; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    body((wave >> 1) * (TILE / 2) + i * 32 + (e >> 2) * 8 + (lane >> 5) * 4 + (e & 3), (wave & 1) * (TILE / 2) + j * 32 + (lane & 31), acc[i][j][e]);
+            for (int j = 0; j < BJ; ++j) {
+                float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                body((wave / WN) * BI * 16 + i * 16 + (lane >> 4) * 4, (wave % WN) * BJ * 16 + j * 16 + (lane & 15), v);
+            }
     }
 };
+
+// Four lanes that hold four rows of a column each, columns side by side, come to hold four columns of a row each: the lane's own row is
+// its place among the four.  The same call takes them back.
+__device__ __forceinline__ void quad_transpose(float (&v)[4])
+{
+    const bool odd = threadIdx.x & 1, upper = threadIdx.x & 2;
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+        const float got = dpp_move<0xB1>(odd ? v[k] : v[k + 1]);
+        if (odd) v[k] = got; else v[k + 1] = got;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const float got = dpp_move<0x4E>(upper ? v[k] : v[k + 2]);
+        if (upper) v[k] = got; else v[k + 2] = got;
+    }
+}
+
+template <bool SPLIT> __device__ __forceinline__ void put4(const Operand &o, uint64_t at, const float (&v)[4])
+{
+    f16x4 h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = (f16)v[e];
+    *reinterpret_cast<f16x4 *>(o.hi + at) = h;
+    if constexpr (SPLIT) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = (f16)(v[e] - (float)h[e]);
+        *reinterpret_cast<f16x4 *>(o.lo + at) = h;
+    }
+}
 
 // Tile t of the lower half, row by row: (row, column), column <= row.
 __device__ __forceinline__ void half_tile(uint32_t t, int32_t &row, int32_t &column)
@@ -269,109 +422,164 @@ __device__ __forceinline__ void half_tile(uint32_t t, int32_t &row, int32_t &col
 }
 
 // A = X X^T (POLY false), P = b f^2 A + c f^4 A^2 (POLY true): the tiles of the lower half, and their reflections.
-template <int TILE, bool SPLIT, bool POLY>
-__global__ void __launch_bounds__(256) update_half_kernel(Group g, bool first)
+template <typename Prod, bool POLY>
+__global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, bool first)
 {
     extern __shared__ __align__(16) uint8_t lds_bytes[];
-    using Prod = Product<TILE, SPLIT>;
     const Matrix &m = g.mat[matrix_of<&Matrix::half_first>(g, blockIdx.x)];
     int32_t ti, tj;
     half_tile(blockIdx.x - m.half_first, ti, tj);
     const Operand &from = POLY ? m.a : m.xr, &to = POLY ? m.p : m.a;
-    const int32_t K = POLY ? m.n_pad : m.m_pad;
-    const uint64_t ld = (uint64_t)K, left = (uint64_t)ti * TILE * ld, right = (uint64_t)tj * TILE * ld;
-    const f16 *src[2 * Prod::PARTS];
-    src[0] = from.hi + left;
-    src[Prod::PARTS] = from.hi + right;
-    if constexpr (SPLIT) { src[1] = from.lo + left; src[3] = from.lo + right; }
-    f32x16 acc[Prod::BLOCKS][Prod::BLOCKS];
-    Prod::run(src, ld, K, reinterpret_cast<f16 *>(lds_bytes), acc);
+    typename Prod::Acc acc;
+    Prod::run({from, ti * Prod::TILE, m.n_pad}, {from, tj * Prod::TILE, m.n_pad}, POLY ? m.n_pad : m.m_pad, reinterpret_cast<f16 *>(lds_bytes), acc);
     float cb = NS_B, cc = NS_C * UNSCALE;
     if (POLY && first) {
         const float f = *m.factor;
         cb *= f * f;
         cc *= f * f * f * f;
     }
-    Prod::each(acc, [&](int r, int c, float v) {
-        const int64_t i = ti * TILE + r, j = tj * TILE + c;
-        const uint64_t at = (uint64_t)i * m.n_pad + j;
-        if (POLY) {
-            float a = (float)m.a.hi[at];
-            if (SPLIT) a += (float)m.a.lo[at];
-            v = cb * a + cc * v;
+    Prod::each(acc, [&](int r, int c, float (&v)[4]) {
+        const int32_t i = ti * Prod::TILE + r, j = tj * Prod::TILE + c;
+        if (i >= m.n_pad || j - (int32_t)(threadIdx.x & 3) >= m.n_pad) return;              // whole quads of lanes: sides are padded to multiples of 64
+        const uint64_t mirror = (uint64_t)j * m.n_pad + i;
+        if constexpr (POLY) {                                     // A from its reflection, which has the four side by side
+            const f16x4 h = *reinterpret_cast<const f16x4 *>(m.a.hi + mirror);
+            f16x4 l = {};
+            if constexpr (Prod::SPLIT) l = *reinterpret_cast<const f16x4 *>(m.a.lo + mirror);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = cb * ((float)h[e] + (float)l[e]) + cc * v[e];
         } else {
-            v *= UNSCALE;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] *= UNSCALE;
         }
-        put(to, at, v, SPLIT);
-        if (ti != tj) put(to, (uint64_t)j * m.n_pad + i, v, SPLIT);
+        if (ti != tj) put4<Prod::SPLIT>(to, mirror, v);
+        quad_transpose(v);
+        put4<Prod::SPLIT>(to, (uint64_t)(i + (threadIdx.x & 3)) * m.n_pad + (j & ~3), v);
     });
 }
 
 // X <- f (a X + P X); behind the last step the result goes out instead.
-template <typename T, int TILE, bool SPLIT, bool LAST>
-__global__ void __launch_bounds__(256) update_apply_kernel(Group g, uint32_t step)
+template <typename T, typename Prod, bool LAST, bool MUON>
+__global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, uint32_t step)
 {
     extern __shared__ __align__(16) uint8_t lds_bytes[];
-    using Prod = Product<TILE, SPLIT>;
     const Matrix &m = g.mat[matrix_of<&Matrix::whole_first>(g, blockIdx.x)];
-    const uint32_t t = blockIdx.x - m.whole_first, across = (uint32_t)m.m_pad / TILE;
+    const uint32_t t = blockIdx.x - m.whole_first, across = ((uint32_t)m.m_pad + Prod::TILE - 1) / Prod::TILE;
     const int32_t ti = (int32_t)(t / across), tj = (int32_t)(t % across);
-    const Operand &columns = m.xt[step & 1], &next = m.xt[(step & 1) ^ 1];
-    const uint64_t ld = (uint64_t)m.n_pad, left = (uint64_t)ti * TILE * ld, right = (uint64_t)tj * TILE * ld;
-    const f16 *src[2 * Prod::PARTS];
-    src[0] = m.p.hi + left;
-    src[Prod::PARTS] = columns.hi + right;
-    if constexpr (SPLIT) { src[1] = m.p.lo + left; src[3] = columns.lo + right; }
-    f32x16 acc[Prod::BLOCKS][Prod::BLOCKS];
-    Prod::run(src, ld, m.n_pad, reinterpret_cast<f16 *>(lds_bytes), acc);
+    typename Prod::Acc acc;
+    Prod::run({m.p, ti * Prod::TILE, m.n_pad}, {m.xt[step & 1], tj * Prod::TILE, m.m_pad}, m.n_pad, reinterpret_cast<f16 *>(lds_bytes), acc);
+    const Operand &next = m.xt[(step & 1) ^ 1];
     const float f = step == 0 ? *m.factor : 1.f;
-    const float grow = g.muon ? g.lr * sqrtf(fmaxf(1.f, (float)m.u.rows / (float)m.u.cols)) : 0.f;
-    Prod::each(acc, [&](int r, int c, float v) {
-        const int32_t i = ti * TILE + r, j = tj * TILE + c;
-        const uint64_t at = (uint64_t)i * m.m_pad + j;
-        v = f * (NS_A * m.x[at] + v * (UNSCALE * UNSCALE));
+    const float grow = MUON ? g.lr * sqrtf(fmaxf(1.f, (float)m.u.rows / (float)m.u.cols)) : 0.f;
+    Prod::each(acc, [&](int r, int c, float (&v)[4]) {
+        const int32_t i0 = ti * Prod::TILE + r, j = tj * Prod::TILE + c;
+        if (i0 >= m.n_pad || j - (int32_t)(threadIdx.x & 3) >= m.m_pad) return;
+        quad_transpose(v);
+        const int32_t i = i0 + (int32_t)(threadIdx.x & 3), j0 = j & ~3;                     // this lane's row, and its first column
+        const uint64_t at = (uint64_t)i * m.m_pad + j0;
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(m.x + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = f * (NS_A * x[e] + v[e] * (UNSCALE * UNSCALE));
         if constexpr (LAST) {
-            if (i >= m.n || j >= m.m) return;
-            const int32_t row = m.tall ? j : i, col = m.tall ? i : j;
-            if (g.muon) v = g.keep * (float)row_at<T>(m.u.weight, m.u.weight_stride, row)[col] - grow * v;
-            row_at<T>(m.u.out, m.u.out_stride, row)[col] = (T)v;
+            // along the output's rows: X's rows, or its columns where X is the transpose
+            if (m.tall) quad_transpose(v);
+            const int32_t row = m.tall ? j : i, col = m.tall ? i0 : j0;
+            const int32_t n = min(4, (int32_t)m.u.cols - col);
+            if (row >= (int32_t)m.u.rows || n <= 0) return;
+            T *out = row_at<T>(m.u.out, m.u.out_stride, row) + col;
+            const T *weight = row_at<T>(m.u.weight, m.u.weight_stride, row) + col;
+            if (n == 4) {
+                if (MUON) {
+                    float w[4];
+                    load_pack(weight, w);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = g.keep * w[e] - grow * v[e];
+                }
+                store_pack(out, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < n) out[e] = (T)(MUON ? g.keep * (float)weight[e] - grow * v[e] : v[e]);
+            }
         } else {
-            m.x[at] = v;
-            put(m.xr, at, v * SCALE, SPLIT);
-            put(next, (uint64_t)j * m.n_pad + i, v * SCALE, SPLIT);
+            *reinterpret_cast<f32x4 *>(m.x + at) = f32x4{v[0], v[1], v[2], v[3]};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] *= SCALE;
+            put4<Prod::SPLIT>(m.xr, at, v);
+            quad_transpose(v);
+            put4<Prod::SPLIT>(next, (uint64_t)j * m.n_pad + i0, v);
         }
     });
 }
 
 // ---------------------------------------------------------------- launches
 // LDS beyond 64 KB has to be asked for, once per kernel and device.
-template <typename K> rg_status allow_lds(K kernel, int bytes)
+template <typename K> rg_status allow_lds(K kernel, int bytes, std::atomic<uint64_t> &known)
 {
     if (bytes <= 64 * 1024) return RG_OK;
+    int dev = 0;
+    RG_HIP(hipGetDevice(&dev));
+    const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (known.load(std::memory_order_relaxed) & bit) return RG_OK;
     RG_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    known.fetch_or(bit, std::memory_order_relaxed);
     return RG_OK;
 }
 
-template <typename T, int TILE, bool SPLIT>
-rg_status launch_group(const Group &g, uint32_t steps, uint32_t sum_grid, uint32_t tiles, uint32_t half, uint32_t whole, hipStream_t st)
+template <typename Prod, bool POLY> rg_status launch_half(const Group &g, uint32_t grid, uint32_t step, hipStream_t st)
 {
-    constexpr int LDS = Product<TILE, SPLIT>::LDS_BYTES;
-    hipLaunchKernelGGL(update_sums_kernel<T>, dim3(sum_grid), dim3(256), 0, st, g);
+    static std::atomic<uint64_t> known{0};
+    RG_TRY(allow_lds(update_half_kernel<Prod, POLY>, Prod::LDS_BYTES, known));
+    hipLaunchKernelGGL((update_half_kernel<Prod, POLY>), dim3(grid), dim3(Prod::THREADS), Prod::LDS_BYTES, st, g, step == 0);
     RG_HIP(hipGetLastError());
-    hipLaunchKernelGGL((update_start_kernel<T, SPLIT>), dim3(tiles), dim3(256), 0, st, g);
+    return RG_OK;
+}
+
+template <typename T, typename Prod, bool LAST, bool MUON> rg_status launch_apply(const Group &g, uint32_t grid, uint32_t step, hipStream_t st)
+{
+    static std::atomic<uint64_t> known{0};
+    RG_TRY(allow_lds(update_apply_kernel<T, Prod, LAST, MUON>, Prod::LDS_BYTES, known));
+    hipLaunchKernelGGL((update_apply_kernel<T, Prod, LAST, MUON>), dim3(grid), dim3(Prod::THREADS), Prod::LDS_BYTES, st, g, step);
     RG_HIP(hipGetLastError());
-    RG_TRY(allow_lds(update_half_kernel<TILE, SPLIT, false>, LDS));
-    RG_TRY(allow_lds(update_half_kernel<TILE, SPLIT, true>, LDS));
-    RG_TRY(allow_lds(update_apply_kernel<T, TILE, SPLIT, false>, LDS));
-    RG_TRY(allow_lds(update_apply_kernel<T, TILE, SPLIT, true>, LDS));
-    for (uint32_t s = 0; s < steps; ++s) {
-        hipLaunchKernelGGL((update_half_kernel<TILE, SPLIT, false>), dim3(half), dim3(256), LDS, st, g, s == 0);
-        RG_HIP(hipGetLastError());
-        hipLaunchKernelGGL((update_half_kernel<TILE, SPLIT, true>), dim3(half), dim3(256), LDS, st, g, s == 0);
-        RG_HIP(hipGetLastError());
-        if (s + 1 < steps) hipLaunchKernelGGL((update_apply_kernel<T, TILE, SPLIT, false>), dim3(whole), dim3(256), LDS, st, g, s);
-        else hipLaunchKernelGGL((update_apply_kernel<T, TILE, SPLIT, true>), dim3(whole), dim3(256), LDS, st, g, s);
-        RG_HIP(hipGetLastError());
+    return RG_OK;
+}
+
+// The tiles.
+template <bool SPLIT> using Tile64Shared = Product<2, 2, 2, 2, 128, SPLIT ? 2 : 3, SPLIT, 4>;
+template <bool SPLIT> using Tile64 = Product<2, 2, 2, 2, 64, 3, SPLIT>;
+template <bool SPLIT> using Tile128 = Product<2, 4, 4, 2, SPLIT ? 32 : 64, 3, SPLIT>;
+template <bool SPLIT> using Tile192 = std::conditional_t<SPLIT, Product<3, 4, 4, 3, 32, 3, true>, Product<2, 4, 6, 3, 64, 3, false>>;
+template <bool SPLIT> using Tile256 = Product<2, 4, 8, 4, 32, SPLIT ? 2 : 4, SPLIT>;
+
+template <bool SPLIT, typename F> rg_status with_tile(int tile, F &&body)
+{
+    switch (tile) {
+    case UPDATE_TILE_SHARED: return body(Tile64Shared<SPLIT>{});
+    case 64: return body(Tile64<SPLIT>{});
+    case 128: return body(Tile128<SPLIT>{});
+    case 192: return body(Tile192<SPLIT>{});
+    default: return body(Tile256<SPLIT>{});
+    }
+}
+
+struct Shape { uint32_t sums, starts, half, whole; int half_tile, whole_tile; };
+
+template <typename T, bool SPLIT>
+rg_status launch_group(const Group &g, uint32_t steps, const Shape &s, hipStream_t st)
+{
+    hipLaunchKernelGGL(update_sums_kernel<T>, dim3(s.sums), dim3(256), 0, st, g);
+    RG_HIP(hipGetLastError());
+    hipLaunchKernelGGL((update_start_kernel<T, SPLIT>), dim3(s.starts), dim3(256), 0, st, g);
+    RG_HIP(hipGetLastError());
+    for (uint32_t k = 0; k < steps; ++k) {
+        RG_TRY(with_tile<SPLIT>(s.half_tile, [&](auto p) {
+            RG_TRY((launch_half<decltype(p), false>(g, s.half, k, st)));
+            return launch_half<decltype(p), true>(g, s.half, k, st);
+        }));
+        RG_TRY(with_tile<SPLIT>(s.whole_tile, [&](auto p) {
+            if (k + 1 < steps) return launch_apply<float, decltype(p), false, false>(g, s.whole, k, st);        // T plays no part in it
+            return g.muon ? launch_apply<T, decltype(p), true, true>(g, s.whole, k, st) : launch_apply<T, decltype(p), true, false>(g, s.whole, k, st);
+        }));
     }
     return RG_OK;
 }
@@ -393,14 +601,14 @@ struct Carver {
     }
 };
 
-void lay_out(Matrix &m, const rg_update &u, int tile, bool split, Carver &c)
+void lay_out(Matrix &m, const rg_update &u, bool split, Carver &c)
 {
     m.u = u;
     m.tall = u.rows > u.cols;
     m.n = (int32_t)(m.tall ? u.cols : u.rows);
     m.m = (int32_t)(m.tall ? u.rows : u.cols);
-    m.n_pad = (m.n + tile - 1) / tile * tile;
-    m.m_pad = (m.m + tile - 1) / tile * tile;
+    m.n_pad = (m.n + UPDATE_PAD - 1) / UPDATE_PAD * UPDATE_PAD;
+    m.m_pad = (m.m + UPDATE_PAD - 1) / UPDATE_PAD * UPDATE_PAD;
     const uint64_t nm = (uint64_t)m.n_pad * m.m_pad, nn = (uint64_t)m.n_pad * m.n_pad;
     c.take(m.sums, SUM_BLOCKS);
     c.take(m.factor, 1);
@@ -417,15 +625,15 @@ struct Options { bool muon, nesterov; float momentum, lr, weight_decay, eps; uin
 
 template <typename F> rg_status each_group(const rg_update *u, uint32_t n, uint32_t type, F &&body)
 {
-    for (const UpdateClass c : {UPDATE_NARROW, UPDATE_SMALL, UPDATE_LARGE}) {
+    for (const UpdateClass kind : {UPDATE_NARROW, UPDATE_SHARED, UPDATE_HALF, UPDATE_FULL}) {
         const rg_update *picked[RG_UPDATES_PER_LAUNCH];
         uint32_t count = 0;
         for (uint32_t k = 0; k < n; ++k) {
-            if (u[k].rows == 0 || u[k].cols == 0 || update_class(u[k].rows, u[k].cols, type == RG_F32) != c) continue;
+            if (u[k].rows == 0 || u[k].cols == 0 || update_class(u[k].rows, u[k].cols, type == RG_F32) != kind) continue;
             picked[count++] = &u[k];
-            if (count == RG_UPDATES_PER_LAUNCH) { RG_TRY(body(c, picked, count)); count = 0; }
+            if (count == RG_UPDATES_PER_LAUNCH) { RG_TRY(body(kind, picked, count)); count = 0; }
         }
-        if (count) RG_TRY(body(c, picked, count));
+        if (count) RG_TRY(body(kind, picked, count));
     }
     return RG_OK;
 }
@@ -433,29 +641,35 @@ template <typename F> rg_status each_group(const rg_update *u, uint32_t n, uint3
 template <typename T>
 rg_status run_group(UpdateClass kind, const rg_update *const *u, uint32_t count, const Options &o, uint8_t *workspace, hipStream_t st)
 {
+    constexpr bool WIDE = sizeof(T) == 4;
+    const bool split = WIDE || kind == UPDATE_NARROW;
+    int n_cu = 0;
+    RG_TRY(compute_units(&n_cu));
     Group g{};
     g.count = count;
     g.muon = o.muon; g.nesterov = o.nesterov;
     g.momentum = o.momentum; g.lr = o.lr; g.keep = (float)(1.0 - (double)o.lr * (double)o.weight_decay);
     g.eps = o.eps;
     Carver c{workspace};
-    constexpr bool WIDE = sizeof(T) == 4;
-    const int tile = tile_of(kind);
-    uint32_t sums = 0, tiles = 0, half = 0, whole = 0;
+    for (uint32_t k = 0; k < count; ++k) lay_out(g.mat[k], *u[k], split, c);
+    const auto tiles = [&](int tile, bool half) {
+        uint64_t all = 0;
+        for (uint32_t k = 0; k < count; ++k) all += half ? half_tiles(g.mat[k].n_pad, tile) : whole_tiles(g.mat[k].n_pad, g.mat[k].m_pad, tile);
+        return all;
+    };
+    Shape s{};
+    s.half_tile = kind != UPDATE_FULL ? UPDATE_TILE_SHARED : update_tile([&](int tile) { return tiles(tile, true); }, n_cu, split);
+    s.whole_tile = kind < UPDATE_HALF ? UPDATE_TILE_SHARED : update_tile([&](int tile) { return tiles(tile, false); }, n_cu, split);
     for (uint32_t k = 0; k < count; ++k) {
         Matrix &m = g.mat[k];
-        lay_out(m, *u[k], tile, WIDE || kind == UPDATE_NARROW, c);
         m.sum_blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(SUM_BLOCKS, (uint64_t)m.n * m.m / 4096));
-        m.sum_first = sums; m.tile_first = tiles; m.half_first = half; m.whole_first = whole;
-        const uint32_t tn = (uint32_t)(m.n_pad / tile), tm = (uint32_t)(m.m_pad / tile);
-        sums += m.sum_blocks;
-        tiles += (uint32_t)(m.n_pad / 64) * (uint32_t)(m.m_pad / 64);
-        half += tn * (tn + 1) / 2;
-        whole += tn * tm;
+        m.sum_first = s.sums; m.tile_first = s.starts; m.half_first = s.half; m.whole_first = s.whole;
+        s.sums += m.sum_blocks;
+        s.starts += (uint32_t)whole_tiles(m.n_pad, m.m_pad, 64);
+        s.half += (uint32_t)half_tiles(m.n_pad, tile_side(s.half_tile));
+        s.whole += (uint32_t)whole_tiles(m.n_pad, m.m_pad, tile_side(s.whole_tile));
     }
-    if (kind == UPDATE_LARGE) return launch_group<T, UPDATE_TILE, WIDE>(g, o.steps, sums, tiles, half, whole, st);
-    if (kind == UPDATE_SMALL) return launch_group<T, UPDATE_TILE_SMALL, WIDE>(g, o.steps, sums, tiles, half, whole, st);
-    return launch_group<T, UPDATE_TILE_SMALL, true>(g, o.steps, sums, tiles, half, whole, st);
+    return split ? launch_group<T, true>(g, o.steps, s, st) : launch_group<T, WIDE>(g, o.steps, s, st);
 }
 
 rg_status check_updates(const rg_update *u, uint32_t n, uint32_t type)
@@ -483,7 +697,7 @@ uint64_t workspace_of(const rg_update *u, uint32_t n, uint32_t type)
         Carver c{nullptr};
         for (uint32_t k = 0; k < count; ++k) {
             Matrix m;
-            lay_out(m, *picked[k], tile_of(kind), type == RG_F32 || kind == UPDATE_NARROW, c);
+            lay_out(m, *picked[k], type == RG_F32 || kind == UPDATE_NARROW, c);
         }
         most = std::max(most, c.used);
         return RG_OK;
