@@ -503,7 +503,7 @@ rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, const void 
  * Outputs may be the inputs that they replace, with the same stride; other
  * overlaps, also between matrices, are not allowed.
  */
-#define RG_MAX_SIDE             32768u
+#define RG_MAX_SIDE             16384u
 #define RG_MAX_STEPS            32u
 #define RG_UPDATES_PER_LAUNCH   12u
 typedef struct rg_update {

@@ -584,7 +584,7 @@ def rg_layer_norm_backward(dy, x, weight, mean, rstd, want_dx=True, want_dweight
     return dx, dw, db
 
 
-RG_MAX_SIDE, RG_MAX_STEPS, RG_UPDATES_PER_LAUNCH = 32768, 32, 12
+RG_MAX_SIDE, RG_MAX_STEPS, RG_UPDATES_PER_LAUNCH = 16384, 32, 12
 
 
 def _updates(grads, outs, weights=None, momenta=None, out_momenta=None):

@@ -133,8 +133,9 @@ inline uint64_t half_tiles(uint64_t n, uint64_t tile)
     return t * (t + 1) / 2;
 }
 inline uint64_t whole_tiles(uint64_t n, uint64_t m, uint64_t tile) { return (n + tile - 1) / tile * ((m + tile - 1) / tile); }
-constexpr int UPDATE_TILE_SHARED = 65;    // names a tile of 64 whose waves are four times as many
-inline int tile_side(int tile) { return tile == UPDATE_TILE_SHARED ? 64 : tile; }
+// Names of tiles: 64, 128, 192; and a tile of 64 whose waves are four times as many, a tile of 128 with less LDS, two of which share a compute unit.
+constexpr int UPDATE_TILE_SHARED = 65, UPDATE_TILE_PAIR = 129;
+inline int tile_side(int tile) { return tile / 64 * 64; }
 // What a matrix' products are made of.  It goes by the matrix alone, so that its result does not depend on what else is in the call: sums along K
 // are taken in one order by all tiles but the shared ones.
 //   NARROW   16-bit types, 32 or less of the narrower side: operands in two parts all the same (see rg_update.hip)
@@ -145,15 +146,15 @@ inline UpdateClass update_class(uint64_t rows, uint64_t cols, bool wide_type)
 {
     const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);
     if (!wide_type && n <= 32) return UPDATE_NARROW;
-    return whole_tiles(n, m, 64) <= 256 ? UPDATE_SHARED : half_tiles(n, 64) <= 256 ? UPDATE_HALF : UPDATE_FULL;
+    return whole_tiles(n, m, 64) <= 256 ? UPDATE_SHARED : half_tiles(n, 64) <= 64 ? UPDATE_HALF : UPDATE_FULL;
 }
 // Of the other tiles the one whose launch is done first: so many tiles to the fullest compute unit, each at what it takes of one that is full (us a step of 64 along K, measured
 // on products of 1024 to 4096 a side), but no less than a tile that has the unit to itself.
 template <typename F> inline int update_tile(F &&tiles, int n_cu, bool split)
 {
     struct Cost { int tile; double full, alone; };
-    static constexpr Cost ONE[] = {{64, 0.20, 0.27}, {128, 0.47, 0.53}, {192, 0.95, 0.95}, {256, 1.6, 1.4}};
-    static constexpr Cost TWO[] = {{64, 0.40, 0.45}, {128, 0.95, 1.0}, {192, 1.9, 1.9}, {256, 3.2, 3.2}};
+    static constexpr Cost ONE[] = {{64, 0.20, 0.27}, {128, 0.55, 0.53}, {UPDATE_TILE_PAIR, 0.49, 0.85}, {192, 0.95, 0.95}};
+    static constexpr Cost TWO[] = {{64, 0.40, 0.45}, {128, 0.95, 0.9}, {UPDATE_TILE_PAIR, 0.85, 1.5}, {192, 1.9, 1.9}};
     int best = 64;
     double least = 0;
     for (const Cost &c : split ? TWO : ONE) {

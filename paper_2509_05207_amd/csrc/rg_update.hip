@@ -37,38 +37,48 @@ typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// An operand: the fp16 numbers nearest to its values, and (fp32 matrices) those nearest to what they leave.
-struct Operand { f16 *hi, *lo; };
+// An operand's rows: the fp16 numbers nearest to its values; in two parts, every 32 of them are followed by the 32 nearest to what they leave, so
+// that both parts of a piece lie in one line of 128 bytes.
+template <bool SPLIT> __host__ __device__ __forceinline__ uint32_t row_length(int32_t n) { return SPLIT ? 2u * (uint32_t)n : (uint32_t)n; }
+template <bool SPLIT> __device__ __forceinline__ uint64_t place(int32_t row, int32_t column, int32_t n_columns)
+{
+    return (uint64_t)row * row_length<SPLIT>(n_columns) + (SPLIT ? (uint32_t)column + ((uint32_t)column & ~31u) : (uint32_t)column);
+}
+constexpr int LO = 32;                   // from a number to what it leaves
 
 struct Matrix {
     rg_update u;
     int32_t n, m, n_pad, m_pad;          // narrower and wider side, and padded
     bool tall;                           // rows > cols: X is the transpose
-    uint32_t sum_blocks, sum_first;      // workgroups of the first pass
-    uint32_t tile_first;                 // of the second
-    uint32_t half_first, whole_first;    // tiles in front of this matrix' in products whose result is symmetric, and in others
+    uint32_t sum_blocks;                 // workgroups of the first pass
     double *sums;                        // [sum_blocks]
     float *factor;                       // f
     float *x;                            // [n_pad][m_pad]
-    Operand xr, xt[2];                   // X's rows [n_pad][m_pad], its columns [m_pad][n_pad] before and after a step
-    Operand a, p;                        // [n_pad][n_pad]
+    f16 *xr, *xt[2];                     // operands: X's rows [n_pad][m_pad], its columns [m_pad][n_pad] before and after a step
+    f16 *a, *p;                          // [n_pad][n_pad]
 };
 
+// Workgroups of a launch in front of each matrix'; beyond the last matrix none comes.
+struct Starts { uint32_t first[RG_UPDATES_PER_LAUNCH]; };
+
 struct Group {
-    Matrix mat[RG_UPDATES_PER_LAUNCH];
-    uint32_t count;
+    Starts sums, starts, half, whole;    // of the launches: sums of squares; X laid out; symmetric products; others
     bool muon, nesterov;
     float momentum, lr, keep;            // keep = 1 - lr * weight_decay
     float eps;
+    Matrix mat[RG_UPDATES_PER_LAUNCH];
 };
 
 static_assert(sizeof(Group) <= 4000, "kernel arguments are 4 KB at most");
 
-// The matrix that workgroup (or tile) t belongs to, counted by FIRST.
-template <uint32_t Matrix::*FIRST> __device__ __forceinline__ uint32_t matrix_of(const Group &g, uint32_t t)
+// The matrix that workgroup t belongs to, and the workgroup's number within it.
+__device__ __forceinline__ uint32_t matrix_of(const Starts &s, uint32_t t, uint32_t &within)
 {
-    uint32_t k = 0;
-    while (k + 1 < g.count && t >= g.mat[k + 1].*FIRST) ++k;
+    uint32_t k = 0, first = 0;
+#pragma unroll
+    for (uint32_t j = 1; j < RG_UPDATES_PER_LAUNCH; ++j)
+        if (t >= s.first[j]) { k = j; first = s.first[j]; }
+    within = t - first;
     return k;
 }
 
@@ -95,8 +105,8 @@ __device__ __forceinline__ float update_of(const Group &g, float grad, float nex
 template <typename T>
 __global__ void __launch_bounds__(256) update_sums_kernel(Group g)
 {
-    const Matrix &m = g.mat[matrix_of<&Matrix::sum_first>(g, blockIdx.x)];
-    const uint32_t block = blockIdx.x - m.sum_first;
+    uint32_t block;
+    const Matrix &m = g.mat[matrix_of(g.sums, blockIdx.x, block)];
     const uint32_t cols = m.u.cols, packs = (cols + PACK - 1) / PACK, all = m.u.rows * packs;
     double s = 0.0;
     for (uint32_t p = block * 256 + threadIdx.x; p < all; p += m.sum_blocks * 256) {
@@ -131,17 +141,18 @@ __global__ void __launch_bounds__(256) update_sums_kernel(Group g)
 }
 
 // ---------------------------------------------------------------- X in the layouts of the products
-// PACK consecutive numbers of an operand.
-template <bool SPLIT> __device__ __forceinline__ void put8(const Operand &o, uint64_t at, const float (&v)[PACK])
+// V consecutive numbers of an operand (V divides 32).
+template <bool SPLIT, int V> __device__ __forceinline__ void put(f16 *to, const float (&v)[V])
 {
-    f16x8 h;
+    typedef f16 P __attribute__((ext_vector_type(V)));
+    P h;
 #pragma unroll
-    for (int e = 0; e < PACK; ++e) h[e] = (f16)v[e];
-    *reinterpret_cast<f16x8 *>(o.hi + at) = h;
+    for (int e = 0; e < V; ++e) h[e] = (f16)v[e];
+    *reinterpret_cast<P *>(to) = h;
     if constexpr (SPLIT) {
 #pragma unroll
-        for (int e = 0; e < PACK; ++e) h[e] = (f16)(v[e] - (float)h[e]);
-        *reinterpret_cast<f16x8 *>(o.lo + at) = h;
+        for (int e = 0; e < V; ++e) h[e] = (f16)(v[e] - (float)h[e]);
+        *reinterpret_cast<P *>(to + LO) = h;
     }
 }
 
@@ -149,8 +160,8 @@ template <bool SPLIT> __device__ __forceinline__ void put8(const Operand &o, uin
 template <typename T, bool SPLIT>
 __global__ void __launch_bounds__(256) update_start_kernel(Group g)
 {
-    const Matrix &m = g.mat[matrix_of<&Matrix::tile_first>(g, blockIdx.x)];
-    const uint32_t tile = blockIdx.x - m.tile_first;
+    uint32_t tile;
+    const Matrix &m = g.mat[matrix_of(g.starts, blockIdx.x, tile)];
     __shared__ double part[4];
     __shared__ float block[64][65];
     // G is read along its rows: along X's rows, or, where X is G's transpose, along its columns.  What is read does not wait for the norm.
@@ -205,10 +216,10 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
         *reinterpret_cast<f32x4 *>(m.x + row + 4) = f32x4{x[4], x[5], x[6], x[7]};
 #pragma unroll
         for (int e = 0; e < PACK; ++e) x[e] *= SCALE;
-        put8<SPLIT>(m.xr, row, x);
+        put<SPLIT>(m.xr + place<SPLIT>(i0 + line, j0 + c, m.m_pad), x);
 #pragma unroll
         for (int e = 0; e < PACK; ++e) x[e] = block[c + e][line] * SCALE;
-        put8<SPLIT>(m.xt[0], (uint64_t)(j0 + line) * m.n_pad + i0 + c, x);
+        put<SPLIT>(m.xt[0] + place<SPLIT>(j0 + line, i0 + c, m.n_pad), x);
     }
 }
 
@@ -227,40 +238,37 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
 template <int WM, int WN, int BI, int BJ, int DEPTH_, int STAGES_, bool SPLIT_, int KG = 1>
 struct Product {
     static constexpr bool SPLIT = SPLIT_;
-    static constexpr int DEPTH = DEPTH_, STAGES = STAGES_;
-    static constexpr int THREADS = WM * WN * KG * 64, TM = WM * BI * 16, TN = WN * BJ * 16;
-    static_assert(TM == TN, "the lower half of a symmetric product is made of square tiles");
-    static constexpr int TILE = TM, CHUNKS = DEPTH / 8, PARTS = SPLIT ? 2 : 1;
-    static constexpr int ROWS = (TM + TN) * PARTS;               // of a step: L's hi, L's lo, R's hi, R's lo
-    static constexpr int STAGE = ROWS * DEPTH;                   // elements
+    static constexpr int DEPTH = DEPTH_, STAGES = STAGES_;       // DEPTH: numbers of a row in a step, of both parts together
+    static constexpr int THREADS = WM * WN * KG * 64, TILE = WM * BI * 16;
+    static_assert(TILE == WN * BJ * 16, "the lower half of a symmetric product is made of square tiles");
+    static constexpr int CHUNKS = DEPTH / 8;
+    static constexpr int STAGE = 2 * TILE * DEPTH;               // numbers: L's rows, R's rows
     static constexpr int LDS_BYTES = STAGES * STAGE * 2;
-    static constexpr int SIDE_LOADS = TILE * CHUNKS / THREADS;   // of a thread, to a part of a step
-    static constexpr int LOADS = 2 * PARTS * SIDE_LOADS;
+    static constexpr int SIDE_LOADS = TILE * CHUNKS / THREADS;   // of a thread, to a step
     static_assert(TILE * CHUNKS % THREADS == 0 && LDS_BYTES <= 160 * 1024, "");
-    static constexpr int SLICES = DEPTH / 32 / KG;               // of a wave; what one matrix operation takes along K each
-    static_assert(DEPTH == SLICES * KG * 32 && (KG == 1 || (KG == BI * BJ && WM * WN * KG * KG * 1024 <= LDS_BYTES)), "");
+    static constexpr int SLICES = DEPTH / 32 / KG;               // of a wave; what one matrix operation takes along K each, hi and lo parts by turns
+    static_assert(DEPTH == SLICES * KG * 32 && SLICES % (SPLIT ? 2 : 1) == 0 && (KG == 1 || (KG == BI * BJ && WM * WN * KG * KG * 1024 <= LDS_BYTES)), "");
     typedef f32x4 Acc[BI][BJ];
 
     static __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ (DEPTH >= 128 ? row & 15 : DEPTH == 64 ? (row >> 1) & 7 : (row >> 2) & 3); }
 
-    // Rows from first on of the operand, of which it has n_rows (a multiple of 16; what a tile has beyond is read from the last row and not used).
-    struct Side { Operand o; int32_t first, n_rows; };
+    // Rows from first on of the operand, of which it has n_rows (what a tile has beyond is read from the last row and not used).
+    struct Side { const f16 *rows; int32_t first, n_rows; };
 
-    // Where a thread's loads of a step come from: a base of each part, and 32-bit offsets that the parts of a side share (sides are RG_MAX_SIDE at
-    // most, an operand 2 GiB).
+    // Where a thread's loads of a step come from: 32-bit offsets (an operand of RG_MAX_SIDE rows is 1 GiB at most).
     struct Source {
-        const uint8_t *base[2 * PARTS];
+        const uint8_t *base[2];
         uint32_t offset[2][SIDE_LOADS];
-        uint32_t along[KG > 1 ? SIDE_LOADS : 1], most;             // KG > 1, where a step can leave K: the bytes along K apart, and the last chunk's
+        uint32_t along[KG > 1 ? SIDE_LOADS : 1], most;             // KG > 1, where a step can leave the row: the bytes along it apart, and the last chunk's
         __device__ __forceinline__ void load(int32_t k0, f16 *stage) const
         {
 #pragma unroll
-            for (int p = 0; p < 2 * PARTS; ++p) {
-                const auto *from = (const __attribute__((address_space(1))) uint8_t *)(base[p] + (KG > 1 ? 0 : 2 * (int64_t)k0));
+            for (int side = 0; side < 2; ++side) {
+                const auto *from = (const __attribute__((address_space(1))) uint8_t *)(base[side] + (KG > 1 ? 0 : 2 * (int64_t)k0));
 #pragma unroll
                 for (int i = 0; i < SIDE_LOADS; ++i) {
-                    f16 *to = stage + p * TILE * DEPTH + (i * THREADS + (int)(threadIdx.x & ~63u)) * 8;
-                    const uint32_t at = KG > 1 ? offset[p / PARTS][i] + min(along[KG > 1 ? i : 0] + 2u * (uint32_t)k0, most) : offset[p / PARTS][i];
+                    f16 *to = stage + side * TILE * DEPTH + (i * THREADS + (int)(threadIdx.x & ~63u)) * 8;
+                    const uint32_t at = KG > 1 ? offset[side][i] + min(along[KG > 1 ? i : 0] + 2u * (uint32_t)k0, most) : offset[side][i];
                     __builtin_amdgcn_global_load_lds(from + at, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
                 }
             }
@@ -279,16 +287,16 @@ struct Product {
         __builtin_amdgcn_sched_barrier(0);
     }
 
+    // K: numbers along a row of the operands, of both parts together; a multiple of 64, SPLIT 128
     static __device__ __forceinline__ void run(const Side &L, const Side &R, int32_t K, f16 *lds, Acc &acc)
     {
-        const int lane = threadIdx.x & 63, group = (threadIdx.x >> 6) / (WM * WN), wave = (threadIdx.x >> 6) % (WM * WN);
+        // The wave's number is the same in all its lanes, and the compiler has to know: matrix operations take no heed of which lanes are active, so that a
+        // slice may only be passed over by a branch of the whole wave.
+        const int all = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+        const int lane = threadIdx.x & 63, group = all / (WM * WN), wave = all % (WM * WN);
         Source src;
-        src.base[0] = reinterpret_cast<const uint8_t *>(L.o.hi);
-        src.base[PARTS] = reinterpret_cast<const uint8_t *>(R.o.hi);
-        if constexpr (SPLIT) {
-            src.base[1] = reinterpret_cast<const uint8_t *>(L.o.lo);
-            src.base[3] = reinterpret_cast<const uint8_t *>(R.o.lo);
-        }
+        src.base[0] = reinterpret_cast<const uint8_t *>(L.rows);
+        src.base[1] = reinterpret_cast<const uint8_t *>(R.rows);
         src.most = (uint32_t)K * 2u - 16u;
 #pragma unroll
         for (int i = 0; i < SIDE_LOADS; ++i) {
@@ -302,17 +310,14 @@ struct Product {
         for (int i = 0; i < BI; ++i)
 #pragma unroll
             for (int j = 0; j < BJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const int row_l = (wave / WN) * BI * 16 + (lane & 15), row_r = TILE * PARTS + (wave % WN) * BJ * 16 + (lane & 15);
-        // Fragments of a step in the order they are read and used: of each slice the hi parts, then the lo parts.
-        constexpr int GROUPS = SLICES * PARTS;
-        f16x8 l[GROUPS][BI], r[GROUPS][BJ];
-        const auto read = [&](const f16 *stage, int g) {
-            const int s = group * SLICES + g / PARTS, p = g % PARTS;
-            const int slot = slot_of(lane & 15, s * 4 + (lane >> 4)) * 8;                  // the rows of a block begin at multiples of 16
+        const int row_l = (wave / WN) * BI * 16 + (lane & 15), row_r = TILE + (wave % WN) * BJ * 16 + (lane & 15);
+        f16x8 l[SLICES][BI], r[SLICES][BJ];
+        const auto read = [&](const f16 *stage, int s) {
+            const int slot = slot_of(lane & 15, (group * SLICES + s) * 4 + (lane >> 4)) * 8;      // the rows of a block begin at multiples of 16
 #pragma unroll
-            for (int i = 0; i < BI; ++i) l[g][i] = *reinterpret_cast<const f16x8 *>(stage + (row_l + p * TILE + i * 16) * DEPTH + slot);
+            for (int i = 0; i < BI; ++i) l[s][i] = *reinterpret_cast<const f16x8 *>(stage + (row_l + i * 16) * DEPTH + slot);
 #pragma unroll
-            for (int j = 0; j < BJ; ++j) r[g][j] = *reinterpret_cast<const f16x8 *>(stage + (row_r + p * TILE + j * 16) * DEPTH + slot);
+            for (int j = 0; j < BJ; ++j) r[s][j] = *reinterpret_cast<const f16x8 *>(stage + (row_r + j * 16) * DEPTH + slot);
         };
         const auto multiply = [&](const f16x8 (&x)[BI], const f16x8 (&y)[BJ]) {
 #pragma unroll
@@ -327,25 +332,25 @@ struct Product {
         for (int q = 0; q < STAGES - 1; ++q) src.load(min(q * DEPTH, last), lds + q * STAGE);
         int now = 0;
         for (int32_t k0 = 0; k0 < K; k0 += DEPTH) {
-            arrive<(STAGES - 2) * LOADS>();
+            arrive<(STAGES - 2) * 2 * SIDE_LOADS>();
             const f16 *stage = lds + now * STAGE;
             f16 *freed = lds + (now == 0 ? STAGES - 1 : now - 1) * STAGE;                  // no wave reads it any more since the barrier
             read(stage, 0);
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
+            for (int s = 0; s < SLICES; ++s) {
                 // What was read is there, what comes next goes out, and the products run meanwhile.  (The wait is explicit because the compiler, with loads into
                 // LDS under way, would wait for the next reads too.)
                 __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));
                 __builtin_amdgcn_sched_barrier(0);
-                if (g + 1 < GROUPS) read(stage, g + 1);
-                if (g == 0) src.load(min(k0 + (STAGES - 1) * DEPTH, last), freed);
+                if (s + 1 < SLICES) read(stage, s + 1);
+                if (s == 0) src.load(min(k0 + (STAGES - 1) * DEPTH, last), freed);
                 __builtin_amdgcn_sched_barrier(0);
-                if (KG > 1 && k0 + (group * SLICES + g / PARTS) * 32 >= K) continue;       // K is a multiple of 64, a slice inside or outside as a whole
-                if (SPLIT && g % 2 == 1) {
-                    multiply(l[g], r[g - 1]);
-                    multiply(l[g - 1], r[g]);
+                if (KG > 1 && k0 + (group * SLICES + s) * 32 >= K) continue;              // a slice is inside or outside as a whole
+                if (SPLIT && s % 2 == 1) {
+                    multiply(l[s], r[s - 1]);                                               // lo hi, hi lo
+                    multiply(l[s - 1], r[s]);
                 } else {
-                    multiply(l[g], r[g]);
+                    multiply(l[s], r[s]);
                 }
             }
             now = now == STAGES - 1 ? 0 : now + 1;
@@ -398,19 +403,6 @@ __device__ __forceinline__ void quad_transpose(float (&v)[4])
     }
 }
 
-template <bool SPLIT> __device__ __forceinline__ void put4(const Operand &o, uint64_t at, const float (&v)[4])
-{
-    f16x4 h;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = (f16)v[e];
-    *reinterpret_cast<f16x4 *>(o.hi + at) = h;
-    if constexpr (SPLIT) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = (f16)(v[e] - (float)h[e]);
-        *reinterpret_cast<f16x4 *>(o.lo + at) = h;
-    }
-}
-
 // Tile t of the lower half, row by row: (row, column), column <= row.
 __device__ __forceinline__ void half_tile(uint32_t t, int32_t &row, int32_t &column)
 {
@@ -426,12 +418,14 @@ template <typename Prod, bool POLY>
 __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, bool first)
 {
     extern __shared__ __align__(16) uint8_t lds_bytes[];
-    const Matrix &m = g.mat[matrix_of<&Matrix::half_first>(g, blockIdx.x)];
+    uint32_t t;
+    const Matrix &m = g.mat[matrix_of(g.half, blockIdx.x, t)];
     int32_t ti, tj;
-    half_tile(blockIdx.x - m.half_first, ti, tj);
-    const Operand &from = POLY ? m.a : m.xr, &to = POLY ? m.p : m.a;
+    half_tile(t, ti, tj);
+    const f16 *from = POLY ? m.a : m.xr;
+    f16 *to = POLY ? m.p : m.a;
     typename Prod::Acc acc;
-    Prod::run({from, ti * Prod::TILE, m.n_pad}, {from, tj * Prod::TILE, m.n_pad}, POLY ? m.n_pad : m.m_pad, reinterpret_cast<f16 *>(lds_bytes), acc);
+    Prod::run({from, ti * Prod::TILE, m.n_pad}, {from, tj * Prod::TILE, m.n_pad}, (int32_t)row_length<Prod::SPLIT>(POLY ? m.n_pad : m.m_pad), reinterpret_cast<f16 *>(lds_bytes), acc);
     float cb = NS_B, cc = NS_C * UNSCALE;
     if (POLY && first) {
         const float f = *m.factor;
@@ -441,20 +435,20 @@ __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, boo
     Prod::each(acc, [&](int r, int c, float (&v)[4]) {
         const int32_t i = ti * Prod::TILE + r, j = tj * Prod::TILE + c;
         if (i >= m.n_pad || j - (int32_t)(threadIdx.x & 3) >= m.n_pad) return;              // whole quads of lanes: sides are padded to multiples of 64
-        const uint64_t mirror = (uint64_t)j * m.n_pad + i;
+        const uint64_t mirror = place<Prod::SPLIT>(j, i, m.n_pad);
         if constexpr (POLY) {                                     // A from its reflection, which has the four side by side
-            const f16x4 h = *reinterpret_cast<const f16x4 *>(m.a.hi + mirror);
+            const f16x4 h = *reinterpret_cast<const f16x4 *>(m.a + mirror);
             f16x4 l = {};
-            if constexpr (Prod::SPLIT) l = *reinterpret_cast<const f16x4 *>(m.a.lo + mirror);
+            if constexpr (Prod::SPLIT) l = *reinterpret_cast<const f16x4 *>(m.a + mirror + LO);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = cb * ((float)h[e] + (float)l[e]) + cc * v[e];
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= UNSCALE;
         }
-        if (ti != tj) put4<Prod::SPLIT>(to, mirror, v);
+        if (ti != tj) put<Prod::SPLIT>(to + mirror, v);
         quad_transpose(v);
-        put4<Prod::SPLIT>(to, (uint64_t)(i + (threadIdx.x & 3)) * m.n_pad + (j & ~3), v);
+        put<Prod::SPLIT>(to + place<Prod::SPLIT>(i + (int32_t)(threadIdx.x & 3), j & ~3, m.n_pad), v);
     });
 }
 
@@ -463,12 +457,13 @@ template <typename T, typename Prod, bool LAST, bool MUON>
 __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, uint32_t step)
 {
     extern __shared__ __align__(16) uint8_t lds_bytes[];
-    const Matrix &m = g.mat[matrix_of<&Matrix::whole_first>(g, blockIdx.x)];
-    const uint32_t t = blockIdx.x - m.whole_first, across = ((uint32_t)m.m_pad + Prod::TILE - 1) / Prod::TILE;
+    uint32_t t;
+    const Matrix &m = g.mat[matrix_of(g.whole, blockIdx.x, t)];
+    const uint32_t across = ((uint32_t)m.m_pad + Prod::TILE - 1) / Prod::TILE;
     const int32_t ti = (int32_t)(t / across), tj = (int32_t)(t % across);
     typename Prod::Acc acc;
-    Prod::run({m.p, ti * Prod::TILE, m.n_pad}, {m.xt[step & 1], tj * Prod::TILE, m.m_pad}, m.n_pad, reinterpret_cast<f16 *>(lds_bytes), acc);
-    const Operand &next = m.xt[(step & 1) ^ 1];
+    Prod::run({m.p, ti * Prod::TILE, m.n_pad}, {m.xt[step & 1], tj * Prod::TILE, m.m_pad}, (int32_t)row_length<Prod::SPLIT>(m.n_pad), reinterpret_cast<f16 *>(lds_bytes), acc);
+    f16 *next = m.xt[(step & 1) ^ 1];
     const float f = step == 0 ? *m.factor : 1.f;
     const float grow = MUON ? g.lr * sqrtf(fmaxf(1.f, (float)m.u.rows / (float)m.u.cols)) : 0.f;
     Prod::each(acc, [&](int r, int c, float (&v)[4]) {
@@ -505,9 +500,9 @@ __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, ui
             *reinterpret_cast<f32x4 *>(m.x + at) = f32x4{v[0], v[1], v[2], v[3]};
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= SCALE;
-            put4<Prod::SPLIT>(m.xr, at, v);
+            put<Prod::SPLIT>(m.xr + place<Prod::SPLIT>(i, j0, m.m_pad), v);
             quad_transpose(v);
-            put4<Prod::SPLIT>(next, (uint64_t)j * m.n_pad + i0, v);
+            put<Prod::SPLIT>(next + place<Prod::SPLIT>(j, i0, m.n_pad), v);
         }
     });
 }
@@ -545,11 +540,11 @@ template <typename T, typename Prod, bool LAST, bool MUON> rg_status launch_appl
 }
 
 // The tiles.
-template <bool SPLIT> using Tile64Shared = Product<2, 2, 2, 2, 128, SPLIT ? 2 : 3, SPLIT, 4>;
+template <bool SPLIT> using Tile64Shared = Product<2, 4, 2, 1, 128, 4, SPLIT, 2>;
 template <bool SPLIT> using Tile64 = Product<2, 2, 2, 2, 64, 3, SPLIT>;
-template <bool SPLIT> using Tile128 = Product<2, 4, 4, 2, SPLIT ? 32 : 64, 3, SPLIT>;
-template <bool SPLIT> using Tile192 = std::conditional_t<SPLIT, Product<3, 4, 4, 3, 32, 3, true>, Product<2, 4, 6, 3, 64, 3, false>>;
-template <bool SPLIT> using Tile256 = Product<2, 4, 8, 4, 32, SPLIT ? 2 : 4, SPLIT>;
+template <bool SPLIT> using Tile128 = Product<2, 4, 4, 2, 64, 3, SPLIT>;
+template <bool SPLIT> using Tile128Pair = Product<2, 4, 4, 2, 64, 2, SPLIT>;
+template <bool SPLIT> using Tile192 = Product<2, 4, 6, 3, 64, 3, SPLIT>;
 
 template <bool SPLIT, typename F> rg_status with_tile(int tile, F &&body)
 {
@@ -557,9 +552,11 @@ template <bool SPLIT, typename F> rg_status with_tile(int tile, F &&body)
     case UPDATE_TILE_SHARED: return body(Tile64Shared<SPLIT>{});
     case 64: return body(Tile64<SPLIT>{});
     case 128: return body(Tile128<SPLIT>{});
+    case UPDATE_TILE_PAIR: return body(Tile128Pair<SPLIT>{});
     case 192: return body(Tile192<SPLIT>{});
-    default: return body(Tile256<SPLIT>{});
     }
+    set_error("no product of tiles of %d", tile);
+    return RG_EHIP;
 }
 
 struct Shape { uint32_t sums, starts, half, whole; int half_tile, whole_tile; };
@@ -593,12 +590,6 @@ struct Carver {
         p = base ? reinterpret_cast<P *>(base + used) : nullptr;
         used += (n * sizeof(P) + 255) & ~255ull;
     }
-    void take(Operand &o, uint64_t n, bool split)
-    {
-        take(o.hi, n);
-        o.lo = nullptr;
-        if (split) take(o.lo, n);
-    }
 };
 
 void lay_out(Matrix &m, const rg_update &u, bool split, Carver &c)
@@ -613,11 +604,9 @@ void lay_out(Matrix &m, const rg_update &u, bool split, Carver &c)
     c.take(m.sums, SUM_BLOCKS);
     c.take(m.factor, 1);
     c.take(m.x, nm);
-    c.take(m.xr, nm, split);
-    c.take(m.xt[0], nm, split);
-    c.take(m.xt[1], nm, split);
-    c.take(m.a, nn, split);
-    c.take(m.p, nn, split);
+    const uint64_t parts = split ? 2 : 1;
+    for (f16 **p : {&m.xr, &m.xt[0], &m.xt[1]}) c.take(*p, nm * parts);
+    for (f16 **p : {&m.a, &m.p}) c.take(*p, nn * parts);
 }
 
 // Groups of matrices of a size class, in order, each with the whole workspace to itself.
@@ -646,7 +635,6 @@ rg_status run_group(UpdateClass kind, const rg_update *const *u, uint32_t count,
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
     Group g{};
-    g.count = count;
     g.muon = o.muon; g.nesterov = o.nesterov;
     g.momentum = o.momentum; g.lr = o.lr; g.keep = (float)(1.0 - (double)o.lr * (double)o.weight_decay);
     g.eps = o.eps;
@@ -654,16 +642,18 @@ rg_status run_group(UpdateClass kind, const rg_update *const *u, uint32_t count,
     for (uint32_t k = 0; k < count; ++k) lay_out(g.mat[k], *u[k], split, c);
     const auto tiles = [&](int tile, bool half) {
         uint64_t all = 0;
-        for (uint32_t k = 0; k < count; ++k) all += half ? half_tiles(g.mat[k].n_pad, tile) : whole_tiles(g.mat[k].n_pad, g.mat[k].m_pad, tile);
+        for (uint32_t k = 0; k < count; ++k) all += half ? half_tiles(g.mat[k].n_pad, tile_side(tile)) : whole_tiles(g.mat[k].n_pad, g.mat[k].m_pad, tile_side(tile));
         return all;
     };
     Shape s{};
     s.half_tile = kind != UPDATE_FULL ? UPDATE_TILE_SHARED : update_tile([&](int tile) { return tiles(tile, true); }, n_cu, split);
     s.whole_tile = kind < UPDATE_HALF ? UPDATE_TILE_SHARED : update_tile([&](int tile) { return tiles(tile, false); }, n_cu, split);
+    for (Starts *p : {&g.sums, &g.starts, &g.half, &g.whole})
+        for (uint32_t &x : p->first) x = UINT32_MAX;
     for (uint32_t k = 0; k < count; ++k) {
         Matrix &m = g.mat[k];
         m.sum_blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(SUM_BLOCKS, (uint64_t)m.n * m.m / 4096));
-        m.sum_first = s.sums; m.tile_first = s.starts; m.half_first = s.half; m.whole_first = s.whole;
+        g.sums.first[k] = s.sums; g.starts.first[k] = s.starts; g.half.first[k] = s.half; g.whole.first[k] = s.whole;
         s.sums += m.sum_blocks;
         s.starts += (uint32_t)whole_tiles(m.n_pad, m.m_pad, 64);
         s.half += (uint32_t)half_tiles(m.n_pad, tile_side(s.half_tile));
