@@ -367,22 +367,30 @@ struct Product {
         }
     }
 
-    // body(row, column of the tile, values): four consecutive rows of a column at a time
-    template <typename F> static __device__ __forceinline__ void each(const Acc &acc, F &&body)
+    // body(row, column of the tile, values, what first(row, column) gave): four consecutive rows of a column at a time.  All of first's reads
+    // are under way before the first of body's writes, which the compiler could not know to be apart from them.
+    template <typename G, typename F> static __device__ __forceinline__ void each(const Acc &acc, G &&first, F &&body)
     {
         const int lane = threadIdx.x & 63, group = (threadIdx.x >> 6) / (WM * WN), wave = (threadIdx.x >> 6) % (WM * WN);
+        const int row = (wave / WN) * BI * 16 + (lane >> 4) * 4, column = (wave % WN) * BJ * 16 + (lane & 15);
         if constexpr (KG > 1) {
             float v[4] = {acc[0][0][0], acc[0][0][1], acc[0][0][2], acc[0][0][3]};
-            body((wave / WN) * BI * 16 + group / BJ * 16 + (lane >> 4) * 4, (wave % WN) * BJ * 16 + group % BJ * 16 + (lane & 15), v);
-            return;
+            const int r = row + group / BJ * 16, c = column + group % BJ * 16;
+            body(r, c, v, first(r, c));
+        } else {
+            decltype(first(0, 0)) had[BI][BJ];
+#pragma unroll
+            for (int i = 0; i < BI; ++i)
+#pragma unroll
+                for (int j = 0; j < BJ; ++j) had[i][j] = first(row + i * 16, column + j * 16);
+#pragma unroll
+            for (int i = 0; i < BI; ++i)
+#pragma unroll
+                for (int j = 0; j < BJ; ++j) {
+                    float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                    body(row + i * 16, column + j * 16, v, had[i][j]);
+                }
         }
-#pragma unroll
-        for (int i = 0; i < BI; ++i)
-#pragma unroll
-            for (int j = 0; j < BJ; ++j) {
-                float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                body((wave / WN) * BI * 16 + i * 16 + (lane >> 4) * 4, (wave % WN) * BJ * 16 + j * 16 + (lane & 15), v);
-            }
     }
 };
 
@@ -403,6 +411,14 @@ __device__ __forceinline__ void quad_transpose(float (&v)[4])
     }
 }
 
+// Workgroup g runs on XCD g mod 8, and every XCD has an L2 of its own: tiles that share operands, which follow one another, go to one XCD.
+__device__ __forceinline__ uint32_t tile_of_workgroup()
+{
+    constexpr uint32_t XCDS = 8;
+    const uint32_t x = blockIdx.x % XCDS, each = gridDim.x / XCDS, rest = gridDim.x % XCDS;
+    return x * each + min(x, rest) + blockIdx.x / XCDS;
+}
+
 // Tile t of the lower half, row by row: (row, column), column <= row.
 __device__ __forceinline__ void half_tile(uint32_t t, int32_t &row, int32_t &column)
 {
@@ -419,7 +435,7 @@ __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, boo
 {
     extern __shared__ __align__(16) uint8_t lds_bytes[];
     uint32_t t;
-    const Matrix &m = g.mat[matrix_of(g.half, blockIdx.x, t)];
+    const Matrix &m = g.mat[matrix_of(g.half, tile_of_workgroup(), t)];
     int32_t ti, tj;
     half_tile(t, ti, tj);
     const f16 *from = POLY ? m.a : m.xr;
@@ -432,21 +448,25 @@ __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, boo
         cb *= f * f;
         cc *= f * f * f * f;
     }
-    Prod::each(acc, [&](int r, int c, float (&v)[4]) {
+    // Whole quads of lanes are inside or outside: sides are padded to multiples of 64.
+    const auto inside = [&](int32_t i, int32_t j) { return i < m.n_pad && j - (int32_t)(threadIdx.x & 3) < m.n_pad; };
+    struct Four { f16x4 hi, lo; };
+    const auto first_of = [&](int r, int c) {                     // A from its reflection, which has the four side by side
         const int32_t i = ti * Prod::TILE + r, j = tj * Prod::TILE + c;
-        if (i >= m.n_pad || j - (int32_t)(threadIdx.x & 3) >= m.n_pad) return;              // whole quads of lanes: sides are padded to multiples of 64
-        const uint64_t mirror = place<Prod::SPLIT>(j, i, m.n_pad);
-        if constexpr (POLY) {                                     // A from its reflection, which has the four side by side
-            const f16x4 h = *reinterpret_cast<const f16x4 *>(m.a + mirror);
-            f16x4 l = {};
-            if constexpr (Prod::SPLIT) l = *reinterpret_cast<const f16x4 *>(m.a + mirror + LO);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = cb * ((float)h[e] + (float)l[e]) + cc * v[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] *= UNSCALE;
+        Four a = {};
+        if (POLY && inside(i, j)) {
+            const f16 *from_a = m.a + place<Prod::SPLIT>(j, i, m.n_pad);
+            a.hi = *reinterpret_cast<const f16x4 *>(from_a);
+            if constexpr (Prod::SPLIT) a.lo = *reinterpret_cast<const f16x4 *>(from_a + LO);
         }
-        if (ti != tj) put<Prod::SPLIT>(to + mirror, v);
+        return a;
+    };
+    Prod::each(acc, first_of, [&](int r, int c, float (&v)[4], const Four &a) {
+        const int32_t i = ti * Prod::TILE + r, j = tj * Prod::TILE + c;
+        if (!inside(i, j)) return;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = POLY ? cb * ((float)a.hi[e] + (float)a.lo[e]) + cc * v[e] : v[e] * UNSCALE;
+        if (ti != tj) put<Prod::SPLIT>(to + place<Prod::SPLIT>(j, i, m.n_pad), v);
         quad_transpose(v);
         put<Prod::SPLIT>(to + place<Prod::SPLIT>(i + (int32_t)(threadIdx.x & 3), j & ~3, m.n_pad), v);
     });
@@ -458,49 +478,66 @@ __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, ui
 {
     extern __shared__ __align__(16) uint8_t lds_bytes[];
     uint32_t t;
-    const Matrix &m = g.mat[matrix_of(g.whole, blockIdx.x, t)];
-    const uint32_t across = ((uint32_t)m.m_pad + Prod::TILE - 1) / Prod::TILE;
-    const int32_t ti = (int32_t)(t / across), tj = (int32_t)(t % across);
+    const Matrix &m = g.mat[matrix_of(g.whole, tile_of_workgroup(), t)];
+    // Column by column: P, the smaller operand, is read by every XCD, X by one each.
+    const uint32_t down = ((uint32_t)m.n_pad + Prod::TILE - 1) / Prod::TILE;
+    const int32_t ti = (int32_t)(t % down), tj = (int32_t)(t / down);
     typename Prod::Acc acc;
     Prod::run({m.p, ti * Prod::TILE, m.n_pad}, {m.xt[step & 1], tj * Prod::TILE, m.m_pad}, (int32_t)row_length<Prod::SPLIT>(m.n_pad), reinterpret_cast<f16 *>(lds_bytes), acc);
     f16 *next = m.xt[(step & 1) ^ 1];
     const float f = step == 0 ? *m.factor : 1.f;
     const float grow = MUON ? g.lr * sqrtf(fmaxf(1.f, (float)m.u.rows / (float)m.u.cols)) : 0.f;
-    Prod::each(acc, [&](int r, int c, float (&v)[4]) {
+    const int32_t mine = threadIdx.x & 3;                          // this lane's place in its quad, all of which is inside or outside
+    const auto inside = [&](int32_t i, int32_t j) { return i < m.n_pad && j - mine < m.m_pad; };
+    // Where four results go that lie side by side: along X's rows, or, in the last step, along its columns where X is the transpose.
+    struct Place { int32_t row, col, n; };
+    const auto goes = [&](int32_t i0, int32_t j) {
+        const int32_t row = m.tall ? j : i0 + mine, col = m.tall ? i0 : j & ~3;
+        return Place{row, col, row < (int32_t)m.u.rows ? min(4, (int32_t)m.u.cols - col) : 0};
+    };
+    struct Before { f32x4 x; float w[MUON ? 4 : 1]; };
+    const auto first_of = [&](int r, int c) {
         const int32_t i0 = ti * Prod::TILE + r, j = tj * Prod::TILE + c;
-        if (i0 >= m.n_pad || j - (int32_t)(threadIdx.x & 3) >= m.m_pad) return;
-        quad_transpose(v);
-        const int32_t i = i0 + (int32_t)(threadIdx.x & 3), j0 = j & ~3;                     // this lane's row, and its first column
-        const uint64_t at = (uint64_t)i * m.m_pad + j0;
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(m.x + at);
+        Before b = {};
+        if (!inside(i0, j)) return b;
+        b.x = *reinterpret_cast<const f32x4 *>(m.x + (uint64_t)(i0 + mine) * m.m_pad + (j & ~3));
+        if constexpr (MUON) {
+            const Place to = goes(i0, j);
+            const T *w = row_at<T>(m.u.weight, m.u.weight_stride, to.row) + to.col;
+            if (to.n == 4) {
+                load_pack(w, b.w);
+            } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = f * (NS_A * x[e] + v[e] * (UNSCALE * UNSCALE));
+                for (int e = 0; e < 3; ++e) b.w[e] = e < to.n ? (float)w[e] : 0.f;
+            }
+        }
+        return b;
+    };
+    Prod::each(acc, first_of, [&](int r, int c, float (&v)[4], const Before &b) {
+        const int32_t i0 = ti * Prod::TILE + r, j = tj * Prod::TILE + c;
+        if (!inside(i0, j)) return;
+        quad_transpose(v);                                         // this lane's row of X, four columns
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = f * (NS_A * b.x[e] + v[e] * (UNSCALE * UNSCALE));
         if constexpr (LAST) {
-            // along the output's rows: X's rows, or its columns where X is the transpose
             if (m.tall) quad_transpose(v);
-            const int32_t row = m.tall ? j : i, col = m.tall ? i0 : j0;
-            const int32_t n = min(4, (int32_t)m.u.cols - col);
-            if (row >= (int32_t)m.u.rows || n <= 0) return;
-            T *out = row_at<T>(m.u.out, m.u.out_stride, row) + col;
-            const T *weight = row_at<T>(m.u.weight, m.u.weight_stride, row) + col;
-            if (n == 4) {
-                if (MUON) {
-                    float w[4];
-                    load_pack(weight, w);
+            const Place to = goes(i0, j);
+            T *out = row_at<T>(m.u.out, m.u.out_stride, to.row) + to.col;
+            if constexpr (MUON)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = g.keep * w[e] - grow * v[e];
-                }
+                for (int e = 0; e < 4; ++e) v[e] = g.keep * b.w[e] - grow * v[e];
+            if (to.n == 4) {
                 store_pack(out, v);
             } else {
 #pragma unroll
                 for (int e = 0; e < 3; ++e)
-                    if (e < n) out[e] = (T)(MUON ? g.keep * (float)weight[e] - grow * v[e] : v[e]);
+                    if (e < to.n) out[e] = (T)v[e];
             }
         } else {
-            *reinterpret_cast<f32x4 *>(m.x + at) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4 *>(m.x + (uint64_t)(i0 + mine) * m.m_pad + (j & ~3)) = f32x4{v[0], v[1], v[2], v[3]};
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= SCALE;
-            put<Prod::SPLIT>(m.xr + place<Prod::SPLIT>(i, j0, m.m_pad), v);
+            put<Prod::SPLIT>(m.xr + place<Prod::SPLIT>(i0 + mine, j & ~3, m.m_pad), v);
             quad_transpose(v);
             put<Prod::SPLIT>(next + place<Prod::SPLIT>(j, i0, m.n_pad), v);
         }
