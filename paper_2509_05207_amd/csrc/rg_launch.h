@@ -133,28 +133,16 @@ inline uint64_t half_tiles(uint64_t n, uint64_t tile)
     return t * (t + 1) / 2;
 }
 inline uint64_t whole_tiles(uint64_t n, uint64_t m, uint64_t tile) { return (n + tile - 1) / tile * ((m + tile - 1) / tile); }
-// Names of tiles: 64, 128, 192; and a tile of 64 whose waves are four times as many, a tile of 128 with less LDS, two of which share a compute unit.
+// Names of tiles: 64, 96, 128, 192; and a tile of 64 whose waves are four times as many, a tile of 128 with less LDS, two of which share a compute unit.
 constexpr int UPDATE_TILE_SHARED = 65, UPDATE_TILE_PAIR = 129;
-inline int tile_side(int tile) { return tile / 64 * 64; }
-// What a matrix' products are made of.  It goes by the matrix alone, so that its result does not depend on what else is in the call: sums along K
-// are taken in one order by all tiles but the shared ones.
-//   NARROW   16-bit types, 32 or less of the narrower side: operands in two parts all the same (see rg_update.hip)
-//   SHARED   no more tiles of 64 than the chip has compute units: waves share them
-//   HALF     so it is with the symmetric products alone
-enum UpdateClass { UPDATE_NARROW, UPDATE_SHARED, UPDATE_HALF, UPDATE_FULL };
-inline UpdateClass update_class(uint64_t rows, uint64_t cols, bool wide_type)
-{
-    const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);
-    if (!wide_type && n <= 32) return UPDATE_NARROW;
-    return whole_tiles(n, m, 64) <= 256 ? UPDATE_SHARED : half_tiles(n, 64) <= 64 ? UPDATE_HALF : UPDATE_FULL;
-}
-// Of the other tiles the one whose launch is done first: so many tiles to the fullest compute unit, each at what it takes of one that is full (us a step of 64 along K, measured
+inline int tile_side(int tile) { return tile / 32 * 32; }
+// Of the tiles that no waves share the one whose launch is done first: so many tiles to the fullest compute unit, each at what it takes of one that is full (us a step of 64 along K, measured
 // on products of 1024 to 4096 a side), but no less than a tile that has the unit to itself.
 template <typename F> inline int update_tile(F &&tiles, int n_cu, bool split)
 {
     struct Cost { int tile; double full, alone; };
-    static constexpr Cost ONE[] = {{64, 0.20, 0.27}, {128, 0.55, 0.53}, {UPDATE_TILE_PAIR, 0.49, 0.85}, {192, 0.95, 0.95}};
-    static constexpr Cost TWO[] = {{64, 0.40, 0.45}, {128, 0.95, 0.9}, {UPDATE_TILE_PAIR, 0.85, 1.5}, {192, 1.9, 1.9}};
+    static constexpr Cost ONE[] = {{64, 0.20, 0.27}, {96, 0.36, 0.45}, {128, 0.55, 0.53}, {UPDATE_TILE_PAIR, 0.48, 0.85}, {192, 1.0, 0.95}};
+    static constexpr Cost TWO[] = {{64, 0.28, 0.45}, {96, 0.60, 0.60}, {128, 0.90, 0.85}, {UPDATE_TILE_PAIR, 0.85, 1.5}, {192, 1.9, 1.9}};
     int best = 64;
     double least = 0;
     for (const Cost &c : split ? TWO : ONE) {
@@ -162,6 +150,26 @@ template <typename F> inline int update_tile(F &&tiles, int n_cu, bool split)
         if (least == 0 || t < least) { least = t; best = c.tile; }
     }
     return best;
+}
+
+// How a matrix' products are made.  Nothing in a result may depend on what else is in the call.  Sums along K are taken in one order by all tiles but the
+// shared ones, which is why those go by the matrix alone.  Operands in two parts have two cross terms, added in an order that is another one in a
+// tile's reflection: which elements are reflected, that is the symmetric products' tile, then goes by the matrix alone too.
+struct UpdateKind {
+    bool split;                          // operands in two parts: fp32, and 32 or less of the narrower side (see rg_update.hip)
+    int half_tile, whole_tile;           // of the symmetric products and of the others; 0: by all matrices of a launch
+    bool operator==(const UpdateKind &o) const { return split == o.split && half_tile == o.half_tile && whole_tile == o.whole_tile; }
+};
+inline UpdateKind update_kind(uint64_t rows, uint64_t cols, bool wide_type, int n_cu)
+{
+    const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);
+    UpdateKind k{wide_type || n <= 32, 0, 0};
+    // Shared tiles where there are so few that they do not fill the chip anyway.
+    if (k.split && !wide_type) k.half_tile = k.whole_tile = UPDATE_TILE_SHARED;
+    if (whole_tiles(n, m, 64) <= 256) k.whole_tile = UPDATE_TILE_SHARED;
+    if (k.whole_tile || half_tiles(n, 64) <= 64) k.half_tile = UPDATE_TILE_SHARED;
+    else if (k.split) k.half_tile = update_tile([&](int tile) { return half_tiles(n, tile); }, n_cu, true);
+    return k;
 }
 
 }  // namespace rg

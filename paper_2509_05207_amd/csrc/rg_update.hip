@@ -312,12 +312,12 @@ struct Product {
             for (int j = 0; j < BJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         const int row_l = (wave / WN) * BI * 16 + (lane & 15), row_r = TILE + (wave % WN) * BJ * 16 + (lane & 15);
         f16x8 l[SLICES][BI], r[SLICES][BJ];
-        const auto read = [&](const f16 *stage, int s) {
+        const auto read = [&](const f16 *stage, int s, f16x8 (&x)[BI], f16x8 (&y)[BJ]) {
             const int slot = slot_of(lane & 15, (group * SLICES + s) * 4 + (lane >> 4)) * 8;      // the rows of a block begin at multiples of 16
 #pragma unroll
-            for (int i = 0; i < BI; ++i) l[s][i] = *reinterpret_cast<const f16x8 *>(stage + (row_l + i * 16) * DEPTH + slot);
+            for (int i = 0; i < BI; ++i) x[i] = *reinterpret_cast<const f16x8 *>(stage + (row_l + i * 16) * DEPTH + slot);
 #pragma unroll
-            for (int j = 0; j < BJ; ++j) r[s][j] = *reinterpret_cast<const f16x8 *>(stage + (row_r + j * 16) * DEPTH + slot);
+            for (int j = 0; j < BJ; ++j) y[j] = *reinterpret_cast<const f16x8 *>(stage + (row_r + j * 16) * DEPTH + slot);
         };
         const auto multiply = [&](const f16x8 (&x)[BI], const f16x8 (&y)[BJ]) {
 #pragma unroll
@@ -325,25 +325,58 @@ struct Product {
 #pragma unroll
                 for (int j = 0; j < BJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], acc[i][j], 0, 0, 0);
         };
-        // The loads that are not waited for belong to the steps behind the next; behind the last step the last one is loaded again, into a stage of
-        // its own, so that their number stays the same.
+        // All stages are filled at first, and a stage again as soon as every wave has read the last of it, which is in the middle of a step: the barrier
+        // there also says that the next step has arrived, whose first slice is read while the present one's last is multiplied.  Behind the last step the
+        // last one is loaded again, so that the number of loads under way stays the same, and read, so that there is no branch.
         const int32_t last = (K - 1) / DEPTH * DEPTH;
+        if (KG > 1 && K <= STAGES * DEPTH) {                       // all of it fits: one wait
+            for (int32_t k0 = 0; k0 < K; k0 += DEPTH) src.load(k0, lds + k0 / DEPTH * STAGE);
+            arrive<0>();
+            for (int32_t k0 = 0; k0 < K; k0 += DEPTH)
 #pragma unroll
-        for (int q = 0; q < STAGES - 1; ++q) src.load(min(q * DEPTH, last), lds + q * STAGE);
+                for (int s = 0; s < SLICES; ++s) {
+                    if (k0 + (group * SLICES + s) * 32 >= K) continue;                      // a slice is inside or outside as a whole
+                    read(lds + k0 / DEPTH * STAGE, s, l[s], r[s]);
+                    if (SPLIT && s % 2 == 1) {
+                        multiply(l[s], r[s - 1]);                                           // lo hi, hi lo
+                        multiply(l[s - 1], r[s]);
+                    } else {
+                        multiply(l[s], r[s]);
+                    }
+                }
+            arrive<0>();                                           // LDS is read, and may be written
+            finish(acc, lds, lane, group, wave);
+            return;
+        }
+#pragma unroll
+        for (int q = 0; q < STAGES; ++q) src.load(min(q * DEPTH, last), lds + q * STAGE);
+        arrive<(STAGES - 1) * 2 * SIDE_LOADS>();
+        f16x8 next_l[BI], next_r[BJ];
+        read(lds, 0, next_l, next_r);
         int now = 0;
         for (int32_t k0 = 0; k0 < K; k0 += DEPTH) {
-            arrive<(STAGES - 2) * 2 * SIDE_LOADS>();
-            const f16 *stage = lds + now * STAGE;
-            f16 *freed = lds + (now == 0 ? STAGES - 1 : now - 1) * STAGE;                  // no wave reads it any more since the barrier
-            read(stage, 0);
+            f16 *stage = lds + now * STAGE;
+            now = now == STAGES - 1 ? 0 : now + 1;
 #pragma unroll
             for (int s = 0; s < SLICES; ++s) {
                 // What was read is there, what comes next goes out, and the products run meanwhile.  (The wait is explicit because the compiler, with loads into
                 // LDS under way, would wait for the next reads too.)
+                __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));
                 __builtin_amdgcn_sched_barrier(0);
-                if (s + 1 < SLICES) read(stage, s + 1);
-                if (s == 0) src.load(min(k0 + (STAGES - 1) * DEPTH, last), freed);
+                if (s == 0) {
+#pragma unroll
+                    for (int i = 0; i < BI; ++i) l[0][i] = next_l[i];
+#pragma unroll
+                    for (int j = 0; j < BJ; ++j) r[0][j] = next_r[j];
+                }
+                if (s + 1 < SLICES) {
+                    read(stage, s + 1, l[s + 1], r[s + 1]);
+                } else {
+                    arrive<(STAGES - 2) * 2 * SIDE_LOADS>();
+                    src.load(min(k0 + STAGES * DEPTH, last), stage);
+                    read(lds + now * STAGE, 0, next_l, next_r);
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 if (KG > 1 && k0 + (group * SLICES + s) * 32 >= K) continue;              // a slice is inside or outside as a whole
                 if (SPLIT && s % 2 == 1) {
@@ -353,9 +386,14 @@ struct Product {
                     multiply(l[s], r[s]);
                 }
             }
-            now = now == STAGES - 1 ? 0 : now + 1;
         }
         arrive<0>();                                               // a workgroup's LDS is not left with loads under way
+        finish(acc, lds, lane, group, wave);
+    }
+
+    // The sums of the waves that share a block: each is left with one block, whole.
+    static __device__ __forceinline__ void finish(Acc &acc, f16 *lds, int lane, int group, int wave)
+    {
         if constexpr (KG > 1) {
             f32x4 *sums = reinterpret_cast<f32x4 *>(lds) + lane;   // [group][wave][block][lane]
 #pragma unroll
@@ -579,6 +617,7 @@ template <typename T, typename Prod, bool LAST, bool MUON> rg_status launch_appl
 // The tiles.
 template <bool SPLIT> using Tile64Shared = Product<2, 4, 2, 1, 128, 4, SPLIT, 2>;
 template <bool SPLIT> using Tile64 = Product<2, 2, 2, 2, 64, 3, SPLIT>;
+template <bool SPLIT> using Tile96 = Product<2, 2, 3, 3, 64, 3, SPLIT>;
 template <bool SPLIT> using Tile128 = Product<2, 4, 4, 2, 64, 3, SPLIT>;
 template <bool SPLIT> using Tile128Pair = Product<2, 4, 4, 2, 64, 2, SPLIT>;
 template <bool SPLIT> using Tile192 = Product<2, 4, 6, 3, 64, 3, SPLIT>;
@@ -588,6 +627,7 @@ template <bool SPLIT, typename F> rg_status with_tile(int tile, F &&body)
     switch (tile) {
     case UPDATE_TILE_SHARED: return body(Tile64Shared<SPLIT>{});
     case 64: return body(Tile64<SPLIT>{});
+    case 96: return body(Tile96<SPLIT>{});
     case 128: return body(Tile128<SPLIT>{});
     case UPDATE_TILE_PAIR: return body(Tile128Pair<SPLIT>{});
     case 192: return body(Tile192<SPLIT>{});
@@ -651,40 +691,46 @@ struct Options { bool muon, nesterov; float momentum, lr, weight_decay, eps; uin
 
 template <typename F> rg_status each_group(const rg_update *u, uint32_t n, uint32_t type, F &&body)
 {
-    for (const UpdateClass kind : {UPDATE_NARROW, UPDATE_SHARED, UPDATE_HALF, UPDATE_FULL}) {
+    int n_cu = 0;
+    RG_TRY(compute_units(&n_cu));
+    const auto empty = [&](uint32_t k) { return u[k].rows == 0 || u[k].cols == 0; };
+    const auto kind_of = [&](uint32_t k) { return update_kind(u[k].rows, u[k].cols, type == RG_F32, n_cu); };
+    for (uint32_t first = 0; first < n; ++first) {
+        if (empty(first)) continue;
+        const UpdateKind kind = kind_of(first);
+        bool seen = false;
+        for (uint32_t k = 0; k < first && !seen; ++k) seen = !empty(k) && kind_of(k) == kind;
+        if (seen) continue;
         const rg_update *picked[RG_UPDATES_PER_LAUNCH];
         uint32_t count = 0;
-        for (uint32_t k = 0; k < n; ++k) {
-            if (u[k].rows == 0 || u[k].cols == 0 || update_class(u[k].rows, u[k].cols, type == RG_F32) != kind) continue;
+        for (uint32_t k = first; k < n; ++k) {
+            if (empty(k) || !(kind_of(k) == kind)) continue;
             picked[count++] = &u[k];
-            if (count == RG_UPDATES_PER_LAUNCH) { RG_TRY(body(kind, picked, count)); count = 0; }
+            if (count == RG_UPDATES_PER_LAUNCH) { RG_TRY(body(kind, n_cu, picked, count)); count = 0; }
         }
-        if (count) RG_TRY(body(kind, picked, count));
+        if (count) RG_TRY(body(kind, n_cu, picked, count));
     }
     return RG_OK;
 }
 
 template <typename T>
-rg_status run_group(UpdateClass kind, const rg_update *const *u, uint32_t count, const Options &o, uint8_t *workspace, hipStream_t st)
+rg_status run_group(const UpdateKind &kind, int n_cu, const rg_update *const *u, uint32_t count, const Options &o, uint8_t *workspace, hipStream_t st)
 {
     constexpr bool WIDE = sizeof(T) == 4;
-    const bool split = WIDE || kind == UPDATE_NARROW;
-    int n_cu = 0;
-    RG_TRY(compute_units(&n_cu));
     Group g{};
     g.muon = o.muon; g.nesterov = o.nesterov;
     g.momentum = o.momentum; g.lr = o.lr; g.keep = (float)(1.0 - (double)o.lr * (double)o.weight_decay);
     g.eps = o.eps;
     Carver c{workspace};
-    for (uint32_t k = 0; k < count; ++k) lay_out(g.mat[k], *u[k], split, c);
+    for (uint32_t k = 0; k < count; ++k) lay_out(g.mat[k], *u[k], kind.split, c);
     const auto tiles = [&](int tile, bool half) {
         uint64_t all = 0;
         for (uint32_t k = 0; k < count; ++k) all += half ? half_tiles(g.mat[k].n_pad, tile_side(tile)) : whole_tiles(g.mat[k].n_pad, g.mat[k].m_pad, tile_side(tile));
         return all;
     };
     Shape s{};
-    s.half_tile = kind != UPDATE_FULL ? UPDATE_TILE_SHARED : update_tile([&](int tile) { return tiles(tile, true); }, n_cu, split);
-    s.whole_tile = kind < UPDATE_HALF ? UPDATE_TILE_SHARED : update_tile([&](int tile) { return tiles(tile, false); }, n_cu, split);
+    s.half_tile = kind.half_tile ? kind.half_tile : update_tile([&](int tile) { return tiles(tile, true); }, n_cu, kind.split);
+    s.whole_tile = kind.whole_tile ? kind.whole_tile : update_tile([&](int tile) { return tiles(tile, false); }, n_cu, kind.split);
     for (Starts *p : {&g.sums, &g.starts, &g.half, &g.whole})
         for (uint32_t &x : p->first) x = UINT32_MAX;
     for (uint32_t k = 0; k < count; ++k) {
@@ -696,7 +742,7 @@ rg_status run_group(UpdateClass kind, const rg_update *const *u, uint32_t count,
         s.half += (uint32_t)half_tiles(m.n_pad, tile_side(s.half_tile));
         s.whole += (uint32_t)whole_tiles(m.n_pad, m.m_pad, tile_side(s.whole_tile));
     }
-    return split ? launch_group<T, true>(g, o.steps, s, st) : launch_group<T, WIDE>(g, o.steps, s, st);
+    return kind.split ? launch_group<T, true>(g, o.steps, s, st) : launch_group<T, WIDE>(g, o.steps, s, st);
 }
 
 rg_status check_updates(const rg_update *u, uint32_t n, uint32_t type)
@@ -717,19 +763,20 @@ rg_status check_array(uint32_t k, const char *what, const void *p, uint64_t stri
     return RG_OK;
 }
 
-uint64_t workspace_of(const rg_update *u, uint32_t n, uint32_t type)
+rg_status workspace_of(const rg_update *u, uint32_t n, uint32_t type, uint64_t *bytes)
 {
     uint64_t most = 0;
-    (void)each_group(u, n, type, [&](UpdateClass kind, const rg_update *const *picked, uint32_t count) {
+    RG_TRY(each_group(u, n, type, [&](const UpdateKind &kind, int, const rg_update *const *picked, uint32_t count) {
         Carver c{nullptr};
         for (uint32_t k = 0; k < count; ++k) {
             Matrix m;
-            lay_out(m, *picked[k], type == RG_F32 || kind == UPDATE_NARROW, c);
+            lay_out(m, *picked[k], kind.split, c);
         }
         most = std::max(most, c.used);
         return RG_OK;
-    });
-    return most;
+    }));
+    *bytes = most;
+    return RG_OK;
 }
 
 rg_status run_updates(const rg_update *u, uint32_t n, uint32_t type, const Options &o, void *workspace, uint64_t workspace_bytes, void *stream)
@@ -748,14 +795,15 @@ rg_status run_updates(const rg_update *u, uint32_t n, uint32_t type, const Optio
         RG_TRY(check_array(k, "momentum", u[k].momentum, u[k].momentum_stride, u[k], 4, false));
         RG_TRY(check_array(k, "momentum_out", u[k].momentum_out, u[k].momentum_out_stride, u[k], 4, true));
     }
-    const uint64_t want = workspace_of(u, n, type);
+    uint64_t want = 0;
+    RG_TRY(workspace_of(u, n, type, &want));
     if (want == 0) return RG_OK;
     if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256) { set_error("the workspace is null or not aligned to 256 bytes"); return RG_EINVAL; }
     if (workspace_bytes < want) { set_error("the workspace holds %llu bytes of %llu", (unsigned long long)workspace_bytes, (unsigned long long)want); return RG_ERANGE; }
     const hipStream_t st = as_stream(stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    return each_group(u, n, type, [&](UpdateClass kind, const rg_update *const *picked, uint32_t count) {
-        return type == RG_F32 ? run_group<float>(kind, picked, count, o, ws, st) : type == RG_BF16 ? run_group<bf16>(kind, picked, count, o, ws, st) : run_group<f16>(kind, picked, count, o, ws, st);
+    return each_group(u, n, type, [&](const UpdateKind &kind, int n_cu, const rg_update *const *picked, uint32_t count) {
+        return type == RG_F32 ? run_group<float>(kind, n_cu, picked, count, o, ws, st) : type == RG_BF16 ? run_group<bf16>(kind, n_cu, picked, count, o, ws, st) : run_group<f16>(kind, n_cu, picked, count, o, ws, st);
     });
 }
 
@@ -768,8 +816,7 @@ extern "C" rg_status rg_update_workspace(const rg_update *u, uint32_t n, uint32_
 {
     if (!bytes) { set_error("null argument"); return RG_EINVAL; }
     RG_TRY(check_updates(u, n, type));
-    *bytes = workspace_of(u, n, type);
-    return RG_OK;
+    return workspace_of(u, n, type, bytes);
 }
 
 extern "C" rg_status rg_orthogonalize(const rg_update *u, uint32_t n, uint32_t type, uint32_t steps, float eps, void *workspace, uint64_t workspace_bytes, void *stream)
