@@ -512,45 +512,51 @@ _ELEMENT = {torch.float32: RG_F32, torch.bfloat16: RG_BF16, torch.float16: RG_F1
 
 
 def _rows(name, t, shape=None, dtype=None):
-    """(pointer, stride in bytes) of a device matrix whose rows are contiguous."""
+    """(address, stride in bytes) of a device matrix whose rows are contiguous."""
     assert t.is_cuda and t.dim() == 2, f"{name}: expected a device matrix"
-    assert shape is None or tuple(t.shape) == tuple(shape), f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}"
-    assert t.dtype in _ELEMENT and (dtype is None or t.dtype == dtype), f"{name}: got {t.dtype}"
-    assert t.shape[1] <= 1 or t.stride(1) == 1, f"{name}: the elements of a row have to be contiguous"
-    return C.c_void_p(t.data_ptr()), t.stride(0) * t.element_size()
+    assert shape is None or t.shape == shape, f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}"
+    assert (dtype is None and t.dtype in _ELEMENT) or t.dtype == dtype, f"{name}: got {t.dtype}"
+    along, across = t.stride()
+    assert across == 1 or t.shape[1] <= 1, f"{name}: the elements of a row have to be contiguous"
+    return t.data_ptr(), along * t.element_size()
 
 
 def _vector(name, t, n, dtype):
     if t is None:
         return None
-    assert t.is_cuda and t.shape == (n,) and (n <= 1 or t.stride(0) == 1) and t.dtype == dtype, f"{name}: expected {n} contiguous {dtype} on the device"
-    return C.c_void_p(t.data_ptr())
+    assert t.is_cuda and t.dtype == dtype and t.shape == (n,) and t.is_contiguous(), f"{name}: expected {n} contiguous {dtype} on the device"
+    return t.data_ptr()
 
 
-def _used_on(stream, *made):
-    """Tensors made here on the current stream are handed to work on `stream`."""
+def _stream_and_use(device, stream, *made):
+    """The raw handle of `stream`, the current one if None (what torch's own generated code asks for: a Stream object costs 3 us a call).  Tensors
+    made here on the current stream are handed to work on a stream that is not."""
+    current = torch._C._cuda_getCurrentRawStream(device.index)
     if stream is None:
-        return
-    stream = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
-    if stream == torch.cuda.current_stream():
-        return
-    stream.wait_stream(torch.cuda.current_stream())              # what had their memory before may still be queued there
-    for t in made:
-        if t is not None:
-            t.record_stream(stream)
+        return current
+    raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if raw != current:
+        stream = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(raw)
+        stream.wait_stream(torch.cuda.current_stream(device))        # what had their memory before may still be queued there
+        for t in made:
+            if t is not None:
+                t.record_stream(stream)
+    return raw
 
 
 def rg_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """(y, mean, rstd) of the rows of `x` (device matrix; rows may be padded).  out: where y goes (x itself: in place)."""
-    n, d = x.shape
+    shape, dt = x.shape, x.dtype
     xp, xs = _rows("x", x)
-    y = torch.empty((n, d), dtype=x.dtype, device=x.device) if out is None else out
-    yp, ys = _rows("out", y, (n, d), x.dtype)
+    n, d = shape
+    y = x.new_empty(shape) if out is None else out
+    yp, ys = _rows("out", y, shape, dt)
     wt = (weight if weight is not None else bias if bias is not None else x).dtype
     stats = torch.empty((2, n), dtype=torch.float32, device=x.device)
-    _used_on(stream, y if out is None else None, stats)
-    _check(lib().rg_layer_norm(xp, xs, n, d, _ELEMENT[x.dtype], _vector("weight", weight, d, wt), _vector("bias", bias, d, wt), _ELEMENT[wt],
-                               eps, yp, ys, stats.data_ptr(), stats.data_ptr() + 4 * n, _stream_ptr(stream)))
+    sp = stats.data_ptr()
+    st = _stream_and_use(x.device, stream, y if out is None else None, stats)
+    _check(lib().rg_layer_norm(xp, xs, n, d, _ELEMENT[dt], _vector("weight", weight, d, wt), _vector("bias", bias, d, wt), _ELEMENT[wt],
+                               eps, yp, ys, sp, sp + 4 * n, st))
     return y, stats[0], stats[1]
 
 
@@ -564,23 +570,26 @@ def rg_layer_norm_workspace(n_rows, n_cols, dtype):
 def rg_layer_norm_backward(dy, x, weight, mean, rstd, want_dx=True, want_dweight=True, want_dbias=True, out=None, workspace=None, stream=None):
     """(dx, dweight, dbias); None for what is not wanted.  weight None: all ones (the gradients of weight and bias are then fp32).
     out: where dx goes (dy itself: in place); workspace: a device tensor of rg_layer_norm_workspace bytes, made here if None."""
-    n, d = x.shape
+    shape, dt, device = x.shape, x.dtype, x.device
     xp, xs = _rows("x", x)
-    gp, gs = _rows("dy", dy, (n, d), x.dtype)
+    gp, gs = _rows("dy", dy, shape, dt)
+    n, d = shape
     wt = weight.dtype if weight is not None else torch.float32
-    dx = (torch.empty((n, d), dtype=x.dtype, device=x.device) if out is None else out) if want_dx else None
-    op, os_ = _rows("out", dx, (n, d), x.dtype) if want_dx else (None, 0)
-    dw = torch.empty(d, dtype=wt, device=x.device) if want_dweight else None
-    db = torch.empty(d, dtype=wt, device=x.device) if want_dbias else None
+    dx, op, os_ = None, None, 0
+    if want_dx:
+        dx = x.new_empty(shape) if out is None else out
+        op, os_ = _rows("out", dx, shape, dt)
+    dw = torch.empty(d, dtype=wt, device=device) if want_dweight else None
+    db = torch.empty(d, dtype=wt, device=device) if want_dbias else None
     made = workspace is None and (want_dweight or want_dbias)
     if made:
-        workspace = torch.empty(max(rg_layer_norm_workspace(n, d, x.dtype), 1), dtype=torch.uint8, device=x.device)
-    _used_on(stream, dx if out is None else None, dw, db, workspace if made else None)
-    _check(lib().rg_layer_norm_backward(gp, gs, xp, xs, n, d, _ELEMENT[x.dtype], _vector("weight", weight, d, wt), _ELEMENT[wt],
+        workspace = torch.empty(max(rg_layer_norm_workspace(n, d, dt), 1), dtype=torch.uint8, device=device)
+    st = _stream_and_use(device, stream, dx if out is None else None, dw, db, workspace if made else None)
+    wp, wb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    assert workspace is None or (workspace.is_cuda and workspace.is_contiguous()), "workspace: expected a contiguous device tensor"
+    _check(lib().rg_layer_norm_backward(gp, gs, xp, xs, n, d, _ELEMENT[dt], _vector("weight", weight, d, wt), _ELEMENT[wt],
                                         _vector("mean", mean, n, torch.float32), _vector("rstd", rstd, n, torch.float32), op, os_,
-                                        dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None,
-                                        _dev_ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                                        _stream_ptr(stream)))
+                                        dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None, wp, wb, st))
     return dx, dw, db
 
 
@@ -603,13 +612,16 @@ def _updates(grads, outs, weights=None, momenta=None, out_momenta=None):
     return u, _ELEMENT[dt]
 
 
-def _update_scratch(u, n, t, workspace, stream):
+def _update_scratch(u, n, t, workspace, device, stream, *made):
+    """(workspace address, its bytes, raw stream)."""
+    mine = None
     if workspace is None:
         b = C.c_uint64()
         _check(lib().rg_update_workspace(u, n, t, C.byref(b)))
-        workspace = torch.empty(max(b.value, 1), dtype=torch.uint8, device="cuda")
-        _used_on(stream, workspace)
-    return _dev_ptr(workspace), workspace.numel() * workspace.element_size()
+        workspace = mine = torch.empty(max(b.value, 1), dtype=torch.uint8, device=device)
+    assert workspace.is_cuda and workspace.is_contiguous(), "workspace: expected a contiguous device tensor"
+    st = _stream_and_use(device, stream, mine, *made)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), st, mine
 
 
 def rg_update_workspace(matrices):
@@ -622,12 +634,13 @@ def rg_update_workspace(matrices):
 
 def rg_orthogonalize(grads, steps=5, eps=1e-7, out=None, workspace=None, stream=None):
     """The orthogonalised form of every device matrix of the list.  out: a list of where they go (the matrices themselves: in place)."""
+    if not grads:
+        return [] if out is None else out
     made = out is None
     out = [torch.empty(g.shape, dtype=g.dtype, device=g.device) for g in grads] if made else out
     u, t = _updates(grads, out)
-    p, b = _update_scratch(u, len(grads), t, workspace, stream)
-    _used_on(stream, *(out if made else ()))
-    _check(lib().rg_orthogonalize(u, len(grads), t, int(steps), eps, p, b, _stream_ptr(stream)))
+    p, b, st, _mine = _update_scratch(u, len(grads), t, workspace, grads[0].device, stream, *(out if made else ()))
+    _check(lib().rg_orthogonalize(u, len(grads), t, int(steps), eps, p, b, st))
     return out
 
 
@@ -637,8 +650,10 @@ def rg_muon_step(weights, grads, momenta, lr, weight_decay=0.0, momentum=0.95, n
     out_weights = weights if out_weights is None else out_weights
     out_momenta = momenta if out_momenta is None else out_momenta
     u, t = _updates(grads, out_weights, weights, momenta, out_momenta)
-    p, b = _update_scratch(u, len(grads), t, workspace, stream)
-    _check(lib().rg_muon_step(u, len(grads), t, lr, weight_decay, momentum, 1 if nesterov else 0, int(steps), eps, p, b, _stream_ptr(stream)))
+    if not grads:
+        return
+    p, b, st, _mine = _update_scratch(u, len(grads), t, workspace, grads[0].device, stream)
+    _check(lib().rg_muon_step(u, len(grads), t, lr, weight_decay, momentum, 1 if nesterov else 0, int(steps), eps, p, b, st))
 
 
 def rg_trim_memory():

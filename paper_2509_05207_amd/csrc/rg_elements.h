@@ -18,18 +18,21 @@ inline uint32_t element_bytes(uint32_t type) { return type == RG_F32 ? 4u : type
 template <typename T, int V> struct PackOf { typedef T type __attribute__((ext_vector_type(V))); };
 template <typename T> struct PackOf<T, 1> { typedef T type; };
 
-template <typename T, int V>
-__device__ __forceinline__ void load_pack(const T *p, float (&v)[V])
+template <typename T, int V> __device__ __forceinline__ typename PackOf<T, V>::type load_raw(const T *p)
 {
     typedef typename PackOf<T, V>::type P __attribute__((aligned(alignof(T))));
+    return *reinterpret_cast<const P *>(p);
+}
+template <typename T, int V> __device__ __forceinline__ void unpack(const typename PackOf<T, V>::type &raw, float (&v)[V])
+{
     if constexpr (V == 1) {
-        v[0] = (float)*p;
+        v[0] = (float)raw;
     } else {
-        const P raw = *reinterpret_cast<const P *>(p);
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = (float)raw[e];
     }
 }
+template <typename T, int V> __device__ __forceinline__ void load_pack(const T *p, float (&v)[V]) { unpack<T, V>(load_raw<T, V>(p), v); }
 
 template <typename T, int V>
 __device__ __forceinline__ void store_pack(T *p, const float (&v)[V])

@@ -95,30 +95,39 @@ inline bool blocks_by_ranks(uint64_t n_nodes, uint32_t L, uint64_t beta, uint64_
 }
 
 // ---------------------------------------------------------------- layer norm
-constexpr int NORM_ELEMENTS = 32;        // of a row in a lane's registers, at most
+// Elements of a row in a lane's registers, at most.  The backward pass holds five values to an element (rows of 8,192 bf16, 256 lanes of 32 / 1,024 lanes of 8, us: 150 / 99).
+constexpr int norm_elements(bool backward) { return backward ? 16 : 32; }
 struct NormShape {
     int pack;                            // elements of an access: 16 bytes, or single elements where a row has fewer
     int lanes;                           // of a row: 8 to 64, or a workgroup of 256 or 1,024; 0: the row is longer than that
     int packs;                           // of a lane
     uint32_t grid;                       // workgroups; their waves, or they, take rows by turns
+    uint32_t parts;                      // workgroups that share a long row
     uint32_t n_partial;                  // partial sums of every column that the backward pass leaves
     uint32_t column_grid;                // workgroups over the columns of long rows
 };
-inline NormShape norm_shape(int64_t n_rows, int64_t n_cols, int element_bytes, int n_cu, bool backward)
+// in_place: the result takes the place of what other workgroups of the row would still read.
+inline NormShape norm_shape(int64_t n_rows, int64_t n_cols, int element_bytes, int n_cu, bool backward, bool in_place)
 {
     NormShape s{};
     const int v = 16 / element_bytes;
     s.pack = n_cols < v ? 1 : v;
     const int64_t need = (n_cols + s.pack - 1) / s.pack;
-    // The backward pass holds five values to an element, which workgroups of 1,024 threads have registers for at half as many.
-    const int64_t wide = 1024 * (int64_t)std::min(4, (backward ? NORM_ELEMENTS / 2 : NORM_ELEMENTS) / s.pack);
-    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : need <= 256 ? 64 : need <= 1024 ? 256 : need <= wide ? 1024 : 0;
-    const int64_t most = (int64_t)n_cu * (s.lanes == 1024 || s.lanes == 0 ? 2 : 8);
+    const int64_t most_packs = std::min(4, norm_elements(backward) / s.pack);
+    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : need <= 64 * most_packs ? 64 : need <= 256 * most_packs ? 256 : need <= 1024 * most_packs ? 1024 : 0;
     const int64_t groups = s.lanes == 0 || s.lanes > 64 ? 1 : 256 / s.lanes;
+    int64_t most = (int64_t)n_cu * (s.lanes == 1024 || s.lanes == 0 ? 2 : 8);
+    if (backward) {
+        // As many workgroups as are resident; fewer where their partial sums, written and read, would be more than a sixteenth of what the rows are (at least one to a compute unit).
+        most = std::min((int64_t)n_cu * (s.lanes == 1024 ? 2 : 4), std::max<int64_t>(n_cu, n_rows * element_bytes * 3 / 128));
+    }
     s.packs = s.lanes ? (int)((need + s.lanes - 1) / s.lanes) : 0;
     s.grid = (uint32_t)std::max<int64_t>(1, std::min(most, (n_rows + groups - 1) / groups));
     s.n_partial = n_rows ? s.grid : 0;
+    s.parts = 1;
     if (s.lanes == 0) {
+        while (!in_place && s.parts < 8 && n_rows * s.parts * 2 <= n_cu) s.parts *= 2;
+        s.grid = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(n_cu / 4, (n_rows + 7) / 8)) * 8 * s.parts;      // eight rows at a time, one to an XCD
         s.column_grid = (uint32_t)((n_cols + 256 * v - 1) / (256 * v));
         s.n_partial = (uint32_t)std::min<int64_t>(n_rows, std::max<int64_t>(1, (int64_t)n_cu * 4 / s.column_grid));
     }

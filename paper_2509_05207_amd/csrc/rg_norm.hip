@@ -32,6 +32,7 @@ struct NormArgs {
     float *mean, *rstd;              // written by the forward pass (or NULL), read by the backward pass
     float *partial;                  // [2][n_partial][n_cols], or NULL: neither dweight nor dbias is wanted
     uint32_t n_partial;
+    uint32_t parts;                  // workgroups to a row of those that do not fit registers
     int64_t n_rows, n_cols;
 };
 
@@ -152,22 +153,40 @@ __global__ void __launch_bounds__(norm_threads(LANES)) norm_grad_kernel(NormArgs
         if (a.weight) load_weights<V>(a.weight, a.weight_type, at.column(j), w[j]);
     }
     constexpr int GROUPS = norm_threads(LANES) / LANES;
-    for (int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES; row < a.n_rows; row += (int64_t)gridDim.x * GROUPS) {
+    // The next row is under way while this one is worked on (behind the last row that one again), where there are registers for it.
+    constexpr bool AHEAD_OF_ROW = LANES < 1024 || NV * V <= 8;
+    typename PackOf<T, V>::type raw_x[NV], raw_dy[NV];
+    float mean = 0.f, rstd = 0.f;
+    const auto fetch = [&](int64_t row) {
         const T *x = reinterpret_cast<const T *>(a.x + (uint64_t)row * a.x_stride);
         const T *dy = reinterpret_cast<const T *>(a.dy + (uint64_t)row * a.dy_stride);
-        float h[NV][V], g[NV][V];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            load_pack(x + at.column(j), h[j]);
-            load_pack(dy + at.column(j), g[j]);
+            raw_x[j] = load_raw<T, V>(x + at.column(j));
+            raw_dy[j] = load_raw<T, V>(dy + at.column(j));
         }
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        mean = a.mean[row];
+        rstd = a.rstd[row];
+    };
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / LANES;
+    if (AHEAD_OF_ROW && row < a.n_rows) fetch(row);
+    for (; row < a.n_rows; row += step) {
+        if (!AHEAD_OF_ROW) fetch(row);
+        float h[NV][V], g[NV][V];
+        const float this_mean = mean, this_rstd = rstd;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            unpack<T, V>(raw_x[j], h[j]);
+            unpack<T, V>(raw_dy[j], g[j]);
+        }
+        if (AHEAD_OF_ROW) fetch(row + step < a.n_rows ? row + step : row);
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                h[j][e] = (h[j][e] - mean) * rstd;
+                h[j][e] = (h[j][e] - this_mean) * this_rstd;
                 const float counted = at.counts(j, e) ? g[j][e] : 0.f;
                 const float along = at.counts(j, e) ? g[j][e] * h[j][e] : 0.f;
                 db[j][e] += counted;
@@ -182,7 +201,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) norm_grad_kernel(NormArgs
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) g[j][e] = rstd * (g[j][e] * w[j][e] - m0 - h[j][e] * m1);
+            for (int e = 0; e < V; ++e) g[j][e] = this_rstd * (g[j][e] * w[j][e] - m0 - h[j][e] * m1);
             if (at.stores(j)) store_pack(dx + at.column(j), g[j]);
         }
     }
@@ -230,6 +249,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) norm_grad_kernel(NormArgs
 
 // ---------------------------------------------------------------- rows that do not fit a workgroup's registers
 constexpr int LONG_THREADS = 1024;
+constexpr int AHEAD = 8;                 // packs that a thread has under way
 
 // Count, mean and squares around it of two disjoint parts put together.
 struct Moments { float n, mean, m2; };
@@ -240,6 +260,19 @@ __device__ __forceinline__ Moments join(const Moments &p, const Moments &q)
     return Moments{n, p.mean + d * part, p.m2 + q.m2 + d * d * p.n * part};
 }
 
+// Few rows are shared out among `parts` workgroups each: all of them take the row's sums (which they read from their L2: workgroup g runs on XCD g mod
+// 8, and a row's workgroups are on one), and each writes its own part.  (61 rows of 131,071 fp32, us: a workgroup a row 35, four 20.)
+struct Part {
+    int64_t row, rows;                   // the first row, and how far the next one is
+    int64_t from, to;                    // packs of the part
+    bool last;
+};
+__device__ __forceinline__ Part part_of(uint32_t parts, int64_t packs)
+{
+    const uint32_t q = blockIdx.x / 8, k = q % parts;
+    return Part{(int64_t)(q / parts) * 8 + blockIdx.x % 8, (int64_t)(gridDim.x / parts), packs * k / parts, packs * (k + 1) / parts, k + 1 == parts};
+}
+
 template <typename T>
 __global__ void __launch_bounds__(LONG_THREADS) norm_long_rows_kernel(NormArgs a)
 {
@@ -248,19 +281,29 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_rows_kernel(NormArgs a
     uint32_t turn = 0;
     const int64_t packs = a.n_cols / V;
     const int64_t rest = packs * V + threadIdx.x;              // what no pack holds: an element a thread
-    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+    const Part part = part_of(a.parts, packs);
+    for (int64_t row = part.row; row < a.n_rows; row += part.rows) {
         const T *x = reinterpret_cast<const T *>(a.x + (uint64_t)row * a.x_stride);
         T *y = reinterpret_cast<T *>(a.out + (uint64_t)row * a.out_stride);
         Moments m{0.f, 0.f, 0.f};
-        for (int64_t p = threadIdx.x; p < packs; p += LONG_THREADS) {
-            float v[V];
-            load_pack(x + p * V, v);
-            Moments q{(float)V, 0.f, 0.f};
+        for (int64_t first = threadIdx.x; first < packs; first += LONG_THREADS * AHEAD) {
+            typename PackOf<T, V>::type raw[AHEAD];
 #pragma unroll
-            for (int e = 0; e < V; ++e) q.mean += v[e];
-            q.mean *= 1.f / V;
+            for (int k = 0; k < AHEAD; ++k) raw[k] = load_raw<T, V>(x + min(first + k * LONG_THREADS, packs - 1) * V);
+            float v[AHEAD][V], s = 0.f, n = 0.f;
 #pragma unroll
-            for (int e = 0; e < V; ++e) q.m2 += (v[e] - q.mean) * (v[e] - q.mean);
+            for (int k = 0; k < AHEAD; ++k) {
+                unpack<T, V>(raw[k], v[k]);
+                const bool there = first + k * LONG_THREADS < packs;
+                n += there ? (float)V : 0.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) s += there ? v[k][e] : 0.f;
+            }
+            Moments q{n, s / n, 0.f};
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                for (int e = 0; e < V; ++e) q.m2 += first + k * LONG_THREADS < packs ? (v[k][e] - q.mean) * (v[k][e] - q.mean) : 0.f;
             m = join(m, q);
         }
         if (rest < a.n_cols) m = join(m, Moments{1.f, (float)x[rest], 0.f});
@@ -273,18 +316,26 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_rows_kernel(NormArgs a
         m = s[0];
         for (int k = 1; k < LONG_THREADS / 64; ++k) m = join(m, s[k]);
         const float mean = m.mean, rstd = 1.f / sqrtf(m.m2 * a.inv_cols + a.eps);
-        for (int64_t p = threadIdx.x; p < packs; p += LONG_THREADS) {
-            float v[V], w[V], b[V];
-            load_pack(x + p * V, v);
+        for (int64_t first = part.from + threadIdx.x; first < part.to; first += LONG_THREADS * AHEAD) {
+            typename PackOf<T, V>::type raw[AHEAD];
 #pragma unroll
-            for (int e = 0; e < V; ++e) { w[e] = 1.f; b[e] = 0.f; }
-            if (a.weight) load_weights<V>(a.weight, a.weight_type, p * V, w);
-            if (a.bias) load_weights<V>(a.bias, a.weight_type, p * V, b);
+            for (int k = 0; k < AHEAD; ++k) raw[k] = load_raw<T, V>(x + min(first + k * LONG_THREADS, packs - 1) * V);
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = (v[e] - mean) * rstd * w[e] + b[e];
-            store_pack(y + p * V, v);
+            for (int k = 0; k < AHEAD; ++k) {
+                const int64_t c = (first + k * LONG_THREADS) * V;
+                if (c >= part.to * V) break;
+                float v[V], w[V], b[V];
+                unpack<T, V>(raw[k], v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) { w[e] = 1.f; b[e] = 0.f; }
+                if (a.weight) load_weights<V>(a.weight, a.weight_type, c, w);
+                if (a.bias) load_weights<V>(a.bias, a.weight_type, c, b);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = (v[e] - mean) * rstd * w[e] + b[e];
+                store_pack(y + c, v);
+            }
         }
-        if (rest < a.n_cols) {
+        if (part.last && rest < a.n_cols) {
             float v[1], w[1] = {1.f}, b[1] = {0.f};
             load_pack(x + rest, v);
             if (a.weight) load_weights<1>(a.weight, a.weight_type, rest, w);
@@ -292,7 +343,7 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_rows_kernel(NormArgs a
             v[0] = (v[0] - mean) * rstd * w[0] + b[0];
             store_pack(y + rest, v);
         }
-        if (threadIdx.x == 0) {
+        if (threadIdx.x == 0 && part.last) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
@@ -308,7 +359,8 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_dx_kernel(NormArgs a)
     uint32_t turn = 0;
     const int64_t packs = a.n_cols / V;
     const int64_t rest = packs * V + threadIdx.x;
-    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+    const Part part = part_of(a.parts, packs);
+    for (int64_t row = part.row; row < a.n_rows; row += part.rows) {
         const T *x = reinterpret_cast<const T *>(a.x + (uint64_t)row * a.x_stride);
         const T *dy = reinterpret_cast<const T *>(a.dy + (uint64_t)row * a.dy_stride);
         T *dx = reinterpret_cast<T *>(a.out + (uint64_t)row * a.out_stride);
@@ -325,6 +377,7 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_dx_kernel(NormArgs a)
 #pragma unroll
             for (int e = 0; e < N; ++e) { h[e] = (h[e] - mean) * rstd; g[e] *= w[e]; }
         };
+#pragma unroll 4
         for (int64_t p = threadIdx.x; p < packs; p += LONG_THREADS) {
             float h[V], g[V];
             add(p * V, h, g);
@@ -339,14 +392,15 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_dx_kernel(NormArgs a)
         }
         row_sums<LONG_THREADS>(s, slots, turn);
         const float m0 = s[0] * a.inv_cols, m1 = s[1] * a.inv_cols;
-        for (int64_t p = threadIdx.x; p < packs; p += LONG_THREADS) {
+        #pragma unroll 2
+        for (int64_t p = part.from + threadIdx.x; p < part.to; p += LONG_THREADS) {
             float h[V], g[V];
             add(p * V, h, g);
 #pragma unroll
             for (int e = 0; e < V; ++e) g[e] = rstd * (g[e] - m0 - h[e] * m1);
             store_pack(dx + p * V, g);
         }
-        if (rest < a.n_cols) {
+        if (part.last && rest < a.n_cols) {
             float h[1], g[1];
             add(rest, h, g);
             g[0] = rstd * (g[0] - m0 - h[0] * m1);
@@ -426,11 +480,9 @@ template <Pass PASS, typename T>
 bool launch_rows(const NormShape &s, const NormArgs &a, hipStream_t st)
 {
     constexpr int V = 16 / (int)sizeof(T);
-    constexpr int MOST = NORM_ELEMENTS / V;                    // packs a lane in a workgroup of 256
-    constexpr int MOST_WIDE = (PASS == Pass::FORWARD ? NORM_ELEMENTS : NORM_ELEMENTS / 2) / V;
     const auto is = [&](int v, int lanes, int packs) { return s.pack == v && s.lanes == lanes && s.packs == packs; };
 #define RG_NORM_SHAPE(v, lanes, packs)                                                                                    \
-    if constexpr ((packs) <= ((lanes) > 256 ? MOST_WIDE : MOST))                                                          \
+    if constexpr ((v) * (packs) <= norm_elements(PASS == Pass::BACKWARD))                                                 \
         if (is(v, lanes, packs)) { launch_one<PASS, T, v, lanes, packs>(s, a, st); return true; }
     RG_NORM_SHAPE(1, 8, 1)
     RG_NORM_SHAPE(V, 8, 1)
@@ -440,9 +492,11 @@ bool launch_rows(const NormShape &s, const NormArgs &a, hipStream_t st)
     RG_NORM_SHAPE(V, 64, 2)
     RG_NORM_SHAPE(V, 64, 3)
     RG_NORM_SHAPE(V, 64, 4)
+    RG_NORM_SHAPE(V, 256, 1)
     RG_NORM_SHAPE(V, 256, 2)
     RG_NORM_SHAPE(V, 256, 3)
     RG_NORM_SHAPE(V, 256, 4)
+    RG_NORM_SHAPE(V, 1024, 1)
     RG_NORM_SHAPE(V, 1024, 2)
     RG_NORM_SHAPE(V, 1024, 3)
     RG_NORM_SHAPE(V, 1024, 4)
@@ -518,7 +572,8 @@ extern "C" rg_status rg_layer_norm(const void *x, uint64_t x_stride, uint64_t n_
     a.mean = mean; a.rstd = rstd;
     a.n_rows = (int64_t)n_rows; a.n_cols = (int64_t)n_cols;
     const hipStream_t st = as_stream(stream);
-    const NormShape s = norm_shape((int64_t)n_rows, (int64_t)n_cols, (int)bytes, n_cu, false);
+    const NormShape s = norm_shape((int64_t)n_rows, (int64_t)n_cols, (int)bytes, n_cu, false, y == x);
+    a.parts = s.parts;
     if (s.lanes == 0) RG_BY_TYPE(norm_long_rows_kernel, dim3(s.grid), LONG_THREADS, st, a);
     else if (!launch_rows_of<Pass::FORWARD>(type, s, a, st)) { set_error("no kernel for rows of %llu elements", (unsigned long long)n_cols); return RG_EHIP; }
     RG_HIP(hipGetLastError());
@@ -531,7 +586,7 @@ extern "C" rg_status rg_layer_norm_workspace(uint64_t n_rows, uint64_t n_cols, u
     RG_TRY(check_sizes(n_rows, n_cols, type));
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
-    const NormShape s = norm_shape((int64_t)n_rows, (int64_t)n_cols, (int)element_bytes(type), n_cu, true);
+    const NormShape s = norm_shape((int64_t)n_rows, (int64_t)n_cols, (int)element_bytes(type), n_cu, true, false);
     *bytes = 2ull * s.n_partial * n_cols * sizeof(float);
     return RG_OK;
 }
@@ -552,7 +607,7 @@ extern "C" rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, 
     RG_TRY(check_rows("rstd", rstd, 0, n_rows, 1, 4, false));
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
-    const NormShape s = norm_shape((int64_t)n_rows, (int64_t)n_cols, (int)bytes, n_cu, true);
+    const NormShape s = norm_shape((int64_t)n_rows, (int64_t)n_cols, (int)bytes, n_cu, true, dx == dy);
     const bool columns = dweight || dbias;
     if (columns && s.n_partial) {
         const uint64_t want = 2ull * s.n_partial * n_cols * sizeof(float);
@@ -568,6 +623,7 @@ extern "C" rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, 
     a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
     a.partial = columns ? static_cast<float *>(workspace) : nullptr;
     a.n_partial = s.n_partial;
+    a.parts = s.parts;
     a.n_rows = (int64_t)n_rows; a.n_cols = (int64_t)n_cols;
     const hipStream_t st = as_stream(stream);
     if (n_rows && (dx || columns)) {

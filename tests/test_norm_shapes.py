@@ -12,12 +12,12 @@ int main()
 {
     long long rows, cols, bytes, cu, backward;
     while (scanf("%lld %lld %lld %lld %lld", &rows, &cols, &bytes, &cu, &backward) == 5) {
-        const rg::NormShape s = rg::norm_shape(rows, cols, (int)bytes, (int)cu, backward != 0);
+        const rg::NormShape s = rg::norm_shape(rows, cols, (int)bytes, (int)cu, backward != 0, false);
         printf("%d %d %d %u %u %u\n", s.pack, s.lanes, s.packs, s.grid, s.n_partial, s.column_grid);
     }
 }
 """
-KERNELS = {(8, 1), (16, 1), (32, 1), (64, 1), (64, 2), (64, 3), (64, 4), (256, 2), (256, 3), (256, 4), (1024, 2), (1024, 3), (1024, 4)}
+KERNELS = {(8, 1), (16, 1), (32, 1), (64, 1), (64, 2), (64, 3), (64, 4), (256, 1), (256, 2), (256, 3), (256, 4), (1024, 1), (1024, 2), (1024, 3), (1024, 4)}
 
 
 @pytest.fixture(scope="module")
@@ -44,7 +44,7 @@ def test_every_width_has_a_kernel_that_holds_it(shapes, element, backward):
             assert cols > (16_384 if backward or element == 4 else 32_768)
             assert 1 <= n_partial <= 1000 and column_grid * 256 * full >= cols
             continue
-        assert (lanes, packs) in KERNELS and pack * packs <= (16 if backward and lanes == 1024 else 32), (cols, lanes, packs)
+        assert (lanes, packs) in KERNELS and pack * packs <= (16 if backward else 32), (cols, lanes, packs)
         assert (packs - 1) * lanes * pack < cols <= packs * lanes * pack          # only a lane's last pack can leave the row
 
 
