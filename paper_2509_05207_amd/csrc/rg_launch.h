@@ -164,15 +164,18 @@ template <typename F> inline int update_tile(F &&tiles, int n_cu, bool split)
 // How a matrix' products are made.  Nothing in a result may depend on what else is in the call.  Sums along K are taken in one order by all tiles but the
 // shared ones, which is why those go by the matrix alone.  Operands in two parts have two cross terms, added in an order that is another one in a
 // tile's reflection: which elements are reflected, that is the symmetric products' tile, then goes by the matrix alone too.
+constexpr uint64_t TINY_WIDE = 256;
 struct UpdateKind {
+    bool tiny;                           // up to 64 x TINY_WIDE: a workgroup does it all
     bool split;                          // operands in two parts: fp32, and 32 or less of the narrower side (see rg_update.hip)
     int half_tile, whole_tile;           // of the symmetric products and of the others; 0: by all matrices of a launch
-    bool operator==(const UpdateKind &o) const { return split == o.split && half_tile == o.half_tile && whole_tile == o.whole_tile; }
+    bool operator==(const UpdateKind &o) const { return tiny == o.tiny && split == o.split && half_tile == o.half_tile && whole_tile == o.whole_tile; }
 };
 inline UpdateKind update_kind(uint64_t rows, uint64_t cols, bool wide_type, int n_cu)
 {
     const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);
-    UpdateKind k{wide_type || n <= 32, 0, 0};
+    if (n <= 64 && m <= TINY_WIDE) return UpdateKind{true, true, 0, 0};
+    UpdateKind k{false, wide_type || n <= 32, 0, 0};
     // Shared tiles where there are so few that they do not fill the chip anyway.
     if (k.split && !wide_type) k.half_tile = k.whole_tile = UPDATE_TILE_SHARED;
     if (whole_tiles(n, m, 64) <= 256) k.whole_tile = UPDATE_TILE_SHARED;

@@ -156,6 +156,15 @@ template <bool SPLIT, int V> __device__ __forceinline__ void put(f16 *to, const 
     }
 }
 
+// f of a matrix of this norm, which starts as G 2^-e2.
+__device__ __forceinline__ float factor_of(double norm, float eps, int &e2)
+{
+    e2 = 0;
+    if (norm > 0.0 && norm < INFINITY) (void)frexp(norm, &e2);
+    if (!(norm < INFINITY)) return NAN;
+    return norm == 0.0 && eps > 0.f ? 0.f : (float)(ldexp(1.0, e2) / (norm + (double)eps));
+}
+
 // A workgroup takes 64 x 64 elements of the padded X.
 template <typename T, bool SPLIT>
 __global__ void __launch_bounds__(256) update_start_kernel(Group g)
@@ -190,13 +199,9 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
     for (int q = 1; q < 64; q <<= 1) s += __shfl_xor(s, q);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
     __syncthreads();
-    const double norm = sqrt(part[0] + part[1] + part[2] + part[3]);
     int e2 = 0;
-    if (norm > 0.0 && norm < INFINITY) (void)frexp(norm, &e2);
-    if (tile == 0 && threadIdx.x == 0) {
-        const double f = ldexp(1.0, e2) / (norm + (double)g.eps);
-        *m.factor = norm == 0.0 && g.eps > 0.f ? 0.f : norm < INFINITY ? (float)f : NAN;
-    }
+    const float f = factor_of(sqrt(part[0] + part[1] + part[2] + part[3]), g.eps, e2);
+    if (tile == 0 && threadIdx.x == 0) *m.factor = f;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -582,6 +587,199 @@ __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, ui
     });
 }
 
+// ---------------------------------------------------------------- small matrices
+// Matrices of up to 64 x TINY_WIDE, one workgroup each, all of it in one launch (47 x 256 bf16, us: 25 so, 78 by 17 launches).  Each of 16 waves keeps strips of 16
+// columns of X in registers, laid out as matrix operations leave their results: a lane has a column, and of each block of 16 rows the
+// four from 4 (lane / 16) on.  P X needs X with eight rows of a column to a lane, and which eight is free as long as P is read to match: a lane's fours
+// of two blocks, so that X never leaves the registers for it.  For X X^T its rows go through LDS, as A and P do, in two parts always (products cost little here).
+// Bound by the latency of LDS and of four barriers a step.
+constexpr int TINY_THREADS = 1024, TINY_WAVES = 16;
+constexpr int TINY_STRIPS = TINY_WIDE / 16 / TINY_WAVES;           // of a wave
+constexpr int TINY_LDS = 64 * TINY_WIDE * 4 + 64 * 64 * 4;         // X, and A or P
+
+// A row's 16-byte chunks in LDS, in an order that depends on the row: 16 rows of one chunk lie on all banks.
+__device__ __forceinline__ f16 *tiny_at(f16 *base, int row, uint32_t length, uint32_t number)
+{
+    return base + (uint32_t)row * length + ((number / 8) ^ (uint32_t)(row & 15)) * 8 + number % 8;
+}
+
+__device__ __forceinline__ void tiny_put(f16 *base, int row, uint32_t length, uint32_t number, const float (&v)[4])
+{
+    f16x4 h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        h[e] = (f16)v[e];
+        l[e] = (f16)(v[e] - (float)h[e]);
+    }
+    *reinterpret_cast<f16x4 *>(tiny_at(base, row, length, number)) = h;
+    *reinterpret_cast<f16x4 *>(tiny_at(base, row, length, number + LO)) = l;
+}
+
+// The product of 16 rows of L and 16 of R (both in LDS, K numbers of both parts a row).
+__device__ __forceinline__ f32x4 tiny_product(f16 *l, int row_l, f16 *r, int row_r, uint32_t K)
+{
+    const int lane = threadIdx.x & 63;
+    row_l += lane & 15;
+    row_r += lane & 15;
+    f32x4 hh = {0.f, 0.f, 0.f, 0.f}, lh = hh, hl = hh;              // three chains: an operation waits for the one before it in its chain
+    for (uint32_t k = 0; k < K; k += 64) {
+        const uint32_t at = k + (uint32_t)(lane >> 4) * 8;
+        const f16x8 lhi = *reinterpret_cast<const f16x8 *>(tiny_at(l, row_l, K, at)), llo = *reinterpret_cast<const f16x8 *>(tiny_at(l, row_l, K, at + LO));
+        const f16x8 rhi = *reinterpret_cast<const f16x8 *>(tiny_at(r, row_r, K, at)), rlo = *reinterpret_cast<const f16x8 *>(tiny_at(r, row_r, K, at + LO));
+        hh = __builtin_amdgcn_mfma_f32_16x16x32_f16(lhi, rhi, hh, 0, 0, 0);
+        lh = __builtin_amdgcn_mfma_f32_16x16x32_f16(llo, rhi, lh, 0, 0, 0);
+        hl = __builtin_amdgcn_mfma_f32_16x16x32_f16(lhi, rlo, hl, 0, 0, 0);
+    }
+    return hh + (lh + hl);
+}
+
+template <typename T, bool MUON>
+__global__ void __launch_bounds__(TINY_THREADS) update_tiny_kernel(Group g, uint32_t steps)
+{
+    extern __shared__ __align__(16) uint8_t lds_bytes[];
+    __shared__ double part[TINY_WAVES];
+    const Matrix &m = g.mat[blockIdx.x];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    f16 *rows = reinterpret_cast<f16 *>(lds_bytes), *square = rows + 64 * TINY_WIDE * 2;
+    const uint32_t length = row_length<true>(m.m_pad);
+    // Where element e of block b of strip s is in X.
+    const auto row_of = [&](int b, int e) { return b * 16 + (lane >> 4) * 4 + e; };
+    const auto column_of = [&](int s) { return (wave + s * TINY_WAVES) * 16 + (lane & 15); };
+    // body(strip, block, element, row and column of G) for what is inside; all reads of a kind are under way before the first write, which the compiler could
+    // not know to be apart from them.
+    const auto each = [&](auto &&body) {
+#pragma unroll
+        for (int s = 0; s < TINY_STRIPS; ++s)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int32_t i = row_of(b, e), j = column_of(s);
+                    if (i < m.n && j < m.m) body(s, b, e, m.tall ? j : i, m.tall ? i : j);
+                }
+    };
+    float x[TINY_STRIPS][4][4] = {};
+    each([&](int s, int b, int e, int32_t r, int32_t c) { x[s][b][e] = (float)row_at<T>(m.u.grad, m.u.grad_stride, r)[c]; });
+    if (MUON) {
+        float next[TINY_STRIPS][4][4] = {};
+        each([&](int s, int b, int e, int32_t r, int32_t c) { next[s][b][e] = row_at<float>(m.u.momentum, m.u.momentum_stride, r)[c]; });
+        each([&](int s, int b, int e, int32_t r, int32_t c) {
+            const float v = g.momentum * next[s][b][e] + x[s][b][e];
+            row_at<float>(m.u.momentum_out, m.u.momentum_out_stride, r)[c] = v;
+            x[s][b][e] = update_of(g, x[s][b][e], v);
+        });
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int s = 0; s < TINY_STRIPS; ++s)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += (double)x[s][b][e] * (double)x[s][b][e];
+    for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int k = 0; k < TINY_WAVES; ++k) sum += part[k];
+    int e2 = 0;
+    float f = factor_of(sqrt(sum), g.eps, e2);
+#pragma unroll
+    for (int s = 0; s < TINY_STRIPS; ++s)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[s][b][e] = ldexpf(x[s][b][e], -e2) * SCALE;          // as the operands are
+    // What lies beyond X's rows stays zero, and is not computed: the vector unit's instructions are what a step takes time for, four waves' on each.
+    const int blocks = (m.n + 15) / 16, bi = (wave / 4) * 16, bj = (wave % 4) * 16;
+    const bool has_block = max(wave / 4, wave % 4) < blocks;
+    const uint32_t mirror = (uint32_t)(bi + (lane >> 4) * 4), mirror_at = mirror + (mirror & ~31u);
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    tiny_put(square, bj + (lane & 15), 128, mirror_at, v);
+    for (uint32_t step = 0; step < steps; ++step) {
+        // X's rows into LDS: strips of columns that m_pad has
+#pragma unroll
+        for (int s = 0; s < TINY_STRIPS; ++s)
+            if ((wave + s * TINY_WAVES) * 16 < m.m_pad)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    float w[4] = {x[s][b][0], x[s][b][1], x[s][b][2], x[s][b][3]};
+                    quad_transpose(w);
+                    const uint32_t column = (uint32_t)column_of(s) & ~3u;
+                    tiny_put(rows, row_of(b, lane & 3), length, column + (column & ~31u), w);
+                }
+        __syncthreads();
+        // A: a block of 16 x 16 a wave.  It is symmetric, and is written by columns.
+        f32x4 p = {0.f, 0.f, 0.f, 0.f};
+        if (has_block) {
+            p = tiny_product(rows, bi, rows, bj, length);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = p[e] * UNSCALE;
+            tiny_put(square, bj + (lane & 15), 128, mirror_at, v);
+        }
+        __syncthreads();
+        if (has_block) p = tiny_product(square, bi, square, bj, 128);
+        __syncthreads();                                           // A is read
+        if (has_block) {
+            const float cb = NS_B * f * f, cc = NS_C * UNSCALE * f * f * f * f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = cb * v[e] + cc * p[e];
+            tiny_put(square, bj + (lane & 15), 128, mirror_at, v);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < TINY_STRIPS; ++s) {
+            if ((wave + s * TINY_WAVES) * 16 >= m.m) continue;
+            f16x8 xh[2], xl[2];                                    // slices of 32 rows: a lane's fours of two blocks
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float w = x[s][q * 2 + e / 4][e % 4];
+                    xh[q][e] = (f16)w;
+                    xl[q][e] = (f16)(w - (float)xh[q][e]);
+                }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                if (b >= blocks) continue;
+                f32x4 big = {0.f, 0.f, 0.f, 0.f}, small = big;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    if (q * 2 >= blocks) continue;
+                    f16x8 ph, pl;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t at = (uint32_t)q * 64 + (uint32_t)half * 16 + (uint32_t)(lane >> 4) * 4;
+                        const f16x4 h = *reinterpret_cast<const f16x4 *>(tiny_at(square, b * 16 + (lane & 15), 128, at));
+                        const f16x4 l = *reinterpret_cast<const f16x4 *>(tiny_at(square, b * 16 + (lane & 15), 128, at + LO));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { ph[half * 4 + e] = h[e]; pl[half * 4 + e] = l[e]; }
+                    }
+                    big = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, xh[q], big, 0, 0, 0);
+                    small = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, xh[q], small, 0, 0, 0);
+                    small = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, xl[q], small, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[s][b][e] = f * (NS_A * x[s][b][e] + (big[e] + small[e]) * UNSCALE);
+            }
+        }
+        f = 1.f;
+    }
+#pragma unroll
+    for (int s = 0; s < TINY_STRIPS; ++s)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[s][b][e] *= UNSCALE;
+    const float grow = MUON ? g.lr * sqrtf(fmaxf(1.f, (float)m.u.rows / (float)m.u.cols)) : 0.f;
+    if (MUON) {
+        float w[TINY_STRIPS][4][4];
+        each([&](int s, int b, int e, int32_t r, int32_t c) { w[s][b][e] = (float)row_at<T>(m.u.weight, m.u.weight_stride, r)[c]; });
+        each([&](int s, int b, int e, int32_t r, int32_t c) { row_at<T>(m.u.out, m.u.out_stride, r)[c] = (T)(g.keep * w[s][b][e] - grow * x[s][b][e]); });
+    } else {
+        each([&](int s, int b, int e, int32_t r, int32_t c) { row_at<T>(m.u.out, m.u.out_stride, r)[c] = (T)x[s][b][e]; });
+    }
+}
+
 // ---------------------------------------------------------------- launches
 // LDS beyond 64 KB has to be asked for, once per kernel and device.
 template <typename K> rg_status allow_lds(K kernel, int bytes, std::atomic<uint64_t> &known)
@@ -658,6 +856,15 @@ rg_status launch_group(const Group &g, uint32_t steps, const Shape &s, hipStream
     return RG_OK;
 }
 
+template <typename T, bool MUON> rg_status launch_tiny(const Group &g, uint32_t count, uint32_t steps, hipStream_t st)
+{
+    static std::atomic<uint64_t> known{0};
+    RG_TRY(allow_lds(update_tiny_kernel<T, MUON>, TINY_LDS, known));
+    hipLaunchKernelGGL((update_tiny_kernel<T, MUON>), dim3(count), dim3(TINY_THREADS), TINY_LDS, st, g, steps);
+    RG_HIP(hipGetLastError());
+    return RG_OK;
+}
+
 // Hands out the workspace; with no workspace it only counts.
 struct Carver {
     uint8_t *base;
@@ -669,7 +876,7 @@ struct Carver {
     }
 };
 
-void lay_out(Matrix &m, const rg_update &u, bool split, Carver &c)
+void lay_out(Matrix &m, const rg_update &u, const UpdateKind &kind, Carver &c)
 {
     m.u = u;
     m.tall = u.rows > u.cols;
@@ -680,8 +887,9 @@ void lay_out(Matrix &m, const rg_update &u, bool split, Carver &c)
     const uint64_t nm = (uint64_t)m.n_pad * m.m_pad, nn = (uint64_t)m.n_pad * m.n_pad;
     c.take(m.sums, SUM_BLOCKS);
     c.take(m.factor, 1);
+    if (kind.tiny) return;                                         // all the rest in registers and LDS
     c.take(m.x, nm);
-    const uint64_t parts = split ? 2 : 1;
+    const uint64_t parts = kind.split ? 2 : 1;
     for (f16 **p : {&m.xr, &m.xt[0], &m.xt[1]}) c.take(*p, nm * parts);
     for (f16 **p : {&m.a, &m.p}) c.take(*p, nn * parts);
 }
@@ -722,7 +930,8 @@ rg_status run_group(const UpdateKind &kind, int n_cu, const rg_update *const *u,
     g.momentum = o.momentum; g.lr = o.lr; g.keep = (float)(1.0 - (double)o.lr * (double)o.weight_decay);
     g.eps = o.eps;
     Carver c{workspace};
-    for (uint32_t k = 0; k < count; ++k) lay_out(g.mat[k], *u[k], kind.split, c);
+    for (uint32_t k = 0; k < count; ++k) lay_out(g.mat[k], *u[k], kind, c);
+    if (kind.tiny) return g.muon ? launch_tiny<T, true>(g, count, o.steps, st) : launch_tiny<T, false>(g, count, o.steps, st);
     const auto tiles = [&](int tile, bool half) {
         uint64_t all = 0;
         for (uint32_t k = 0; k < count; ++k) all += half ? half_tiles(g.mat[k].n_pad, tile_side(tile)) : whole_tiles(g.mat[k].n_pad, g.mat[k].m_pad, tile_side(tile));
@@ -770,7 +979,7 @@ rg_status workspace_of(const rg_update *u, uint32_t n, uint32_t type, uint64_t *
         Carver c{nullptr};
         for (uint32_t k = 0; k < count; ++k) {
             Matrix m;
-            lay_out(m, *picked[k], kind.split, c);
+            lay_out(m, *picked[k], kind, c);
         }
         most = std::max(most, c.used);
         return RG_OK;
@@ -797,8 +1006,7 @@ rg_status run_updates(const rg_update *u, uint32_t n, uint32_t type, const Optio
     }
     uint64_t want = 0;
     RG_TRY(workspace_of(u, n, type, &want));
-    if (want == 0) return RG_OK;
-    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256) { set_error("the workspace is null or not aligned to 256 bytes"); return RG_EINVAL; }
+    if (want && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256)) { set_error("the workspace is null or not aligned to 256 bytes"); return RG_EINVAL; }
     if (workspace_bytes < want) { set_error("the workspace holds %llu bytes of %llu", (unsigned long long)workspace_bytes, (unsigned long long)want); return RG_ERANGE; }
     const hipStream_t st = as_stream(stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
