@@ -522,9 +522,11 @@ __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, ui
     extern __shared__ __align__(16) uint8_t lds_bytes[];
     uint32_t t;
     const Matrix &m = g.mat[matrix_of(g.whole, tile_of_workgroup(), t)];
-    // Column by column: P, the smaller operand, is read by every XCD, X by one each.
-    const uint32_t down = ((uint32_t)m.n_pad + Prod::TILE - 1) / Prod::TILE;
-    const int32_t ti = (int32_t)(t % down), tj = (int32_t)(t / down);
+    // Eight columns of tiles at a time, row by row: what an XCD works on at once is about square, and reads the fewest rows of P and columns of X.
+    constexpr uint32_t ABREAST = 8;
+    const uint32_t down = ((uint32_t)m.n_pad + Prod::TILE - 1) / Prod::TILE, across = ((uint32_t)m.m_pad + Prod::TILE - 1) / Prod::TILE;
+    const uint32_t band = t / (down * ABREAST), in_band = t - band * down * ABREAST, width = min(ABREAST, across - band * ABREAST);
+    const int32_t ti = (int32_t)(in_band / width), tj = (int32_t)(band * ABREAST + in_band % width);
     typename Prod::Acc acc;
     Prod::run({m.p, ti * Prod::TILE, m.n_pad}, {m.xt[step & 1], tj * Prod::TILE, m.m_pad}, (int32_t)row_length<Prod::SPLIT>(m.n_pad), reinterpret_cast<f16 *>(lds_bytes), acc);
     f16 *next = m.xt[(step & 1) ^ 1];
