@@ -1,0 +1,74 @@
+"""How the products of an orthogonalised update are cut, computed on the host and compiled by itself: every matrix has one kind, by itself alone, and
+every kind a tile that there is a kernel for."""
+import os
+import subprocess
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2509_05207_amd", "csrc")
+DRIVER = r"""
+#include "rg_launch.h"
+#include <cstdio>
+int main()
+{
+    long long rows, cols, wide, copies;
+    while (scanf("%lld %lld %lld %lld", &rows, &cols, &wide, &copies) == 4) {
+        const rg::UpdateKind k = rg::update_kind(rows, cols, wide != 0, 256);
+        const unsigned long long n = (std::min(rows, cols) + 63) / 64 * 64, m = (std::max(rows, cols) + 63) / 64 * 64;
+        const int half = k.half_tile ? k.half_tile : rg::update_tile([&](int t) { return copies * rg::half_tiles(n, rg::tile_side(t)); }, 256, k.split);
+        const int whole = k.whole_tile ? k.whole_tile : rg::update_tile([&](int t) { return copies * rg::whole_tiles(n, m, rg::tile_side(t)); }, 256, k.split);
+        printf("%d %d %d %d %d %d\n", k.tiny, k.split, k.half_tile, k.whole_tile, half, whole);
+    }
+}
+"""
+SHARED, PAIR = 65, 129
+
+
+@pytest.fixture(scope="module")
+def kinds(tmp_path_factory):
+    d = tmp_path_factory.mktemp("kinds")
+    (d / "driver.cpp").write_text(DRIVER)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-o", str(d / "driver"), str(d / "driver.cpp")])
+
+    def ask(cases):
+        text = "\n".join(" ".join(str(int(x)) for x in c) for c in cases) + "\n"
+        out = subprocess.run([str(d / "driver")], input=text, capture_output=True, text=True, check=True).stdout.split("\n")
+        return [[int(x) for x in line.split()] for line in out[: len(cases)]]
+    return ask
+
+
+SIDES = [1, 2, 16, 31, 32, 33, 47, 63, 64, 65, 100, 255, 256, 257, 512, 602, 640, 1000, 1024, 1500, 2047, 2048, 4096, 9000, 16_384]
+
+
+@pytest.mark.parametrize("wide", [0, 1])
+@pytest.mark.parametrize("copies", [1, 12])
+def test_every_matrix_has_tiles(kinds, wide, copies):
+    cases = [(r, c, wide, copies) for r in SIDES for c in SIDES]
+    for (r, c, _, _), (tiny, split, fixed_half, fixed_whole, half, whole) in zip(cases, kinds(cases)):
+        n, m = min(r, c), max(r, c)
+        assert tiny == (n <= 64 and m <= 256)
+        if tiny:
+            continue
+        assert split == (wide or n <= 32)
+        assert half in (SHARED, 64, 96, 128, PAIR, 192) and whole in (SHARED, 64, 96, 128, PAIR, 192)
+        # operands in two parts: what is reflected goes by the matrix alone; and shared tiles always do
+        assert fixed_half or not split
+        assert half != SHARED or fixed_half == SHARED
+        assert whole != SHARED or fixed_whole == SHARED
+
+
+def test_the_same_either_way_round(kinds):
+    a, b = kinds([(r, c, w, 3) for r in SIDES for c in SIDES for w in (0, 1)]), kinds([(c, r, w, 3) for r in SIDES for c in SIDES for w in (0, 1)])
+    assert a == b
+
+
+@pytest.mark.parametrize("rows,cols,wide,copies,half,whole", [
+    # measured: see update_tile and update_kind
+    (4096, 4096, 0, 1, 192, PAIR),
+    (1024, 4096, 0, 6, 128, PAIR),
+    (2048, 2048, 1, 1, 96, 128),
+    (1999, 517, 1, 1, SHARED, 64),
+    (256, 1204, 1, 1, SHARED, SHARED),
+])
+def test_tiles_by_what_is_done_first(kinds, rows, cols, wide, copies, half, whole):
+    assert kinds([(rows, cols, wide, copies)])[0][4:] == [half, whole]
