@@ -95,7 +95,7 @@ inline bool blocks_by_ranks(uint64_t n_nodes, uint32_t L, uint64_t beta, uint64_
 }
 
 // ---------------------------------------------------------------- layer norm
-// Elements of a row in a lane's registers, at most.  The backward pass holds five values to an element (rows of 8,192 bf16, 256 lanes of 32 / 1,024 lanes of 8, us: 150 / 99).
+// Elements of a row in a lane's registers, at most.  The backward pass holds five values to an element (rows of 8,192 bf16, 256 lanes of 32 / 1,024 lanes of 8, us: 150 / 84).
 constexpr int norm_elements(bool backward) { return backward ? 16 : 32; }
 struct NormShape {
     int pack;                            // elements of an access: 16 bytes, or single elements where a row has fewer
@@ -118,8 +118,10 @@ inline NormShape norm_shape(int64_t n_rows, int64_t n_cols, int element_bytes, i
     const int64_t groups = s.lanes == 0 || s.lanes > 64 ? 1 : 256 / s.lanes;
     int64_t most = (int64_t)n_cu * (s.lanes == 1024 || s.lanes == 0 ? 2 : 8);
     if (backward) {
-        // As many workgroups as are resident; fewer where their partial sums, written and read, would be more than a sixteenth of what the rows are (at least one to a compute unit).
-        most = std::min((int64_t)n_cu * (s.lanes == 1024 ? 2 : 4), std::max<int64_t>(n_cu, n_rows * element_bytes * 3 / 128));
+        // As many workgroups as are resident, by the registers that their elements take, so that none waits for another's end; fewer where their partial sums, written and
+        // read, would be more than a sixteenth of what the rows are (at least one to a compute unit).
+        const int64_t elements = (need + std::max(s.lanes, 1) - 1) / std::max(s.lanes, 1) * s.pack;
+        most = std::min((int64_t)n_cu * (s.lanes == 1024 ? 1 : elements <= 4 ? 8 : elements <= 8 ? 4 : 3), std::max<int64_t>(n_cu, n_rows * element_bytes * 3 / 128));
     }
     s.packs = s.lanes ? (int)((need + s.lanes - 1) / s.lanes) : 0;
     s.grid = (uint32_t)std::max<int64_t>(1, std::min(most, (n_rows + groups - 1) / groups));

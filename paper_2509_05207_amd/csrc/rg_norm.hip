@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) norm_rows_kernel(NormArgs
 }
 
 template <typename T, int V, int LANES, int NV>
-__global__ void __launch_bounds__(norm_threads(LANES)) norm_grad_kernel(NormArgs a)
+__global__ void __launch_bounds__(norm_threads(LANES), LANES > 256 ? 1 : V * NV > 8 ? 3 : 4) norm_grad_kernel(NormArgs a)
 {
     __shared__ float slots[2][2][16];
     uint32_t turn = 0;
