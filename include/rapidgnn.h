@@ -490,7 +490,9 @@ rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, const void 
  *     W' = W - lr * (weight_decay * W + sqrt(max(1, rows / cols)) * orthogonalized(U)).
  *
  * All matrices of a model go in one call: what is small is bound by launches,
- * of which there are 2 + 3 * steps for every RG_UPDATES_PER_LAUNCH matrices of a size class.
+ * of which there are 2 + 3 * steps for every RG_UPDATES_PER_LAUNCH matrices that
+ * are cut alike, and one for as many of up to 64 x 256.  A matrix' result does not
+ * depend on what else is in the call.
  *
  *   u        host, [n]: the matrices (the arrays on the device)
  *   type     of grad, weight and out; momenta are fp32

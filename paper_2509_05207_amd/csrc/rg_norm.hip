@@ -536,6 +536,14 @@ rg_status check_rows(const char *what, const void *p, uint64_t stride, uint64_t 
     return RG_OK;
 }
 
+// A result in the place of an input has its rows where the input has them.
+rg_status check_place(const char *what, const void *out, uint64_t out_stride, const void *in, uint64_t in_stride, uint64_t n_rows)
+{
+    if (out != in || out_stride == in_stride || n_rows <= 1) return RG_OK;
+    set_error("%s: in place, but with another stride", what);
+    return RG_EINVAL;
+}
+
 rg_status check_vector(const char *what, const void *p, uint32_t weight_type, uint32_t type)
 {
     if (!p) return RG_OK;
@@ -556,6 +564,7 @@ extern "C" rg_status rg_layer_norm(const void *x, uint64_t x_stride, uint64_t n_
     const uint32_t bytes = element_bytes(type);
     RG_TRY(check_rows("x", x, x_stride, n_rows, n_cols, bytes, false));
     RG_TRY(check_rows("y", y, y_stride, n_rows, n_cols, bytes, true));
+    RG_TRY(check_place("y", y, y_stride, x, x_stride, n_rows));
     RG_TRY(check_vector("weight", weight, weight_type, type));
     RG_TRY(check_vector("bias", bias, weight_type, type));
     RG_TRY(check_vector("mean", mean, RG_F32, type));
@@ -599,7 +608,10 @@ extern "C" rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, 
     const uint32_t bytes = element_bytes(type);
     RG_TRY(check_rows("dy", dy, dy_stride, n_rows, n_cols, bytes, false));
     RG_TRY(check_rows("x", x, x_stride, n_rows, n_cols, bytes, false));
-    if (dx) RG_TRY(check_rows("dx", dx, dx_stride, n_rows, n_cols, bytes, true));
+    if (dx) {
+        RG_TRY(check_rows("dx", dx, dx_stride, n_rows, n_cols, bytes, true));
+        RG_TRY(check_place("dx", dx, dx_stride, dy, dy_stride, n_rows));
+    }
     RG_TRY(check_vector("weight", weight, weight_type, type));
     RG_TRY(check_vector("dweight", dweight, weight_type, type));
     RG_TRY(check_vector("dbias", dbias, weight_type, type));

@@ -7,7 +7,7 @@
 // Precision.  A rounding of X itself is noise in the directions of X's small singular values, which every step
 // multiplies by 3.4; a rounding of P only tilts the directions that are there.  So the state X is kept in fp32 and a X is added from it, and
 // only the operands of the products are 16 bits: fp16, scaled by 2^14, since nothing here is four or more (singular values stay below
-// 1.21, A's entries below 1.46, P's below 2.9).  A update of rank 8 with 16-bit products comes out 4e-4 off so (relative, 2-norm), 2e-2 with X in fp16,
+// 1.21, A's entries below 1.46, P's below 2.9).  An update of rank 8 with 16-bit products comes out 4e-4 off so (relative, 2-norm), 2e-2 with X in fp16,
 // 3e-1 with X in bf16.  For fp32 matrices an operand is the sum of two fp16 numbers, 22 bits, and a product is three: 4e-7 to 6e-6 off, as fp32 products are.
 // So it is for matrices of 16 bits whose narrower side is 32 or less: over so few singular values the roundings do not average out
 // (up to 9e-3 off with 2 rows, 2e-3 with 32), and their products cost nothing beside the launches.
@@ -229,14 +229,16 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
 }
 
 // ---------------------------------------------------------------- products
-// C = L R^T of a tile of TM x TN by WM x WN waves of BI x BJ blocks of 16 x 16; both operands run along K contiguously, K a multiple of 64.  Steps of
+// C = L R^T of a tile of TILE x TILE by WM x WN waves of BI x BJ blocks of 16 x 16; both operands run along K contiguously, K a multiple of 64.  Steps of
 // DEPTH along K pass through LDS, STAGES of them there: one is multiplied while the others arrive, written into LDS by the loads
 // themselves.  A row of a step is 16-byte chunks, stored in an order that depends on the row, so that the 16 lanes that LDS serves at a time (16 rows, one
 // chunk of each) fall on all banks once.
 //
-// What bounds a step is the sum of what LDS takes in, what the waves read from it and the matrix operations: all waves stand at the same
-// point of a step.  Larger tiles read less for the same products (16 bits, 4096 x 4096, K = 4096, us: tiles of 64 188, 128 128, 192 130, 256 104 to 120; the
-// library's product 112); smaller ones fill the chip with less work, where a third stage hides the way from memory (2048 x 2048, K = 2048, tiles of 128: 27 with two stages, 21).
+// What bounds a step is the sum of what LDS takes in, what the waves read from it and the matrix operations, which overlap in part: all waves stand at about
+// the same point of a step (2048 x 2048 fp32, X X^T by tiles of 128, us: 50; without matrix operations 37, without reads from LDS 42, without loads 44, matrix operations
+// alone 36, of which 12 are the launch, the first loads and the results).  Larger tiles read less for the same products (16 bits, a product 4096 x 4096 x 4096 alone, us: tiles of 64 190,
+// 128 129, 192 131; the library's 112); smaller ones fill the chip with less work (2048 x 2048 x 2048, the lower half, us: 64 21, 96 19, 128 19, 192 30), where a
+// third stage hides the way from memory (tiles of 128: 27 with two).
 //
 // Where there are no more tiles than compute units a wave alone on its vector unit waits for LDS most of a step.  KG > 1: KG waves share a block, each with
 // its own slices of a step; their sums meet in LDS at the end, and each finishes one block of the wave's BI x BJ.
@@ -250,12 +252,12 @@ struct Product {
     static constexpr int STAGE = 2 * TILE * DEPTH;               // numbers: L's rows, R's rows
     static constexpr int LDS_BYTES = STAGES * STAGE * 2;
     static constexpr int SIDE_LOADS = TILE * CHUNKS / THREADS;   // of a thread, to a step
-    static_assert(TILE * CHUNKS % THREADS == 0 && LDS_BYTES <= 160 * 1024, "");
+    static_assert(DEPTH % 64 == 0 && TILE * CHUNKS % THREADS == 0 && LDS_BYTES <= 160 * 1024, "");
     static constexpr int SLICES = DEPTH / 32 / KG;               // of a wave; what one matrix operation takes along K each, hi and lo parts by turns
     static_assert(DEPTH == SLICES * KG * 32 && SLICES % (SPLIT ? 2 : 1) == 0 && (KG == 1 || (KG == BI * BJ && WM * WN * KG * KG * 1024 <= LDS_BYTES)), "");
     typedef f32x4 Acc[BI][BJ];
 
-    static __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ (DEPTH >= 128 ? row & 15 : DEPTH == 64 ? (row >> 1) & 7 : (row >> 2) & 3); }
+    static __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ (DEPTH == 64 ? (row >> 1) & 7 : row & 15); }
 
     // Rows from first on of the operand, of which it has n_rows (what a tile has beyond is read from the last row and not used).
     struct Side { const f16 *rows; int32_t first, n_rows; };
@@ -974,6 +976,14 @@ rg_status check_array(uint32_t k, const char *what, const void *p, uint64_t stri
     return RG_OK;
 }
 
+// A result in the place of an input has its rows where the input has them.
+rg_status check_place(uint32_t k, const char *what, const void *out, uint64_t out_stride, const void *in, uint64_t in_stride, const rg_update &u)
+{
+    if (out != in || out_stride == in_stride || u.rows <= 1) return RG_OK;
+    set_error("matrix %u: %s: in place, but with another stride", k, what);
+    return RG_EINVAL;
+}
+
 rg_status workspace_of(const rg_update *u, uint32_t n, uint32_t type, uint64_t *bytes)
 {
     uint64_t most = 0;
@@ -1001,10 +1011,13 @@ rg_status run_updates(const rg_update *u, uint32_t n, uint32_t type, const Optio
         if (u[k].rows == 0 || u[k].cols == 0) continue;
         RG_TRY(check_array(k, "grad", u[k].grad, u[k].grad_stride, u[k], bytes, false));
         RG_TRY(check_array(k, "out", u[k].out, u[k].out_stride, u[k], bytes, true));
+        RG_TRY(check_place(k, "out", u[k].out, u[k].out_stride, u[k].grad, u[k].grad_stride, u[k]));
         if (!o.muon) continue;
         RG_TRY(check_array(k, "weight", u[k].weight, u[k].weight_stride, u[k], bytes, false));
         RG_TRY(check_array(k, "momentum", u[k].momentum, u[k].momentum_stride, u[k], 4, false));
         RG_TRY(check_array(k, "momentum_out", u[k].momentum_out, u[k].momentum_out_stride, u[k], 4, true));
+        RG_TRY(check_place(k, "out", u[k].out, u[k].out_stride, u[k].weight, u[k].weight_stride, u[k]));
+        RG_TRY(check_place(k, "momentum_out", u[k].momentum_out, u[k].momentum_out_stride, u[k].momentum, u[k].momentum_stride, u[k]));
     }
     uint64_t want = 0;
     RG_TRY(workspace_of(u, n, type, &want));

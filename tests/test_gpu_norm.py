@@ -318,3 +318,14 @@ def test_refusals(rg):
                 lambda: rg.rg_layer_norm(x, out=torch.empty((4, 32), device="cuda")), lambda: rg.rg_layer_norm_backward(x[:2], x, w, st[0], st[1])):
         with pytest.raises((AssertionError, KeyError)):
             bad()
+
+
+def test_in_place_with_another_stride_is_refused(rg):
+    """Rows that are written where other rows are still to be read."""
+    L = rg.lib()
+    buf = torch.zeros(4 * 80, device="cuda")
+    v = torch.ones((2, 4), device="cuda")
+    p = buf.data_ptr()
+    assert L.rg_layer_norm(p, 320, 4, 64, 0, None, None, 0, 1e-5, p, 256, v.data_ptr(), v.data_ptr(), None) == rg.RG_EINVAL
+    assert L.rg_layer_norm_backward(p, 320, buf.data_ptr(), 320, 4, 64, 0, None, 0, v.data_ptr(), v.data_ptr(), p, 256, None, None, None, 0, None) == rg.RG_EINVAL
+    assert L.rg_layer_norm(p, 320, 1, 64, 0, None, None, 0, 1e-5, p, 256, v.data_ptr(), v.data_ptr(), None) == rg.RG_OK       # a single row has no stride

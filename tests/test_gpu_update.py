@@ -272,3 +272,16 @@ def test_refusals(rg):
                 lambda: rg.rg_orthogonalize([g.cpu()]), lambda: rg.rg_muon_step([g], [g], [g.half()], lr=0.1), lambda: rg.rg_muon_step([g], [g], [], lr=0.1)):
         with pytest.raises((AssertionError, KeyError)):
             bad()
+
+
+def test_in_place_with_another_stride_is_refused(rg):
+    """Rows that are written where other rows are still to be read."""
+    buf = torch.zeros(64 * 80, device="cuda")
+    wide, tight = torch.as_strided(buf, (64, 64), (80, 1)), torch.as_strided(buf, (64, 64), (64, 1))
+    other = torch.zeros((64, 64), device="cuda")
+    for call in (lambda: rg.rg_orthogonalize([wide], out=[tight]),
+                 lambda: rg.rg_muon_step([wide], [other], [other.clone()], lr=0.1, out_weights=[tight]),
+                 lambda: rg.rg_muon_step([other], [other.clone()], [wide], lr=0.1, out_momenta=[tight])):
+        with pytest.raises(rg.RgError) as e:
+            call()
+        assert e.value.status == rg.RG_EINVAL
