@@ -144,7 +144,8 @@ inline uint64_t half_tiles(uint64_t n, uint64_t tile)
     return t * (t + 1) / 2;
 }
 inline uint64_t whole_tiles(uint64_t n, uint64_t m, uint64_t tile) { return (n + tile - 1) / tile * ((m + tile - 1) / tile); }
-// Names of tiles: 64, 96, 128, 192; and a tile of 64 whose waves are four times as many, a tile of 128 with less LDS, two of which share a compute unit.
+// Names of tiles: 64, 96, 128, 192; tiles of 32 and 64 whose blocks have two waves each (32, UPDATE_TILE_SHARED);
+// a tile of 128 with less LDS, two of which share a compute unit.
 constexpr int UPDATE_TILE_SHARED = 65, UPDATE_TILE_PAIR = 129;
 inline int tile_side(int tile) { return tile / 32 * 32; }
 // Of the tiles that no waves share the one whose launch is done first: so many tiles to the fullest compute unit, each at what it takes of one that is full (us a step of 64 along K, measured
@@ -163,8 +164,12 @@ template <typename F> inline int update_tile(F &&tiles, int n_cu, bool split)
     return best;
 }
 
+// Of the two shared tiles, which add along K in the same order: that of 32, as long as the chip holds all of them at once.  What a compute unit loads bounds them, and a
+// tile of 32 needs half of it (1999 x 517 fp32, us: X X^T by tiles of 64 16.5, of 32 10.8, A^2 9.7 and 6.0).
+template <typename F> inline int shared_tile(F &&tiles, int n_cu) { return tiles(32) <= (uint64_t)n_cu * 2 ? 32 : UPDATE_TILE_SHARED; }
+
 // How a matrix' products are made.  Nothing in a result may depend on what else is in the call.  Sums along K are taken in one order by all tiles but the
-// shared ones, which is why those go by the matrix alone.  Operands in two parts have two cross terms, added in an order that is another one in a
+// shared ones, so that whether tiles are shared goes by the matrix alone.  Operands in two parts have two cross terms, added in an order that is another one in a
 // tile's reflection: which elements are reflected, that is the symmetric products' tile, then goes by the matrix alone too.
 constexpr uint64_t TINY_WIDE = 256;
 struct UpdateKind {
@@ -181,7 +186,7 @@ inline UpdateKind update_kind(uint64_t rows, uint64_t cols, bool wide_type, int 
     // Shared tiles where there are so few that they do not fill the chip anyway.
     if (k.split && !wide_type) k.half_tile = k.whole_tile = UPDATE_TILE_SHARED;
     if (whole_tiles(n, m, 64) <= 256) k.whole_tile = UPDATE_TILE_SHARED;
-    if (k.whole_tile || half_tiles(n, 64) <= 64) k.half_tile = UPDATE_TILE_SHARED;
+    if (k.whole_tile || half_tiles(n, 32) <= 256) k.half_tile = UPDATE_TILE_SHARED;
     else if (k.split) k.half_tile = update_tile([&](int tile) { return half_tiles(n, tile); }, n_cu, true);
     return k;
 }

@@ -241,7 +241,8 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
 // third stage hides the way from memory (tiles of 128: 27 with two).
 //
 // Where there are no more tiles than compute units a wave alone on its vector unit waits for LDS most of a step.  KG > 1: KG waves share a block, each with
-// its own slices of a step; their sums meet in LDS at the end, and each finishes one block of the wave's BI x BJ.
+// its own slices of a step; their sums meet in LDS at the end, and each finishes one block of the wave's BI x BJ (or one of them the only block).  There the cross terms
+// of operands in two parts have sums of their own, lo hi + hi lo, so that a result and its reflection are the same bits whatever the tile.
 template <int WM, int WN, int BI, int BJ, int DEPTH_, int STAGES_, bool SPLIT_, int KG = 1>
 struct Product {
     static constexpr bool SPLIT = SPLIT_;
@@ -254,7 +255,8 @@ struct Product {
     static constexpr int SIDE_LOADS = TILE * CHUNKS / THREADS;   // of a thread, to a step
     static_assert(DEPTH % 64 == 0 && TILE * CHUNKS % THREADS == 0 && LDS_BYTES <= 160 * 1024, "");
     static constexpr int SLICES = DEPTH / 32 / KG;               // of a wave; what one matrix operation takes along K each, hi and lo parts by turns
-    static_assert(DEPTH == SLICES * KG * 32 && SLICES % (SPLIT ? 2 : 1) == 0 && (KG == 1 || (KG == BI * BJ && WM * WN * KG * KG * 1024 <= LDS_BYTES)), "");
+    static_assert(DEPTH == SLICES * KG * 32 && SLICES % (SPLIT ? 2 : 1) == 0 && (KG == 1 || ((KG == BI * BJ || BI * BJ == 1) && WM * WN * KG * BI * BJ * 1024 <= LDS_BYTES)), "");
+    static constexpr bool APART = SPLIT && KG > 1;               // sums of the cross terms
     typedef f32x4 Acc[BI][BJ];
 
     static __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ (DEPTH == 64 ? (row >> 1) & 7 : row & 15); }
@@ -317,6 +319,12 @@ struct Product {
         for (int i = 0; i < BI; ++i)
 #pragma unroll
             for (int j = 0; j < BJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        Acc lo_hi, hi_lo;
+        if constexpr (APART)
+#pragma unroll
+            for (int i = 0; i < BI; ++i)
+#pragma unroll
+                for (int j = 0; j < BJ; ++j) lo_hi[i][j] = hi_lo[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         const int row_l = (wave / WN) * BI * 16 + (lane & 15), row_r = TILE + (wave % WN) * BJ * 16 + (lane & 15);
         f16x8 l[SLICES][BI], r[SLICES][BJ];
         const auto read = [&](const f16 *stage, int s, f16x8 (&x)[BI], f16x8 (&y)[BJ]) {
@@ -326,11 +334,19 @@ struct Product {
 #pragma unroll
             for (int j = 0; j < BJ; ++j) y[j] = *reinterpret_cast<const f16x8 *>(stage + (row_r + j * 16) * DEPTH + slot);
         };
-        const auto multiply = [&](const f16x8 (&x)[BI], const f16x8 (&y)[BJ]) {
+        const auto add = [&](Acc &to, const f16x8 (&x)[BI], const f16x8 (&y)[BJ]) {
 #pragma unroll
             for (int i = 0; i < BI; ++i)
 #pragma unroll
-                for (int j = 0; j < BJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < BJ; ++j) to[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], to[i][j], 0, 0, 0);
+        };
+        const auto multiply = [&](int s) {                         // slice s, which has been read
+            if (SPLIT && s % 2 == 1) {
+                add(APART ? lo_hi : acc, l[s], r[s - 1]);
+                add(APART ? hi_lo : acc, l[s - 1], r[s]);
+            } else {
+                add(acc, l[s], r[s]);
+            }
         };
         // All stages are filled at first, and a stage again as soon as every wave has read the last of it, which is in the middle of a step: the barrier
         // there also says that the next step has arrived, whose first slice is read while the present one's last is multiplied.  Behind the last step the
@@ -344,15 +360,10 @@ struct Product {
                 for (int s = 0; s < SLICES; ++s) {
                     if (k0 + (group * SLICES + s) * 32 >= K) continue;                      // a slice is inside or outside as a whole
                     read(lds + k0 / DEPTH * STAGE, s, l[s], r[s]);
-                    if (SPLIT && s % 2 == 1) {
-                        multiply(l[s], r[s - 1]);                                           // lo hi, hi lo
-                        multiply(l[s - 1], r[s]);
-                    } else {
-                        multiply(l[s], r[s]);
-                    }
+                    multiply(s);
                 }
             arrive<0>();                                           // LDS is read, and may be written
-            finish(acc, lds, lane, group, wave);
+            finish(acc, lo_hi, hi_lo, lds, lane, group, wave);
             return;
         }
 #pragma unroll
@@ -386,29 +397,30 @@ struct Product {
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (KG > 1 && k0 + (group * SLICES + s) * 32 >= K) continue;              // a slice is inside or outside as a whole
-                if (SPLIT && s % 2 == 1) {
-                    multiply(l[s], r[s - 1]);                                               // lo hi, hi lo
-                    multiply(l[s - 1], r[s]);
-                } else {
-                    multiply(l[s], r[s]);
-                }
+                multiply(s);
             }
         }
         arrive<0>();                                               // a workgroup's LDS is not left with loads under way
-        finish(acc, lds, lane, group, wave);
+        finish(acc, lo_hi, hi_lo, lds, lane, group, wave);
     }
 
-    // The sums of the waves that share a block: each is left with one block, whole.
-    static __device__ __forceinline__ void finish(Acc &acc, f16 *lds, int lane, int group, int wave)
+    // The sums of the waves that share blocks: each is left with one block, whole.
+    static __device__ __forceinline__ void finish(Acc &acc, const Acc &lo_hi, const Acc &hi_lo, f16 *lds, int lane, int group, int wave)
     {
         if constexpr (KG > 1) {
+            constexpr int BLOCKS = BI * BJ;
             f32x4 *sums = reinterpret_cast<f32x4 *>(lds) + lane;   // [group][wave][block][lane]
 #pragma unroll
-            for (int b = 0; b < KG; ++b) sums[((group * WM * WN + wave) * KG + b) * 64] = acc[b / BJ][b % BJ];
+            for (int b = 0; b < BLOCKS; ++b) {
+                f32x4 v = acc[b / BJ][b % BJ];
+                if constexpr (APART) v += lo_hi[b / BJ][b % BJ] + hi_lo[b / BJ][b % BJ];
+                sums[((group * WM * WN + wave) * BLOCKS + b) * 64] = v;
+            }
             __syncthreads();
-            acc[0][0] = sums[(wave * KG + group) * 64];
+            if (group >= BLOCKS) return;
+            acc[0][0] = sums[(wave * BLOCKS + group) * 64];
 #pragma unroll
-            for (int q = 1; q < KG; ++q) acc[0][0] += sums[((q * WM * WN + wave) * KG + group) * 64];
+            for (int q = 1; q < KG; ++q) acc[0][0] += sums[((q * WM * WN + wave) * BLOCKS + group) * 64];
         }
     }
 
@@ -419,6 +431,7 @@ struct Product {
         const int lane = threadIdx.x & 63, group = (threadIdx.x >> 6) / (WM * WN), wave = (threadIdx.x >> 6) % (WM * WN);
         const int row = (wave / WN) * BI * 16 + (lane >> 4) * 4, column = (wave % WN) * BJ * 16 + (lane & 15);
         if constexpr (KG > 1) {
+            if (group >= BI * BJ) return;
             float v[4] = {acc[0][0][0], acc[0][0][1], acc[0][0][2], acc[0][0][3]};
             const int r = row + group / BJ * 16, c = column + group % BJ * 16;
             body(r, c, v, first(r, c));
@@ -817,6 +830,7 @@ template <typename T, typename Prod, bool LAST, bool MUON> rg_status launch_appl
 }
 
 // The tiles.
+template <bool SPLIT> using Tile32Shared = Product<2, 2, 1, 1, 128, 4, SPLIT, 2>;
 template <bool SPLIT> using Tile64Shared = Product<2, 4, 2, 1, 128, 4, SPLIT, 2>;
 template <bool SPLIT> using Tile64 = Product<2, 2, 2, 2, 64, 3, SPLIT>;
 template <bool SPLIT> using Tile96 = Product<2, 2, 3, 3, 64, 3, SPLIT>;
@@ -827,6 +841,7 @@ template <bool SPLIT> using Tile192 = Product<2, 4, 6, 3, 64, 3, SPLIT>;
 template <bool SPLIT, typename F> rg_status with_tile(int tile, F &&body)
 {
     switch (tile) {
+    case 32: return body(Tile32Shared<SPLIT>{});
     case UPDATE_TILE_SHARED: return body(Tile64Shared<SPLIT>{});
     case 64: return body(Tile64<SPLIT>{});
     case 96: return body(Tile96<SPLIT>{});
@@ -942,8 +957,12 @@ rg_status run_group(const UpdateKind &kind, int n_cu, const rg_update *const *u,
         return all;
     };
     Shape s{};
-    s.half_tile = kind.half_tile ? kind.half_tile : update_tile([&](int tile) { return tiles(tile, true); }, n_cu, kind.split);
-    s.whole_tile = kind.whole_tile ? kind.whole_tile : update_tile([&](int tile) { return tiles(tile, false); }, n_cu, kind.split);
+    const auto pick = [&](int asked, bool half) {
+        const auto count_of = [&](int tile) { return tiles(tile, half); };
+        return asked == UPDATE_TILE_SHARED ? shared_tile(count_of, n_cu) : asked ? asked : update_tile(count_of, n_cu, kind.split);
+    };
+    s.half_tile = pick(kind.half_tile, true);
+    s.whole_tile = pick(kind.whole_tile, false);
     for (Starts *p : {&g.sums, &g.starts, &g.half, &g.whole})
         for (uint32_t &x : p->first) x = UINT32_MAX;
     for (uint32_t k = 0; k < count; ++k) {
