@@ -340,14 +340,6 @@ struct Product {
 #pragma unroll
                 for (int j = 0; j < BJ; ++j) to[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[i], y[j], to[i][j], 0, 0, 0);
         };
-        const auto multiply = [&](int s) {                         // slice s, which has been read
-            if (SPLIT && s % 2 == 1) {
-                add(APART ? lo_hi : acc, l[s], r[s - 1]);
-                add(APART ? hi_lo : acc, l[s - 1], r[s]);
-            } else {
-                add(acc, l[s], r[s]);
-            }
-        };
         // All stages are filled at first, and a stage again as soon as every wave has read the last of it, which is in the middle of a step: the barrier
         // there also says that the next step has arrived, whose first slice is read while the present one's last is multiplied.  Behind the last step the
         // last one is loaded again, so that the number of loads under way stays the same, and read, so that there is no branch.
@@ -360,7 +352,12 @@ struct Product {
                 for (int s = 0; s < SLICES; ++s) {
                     if (k0 + (group * SLICES + s) * 32 >= K) continue;                      // a slice is inside or outside as a whole
                     read(lds + k0 / DEPTH * STAGE, s, l[s], r[s]);
-                    multiply(s);
+                    if (SPLIT && s % 2 == 1) {
+                        add(APART ? lo_hi : acc, l[s], r[s - 1]);
+                        add(APART ? hi_lo : acc, l[s - 1], r[s]);
+                    } else {
+                        add(acc, l[s], r[s]);
+                    }
                 }
             arrive<0>();                                           // LDS is read, and may be written
             finish(acc, lo_hi, hi_lo, lds, lane, group, wave);
@@ -397,7 +394,12 @@ struct Product {
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (KG > 1 && k0 + (group * SLICES + s) * 32 >= K) continue;              // a slice is inside or outside as a whole
-                multiply(s);
+                if (SPLIT && s % 2 == 1) {
+                    add(APART ? lo_hi : acc, l[s], r[s - 1]);
+                    add(APART ? hi_lo : acc, l[s - 1], r[s]);
+                } else {
+                    add(acc, l[s], r[s]);
+                }
             }
         }
         arrive<0>();                                               // a workgroup's LDS is not left with loads under way
