@@ -116,6 +116,16 @@ def test_many_matrices_in_one_call(rg, dtype):
     assert rg.rg_orthogonalize([]) == []
 
 
+@pytest.mark.parametrize("dtype", list(BOUND))
+@pytest.mark.parametrize("rows,cols", [(300, 400), (900, 200), (30, 2500)])
+def test_the_other_matrices_of_a_call_change_no_bit(rg, dtype, rows, cols):
+    """A dozen of one size are cut into larger tiles than one alone."""
+    gs = [made(rows, cols, dtype, k) for k in range(12)]
+    for g, o in zip(gs, rg.rg_orthogonalize(gs)):
+        assert torch.equal(o, rg.rg_orthogonalize([g])[0])
+    assert off(o, definition(g)) <= BOUND[dtype]
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("size", [1e-30, 1e-20, 1e-4, 1e10, 1e25, 3e36])
 def test_sizes(rg, dtype, size):
