@@ -45,6 +45,21 @@ __device__ __forceinline__ void load_weights(const void *p, uint32_t type, int64
     else load_pack(static_cast<const f16 *>(p) + c, v);
 }
 
+// A product that is rounded before it goes into a sum or a difference.  In dx what is rounded cancels: of a row of one column nothing is left, of one of two a part of
+// eps / variance, and a product that were fused with the difference behind it would leave its own rounding there instead.
+__device__ __forceinline__ float rounded(float a, float b)
+{
+#pragma clang fp contract(off)
+    return a * b;
+}
+
+// 1 / sqrt(v), rounded once: the device's approximation r, corrected by what v r^2 is off from one (r^2 in two parts).  Where that leaves the range, r as it is.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = rsqrtf(v), p = rounded(r, r), off = fmaf(-v, fmaf(r, r, -p), fmaf(-v, p, 1.f));
+    return fabsf(off) < 0.5f ? fmaf(0.5f * r, off, r) : r;
+}
+
 // Sums over all lanes of a row.  Beyond a wave they meet in LDS, in slots taken by turns: whoever writes a slot again has passed a barrier
 // that every wave reaches only after it has read that slot.
 template <int LANES, int N>
@@ -124,10 +139,10 @@ __global__ void __launch_bounds__(norm_threads(LANES)) norm_rows_kernel(NormArgs
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 v[j][e] -= mean;
-                s[0] += at.counts(j, e) ? v[j][e] * v[j][e] : 0.f;
+                s[0] += at.counts(j, e) ? rounded(v[j][e], v[j][e]) : 0.f;
             }
         row_sums<LANES>(s, slots, turn);
-        const float rstd = 1.f / sqrtf(s[0] * a.inv_cols + a.eps);
+        const float rstd = inverse_root(s[0] * a.inv_cols + a.eps);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
 #pragma unroll
@@ -190,22 +205,22 @@ __global__ void __launch_bounds__(norm_threads(LANES), LANES > 256 ? 1 : V * NV 
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                h[j][e] = (h[j][e] - this_mean) * this_rstd;
+                h[j][e] = rounded(h[j][e] - this_mean, this_rstd);
                 const float counted = at.counts(j, e) ? g[j][e] : 0.f;
-                const float along = at.counts(j, e) ? g[j][e] * h[j][e] : 0.f;
                 db[j][e] += counted;
-                dw[j][e] += along;
-                s[0] += counted * w[j][e];
-                s[1] += along * w[j][e];
+                dw[j][e] += at.counts(j, e) ? g[j][e] * h[j][e] : 0.f;
+                g[j][e] = rounded(g[j][e], w[j][e]);               // q from here on
+                s[0] += at.counts(j, e) ? g[j][e] : 0.f;
+                s[1] += at.counts(j, e) ? rounded(g[j][e], h[j][e]) : 0.f;
             }
         if (!a.out) continue;
         row_sums<LANES>(s, slots, turn);
-        const float m0 = s[0] * a.inv_cols, m1 = s[1] * a.inv_cols;
+        const float m0 = rounded(s[0], a.inv_cols), m1 = rounded(s[1], a.inv_cols);
         T *dx = reinterpret_cast<T *>(a.out + (uint64_t)row * a.out_stride);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) g[j][e] = this_rstd * (g[j][e] * w[j][e] - m0 - h[j][e] * m1);
+            for (int e = 0; e < V; ++e) g[j][e] = this_rstd * (g[j][e] - m0 - rounded(h[j][e], m1));
             if (at.stores(j)) store_pack(dx + at.column(j), g[j]);
         }
     }
@@ -319,7 +334,7 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_rows_kernel(NormArgs a
         __syncthreads();
         m = s[0];
         for (int k = 1; k < LONG_THREADS / 64; ++k) m = join(m, s[k]);
-        const float mean = m.mean, rstd = 1.f / sqrtf(m.m2 * a.inv_cols + a.eps);
+        const float mean = m.mean, rstd = inverse_root(m.m2 * a.inv_cols + a.eps);
         for (int64_t first = part.from + threadIdx.x; first < part.to; first += LONG_THREADS * AHEAD) {
             typename PackOf<T, V>::type raw[AHEAD];
 #pragma unroll

@@ -178,6 +178,27 @@ def test_large_means_and_sizes(rg, cols):
     compare(rg, *made(20, cols, torch.float32, torch.float32, 9, scale=1e-10), eps=0.0)
 
 
+def plain(x, dy, weight, eps=EPS):
+    """dx by the formula's operations in 32 bits, each rounded."""
+    x, dy, w, d = x.float(), dy.float(), weight.float(), x.shape[1]
+    c = x - (x.sum(1, keepdim=True) / d)
+    rstd = torch.rsqrt((c * c).sum(1, keepdim=True) / d + eps)
+    q, h = dy * w, c * rstd
+    return (rstd * (q - q.sum(1, keepdim=True) / d - h * ((q * h).sum(1, keepdim=True) / d)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("cols", [1, 2])
+def test_rows_of_which_nothing_is_left(rg, cols, dtype):
+    """What dx is made of cancels: wholly in a row of one column, and to eps / variance in one of two, where nothing but the roundings is left.
+    One is exactly zero, and the other as the rounded operations leave it, to the bit."""
+    x, dy, weight, bias = made(3001, cols, dtype, torch.float32, 5)
+    got = run_both(rg, x, dy, weight, bias)["dx"]
+    assert torch.equal(got, plain(x, dy, weight).to(dtype))
+    if cols == 1:
+        assert not got.any()
+
+
 def test_constant_rows(rg):
     x = torch.full((9, 300), 0.75, device="cuda")
     y, mean, rstd = rg.rg_layer_norm(x, None, None, eps=EPS)
