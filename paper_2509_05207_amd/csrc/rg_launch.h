@@ -171,10 +171,10 @@ template <typename F> inline int shared_tile(F &&tiles, int n_cu) { return tiles
 // How a matrix' products are made.  Nothing in a result may depend on what else is in the call.  Sums along K are taken in one order by all tiles but the
 // shared ones, so that whether tiles are shared goes by the matrix alone.  Operands in two parts have two cross terms, added in an order that is another one in a
 // tile's reflection: which elements are reflected, that is the symmetric products' tile, then goes by the matrix alone too.
-constexpr uint64_t TINY_WIDE = 256;
+constexpr uint64_t TINY_WIDE = 256, UPDATE_NARROW = 32;
 struct UpdateKind {
     bool tiny;                           // up to 64 x TINY_WIDE: a workgroup does it all
-    bool split;                          // operands in two parts: fp32, and 32 or less of the narrower side (see rg_update.hip)
+    bool split;                          // operands in two parts: fp32, and UPDATE_NARROW or less of the narrower side (see rg_update.hip)
     int half_tile, whole_tile;           // of the symmetric products and of the others; 0: by all matrices of a launch
     bool operator==(const UpdateKind &o) const { return tiny == o.tiny && split == o.split && half_tile == o.half_tile && whole_tile == o.whole_tile; }
 };
@@ -182,9 +182,8 @@ inline UpdateKind update_kind(uint64_t rows, uint64_t cols, bool wide_type, int 
 {
     const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);
     if (n <= 64 && m <= TINY_WIDE) return UpdateKind{true, true, 0, 0};
-    UpdateKind k{false, wide_type || n <= 32, 0, 0};
+    UpdateKind k{false, wide_type || n <= UPDATE_NARROW, 0, 0};
     // Shared tiles where there are so few that they do not fill the chip anyway.
-    if (k.split && !wide_type) k.half_tile = k.whole_tile = UPDATE_TILE_SHARED;
     if (whole_tiles(n, m, 64) <= 256) k.whole_tile = UPDATE_TILE_SHARED;
     if (k.whole_tile || half_tiles(n, 32) <= 256) k.half_tile = UPDATE_TILE_SHARED;
     else if (k.split) k.half_tile = update_tile([&](int tile) { return half_tiles(n, tile); }, n_cu, true);

@@ -9,8 +9,9 @@
 // only the operands of the products are 16 bits: fp16, scaled by 2^14, since nothing here is four or more (singular values stay below
 // 1.21, A's entries below 1.46, P's below 2.9).  An update of rank 8 with 16-bit products comes out 4e-4 off so (relative, 2-norm), 2e-2 with X in fp16,
 // 3e-1 with X in bf16.  For fp32 matrices an operand is the sum of two fp16 numbers, 22 bits, and a product is three: 4e-7 to 6e-6 off, as fp32 products are.
-// So it is for matrices of 16 bits whose narrower side is 32 or less: over so few singular values the roundings do not average out
-// (up to 9e-3 off with 2 rows, 2e-3 with 32), and their products cost nothing beside the launches.
+// So it is for matrices of 16 bits whose narrower side is 32 or less: over so few singular values, which a wide matrix has all alike, the roundings do not
+// average out (up to 9e-3 off with 2 rows).  Beyond that one part is off by 3e-3 (33 x 4,000) to 1.8e-3 (128 x 4,000), about what the result's own rounding to bf16 is, and
+// two would cost half as much again (100 x 4,096, us: 96, 138).
 //
 // The division by the norm is exact: X starts as G 2^-e with a norm in [1/2, 1), and the factor f = 2^e / (|G| + eps) that is left
 // goes into the first step's coefficients: P = b f^2 A + c f^4 A^2, X <- f (a X + P X).
@@ -235,11 +236,11 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
 // themselves.  A row of a step is 16-byte chunks, stored in an order that depends on the row, so that the 16 lanes that LDS serves at a time (16 rows, one
 // chunk of each) fall on all banks once.
 //
-// What bounds a step is the sum of what LDS takes in, what the waves read from it and the matrix operations, which overlap in part: all waves stand at about
-// the same point of a step (2048 x 2048 fp32, X X^T by tiles of 128, us: 50; without matrix operations 37, without reads from LDS 42, without loads 44, matrix operations
-// alone 36, of which 12 are the launch, the first loads and the results).  Larger tiles read less for the same products (16 bits, a product 4096 x 4096 x 4096 alone, us: tiles of 64 190,
-// 128 129, 192 131; the library's 112); smaller ones fill the chip with less work (2048 x 2048 x 2048, the lower half, us: 64 21, 96 19, 128 19, 192 30), where a
-// third stage hides the way from memory (tiles of 128: 27 with two).
+// A step is what LDS takes in, what the waves read from it and the matrix operations, which overlap in part: all waves stand at about the same point of a
+// step (4,096 x 4,096 bf16, X X^T by tiles of 192, us: 80; without matrix operations 51, without reads from LDS 59, without loads 68, matrix operations alone 51, loads
+// alone 51).  Larger tiles read less for the same products (the same matrix, tiles of 64, 96, 128, 192, us: X X^T 160, 119, 109, 80, P X 236, 206, 172, 174, and 168 by pairs of 128,
+// of which one finishes while the other multiplies); smaller ones fill the chip with less work (2,048 x 2,048, X X^T 25, 18, 21, 33, P X 41, 34, 30, 44).  Waves of 96 x 96 and 128 x 128,
+// one to a vector unit, read half as much and are slower: nothing else runs while such a wave waits (X X^T by tiles of 192 130).
 //
 // Where there are no more tiles than compute units a wave alone on its vector unit waits for LDS most of a step.  KG > 1: KG waves share a block, each with
 // its own slices of a step; their sums meet in LDS at the end, and each finishes one block of the wave's BI x BJ (or one of them the only block).  There the cross terms
@@ -509,8 +510,8 @@ __device__ __forceinline__ void half_tile(uint32_t t, int32_t &row, int32_t &col
     column = (int32_t)(t - r * (r + 1) / 2);
 }
 
-// A = X X^T (POLY false), P = b f^2 A + c f^4 A^2 (POLY true): the tiles of the lower half, and their reflections.  (4,096 x 4,096 bf16, us: 89 to 92, 760 TFLOP/s;
-// six of 1,024 x 4,096 43 and 19, 590 and 340.)
+// A = X X^T (POLY false), P = b f^2 A + c f^4 A^2 (POLY true): the tiles of the lower half, and their reflections.  (4,096 x 4,096 bf16, us: 81 and 86, 850 and 800 TFLOP/s;
+// six of 1,024 x 4,096 41 and 18, 630 and 360.)
 template <typename Prod, bool POLY>
 __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, bool first)
 {
