@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, boo
 }
 
 // X <- f (a X + P X); behind the last step the result goes out instead.  What a tile's results read and write (12 bytes an element, 16 in two parts) overlaps with another tile's
-// product where two share a compute unit.  (4,096 x 4,096 bf16, us: 173, 790 TFLOP/s; six of 1,024 x 4,096 131, 390 TFLOP/s beside 2.7 TB/s.)  Reads of X ahead of the
+// product where two share a compute unit.  (4,096 x 4,096 bf16, us: 175, 780 TFLOP/s; six of 1,024 x 4,096 134, 380 TFLOP/s beside 2.6 TB/s.)  Reads of X ahead of the
 // product gained nothing (1999 x 517 fp32, us: 17.6 so, 18.4 ahead).
 template <typename T, typename Prod, bool LAST, bool MUON>
 __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, uint32_t step)
