@@ -436,8 +436,9 @@ void rg_prefetcher_destroy(rg_prefetcher *p);
  * Strides are bytes between the starts of consecutive rows, multiples of the
  * element size; an output's is at least its row's bytes, so that the padded
  * rows of rg_gather_batch are taken as they are, and bytes between rows are left
- * untouched.  Arithmetic and sums are in 32 bits and more whatever the type; a
- * result is rounded once, to nearest even.  The same call gives the same bits.
+ * untouched.  Arithmetic and sums are in 32 bits and more whatever the type (the
+ * operands of rg_orthogonalize's products: 22, see there); a result is rounded
+ * once, to nearest even.  The same call gives the same bits.
  * RG_EINVAL: a null pointer, an unknown type, a stride or address that does not
  * suit the type; RG_ERANGE: a size beyond what is said here, or too small a
  * workspace.  Nothing is written then. */
@@ -498,10 +499,11 @@ rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, const void 
  *   type     of grad, weight and out; momenta are fp32
  *   steps    1 to RG_MAX_STEPS
  *   workspace  dev, 256-byte aligned, as many bytes as rg_update_workspace says for the same u
- * The state X is fp32 throughout.  Products take it rounded to 16 bits for the
- * 16-bit types (the result is off by 3e-3 and less, 2-norm), in two such parts, 22 bits, for
- * RG_F32 and where the narrower side is 32 or less.  A matrix with an infinity or a NaN comes out
- * all NaN.  rows and cols up to RG_MAX_SIDE; matrices without elements are passed over.
+ * The state X is fp32 throughout and sums are in 32 bits; the operands of the
+ * products have 22 bits, and none below 2^-38 of the matrix' norm, whatever the
+ * type.  Before its rounding a result is off by 1e-5 and less of its 2-norm, or
+ * 1.2e-4 where G's singular values lie further apart than a factor of a hundred.
+ * A matrix with an infinity or a NaN comes out all NaN.  rows and cols up to RG_MAX_SIDE; matrices without elements are passed over.
  * Outputs may be the inputs that they replace, with the same stride; other
  * overlaps, also between matrices, are not allowed.
  */

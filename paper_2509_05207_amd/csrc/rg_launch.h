@@ -174,10 +174,11 @@ template <typename F> inline int shared_tile(F &&tiles, int n_cu) { return tiles
 constexpr uint64_t TINY_WIDE = 256, UPDATE_NARROW = 32;
 struct UpdateKind {
     bool tiny;                           // up to 64 x TINY_WIDE: a workgroup does it all
-    bool split;                          // operands in two parts: fp32, and UPDATE_NARROW or less of the narrower side (see rg_update.hip)
+    bool split;                          // operands in two parts
     int half_tile, whole_tile;           // of the symmetric products and of the others; 0: by all matrices of a launch
     bool operator==(const UpdateKind &o) const { return tiny == o.tiny && split == o.split && half_tile == o.half_tile && whole_tile == o.whole_tile; }
 };
+// wide_type: two parts whatever the size, which is what a result that is rounded once takes, of any type (rg_update.hip asks for nothing else).
 inline UpdateKind update_kind(uint64_t rows, uint64_t cols, bool wide_type, int n_cu)
 {
     const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);

@@ -5,13 +5,11 @@
 // reflection.  Large matrices are bound by the matrix cores, small ones by the launches.
 //
 // Precision.  A rounding of X itself is noise in the directions of X's small singular values, which every step
-// multiplies by 3.4; a rounding of P only tilts the directions that are there.  So the state X is kept in fp32 and a X is added from it, and
-// only the operands of the products are 16 bits: fp16, scaled by 2^14, since nothing here is four or more (singular values stay below
-// 1.21, A's entries below 1.46, P's below 2.9).  An update of rank 8 with 16-bit products comes out 4e-4 off so (relative, 2-norm), 2e-2 with X in fp16,
-// 3e-1 with X in bf16.  For fp32 matrices an operand is the sum of two fp16 numbers, 22 bits, and a product is three: 4e-7 to 6e-6 off, as fp32 products are.
-// So it is for matrices of 16 bits whose narrower side is 32 or less: over so few singular values, which a wide matrix has all alike, the roundings do not
-// average out (up to 9e-3 off with 2 rows).  Beyond that one part is off by 3e-3 (33 x 4,000) to 1.8e-3 (128 x 4,000), about what the result's own rounding to bf16 is, and
-// two would cost half as much again (100 x 4,096, us: 96, 138).
+// multiplies by 3.4; a rounding of P only tilts the directions that are there.  So the state X is kept in fp32 and a X is added from it.  The operands of
+// the products are fp16 numbers, scaled by 2^14, since nothing here is four or more (singular values stay below 1.21, A's entries below 1.46, P's below 2.9), and
+// always the sum of two, 22 bits, with no digits below 2^-38 of the matrix' norm; a product is three, hi hi + hi lo + lo hi.  Results are 1e-7 to 6e-6 off so (relative, 2-norm), as much as by
+// fp32 products, whatever the type; its own rounding comes last, once.  One part, 11 bits, is not enough for matrices of 16 bits either: roundings of singular values that are alike
+// do not average out (43 rows of a unit matrix 8e-3 off, 48 x 4,096 orthonormal rows 4e-3, 400 x 500 of noise 1.6e-3, where rounding to bf16 costs 1.7e-3 and to fp16 2e-4).
 //
 // The division by the norm is exact: X starts as G 2^-e with a norm in [1/2, 1), and the factor f = 2^e / (|G| + eps) that is left
 // goes into the first step's coefficients: P = b f^2 A + c f^4 A^2, X <- f (a X + P X).
@@ -38,12 +36,12 @@ typedef f16 f16x8 __attribute__((ext_vector_type(8)));
 typedef f16 f16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// An operand's rows: the fp16 numbers nearest to its values; in two parts, every 32 of them are followed by the 32 nearest to what they leave, so
-// that both parts of a piece lie in one line of 128 bytes.
-template <bool SPLIT> __host__ __device__ __forceinline__ uint32_t row_length(int32_t n) { return SPLIT ? 2u * (uint32_t)n : (uint32_t)n; }
-template <bool SPLIT> __device__ __forceinline__ uint64_t place(int32_t row, int32_t column, int32_t n_columns)
+// An operand's rows: the fp16 numbers nearest to its values, every 32 of them followed by the 32 nearest to what they leave, so that both parts
+// of a piece lie in one line of 128 bytes.
+__host__ __device__ __forceinline__ uint32_t row_length(int32_t n) { return 2u * (uint32_t)n; }
+__device__ __forceinline__ uint64_t place(int32_t row, int32_t column, int32_t n_columns)
 {
-    return (uint64_t)row * row_length<SPLIT>(n_columns) + (SPLIT ? (uint32_t)column + ((uint32_t)column & ~31u) : (uint32_t)column);
+    return (uint64_t)row * row_length(n_columns) + (uint32_t)column + ((uint32_t)column & ~31u);
 }
 constexpr int LO = 32;                   // from a number to what it leaves
 
@@ -144,18 +142,16 @@ __global__ void __launch_bounds__(256) update_sums_kernel(Group g)
 
 // ---------------------------------------------------------------- X in the layouts of the products
 // V consecutive numbers of an operand (V divides 32).
-template <bool SPLIT, int V> __device__ __forceinline__ void put(f16 *to, const float (&v)[V])
+template <int V> __device__ __forceinline__ void put(f16 *to, const float (&v)[V])
 {
     typedef f16 P __attribute__((ext_vector_type(V)));
     P h;
 #pragma unroll
     for (int e = 0; e < V; ++e) h[e] = (f16)v[e];
     *reinterpret_cast<P *>(to) = h;
-    if constexpr (SPLIT) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) h[e] = (f16)(v[e] - (float)h[e]);
-        *reinterpret_cast<P *>(to + LO) = h;
-    }
+    for (int e = 0; e < V; ++e) h[e] = (f16)(v[e] - (float)h[e]);
+    *reinterpret_cast<P *>(to + LO) = h;
 }
 
 // f of a matrix of this norm, which starts as G 2^-e2.
@@ -168,7 +164,7 @@ __device__ __forceinline__ float factor_of(double norm, float eps, int &e2)
 }
 
 // A workgroup takes 64 x 64 elements of the padded X, which go through LDS to be written by columns too.  Bound by HBM.  (The same six, us: 68; 352 MB, 5.2 TB/s.)
-template <typename T, bool SPLIT>
+template <typename T>
 __global__ void __launch_bounds__(256) update_start_kernel(Group g)
 {
     uint32_t tile;
@@ -223,10 +219,10 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
         *reinterpret_cast<f32x4 *>(m.x + row + 4) = f32x4{x[4], x[5], x[6], x[7]};
 #pragma unroll
         for (int e = 0; e < PACK; ++e) x[e] *= SCALE;
-        put<SPLIT>(m.xr + place<SPLIT>(i0 + line, j0 + c, m.m_pad), x);
+        put(m.xr + place(i0 + line, j0 + c, m.m_pad), x);
 #pragma unroll
         for (int e = 0; e < PACK; ++e) x[e] = block[c + e][line] * SCALE;
-        put<SPLIT>(m.xt[0] + place<SPLIT>(j0 + line, i0 + c, m.n_pad), x);
+        put(m.xt[0] + place(j0 + line, i0 + c, m.n_pad), x);
     }
 }
 
@@ -245,9 +241,8 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
 // Where there are no more tiles than compute units a wave alone on its vector unit waits for LDS most of a step.  KG > 1: KG waves share a block, each with
 // its own slices of a step; their sums meet in LDS at the end, and each finishes one block of the wave's BI x BJ (or one of them the only block).  There the cross terms
 // of operands in two parts have sums of their own, lo hi + hi lo, so that a result and its reflection are the same bits whatever the tile.
-template <int WM, int WN, int BI, int BJ, int DEPTH_, int STAGES_, bool SPLIT_, int KG = 1>
+template <int WM, int WN, int BI, int BJ, int DEPTH_, int STAGES_, int KG = 1>
 struct Product {
-    static constexpr bool SPLIT = SPLIT_;
     static constexpr int DEPTH = DEPTH_, STAGES = STAGES_;       // DEPTH: numbers of a row in a step, of both parts together
     static constexpr int THREADS = WM * WN * KG * 64, TILE = WM * BI * 16;
     static_assert(TILE == WN * BJ * 16, "the lower half of a symmetric product is made of square tiles");
@@ -257,8 +252,8 @@ struct Product {
     static constexpr int SIDE_LOADS = TILE * CHUNKS / THREADS;   // of a thread, to a step
     static_assert(DEPTH % 64 == 0 && TILE * CHUNKS % THREADS == 0 && LDS_BYTES <= 160 * 1024, "");
     static constexpr int SLICES = DEPTH / 32 / KG;               // of a wave; what one matrix operation takes along K each, hi and lo parts by turns
-    static_assert(DEPTH == SLICES * KG * 32 && SLICES % (SPLIT ? 2 : 1) == 0 && (KG == 1 || ((KG == BI * BJ || BI * BJ == 1) && WM * WN * KG * BI * BJ * 1024 <= LDS_BYTES)), "");
-    static constexpr bool APART = SPLIT && KG > 1;               // sums of the cross terms
+    static_assert(DEPTH == SLICES * KG * 32 && SLICES % 2 == 0 && (KG == 1 || ((KG == BI * BJ || BI * BJ == 1) && WM * WN * KG * BI * BJ * 1024 <= LDS_BYTES)), "");
+    static constexpr bool APART = KG > 1;                        // sums of the cross terms
     typedef f32x4 Acc[BI][BJ];
 
     static __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ (DEPTH == 64 ? (row >> 1) & 7 : row & 15); }
@@ -299,7 +294,7 @@ struct Product {
         __builtin_amdgcn_sched_barrier(0);
     }
 
-    // K: numbers along a row of the operands, of both parts together; a multiple of 64, SPLIT 128
+    // K: numbers along a row of the operands, of both parts together; a multiple of 128
     static __device__ __forceinline__ void run(const Side &L, const Side &R, int32_t K, f16 *lds, Acc &acc)
     {
         // The wave's number is the same in all its lanes, and the compiler has to know: matrix operations take no heed of which lanes are active, so that a
@@ -358,7 +353,7 @@ struct Product {
                     read(lds + k0 / DEPTH * STAGE, s, l[s], r[s]);
 #pragma unroll
                     for (int i = 0; i < BI; ++i)
-                        if (SPLIT && s % 2 == 1) {
+                        if (s % 2 == 1) {
                             add_row(APART ? lo_hi : acc, i, l[s], r[s - 1]);
                             add_row(APART ? hi_lo : acc, i, l[s - 1], r[s]);
                         } else {
@@ -412,7 +407,7 @@ struct Product {
                             if (q < 2 * SIDE_LOADS) src.load_one(min(k0 + STAGES * DEPTH, last), stage, q / SIDE_LOADS, q % SIDE_LOADS);
                     __builtin_amdgcn_sched_barrier(0);
                     if (inside) {
-                        if (SPLIT && s % 2 == 1) {
+                        if (s % 2 == 1) {
                             add_row(APART ? lo_hi : acc, i, l[s], r[s - 1]);
                             add_row(APART ? hi_lo : acc, i, l[s - 1], r[s]);
                         } else {
@@ -523,7 +518,7 @@ __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, boo
     const f16 *from = POLY ? m.a : m.xr;
     f16 *to = POLY ? m.p : m.a;
     typename Prod::Acc acc;
-    Prod::run({from, ti * Prod::TILE, m.n_pad}, {from, tj * Prod::TILE, m.n_pad}, (int32_t)row_length<Prod::SPLIT>(POLY ? m.n_pad : m.m_pad), reinterpret_cast<f16 *>(lds_bytes), acc);
+    Prod::run({from, ti * Prod::TILE, m.n_pad}, {from, tj * Prod::TILE, m.n_pad}, (int32_t)row_length(POLY ? m.n_pad : m.m_pad), reinterpret_cast<f16 *>(lds_bytes), acc);
     float cb = NS_B, cc = NS_C * UNSCALE;
     if (POLY && first) {
         const float f = *m.factor;
@@ -537,9 +532,9 @@ __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, boo
         const int32_t i = ti * Prod::TILE + r, j = tj * Prod::TILE + c;
         Four a = {};
         if (POLY && inside(i, j)) {
-            const f16 *from_a = m.a + place<Prod::SPLIT>(j, i, m.n_pad);
+            const f16 *from_a = m.a + place(j, i, m.n_pad);
             a.hi = *reinterpret_cast<const f16x4 *>(from_a);
-            if constexpr (Prod::SPLIT) a.lo = *reinterpret_cast<const f16x4 *>(from_a + LO);
+            a.lo = *reinterpret_cast<const f16x4 *>(from_a + LO);
         }
         return a;
     };
@@ -548,9 +543,9 @@ __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, boo
         if (!inside(i, j)) return;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = POLY ? cb * ((float)a.hi[e] + (float)a.lo[e]) + cc * v[e] : v[e] * UNSCALE;
-        if (ti != tj) put<Prod::SPLIT>(to + place<Prod::SPLIT>(j, i, m.n_pad), v);
+        if (ti != tj) put(to + place(j, i, m.n_pad), v);
         quad_transpose(v);
-        put<Prod::SPLIT>(to + place<Prod::SPLIT>(i + (int32_t)(threadIdx.x & 3), j & ~3, m.n_pad), v);
+        put(to + place(i + (int32_t)(threadIdx.x & 3), j & ~3, m.n_pad), v);
     });
 }
 
@@ -569,7 +564,7 @@ __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, ui
     const uint32_t band = t / (down * ABREAST), in_band = t - band * down * ABREAST, width = min(ABREAST, across - band * ABREAST);
     const int32_t ti = (int32_t)(in_band / width), tj = (int32_t)(band * ABREAST + in_band % width);
     typename Prod::Acc acc;
-    Prod::run({m.p, ti * Prod::TILE, m.n_pad}, {m.xt[step & 1], tj * Prod::TILE, m.m_pad}, (int32_t)row_length<Prod::SPLIT>(m.n_pad), reinterpret_cast<f16 *>(lds_bytes), acc);
+    Prod::run({m.p, ti * Prod::TILE, m.n_pad}, {m.xt[step & 1], tj * Prod::TILE, m.m_pad}, (int32_t)row_length(m.n_pad), reinterpret_cast<f16 *>(lds_bytes), acc);
     f16 *next = m.xt[(step & 1) ^ 1];
     const float f = step == 0 ? *m.factor : 1.f;
     const float grow = MUON ? g.lr * sqrtf(fmaxf(1.f, (float)m.u.rows / (float)m.u.cols)) : 0.f;
@@ -623,9 +618,9 @@ __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, ui
             *reinterpret_cast<f32x4 *>(m.x + (uint64_t)(i0 + mine) * m.m_pad + (j & ~3)) = f32x4{v[0], v[1], v[2], v[3]};
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= SCALE;
-            put<Prod::SPLIT>(m.xr + place<Prod::SPLIT>(i0 + mine, j & ~3, m.m_pad), v);
+            put(m.xr + place(i0 + mine, j & ~3, m.m_pad), v);
             quad_transpose(v);
-            put<Prod::SPLIT>(next + place<Prod::SPLIT>(j, i0, m.n_pad), v);
+            put(next + place(j, i0, m.n_pad), v);
         }
     });
 }
@@ -684,7 +679,7 @@ __global__ void __launch_bounds__(TINY_THREADS) update_tiny_kernel(Group g, uint
     const Matrix &m = g.mat[blockIdx.x];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
     f16 *rows = reinterpret_cast<f16 *>(lds_bytes), *square = rows + 64 * TINY_WIDE * 2;
-    const uint32_t length = row_length<true>(m.m_pad);
+    const uint32_t length = row_length(m.m_pad);
     // Where element e of block b of strip s is in X.
     const auto row_of = [&](int b, int e) { return b * 16 + (lane >> 4) * 4 + e; };
     const auto column_of = [&](int s) { return (wave + s * TINY_WAVES) * 16 + (lane & 15); };
@@ -856,24 +851,24 @@ template <typename T, typename Prod, bool LAST, bool MUON> rg_status launch_appl
 }
 
 // The tiles.
-template <bool SPLIT> using Tile32Shared = Product<2, 2, 1, 1, 128, 4, SPLIT, 2>;
-template <bool SPLIT> using Tile64Shared = Product<2, 4, 2, 1, 128, 4, SPLIT, 2>;
-template <bool SPLIT> using Tile64 = Product<2, 2, 2, 2, 64, 3, SPLIT>;
-template <bool SPLIT> using Tile96 = Product<2, 2, 3, 3, 64, 3, SPLIT>;
-template <bool SPLIT> using Tile128 = Product<2, 4, 4, 2, 64, 3, SPLIT>;
-template <bool SPLIT> using Tile128Pair = Product<2, 4, 4, 2, 64, 2, SPLIT>;
-template <bool SPLIT> using Tile192 = Product<2, 4, 6, 3, 64, 3, SPLIT>;
+using Tile32Shared = Product<2, 2, 1, 1, 128, 4, 2>;
+using Tile64Shared = Product<2, 4, 2, 1, 128, 4, 2>;
+using Tile64 = Product<2, 2, 2, 2, 64, 3>;
+using Tile96 = Product<2, 2, 3, 3, 64, 3>;
+using Tile128 = Product<2, 4, 4, 2, 64, 3>;
+using Tile128Pair = Product<2, 4, 4, 2, 64, 2>;
+using Tile192 = Product<2, 4, 6, 3, 64, 3>;
 
-template <bool SPLIT, typename F> rg_status with_tile(int tile, F &&body)
+template <typename F> rg_status with_tile(int tile, F &&body)
 {
     switch (tile) {
-    case 32: return body(Tile32Shared<SPLIT>{});
-    case UPDATE_TILE_SHARED: return body(Tile64Shared<SPLIT>{});
-    case 64: return body(Tile64<SPLIT>{});
-    case 96: return body(Tile96<SPLIT>{});
-    case 128: return body(Tile128<SPLIT>{});
-    case UPDATE_TILE_PAIR: return body(Tile128Pair<SPLIT>{});
-    case 192: return body(Tile192<SPLIT>{});
+    case 32: return body(Tile32Shared{});
+    case UPDATE_TILE_SHARED: return body(Tile64Shared{});
+    case 64: return body(Tile64{});
+    case 96: return body(Tile96{});
+    case 128: return body(Tile128{});
+    case UPDATE_TILE_PAIR: return body(Tile128Pair{});
+    case 192: return body(Tile192{});
     }
     set_error("no product of tiles of %d", tile);
     return RG_EHIP;
@@ -881,19 +876,19 @@ template <bool SPLIT, typename F> rg_status with_tile(int tile, F &&body)
 
 struct Shape { uint32_t sums, starts, half, whole; int half_tile, whole_tile; };
 
-template <typename T, bool SPLIT>
+template <typename T>
 rg_status launch_group(const Group &g, uint32_t steps, const Shape &s, hipStream_t st)
 {
     hipLaunchKernelGGL(update_sums_kernel<T>, dim3(s.sums), dim3(256), 0, st, g);
     RG_HIP(hipGetLastError());
-    hipLaunchKernelGGL((update_start_kernel<T, SPLIT>), dim3(s.starts), dim3(256), 0, st, g);
+    hipLaunchKernelGGL(update_start_kernel<T>, dim3(s.starts), dim3(256), 0, st, g);
     RG_HIP(hipGetLastError());
     for (uint32_t k = 0; k < steps; ++k) {
-        RG_TRY(with_tile<SPLIT>(s.half_tile, [&](auto p) {
+        RG_TRY(with_tile(s.half_tile, [&](auto p) {
             RG_TRY((launch_half<decltype(p), false>(g, s.half, k, st)));
             return launch_half<decltype(p), true>(g, s.half, k, st);
         }));
-        RG_TRY(with_tile<SPLIT>(s.whole_tile, [&](auto p) {
+        RG_TRY(with_tile(s.whole_tile, [&](auto p) {
             if (k + 1 < steps) return launch_apply<float, decltype(p), false, false>(g, s.whole, k, st);        // T plays no part in it
             return g.muon ? launch_apply<T, decltype(p), true, true>(g, s.whole, k, st) : launch_apply<T, decltype(p), true, false>(g, s.whole, k, st);
         }));
@@ -934,20 +929,19 @@ void lay_out(Matrix &m, const rg_update &u, const UpdateKind &kind, Carver &c)
     c.take(m.factor, 1);
     if (kind.tiny) return;                                         // all the rest in registers and LDS
     c.take(m.x, nm);
-    const uint64_t parts = kind.split ? 2 : 1;
-    for (f16 **p : {&m.xr, &m.xt[0], &m.xt[1]}) c.take(*p, nm * parts);
-    for (f16 **p : {&m.a, &m.p}) c.take(*p, nn * parts);
+    for (f16 **p : {&m.xr, &m.xt[0], &m.xt[1]}) c.take(*p, nm * 2);
+    for (f16 **p : {&m.a, &m.p}) c.take(*p, nn * 2);
 }
 
 // Groups of matrices of a size class, in order, each with the whole workspace to itself.
 struct Options { bool muon, nesterov; float momentum, lr, weight_decay, eps; uint32_t steps; };
 
-template <typename F> rg_status each_group(const rg_update *u, uint32_t n, uint32_t type, F &&body)
+template <typename F> rg_status each_group(const rg_update *u, uint32_t n, F &&body)
 {
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
     const auto empty = [&](uint32_t k) { return u[k].rows == 0 || u[k].cols == 0; };
-    const auto kind_of = [&](uint32_t k) { return update_kind(u[k].rows, u[k].cols, type == RG_F32, n_cu); };
+    const auto kind_of = [&](uint32_t k) { return update_kind(u[k].rows, u[k].cols, true, n_cu); };
     for (uint32_t first = 0; first < n; ++first) {
         if (empty(first)) continue;
         const UpdateKind kind = kind_of(first);
@@ -969,7 +963,6 @@ template <typename F> rg_status each_group(const rg_update *u, uint32_t n, uint3
 template <typename T>
 rg_status run_group(const UpdateKind &kind, int n_cu, const rg_update *const *u, uint32_t count, const Options &o, uint8_t *workspace, hipStream_t st)
 {
-    constexpr bool WIDE = sizeof(T) == 4;
     Group g{};
     g.muon = o.muon; g.nesterov = o.nesterov;
     g.momentum = o.momentum; g.lr = o.lr; g.keep = (float)(1.0 - (double)o.lr * (double)o.weight_decay);
@@ -1000,7 +993,7 @@ rg_status run_group(const UpdateKind &kind, int n_cu, const rg_update *const *u,
         s.half += (uint32_t)half_tiles(m.n_pad, tile_side(s.half_tile));
         s.whole += (uint32_t)whole_tiles(m.n_pad, m.m_pad, tile_side(s.whole_tile));
     }
-    return kind.split ? launch_group<T, true>(g, o.steps, s, st) : launch_group<T, WIDE>(g, o.steps, s, st);
+    return launch_group<T>(g, o.steps, s, st);
 }
 
 rg_status check_updates(const rg_update *u, uint32_t n, uint32_t type)
@@ -1029,10 +1022,10 @@ rg_status check_place(uint32_t k, const char *what, const void *out, uint64_t ou
     return RG_EINVAL;
 }
 
-rg_status workspace_of(const rg_update *u, uint32_t n, uint32_t type, uint64_t *bytes)
+rg_status workspace_of(const rg_update *u, uint32_t n, uint64_t *bytes)
 {
     uint64_t most = 0;
-    RG_TRY(each_group(u, n, type, [&](const UpdateKind &kind, int, const rg_update *const *picked, uint32_t count) {
+    RG_TRY(each_group(u, n, [&](const UpdateKind &kind, int, const rg_update *const *picked, uint32_t count) {
         Carver c{nullptr};
         for (uint32_t k = 0; k < count; ++k) {
             Matrix m;
@@ -1065,12 +1058,12 @@ rg_status run_updates(const rg_update *u, uint32_t n, uint32_t type, const Optio
         RG_TRY(check_place(k, "momentum_out", u[k].momentum_out, u[k].momentum_out_stride, u[k].momentum, u[k].momentum_stride, u[k]));
     }
     uint64_t want = 0;
-    RG_TRY(workspace_of(u, n, type, &want));
+    RG_TRY(workspace_of(u, n, &want));
     if (want && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256)) { set_error("the workspace is null or not aligned to 256 bytes"); return RG_EINVAL; }
     if (workspace_bytes < want) { set_error("the workspace holds %llu bytes of %llu", (unsigned long long)workspace_bytes, (unsigned long long)want); return RG_ERANGE; }
     const hipStream_t st = as_stream(stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    return each_group(u, n, type, [&](const UpdateKind &kind, int n_cu, const rg_update *const *picked, uint32_t count) {
+    return each_group(u, n, [&](const UpdateKind &kind, int n_cu, const rg_update *const *picked, uint32_t count) {
         return type == RG_F32 ? run_group<float>(kind, n_cu, picked, count, o, ws, st) : type == RG_BF16 ? run_group<bf16>(kind, n_cu, picked, count, o, ws, st) : run_group<f16>(kind, n_cu, picked, count, o, ws, st);
     });
 }
@@ -1084,7 +1077,7 @@ extern "C" rg_status rg_update_workspace(const rg_update *u, uint32_t n, uint32_
 {
     if (!bytes) { set_error("null argument"); return RG_EINVAL; }
     RG_TRY(check_updates(u, n, type));
-    return workspace_of(u, n, type, bytes);
+    return workspace_of(u, n, bytes);
 }
 
 extern "C" rg_status rg_orthogonalize(const rg_update *u, uint32_t n, uint32_t type, uint32_t steps, float eps, void *workspace, uint64_t workspace_bytes, void *stream)

@@ -295,3 +295,40 @@ def test_in_place_with_another_stride_is_refused(rg):
         with pytest.raises(rg.RgError) as e:
             call()
         assert e.value.status == rg.RG_EINVAL
+
+
+def structured(kind, rows, cols, dtype):
+    """Matrices whose singular values are all alike, so that their roundings are too and do not average out; and noise."""
+    if kind == "unit":
+        t = torch.zeros((rows, cols), dtype=torch.float64, device="cuda")
+        t.fill_diagonal_(1.0)
+    elif kind == "orthonormal":
+        g = torch.Generator().manual_seed(rows)
+        t = torch.linalg.qr(torch.randn((max(rows, cols), min(rows, cols)), generator=g, dtype=torch.float64))[0]
+        t = (t.t() if rows < cols else t).contiguous().cuda()
+    else:
+        return made(rows, cols, dtype, rows + 3 * cols, kind)
+    return t.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", list(BOUND))
+@pytest.mark.parametrize("kind,rows,cols", [("unit", 43, 300), ("unit", 400, 74), ("unit", 79, 260), ("unit", 300, 310), ("orthonormal", 48, 4096), ("orthonormal", 900, 500), ("orthonormal", 1400, 1500),
+                                            ("noise", 33, 300), ("noise", 4000, 33), ("noise", 100, 4096), ("noise", 1300, 1400), ("low", 300, 250)])
+def test_a_result_is_rounded_once(rg, kind, rows, cols, dtype):
+    """Whatever the type, operands have 22 bits (the bounds of fp32 above), and a result is their type's number nearest to what they give.  Of an error e before it a rounding to a grid makes at most
+    2 |e| + the distance of the exact result from the grid."""
+    g = structured(kind, rows, cols, dtype)
+    want = definition(g)
+    assert off(rg.rg_orthogonalize([g])[0], want) <= 2 * (1.2e-4 if kind == "low" else 1e-5) + off(want.to(dtype), want)
+
+
+@pytest.mark.parametrize("dtype", list(BOUND))
+@pytest.mark.parametrize("rows,cols", [(43, 300), (1400, 1300)])
+def test_muon_step_is_rounded_once(rg, dtype, rows, cols):
+    """The same of the new weights: the update's error, lr times as large, and one rounding."""
+    w, g, m = made(rows, cols, dtype, 20), structured("unit", rows, cols, dtype), torch.zeros((rows, cols), device="cuda")
+    want, _ = step_definition(w, g, m, 0.5, 0.1, 0.9, True)
+    before = float((want - w.double() * (1 - 0.5 * 0.1)).norm())
+    rg.rg_muon_step([w], [g], [m], lr=0.5, weight_decay=0.1, momentum=0.9)
+    # the sum's own rounding to fp32, two of them
+    assert float((w.double() - want).norm()) <= 2 * (1e-5 * before + 2.0 ** -23 * float(want.norm())) + float((want.to(dtype).double() - want).norm())
