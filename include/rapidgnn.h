@@ -468,11 +468,11 @@ rg_status rg_layer_norm(const void *x, uint64_t x_stride, uint64_t n_rows, uint6
  *     dweight = sum over the rows of dy * xhat,  dbias = sum over the rows of dy.
  *
  *   mean, rstd   as rg_layer_norm left them
- *   dx           dev, of `type`, or NULL where x is data and no gradient is wanted; may be dy itself, with the same stride
+ *   dx           dev, of `type`, or NULL where x is data and no gradient is wanted; may be dy or x itself, with the same stride
  *   dweight, dbias  dev, [n_cols] of weight_type; each may be NULL
  *   workspace    dev, 16-byte aligned, as many bytes as rg_layer_norm_workspace says; may be NULL where neither
  *                dweight nor dbias is wanted
- * With no rows dweight and dbias are zero.
+ * With no rows dweight and dbias are zero.  Outputs overlap neither the inputs, but for what is said, nor one another; nor do those of rg_layer_norm.
  */
 rg_status rg_layer_norm_workspace(uint64_t n_rows, uint64_t n_cols, uint32_t type, uint64_t *bytes);
 rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, const void *x, uint64_t x_stride, uint64_t n_rows, uint64_t n_cols,

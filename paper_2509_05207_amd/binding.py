@@ -569,7 +569,7 @@ def rg_layer_norm_workspace(n_rows, n_cols, dtype):
 
 def rg_layer_norm_backward(dy, x, weight, mean, rstd, want_dx=True, want_dweight=True, want_dbias=True, out=None, workspace=None, stream=None):
     """(dx, dweight, dbias); None for what is not wanted.  weight None: all ones (the gradients of weight and bias are then fp32).
-    out: where dx goes (dy itself: in place); workspace: a device tensor of rg_layer_norm_workspace bytes, made here if None."""
+    out: where dx goes (dy or x itself: in place); workspace: a device tensor of rg_layer_norm_workspace bytes, made here if None."""
     shape, dt, device = x.shape, x.dtype, x.device
     xp, xs = _rows("x", x)
     gp, gs = _rows("dy", dy, shape, dt)

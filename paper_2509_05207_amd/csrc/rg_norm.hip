@@ -630,6 +630,7 @@ extern "C" rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, 
     if (dx) {
         RG_TRY(check_rows("dx", dx, dx_stride, n_rows, n_cols, bytes, true));
         RG_TRY(check_place("dx", dx, dx_stride, dy, dy_stride, n_rows));
+        RG_TRY(check_place("dx", dx, dx_stride, x, x_stride, n_rows));
     }
     RG_TRY(check_vector("weight", weight, weight_type, type));
     RG_TRY(check_vector("dweight", dweight, weight_type, type));
@@ -638,7 +639,7 @@ extern "C" rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, 
     RG_TRY(check_rows("rstd", rstd, 0, n_rows, 1, 4, false));
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
-    const NormShape s = norm_shape((int64_t)n_rows, (int64_t)n_cols, (int)bytes, n_cu, true, dx == dy);
+    const NormShape s = norm_shape((int64_t)n_rows, (int64_t)n_cols, (int)bytes, n_cu, true, dx == dy || dx == x);
     const bool columns = dweight || dbias;
     if (columns && s.n_partial) {
         const uint64_t want = 2ull * s.n_partial * n_cols * sizeof(float);

@@ -350,3 +350,27 @@ def test_in_place_with_another_stride_is_refused(rg):
     assert L.rg_layer_norm(p, 320, 4, 64, 0, None, None, 0, 1e-5, p, 256, v.data_ptr(), v.data_ptr(), None) == rg.RG_EINVAL
     assert L.rg_layer_norm_backward(p, 320, buf.data_ptr(), 320, 4, 64, 0, None, 0, v.data_ptr(), v.data_ptr(), p, 256, None, None, None, 0, None) == rg.RG_EINVAL
     assert L.rg_layer_norm(p, 320, 1, 64, 0, None, None, 0, 1e-5, p, 256, v.data_ptr(), v.data_ptr(), None) == rg.RG_OK       # a single row has no stride
+
+
+@pytest.mark.parametrize("rows", [5, 100, 300])
+@pytest.mark.parametrize("cols", [5, 64, 602, 3000, 20_000, 40_000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_dx_in_the_place_of_x(rg, rows, cols, dtype):
+    """Few long rows are shared by workgroups, of which none may write what another still reads: neither of dy nor of x."""
+    x, dy, w, b = made(rows, cols, dtype, torch.float32, 18)
+    want = run_both(rg, x, dy, w, b)
+    for which in (0, 1):
+        at = [x.clone(), dy.clone()]
+        dx, dw, db = rg.rg_layer_norm_backward(at[1], at[0], w, want["mean"], want["rstd"], out=at[which])
+        assert dx is at[which]
+        for k, t in dict(dx=dx, dweight=dw, dbias=db).items():
+            assert torch.equal(t, want[k]), (k, which)
+
+
+def test_dx_in_the_place_of_x_with_another_stride_is_refused(rg):
+    buf, dy = torch.zeros(4 * 80, device="cuda"), torch.zeros((4, 64), device="cuda")
+    st = torch.ones(4, device="cuda")
+    wide, tight = torch.as_strided(buf, (4, 64), (80, 1)), torch.as_strided(buf, (4, 64), (64, 1))
+    with pytest.raises(rg.RgError) as e:
+        rg.rg_layer_norm_backward(dy, wide, None, st, st, out=tight)
+    assert e.value.status == rg.RG_EINVAL
