@@ -97,6 +97,7 @@ inline bool blocks_by_ranks(uint64_t n_nodes, uint32_t L, uint64_t beta, uint64_
 // ---------------------------------------------------------------- layer norm
 // Elements of a row in a lane's registers, at most.  The backward pass holds five values to an element (rows of 8,192 bf16, 256 lanes of 32 / 1,024 lanes of 8, us: 150 / 84).
 constexpr int norm_elements(bool backward) { return backward ? 16 : 32; }
+constexpr int NORM_SUM_COLUMNS = 32, NORM_SUM_THREADS = 1024;
 struct NormShape {
     int pack;                            // elements of an access: 16 bytes, or single elements where a row has fewer
     int lanes;                           // of a row: 8 to 64, or a workgroup of 256 or 1,024; 0: the row is longer than that
@@ -105,6 +106,7 @@ struct NormShape {
     uint32_t parts;                      // workgroups that share a long row
     uint32_t n_partial;                  // partial sums of every column that the backward pass leaves
     uint32_t column_grid;                // workgroups over the columns of long rows
+    uint32_t sum_grid;                   // workgroups that add the partial sums up, NORM_SUM_COLUMNS columns at a time
 };
 // in_place: the result takes the place of what other workgroups of the row would still read.
 inline NormShape norm_shape(int64_t n_rows, int64_t n_cols, int element_bytes, int n_cu, bool backward, bool in_place)
@@ -126,6 +128,7 @@ inline NormShape norm_shape(int64_t n_rows, int64_t n_cols, int element_bytes, i
     s.packs = s.lanes ? (int)((need + s.lanes - 1) / s.lanes) : 0;
     s.grid = (uint32_t)std::max<int64_t>(1, std::min(most, (n_rows + groups - 1) / groups));
     s.n_partial = n_rows ? s.grid : 0;
+    s.sum_grid = grid_for((n_cols + NORM_SUM_COLUMNS - 1) / NORM_SUM_COLUMNS, NORM_SUM_THREADS);
     s.parts = 1;
     if (s.lanes == 0) {
         while (!in_place && s.parts < 8 && n_rows * s.parts * 2 <= n_cu) s.parts *= 2;

@@ -461,28 +461,33 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormArgs a)
 }
 
 // ---------------------------------------------------------------- the partial sums put together
-// 32 columns a workgroup, 32 threads to a column; blockIdx.y 0: dweight, 1: dbias.  (4 to 5 us for up to 8,192 columns, most of it a launch's latency.)
-__global__ void __launch_bounds__(1024) norm_partials_kernel(const float *__restrict__ partial, uint32_t n_partial, int64_t n_cols, void *dweight, void *dbias, uint32_t type)
+// 32 columns a workgroup at a time, 32 threads to a column; blockIdx.y 0: dweight, 1: dbias.  (4 to 5 us for up to 8,192 columns, most of it a launch's latency.)
+__global__ void __launch_bounds__(NORM_SUM_THREADS) norm_partials_kernel(const float *__restrict__ partial, uint32_t n_partial, int64_t n_cols, void *dweight, void *dbias, uint32_t type)
 {
+    static_assert(NORM_SUM_COLUMNS == 32 && NORM_SUM_THREADS == 32 * 32, "");
     void *out = blockIdx.y == 0 ? dweight : dbias;
     if (!out) return;
     __shared__ float part[32][33];
     const float *src = partial + (uint64_t)blockIdx.y * n_partial * (uint64_t)n_cols;
-    const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
     const uint32_t k = threadIdx.x >> 5;
-    float s = 0.f;
-    if (c < n_cols)
+    for (int64_t first = (int64_t)blockIdx.x * 32; first < n_cols; first += (int64_t)gridDim.x * 32) {
+        const int64_t c = first + (threadIdx.x & 31);
+        float s = 0.f;
+        if (c < n_cols)
 #pragma unroll 8
-        for (uint32_t p = k; p < n_partial; p += 32) s += src[(uint64_t)p * (uint64_t)n_cols + c];
-    part[k][threadIdx.x & 31] = s;
-    __syncthreads();
-    if (threadIdx.x >= 32 || c >= n_cols) return;
-    s = 0.f;
+            for (uint32_t p = k; p < n_partial; p += 32) s += src[(uint64_t)p * (uint64_t)n_cols + c];
+        part[k][threadIdx.x & 31] = s;
+        __syncthreads();
+        if (threadIdx.x < 32 && c < n_cols) {
+            s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) s += part[j][threadIdx.x];
-    if (type == RG_F32) static_cast<float *>(out)[c] = s;
-    else if (type == RG_BF16) static_cast<bf16 *>(out)[c] = (bf16)s;
-    else static_cast<f16 *>(out)[c] = (f16)s;
+            for (int j = 0; j < 32; ++j) s += part[j][threadIdx.x];
+            if (type == RG_F32) static_cast<float *>(out)[c] = s;
+            else if (type == RG_BF16) static_cast<bf16 *>(out)[c] = (bf16)s;
+            else static_cast<f16 *>(out)[c] = (f16)s;
+        }
+        __syncthreads();                                       // part is read, and may be written
+    }
 }
 
 // ---------------------------------------------------------------- launches
@@ -669,7 +674,7 @@ extern "C" rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, 
         RG_HIP(hipGetLastError());
     }
     if (columns) {
-        hipLaunchKernelGGL(norm_partials_kernel, dim3((uint32_t)((n_cols + 31) / 32), 2), dim3(1024), 0, st, static_cast<const float *>(workspace), s.n_partial, (int64_t)n_cols, dweight, dbias,
+        hipLaunchKernelGGL(norm_partials_kernel, dim3(s.sum_grid, 2), dim3(NORM_SUM_THREADS), 0, st, static_cast<const float *>(workspace), s.n_partial, (int64_t)n_cols, dweight, dbias,
                            weight_type);
         RG_HIP(hipGetLastError());
     }

@@ -374,3 +374,16 @@ def test_dx_in_the_place_of_x_with_another_stride_is_refused(rg):
     with pytest.raises(rg.RgError) as e:
         rg.rg_layer_norm_backward(dy, wide, None, st, st, out=tight)
     assert e.value.status == rg.RG_EINVAL
+
+
+def test_more_columns_than_a_launch_has_work_items(rg):
+    """Sums of 2^27 + 33 columns, 32 threads to a column: by a launch whose workgroups take several groups of them."""
+    cols = 2 ** 27 + 33
+    g = torch.Generator(device="cuda").manual_seed(19)
+    x, dy = (torch.randn((1, cols), generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    mean, rstd = x.float().mean(1), torch.ones(1, device="cuda")
+    _, dw, db = rg.rg_layer_norm_backward(dy, x, None, mean, rstd, want_dx=False)
+    # one term to a sum: the difference rounded, and the product
+    assert torch.equal(db, dy[0].float())
+    want = dy[0].double() * (x[0].double() - mean.double())
+    assert bool(((dw.double() - want).abs() <= 3 * U * (dy[0].double().abs() * (x[0].double().abs() + mean.double().abs()))).all())
