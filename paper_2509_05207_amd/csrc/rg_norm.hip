@@ -270,13 +270,14 @@ __global__ void __launch_bounds__(norm_threads(LANES), LANES > 256 ? 1 : V * NV 
 constexpr int LONG_THREADS = 1024;
 constexpr int AHEAD = 8;                 // packs that a thread has under way
 
-// Count, mean and squares around it of two disjoint parts put together.
+// Count, mean and squares around it of two disjoint parts put together.  Of an empty part the difference is a whole mean, whose square may be beyond the range: the
+// counts come in before it is squared.
 struct Moments { float n, mean, m2; };
 __device__ __forceinline__ Moments join(const Moments &p, const Moments &q)
 {
     const float n = p.n + q.n;
     const float part = n > 0.f ? q.n / n : 0.f, d = q.mean - p.mean;
-    return Moments{n, p.mean + d * part, p.m2 + q.m2 + d * d * p.n * part};
+    return Moments{n, p.mean + d * part, p.m2 + q.m2 + d * (d * (p.n * part))};
 }
 
 // Few rows are shared out among `parts` workgroups each: all of them take the row's sums (which they read from their L2: workgroup g runs on XCD g mod

@@ -387,3 +387,23 @@ def test_more_columns_than_a_launch_has_work_items(rg):
     assert torch.equal(db, dy[0].float())
     want = dy[0].double() * (x[0].double() - mean.double())
     assert bool(((dw.double() - want).abs() <= 3 * U * (dy[0].double().abs() * (x[0].double().abs() + mean.double().abs()))).all())
+
+
+@pytest.mark.parametrize("cols", [3, 602, 5000, 20_000, 40_000])
+def test_means_whose_squares_are_beyond_the_range(rg, cols):
+    """Only differences from the mean are squared: rows around 2^70 are in range as long as these are (eight units in the last place, 2^47 each; of bf16, whose units there are
+    2^63, they are not)."""
+    g = torch.Generator(device="cuda").manual_seed(20)
+    x = (2.0 ** 70 + 2.0 ** 47 * torch.randint(0, 9, (7, cols), generator=g, device="cuda").double()).float()
+    y, mean, rstd = rg.rg_layer_norm(x, eps=EPS)
+    want = reference(x, x, None, None)
+    check("y", y, want["y"])
+    check("mean", mean, want["mean"])
+
+
+@pytest.mark.parametrize("cols", [3, 602, 5000, 20_000, 40_000])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_constant_rows_whose_squares_are_beyond_the_range(rg, cols, dtype):
+    constant = torch.full((3, cols), 1e30, dtype=dtype, device="cuda")
+    y, mean, rstd = rg.rg_layer_norm(constant, eps=EPS)
+    assert bool(y.isfinite().all()) and bool(rstd.isfinite().all()) and bool((mean.double() / constant[:, 0].double() - 1).abs().max() <= (64 + cols / 2048) * U)
