@@ -1,7 +1,8 @@
 // Layer norm of rows and its gradients: the norm a trainer runs on the gathered blocks (Sec. 4 par. (8)).
 //
-// Both directions are bound by HBM: a row is read once into registers, its sums are taken there (the mean first, then the squares
-// around it, so that a large mean costs no digits), and the result is written once.  A row belongs to 8 to 64 lanes of a wave, or to
+// Both directions are bound by HBM: a row is read once into registers, its sums are taken there, and the result is written once.  The mean comes first, then
+// the squares around it and the sum of what it leaves, by which it is corrected: y of rows far from zero has the digits of their deviations, and of a constant row is
+// nothing.  (The gradients take the mean as it was given out, rounded to fp32.)  A row belongs to 8 to 64 lanes of a wave, or to
 // a workgroup, whatever holds it in 32 elements a lane or fewer; rows beyond that are read twice.  The last pack of a row is the one that
 // ENDS at the row's end: it overlaps its predecessor, both write the same values there, and the elements that it repeats count in
 // no sum.
@@ -60,11 +61,19 @@ __device__ __forceinline__ float inverse_root(float v)
     return fabsf(off) < 0.5f ? fmaf(0.5f * r, off, r) : r;
 }
 
+// Squares around the mean out of those around a point near it: sum is what is left over of that point, rest its share to an element.  (Not below zero, and a NaN stays.)
+__device__ __forceinline__ float squares_around(float squares, float sum, float rest)
+{
+    const float m2 = fmaf(-sum, rest, squares);
+    return m2 < 0.f ? 0.f : m2;
+}
+
 // Sums over all lanes of a row.  Beyond a wave they meet in LDS, in slots taken by turns: whoever writes a slot again has passed a barrier
 // that every wave reaches only after it has read that slot.
 template <int LANES, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float (*slots)[N][16], uint32_t &turn)
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*slots)[2][16], uint32_t &turn)
 {
+    static_assert(N <= 2, "");
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = lanes_sum<(LANES < 64 ? LANES : 64)>(v[k]);
     if constexpr (LANES > 64) {
@@ -109,7 +118,7 @@ constexpr int norm_threads(int lanes) { return lanes > 256 ? lanes : 256; }
 template <typename T, int V, int LANES, int NV>
 __global__ void __launch_bounds__(norm_threads(LANES)) norm_rows_kernel(NormArgs a)
 {
-    __shared__ float slots[2][1][16];
+    __shared__ float slots[2][2][16];
     uint32_t turn = 0;
     const RowLane<V, LANES, NV> at((int32_t)a.n_cols);
     float w[NV][V], b[NV][V];
@@ -132,21 +141,25 @@ __global__ void __launch_bounds__(norm_threads(LANES)) norm_rows_kernel(NormArgs
 #pragma unroll
             for (int e = 0; e < V; ++e) s[0] += at.counts(j, e) ? v[j][e] : 0.f;
         row_sums<LANES>(s, slots, turn);
-        const float mean = s[0] / a.cols;            // divided, not multiplied by a rounded inverse: a constant row's mean is the constant
-        s[0] = 0.f;
+        // What the mean leaves of a constant row are a few units of its last place, whose sums are exact, and so are the quotient (of a division, not of a rounded inverse) and the difference.
+        const float about = s[0] / a.cols;
+        float t[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                v[j][e] -= mean;
-                s[0] += at.counts(j, e) ? rounded(v[j][e], v[j][e]) : 0.f;
+                v[j][e] -= about;
+                t[0] += at.counts(j, e) ? v[j][e] : 0.f;
+                t[1] += at.counts(j, e) ? rounded(v[j][e], v[j][e]) : 0.f;
             }
-        row_sums<LANES>(s, slots, turn);
-        const float rstd = inverse_root(s[0] * a.inv_cols + a.eps);
+        row_sums<LANES>(t, slots, turn);
+        // Up to the differences' own roundings what is left is nothing but these.
+        const float left = t[0] / a.cols, rest = fabsf(left) <= 0x1p-23f * sqrtf(t[1] * a.inv_cols) ? 0.f : left;
+        const float mean = about + rest, rstd = inverse_root(squares_around(t[1], t[0], rest) * a.inv_cols + a.eps);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[j][e] = v[j][e] * rstd * w[j][e] + b[j][e];
+            for (int e = 0; e < V; ++e) v[j][e] = (v[j][e] - rest) * rstd * w[j][e] + b[j][e];
             if (at.stores(j)) store_pack(y + at.column(j), v[j]);
         }
         if (at.lane == 0) {
@@ -270,14 +283,16 @@ __global__ void __launch_bounds__(norm_threads(LANES), LANES > 256 ? 1 : V * NV 
 constexpr int LONG_THREADS = 1024;
 constexpr int AHEAD = 8;                 // packs that a thread has under way
 
-// Count, mean and squares around it of two disjoint parts put together.  Of an empty part the difference is a whole mean, whose square may be beyond the range: the
-// counts come in before it is squared.
-struct Moments { float n, mean, m2; };
+// Count, mean (mean + low, what the first rounded away) and squares around it of two disjoint parts put together.  The counts come in before the difference is squared: of
+// an empty q it is a whole mean, whose square may be beyond the range.
+struct Moments { float n, mean, low, m2; };
 __device__ __forceinline__ Moments join(const Moments &p, const Moments &q)
 {
+    if (p.n == 0.f) return q;
     const float n = p.n + q.n;
-    const float part = n > 0.f ? q.n / n : 0.f, d = q.mean - p.mean;
-    return Moments{n, p.mean + d * part, p.m2 + q.m2 + d * (d * (p.n * part))};
+    const float part = q.n / n, d = (q.mean - p.mean) + (q.low - p.low);
+    const float step = rounded(d, part), mean = p.mean + step, moved = mean - p.mean;
+    return Moments{n, mean, p.low + ((p.mean - (mean - moved)) + (step - moved)), p.m2 + q.m2 + d * (d * (p.n * part))};
 }
 
 // Few rows are shared out among `parts` workgroups each: all of them take the row's sums (which they read from their L2: workgroup g runs on XCD g mod
@@ -305,7 +320,7 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_rows_kernel(NormArgs a
     for (int64_t row = part.row; row < a.n_rows; row += part.rows) {
         const T *x = reinterpret_cast<const T *>(a.x + (uint64_t)row * a.x_stride);
         T *y = reinterpret_cast<T *>(a.out + (uint64_t)row * a.out_stride);
-        Moments m{0.f, 0.f, 0.f};
+        Moments m{0.f, 0.f, 0.f, 0.f};
         for (int64_t first = threadIdx.x; first < packs; first += LONG_THREADS * AHEAD) {
             typename PackOf<T, V>::type raw[AHEAD];
 #pragma unroll
@@ -319,23 +334,30 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_rows_kernel(NormArgs a
 #pragma unroll
                 for (int e = 0; e < V; ++e) s += there ? v[k][e] : 0.f;
             }
-            Moments q{n, s / n, 0.f};
+            Moments q{n, s / n, 0.f, 0.f};
+            s = 0.f;
 #pragma unroll
             for (int k = 0; k < AHEAD; ++k)
 #pragma unroll
-                for (int e = 0; e < V; ++e) q.m2 += first + k * LONG_THREADS < packs ? (v[k][e] - q.mean) * (v[k][e] - q.mean) : 0.f;
+                for (int e = 0; e < V; ++e) {
+                    const float c = first + k * LONG_THREADS < packs ? v[k][e] - q.mean : 0.f;
+                    s += c;
+                    q.m2 += rounded(c, c);
+                }
+            q.low = s / n;
+            q.m2 = squares_around(q.m2, s, q.low);
             m = join(m, q);
         }
-        if (rest < a.n_cols) m = join(m, Moments{1.f, (float)x[rest], 0.f});
+        if (rest < a.n_cols) m = join(m, Moments{1.f, (float)x[rest], 0.f, 0.f});
 #pragma unroll
-        for (int k = 1; k < 64; k <<= 1) m = join(m, Moments{__shfl_xor(m.n, k), __shfl_xor(m.mean, k), __shfl_xor(m.m2, k)});
+        for (int k = 1; k < 64; k <<= 1) m = join(m, Moments{__shfl_xor(m.n, k), __shfl_xor(m.mean, k), __shfl_xor(m.low, k), __shfl_xor(m.m2, k)});
         Moments *s = waves[turn & 1];
         ++turn;
         if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = m;
         __syncthreads();
         m = s[0];
         for (int k = 1; k < LONG_THREADS / 64; ++k) m = join(m, s[k]);
-        const float mean = m.mean, rstd = inverse_root(m.m2 * a.inv_cols + a.eps);
+        const float mean = m.mean, low = m.low, rstd = inverse_root(m.m2 * a.inv_cols + a.eps);
         for (int64_t first = part.from + threadIdx.x; first < part.to; first += LONG_THREADS * AHEAD) {
             typename PackOf<T, V>::type raw[AHEAD];
 #pragma unroll
@@ -351,7 +373,7 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_rows_kernel(NormArgs a
                 if (a.weight) load_weights<V>(a.weight, a.weight_type, c, w);
                 if (a.bias) load_weights<V>(a.bias, a.weight_type, c, b);
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[e] = (v[e] - mean) * rstd * w[e] + b[e];
+                for (int e = 0; e < V; ++e) v[e] = (v[e] - mean - low) * rstd * w[e] + b[e];
                 store_pack(y + c, v);
             }
         }
@@ -360,11 +382,11 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_rows_kernel(NormArgs a
             load_pack(x + rest, v);
             if (a.weight) load_weights<1>(a.weight, a.weight_type, rest, w);
             if (a.bias) load_weights<1>(a.bias, a.weight_type, rest, b);
-            v[0] = (v[0] - mean) * rstd * w[0] + b[0];
+            v[0] = (v[0] - mean - low) * rstd * w[0] + b[0];
             store_pack(y + rest, v);
         }
         if (threadIdx.x == 0 && part.last) {
-            if (a.mean) a.mean[row] = mean;
+            if (a.mean) a.mean[row] = mean + low;
             if (a.rstd) a.rstd[row] = rstd;
         }
     }

@@ -407,3 +407,34 @@ def test_constant_rows_whose_squares_are_beyond_the_range(rg, cols, dtype):
     constant = torch.full((3, cols), 1e30, dtype=dtype, device="cuda")
     y, mean, rstd = rg.rg_layer_norm(constant, eps=EPS)
     assert bool(y.isfinite().all()) and bool(rstd.isfinite().all()) and bool((mean.double() / constant[:, 0].double() - 1).abs().max() <= (64 + cols / 2048) * U)
+
+
+@pytest.mark.parametrize("cols", WIDTHS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_constant_rows_come_to_nothing(rg, cols, dtype):
+    """A mean out of rounded sums is a few units of the last place off; their sum over the row is a whole number of them, and what it leaves is none."""
+    x = torch.tensor([0.1, -12.7, 100.1, 1000.1, 30000.3, 1e-3], device="cuda").to(dtype)[:, None].expand(6, cols).contiguous()
+    y, mean, rstd = rg.rg_layer_norm(x, eps=EPS)
+    assert torch.equal(mean, x[:, 0].float())
+    assert not y.any() and torch.allclose(rstd, torch.full_like(rstd, EPS ** -0.5), rtol=4 * U)
+
+
+@pytest.mark.parametrize("cols", [40, 77, 602, 1000, 5000, 8192, 16_384, 20_000, 40_000, 70_001])
+@pytest.mark.parametrize("shift", [100.0, 1e4, -1e4])
+def test_rows_far_from_zero_keep_the_digits_of_their_deviations(rg, cols, shift):
+    """x - mean is exact there, and the mean is corrected by what is left over: the bound of y (see above) with the deviation r = |x - mean| in the place of |x|.  The mean itself is rounded to fp32 at last."""
+    x, _, w, b = made(20, cols, torch.float32, torch.float32, 21, shift=shift)
+    y, mean, rstd = rg.rg_layer_norm(x, w, b, eps=EPS)
+    xd, row = x.double(), 64 + cols / 2048
+    m = xd.mean(1, keepdim=True)
+    r = (xd - m).abs()
+    s = 1 / torch.sqrt((r ** 2).mean(1, keepdim=True) + EPS)
+    dm, dr = (row + 4) * U * r.mean(1, keepdim=True), (row + 6) * U
+    dm = dm + (row * U) ** 2 * xd.abs().mean(1, keepdim=True)
+    dr = dr + 2 * dm * s
+    h = (xd - m) * s
+    want = h * w.double() + b.double()
+    tol = ((dm + 2 * U * r) * s + dr * h.abs()) * w.double().abs() + 2 * U * (want.abs() + (h * w.double()).abs())
+    check("y", y, (want, tol))
+    check("mean", mean, (m[:, 0], dm[:, 0]))
+    check("rstd", rstd, (s[:, 0], (dr * s)[:, 0]))
