@@ -11,12 +11,13 @@ import sys
 import time
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import synth
 
 
 def layer_norm(rg, eps=1e-5):
-    """rg_layer_norm as a function that torch can differentiate."""
+    """rg_layer_norm as a function that torch can differentiate, once."""
     class Norm(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, weight, bias):
@@ -25,6 +26,7 @@ def layer_norm(rg, eps=1e-5):
             return y
 
         @staticmethod
+        @once_differentiable                              # a second derivative raises: torch does not see into the library's gradients
         def backward(ctx, dy):
             x, weight, mean, rstd = ctx.saved_tensors
             return rg.rg_layer_norm_backward(dy.contiguous(), x, weight, mean, rstd, want_dx=ctx.needs_input_grad[0])
