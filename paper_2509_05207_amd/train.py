@@ -29,7 +29,8 @@ def layer_norm(rg, eps=1e-5):
         @once_differentiable                              # a second derivative raises: torch does not see into the library's gradients
         def backward(ctx, dy):
             x, weight, mean, rstd = ctx.saved_tensors
-            return rg.rg_layer_norm_backward(dy.contiguous(), x, weight, mean, rstd, want_dx=ctx.needs_input_grad[0])
+            dx, dweight, dbias = ctx.needs_input_grad
+            return rg.rg_layer_norm_backward(dy.contiguous(), x, weight, mean, rstd, want_dx=dx, want_dweight=dweight, want_dbias=dbias)
     return Norm.apply
 
 

@@ -43,3 +43,12 @@ def test_a_second_derivative_raises():
     dx, = torch.autograd.grad(loss, x, create_graph=True)
     with pytest.raises(RuntimeError, match="twice"):
         (loss + dx.square().sum()).backward()
+
+
+@pytest.mark.parametrize("needs", [(False, True, True), (True, False, False), (True, True, False), (False, False, True)])
+def test_only_gradients_that_are_asked_for_are_computed(needs):
+    calls = Calls()
+    at = inputs(*needs)
+    train.layer_norm(calls)(*at).sum().backward()
+    assert calls.wanted == [needs]
+    assert [t.grad is not None for t in at] == list(needs)
