@@ -511,9 +511,10 @@ RG_F32, RG_BF16, RG_F16 = 0, 1, 2
 _ELEMENT = {torch.float32: RG_F32, torch.bfloat16: RG_BF16, torch.float16: RG_F16}
 
 
-def _rows(name, t, shape=None, dtype=None):
-    """(address, stride in bytes) of a device matrix whose rows are contiguous."""
+def _rows(name, t, device, shape=None, dtype=None):
+    """(address, stride in bytes) of a matrix on `device` whose rows are contiguous."""
     assert t.is_cuda and t.dim() == 2, f"{name}: expected a device matrix"
+    assert t.device == device, f"{name}: expected it on {device}, got {t.device}"
     assert shape is None or t.shape == shape, f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}"
     assert (dtype is None and t.dtype in _ELEMENT) or t.dtype == dtype, f"{name}: got {t.dtype}"
     along, across = t.stride()
@@ -521,11 +522,26 @@ def _rows(name, t, shape=None, dtype=None):
     return t.data_ptr(), along * t.element_size()
 
 
-def _vector(name, t, n, dtype):
+def _vector(name, t, device, n, dtype):
     if t is None:
         return None
-    assert t.is_cuda and t.dtype == dtype and t.shape == (n,) and t.is_contiguous(), f"{name}: expected {n} contiguous {dtype} on the device"
+    assert t.device == device and t.dtype == dtype and t.shape == (n,) and t.is_contiguous(), f"{name}: expected {n} contiguous {dtype} on {device}"
     return t.data_ptr()
+
+
+def _scratch(t, device):
+    """(address, bytes) of a workspace."""
+    assert t.device == device and t.is_contiguous(), f"workspace: expected a contiguous tensor on {device}"
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _call(device, entry, *args):
+    """The entry point with the operands' device the current one, to which the library's launches and questions go."""
+    if device.index == torch._C._cuda_getDevice():
+        _check(entry(*args))
+    else:
+        with torch.cuda.device(device):
+            _check(entry(*args))
 
 
 def _stream_and_use(device, stream, *made):
@@ -546,17 +562,17 @@ def _stream_and_use(device, stream, *made):
 
 def rg_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """(y, mean, rstd) of the rows of `x` (device matrix; rows may be padded).  out: where y goes (x itself: in place)."""
-    shape, dt = x.shape, x.dtype
-    xp, xs = _rows("x", x)
+    shape, dt, device = x.shape, x.dtype, x.device
+    xp, xs = _rows("x", x, device)
     n, d = shape
     y = x.new_empty(shape) if out is None else out
-    yp, ys = _rows("out", y, shape, dt)
+    yp, ys = _rows("out", y, device, shape, dt)
     wt = (weight if weight is not None else bias if bias is not None else x).dtype
-    stats = torch.empty((2, n), dtype=torch.float32, device=x.device)
+    stats = torch.empty((2, n), dtype=torch.float32, device=device)
     sp = stats.data_ptr()
-    st = _stream_and_use(x.device, stream, y if out is None else None, stats)
-    _check(lib().rg_layer_norm(xp, xs, n, d, _ELEMENT[dt], _vector("weight", weight, d, wt), _vector("bias", bias, d, wt), _ELEMENT[wt],
-                               eps, yp, ys, sp, sp + 4 * n, st))
+    st = _stream_and_use(device, stream, y if out is None else None, stats)
+    _call(device, lib().rg_layer_norm, xp, xs, n, d, _ELEMENT[dt], _vector("weight", weight, device, d, wt), _vector("bias", bias, device, d, wt), _ELEMENT[wt],
+          eps, yp, ys, sp, sp + 4 * n, st)
     return y, stats[0], stats[1]
 
 
@@ -571,25 +587,26 @@ def rg_layer_norm_backward(dy, x, weight, mean, rstd, want_dx=True, want_dweight
     """(dx, dweight, dbias); None for what is not wanted.  weight None: all ones (the gradients of weight and bias are then fp32).
     out: where dx goes (dy or x itself: in place); workspace: a device tensor of rg_layer_norm_workspace bytes, made here if None."""
     shape, dt, device = x.shape, x.dtype, x.device
-    xp, xs = _rows("x", x)
-    gp, gs = _rows("dy", dy, shape, dt)
+    xp, xs = _rows("x", x, device)
+    gp, gs = _rows("dy", dy, device, shape, dt)
     n, d = shape
     wt = weight.dtype if weight is not None else torch.float32
     dx, op, os_ = None, None, 0
     if want_dx:
         dx = x.new_empty(shape) if out is None else out
-        op, os_ = _rows("out", dx, shape, dt)
+        op, os_ = _rows("out", dx, device, shape, dt)
     dw = torch.empty(d, dtype=wt, device=device) if want_dweight else None
     db = torch.empty(d, dtype=wt, device=device) if want_dbias else None
     made = workspace is None and (want_dweight or want_dbias)
     if made:
-        workspace = torch.empty(max(rg_layer_norm_workspace(n, d, dt), 1), dtype=torch.uint8, device=device)
+        b = C.c_uint64()
+        _call(device, lib().rg_layer_norm_workspace, n, d, _ELEMENT[dt], C.byref(b))
+        workspace = torch.empty(max(b.value, 1), dtype=torch.uint8, device=device)
     st = _stream_and_use(device, stream, dx if out is None else None, dw, db, workspace if made else None)
-    wp, wb = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    assert workspace is None or (workspace.is_cuda and workspace.is_contiguous()), "workspace: expected a contiguous device tensor"
-    _check(lib().rg_layer_norm_backward(gp, gs, xp, xs, n, d, _ELEMENT[dt], _vector("weight", weight, d, wt), _ELEMENT[wt],
-                                        _vector("mean", mean, n, torch.float32), _vector("rstd", rstd, n, torch.float32), op, os_,
-                                        dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None, wp, wb, st))
+    wp, wb = (None, 0) if workspace is None else _scratch(workspace, device)
+    _call(device, lib().rg_layer_norm_backward, gp, gs, xp, xs, n, d, _ELEMENT[dt], _vector("weight", weight, device, d, wt), _ELEMENT[wt],
+          _vector("mean", mean, device, n, torch.float32), _vector("rstd", rstd, device, n, torch.float32), op, os_,
+          dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None, wp, wb, st)
     return dx, dw, db
 
 
@@ -597,18 +614,18 @@ RG_MAX_SIDE, RG_MAX_STEPS, RG_UPDATES_PER_LAUNCH = 16384, 32, 12
 
 
 def _updates(grads, outs, weights=None, momenta=None, out_momenta=None):
-    """The host array of rg_update over lists of device matrices, and their type."""
+    """The host array of rg_update over lists of matrices on one device, and their type."""
     assert len(grads) == len(outs) and all(x is None or len(x) == len(grads) for x in (weights, momenta, out_momenta)), "lists of one length are expected"
     u = (rg_update * max(len(grads), 1))()
-    dt = grads[0].dtype if grads else torch.float32
+    dt, device = (grads[0].dtype, grads[0].device) if grads else (torch.float32, None)
     for k, (e, g, o) in enumerate(zip(u, grads, outs)):
         e.rows, e.cols = g.shape
-        e.grad, e.grad_stride = _rows("grad", g, None, dt)
-        e.out, e.out_stride = _rows("out", o, g.shape, dt)
+        e.grad, e.grad_stride = _rows("grad", g, device, None, dt)
+        e.out, e.out_stride = _rows("out", o, device, g.shape, dt)
         if weights is not None:
-            e.weight, e.weight_stride = _rows("weight", weights[k], g.shape, dt)
-            e.momentum, e.momentum_stride = _rows("momentum", momenta[k], g.shape, torch.float32)
-            e.momentum_out, e.momentum_out_stride = _rows("momentum", out_momenta[k], g.shape, torch.float32)
+            e.weight, e.weight_stride = _rows("weight", weights[k], device, g.shape, dt)
+            e.momentum, e.momentum_stride = _rows("momentum", momenta[k], device, g.shape, torch.float32)
+            e.momentum_out, e.momentum_out_stride = _rows("momentum", out_momenta[k], device, g.shape, torch.float32)
     return u, _ELEMENT[dt]
 
 
@@ -617,18 +634,19 @@ def _update_scratch(u, n, t, workspace, device, stream, *made):
     mine = None
     if workspace is None:
         b = C.c_uint64()
-        _check(lib().rg_update_workspace(u, n, t, C.byref(b)))
+        _call(device, lib().rg_update_workspace, u, n, t, C.byref(b))
         workspace = mine = torch.empty(max(b.value, 1), dtype=torch.uint8, device=device)
-    assert workspace.is_cuda and workspace.is_contiguous(), "workspace: expected a contiguous device tensor"
-    st = _stream_and_use(device, stream, mine, *made)
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), st, mine
+    p, size = _scratch(workspace, device)
+    return p, size, _stream_and_use(device, stream, mine, *made), mine
 
 
 def rg_update_workspace(matrices):
     """Bytes of scratch for an update of these matrices in one call."""
+    if not matrices:
+        return 0
     u, t = _updates(matrices, matrices)
     b = C.c_uint64()
-    _check(lib().rg_update_workspace(u, len(matrices), t, C.byref(b)))
+    _call(matrices[0].device, lib().rg_update_workspace, u, len(matrices), t, C.byref(b))
     return b.value
 
 
@@ -639,8 +657,9 @@ def rg_orthogonalize(grads, steps=5, eps=1e-7, out=None, workspace=None, stream=
     made = out is None
     out = [torch.empty(g.shape, dtype=g.dtype, device=g.device) for g in grads] if made else out
     u, t = _updates(grads, out)
-    p, b, st, _mine = _update_scratch(u, len(grads), t, workspace, grads[0].device, stream, *(out if made else ()))
-    _check(lib().rg_orthogonalize(u, len(grads), t, int(steps), eps, p, b, st))
+    device = grads[0].device
+    p, b, st, _mine = _update_scratch(u, len(grads), t, workspace, device, stream, *(out if made else ()))
+    _call(device, lib().rg_orthogonalize, u, len(grads), t, int(steps), eps, p, b, st)
     return out
 
 
@@ -652,8 +671,9 @@ def rg_muon_step(weights, grads, momenta, lr, weight_decay=0.0, momentum=0.95, n
     u, t = _updates(grads, out_weights, weights, momenta, out_momenta)
     if not grads:
         return
-    p, b, st, _mine = _update_scratch(u, len(grads), t, workspace, grads[0].device, stream)
-    _check(lib().rg_muon_step(u, len(grads), t, lr, weight_decay, momentum, 1 if nesterov else 0, int(steps), eps, p, b, st))
+    device = grads[0].device
+    p, b, st, _mine = _update_scratch(u, len(grads), t, workspace, device, stream)
+    _call(device, lib().rg_muon_step, u, len(grads), t, lr, weight_decay, momentum, 1 if nesterov else 0, int(steps), eps, p, b, st)
 
 
 def rg_trim_memory():
