@@ -535,6 +535,11 @@ def _scratch(t, device):
     return t.data_ptr(), t.numel() * t.element_size()
 
 
+def _written(*tensors):
+    """Tells autograd that what lies in these was written over (a call writes through raw addresses, which it does not see)."""
+    torch.autograd.graph.increment_version(tensors)
+
+
 def _call(device, entry, *args):
     """The entry point with the operands' device the current one, to which the library's launches and questions go."""
     if device.index == torch._C._cuda_getDevice():
@@ -573,6 +578,8 @@ def rg_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     st = _stream_and_use(device, stream, y if out is None else None, stats)
     _call(device, lib().rg_layer_norm, xp, xs, n, d, _ELEMENT[dt], _vector("weight", weight, device, d, wt), _vector("bias", bias, device, d, wt), _ELEMENT[wt],
           eps, yp, ys, sp, sp + 4 * n, st)
+    if out is not None:
+        _written(out)
     return y, stats[0], stats[1]
 
 
@@ -607,6 +614,8 @@ def rg_layer_norm_backward(dy, x, weight, mean, rstd, want_dx=True, want_dweight
     _call(device, lib().rg_layer_norm_backward, gp, gs, xp, xs, n, d, _ELEMENT[dt], _vector("weight", weight, device, d, wt), _ELEMENT[wt],
           _vector("mean", mean, device, n, torch.float32), _vector("rstd", rstd, device, n, torch.float32), op, os_,
           dw.data_ptr() if want_dweight else None, db.data_ptr() if want_dbias else None, wp, wb, st)
+    if want_dx and out is not None:
+        _written(out)
     return dx, dw, db
 
 
@@ -660,6 +669,8 @@ def rg_orthogonalize(grads, steps=5, eps=1e-7, out=None, workspace=None, stream=
     device = grads[0].device
     p, b, st, _mine = _update_scratch(u, len(grads), t, workspace, device, stream, *(out if made else ()))
     _call(device, lib().rg_orthogonalize, u, len(grads), t, int(steps), eps, p, b, st)
+    if not made:
+        _written(*out)
     return out
 
 
@@ -674,6 +685,7 @@ def rg_muon_step(weights, grads, momenta, lr, weight_decay=0.0, momentum=0.95, n
     device = grads[0].device
     p, b, st, _mine = _update_scratch(u, len(grads), t, workspace, device, stream)
     _call(device, lib().rg_muon_step, u, len(grads), t, lr, weight_decay, momentum, 1 if nesterov else 0, int(steps), eps, p, b, st)
+    _written(*out_weights, *out_momenta)
 
 
 def rg_trim_memory():

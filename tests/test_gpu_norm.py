@@ -438,3 +438,19 @@ def test_rows_far_from_zero_keep_the_digits_of_their_deviations(rg, cols, shift)
     check("y", y, (want, tol))
     check("mean", mean, (m[:, 0], dm[:, 0]))
     check("rstd", rstd, (s[:, 0], (dr * s)[:, 0]))
+
+
+def test_what_a_call_writes_is_known_to_autograd(rg):
+    """Results in tensors of the caller's raise their version, so that a backward pass that had kept the old values refuses them."""
+    x, dy, w, b = made(6, 20, torch.float32, torch.float32, 22)
+    _, mean, rstd = rg.rg_layer_norm(x, w, b)
+    for write in (lambda t: rg.rg_layer_norm(x, w, b, out=t), lambda t: rg.rg_layer_norm_backward(dy, x, w, mean, rstd, out=t)):
+        t, v = torch.zeros((6, 20), device="cuda"), torch.ones((6, 20), device="cuda", requires_grad=True)
+        before, product = t._version, t * v
+        write(t)
+        assert t._version == before + 1
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            product.sum().backward()
+    versions = [t._version for t in (x, dy, w, b, mean, rstd)]
+    run_both(rg, x, dy, w, b)
+    assert versions == [t._version for t in (x, dy, w, b, mean, rstd)]

@@ -332,3 +332,18 @@ def test_muon_step_is_rounded_once(rg, dtype, rows, cols):
     rg.rg_muon_step([w], [g], [m], lr=0.5, weight_decay=0.1, momentum=0.9)
     # the sum's own rounding to fp32, two of them
     assert float((w.double() - want).norm()) <= 2 * (1e-5 * before + 2.0 ** -23 * float(want.norm())) + float((want.to(dtype).double() - want).norm())
+
+
+def test_what_a_call_writes_is_known_to_autograd(rg):
+    """Results in tensors of the caller's raise their version, and those of what they are detached from."""
+    w, g, m, o = (made(8, 20, torch.float32, k) for k in range(4))
+    w.requires_grad_()
+    versions = lambda: [t._version for t in (w, g, m, o)]                                  # noqa: E731
+    assert versions() == [0] * 4
+    rg.rg_muon_step([w.detach()], [g], [m], lr=0.1)
+    assert versions() == [1, 0, 1, 0]
+    rg.rg_muon_step([w.detach()], [g], [m], lr=0.1, out_weights=[o], out_momenta=[m])
+    assert versions() == [1, 0, 2, 1]
+    rg.rg_orthogonalize([g], out=[g])
+    rg.rg_orthogonalize([g])
+    assert versions() == [1, 1, 2, 1]
