@@ -16,6 +16,8 @@ import math
 import pytest
 import torch
 
+from update_cases import CUT_OTHERWISE, EVERY_TILE
+
 pytestmark = pytest.mark.gpu
 A, B, CC = 3.4445, -4.7750, 2.0315
 BOUND = {torch.float32: 1e-5, torch.bfloat16: 5e-3, torch.float16: 4e-3}
@@ -347,3 +349,74 @@ def test_what_a_call_writes_is_known_to_autograd(rg):
     rg.rg_orthogonalize([g], out=[g])
     rg.rg_orthogonalize([g])
     assert versions() == [1, 1, 2, 1]
+
+
+def definition_there(g, steps=5, eps=1e-7):
+    """The definition in 64 bits, where the CPU would take minutes."""
+    x = g.double()
+    tall = x.shape[0] > x.shape[1]
+    x = x.t().contiguous() if tall else x
+    x = x / (torch.linalg.vector_norm(x) + eps)
+    for _ in range(steps):
+        s = x @ x.t().contiguous()
+        x = A * x + (B * s + CC * (s @ s)) @ x
+    return x.t() if tall else x
+
+
+# Of a square matrix' singular values one in a hundred lies below a hundredth of the largest: sqrt(1 / 100) of 1.2e-4 beside 1e-5 of the others.
+SQUARE = 2.2e-5
+
+
+@pytest.mark.parametrize("rows,cols", EVERY_TILE + [(16_384, 70), (30, 16_384), (16_384, 300)])
+@pytest.mark.parametrize("dtype", list(BOUND))
+def test_every_tile(rg, dtype, rows, cols):
+    """The update and the optimiser step by every tile of either kind of product, none of which divides the sides; and the longest sides."""
+    g = made(rows, cols, dtype, rows + 5, "sizes")
+    want = definition_there(g)
+    assert off(rg.rg_orthogonalize([g])[0], want) <= 2 * SQUARE + off(want.to(dtype), want)
+    w, m = made(rows, cols, dtype, rows + 6), made(rows, cols, torch.float32, rows + 7) * 4
+    want_m = 0.9 * m.double() + g.double()
+    change = 0.5 * math.sqrt(max(1.0, rows / cols)) * definition_there(g.double() + 0.9 * want_m)
+    want = w.double() * (1 - 0.5 * 0.1) - change
+    rg.rg_muon_step([w], [g], [m], lr=0.5, weight_decay=0.1, momentum=0.9)
+    # the sum's own rounding to fp32, two of them
+    assert float((w.double() - want).norm()) <= 2 * (SQUARE * float(change.norm()) + 2.0 ** -23 * float(want.norm())) + float((want.to(dtype).double() - want).norm())
+    assert off(m, want_m) <= 2.0 ** -23
+
+
+@pytest.mark.parametrize("dtype", list(BOUND))
+@pytest.mark.parametrize("rows,cols,copies", CUT_OTHERWISE)
+def test_tiles_that_other_matrices_change_change_no_bit(rg, dtype, rows, cols, copies):
+    """Tiles that no waves share, one size for a matrix alone and another for several."""
+    gs = [made(rows, cols, dtype, k) for k in range(copies)]
+    outs = rg.rg_orthogonalize(gs)
+    for k in (0, copies - 1):
+        assert torch.equal(outs[k], rg.rg_orthogonalize([gs[k]])[0])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_launches_recorded_into_a_graph(rg, dtype):
+    """Matrices of several launches a step, of shared tiles and of others, in two groups."""
+    shapes = [(300, 400), (1400, 1300), (60, 90), (1300, 40)]
+    w, g = [made(r, c, dtype, 40 + r) for r, c in shapes], [made(r, c, dtype, 50 + r) for r, c in shapes]
+    m = [made(r, c, torch.float32, 60 + r) for r, c in shapes]
+    w2, m2 = [torch.empty_like(t) for t in w], [torch.empty_like(t) for t in m]
+    ws = torch.empty(rg.rg_update_workspace(g), dtype=torch.uint8, device="cuda")
+
+    def step():
+        rg.rg_muon_step(w, g, m, lr=0.1, out_weights=w2, out_momenta=m2, workspace=ws)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        for t, (r, c) in zip(g, shapes):
+            t.copy_(made(r, c, dtype, 70 + r + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in w2 + m2]
+        for t in w2 + m2:
+            t.fill_(7.0)
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(got, w2 + m2))

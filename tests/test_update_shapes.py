@@ -5,6 +5,8 @@ import subprocess
 
 import pytest
 
+from update_cases import CUT_OTHERWISE, EVERY_TILE
+
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2509_05207_amd", "csrc")
 DRIVER = r"""
 #include "rg_launch.h"
@@ -72,3 +74,49 @@ def test_the_same_either_way_round(kinds):
 ])
 def test_tiles_by_what_is_done_first(kinds, rows, cols, wide, copies, half, whole):
     assert kinds([(rows, cols, wide, copies)])[0][4:] == [half, whole]
+
+
+TILES = r"""
+#include "rg_launch.h"
+#include <cstdio>
+int main()
+{
+    long long rows, cols, copies;
+    while (scanf("%lld %lld %lld", &rows, &cols, &copies) == 3) {
+        const rg::UpdateKind k = rg::update_kind(rows, cols, true, 256);
+        const unsigned long long n = (std::min(rows, cols) + 63) / 64 * 64, m = (std::max(rows, cols) + 63) / 64 * 64;
+        const auto half = [&](int t) { return copies * rg::half_tiles(n, rg::tile_side(t)); };
+        const auto whole = [&](int t) { return copies * rg::whole_tiles(n, m, rg::tile_side(t)); };
+        const auto pick = [&](int asked, auto &&count) { return asked == rg::UPDATE_TILE_SHARED ? rg::shared_tile(count, 256) : asked ? asked : rg::update_tile(count, 256, true); };
+        printf("%d %d %d\n", k.tiny, k.tiny ? 0 : pick(k.half_tile, half), k.tiny ? 0 : pick(k.whole_tile, whole));
+    }
+}
+"""
+ALL_TILES = {32, SHARED, 64, 96, 128, PAIR, 192}
+
+
+@pytest.fixture(scope="module")
+def tiles(tmp_path_factory):
+    d = tmp_path_factory.mktemp("tiles")
+    (d / "driver.cpp").write_text(TILES)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-o", str(d / "driver"), str(d / "driver.cpp")])
+
+    def ask(cases):
+        text = "\n".join(" ".join(str(int(x)) for x in c) for c in cases) + "\n"
+        out = subprocess.run([str(d / "driver")], input=text, capture_output=True, text=True, check=True).stdout.split("\n")
+        return [[int(x) for x in line.split()] for line in out[: len(cases)]]
+    return ask
+
+
+def test_every_tile_that_the_rules_give_is_run_on_the_gpu(tiles):
+    given = tiles([(r, c, k) for r in SIDES for c in SIDES for k in (1, 2, 5, 12)])
+    halves, wholes = {h for t, h, _ in given if not t}, {w for t, _, w in given if not t}
+    assert halves <= ALL_TILES and wholes <= ALL_TILES
+    run = tiles([(r, c, 1) for r, c in EVERY_TILE])
+    assert {h for _, h, _ in run} == ALL_TILES and {w for _, _, w in run} == ALL_TILES
+
+
+def test_matrices_that_are_cut_otherwise_beside_others(tiles):
+    alone, beside = tiles([(r, c, 1) for r, c, _ in CUT_OTHERWISE]), tiles(CUT_OTHERWISE)
+    for (_, h, w), (_, half, whole) in zip(alone, beside):
+        assert h == half and w != whole and not {w, whole} & {32, SHARED}
