@@ -70,3 +70,34 @@ def test_first_steps_are_the_plain_ones(rg):
         model = train.Sage(W.cfg.feat_dim, 64, 8, len(W.cfg.fanout), W.local_rows.dtype)
         got.append((train.train_epoch(rg, batches, model, make(rg, model), train.labels_of(W, 8), norm)[:3], [w.detach().clone() for w in model.weights]))
     assert torch.allclose(got[0][0], got[1][0], rtol=1e-3)
+
+
+class FewBatches(train.Batches):
+    steps = 1
+
+    def __len__(self):
+        return self.steps
+
+
+@pytest.mark.parametrize("steps,bound", [(1, 1e-3), (3, 1e-2)])
+def test_parameters_are_the_plain_ones(rg, steps, bound):
+    """Every weight, scale, shift and momentum of the two models, relative to how far it has come.  Gradients differ by fp32's roundings, 1e-6 of them, which five steps of products multiply by 485 where
+    singular values are small: 5e-4 of an update, and as much again for the momentum's share; behind three steps three times that, and what follows from it through the model, for which there is a factor of
+    three."""
+    W = workload("small")
+    batches = FewBatches(rg, W)
+    batches.steps = steps
+    models, momenta = [], []
+    for make, norm in ((train.Muon, train.layer_norm(rg)), (PlainMuon, plain_norm)):
+        model = train.Sage(W.cfg.feat_dim, 64, 8, len(W.cfg.fanout), W.local_rows.dtype)
+        optimiser = make(rg, model)
+        train.train_epoch(rg, batches, model, optimiser, train.labels_of(W, 8), norm)
+        models.append([t.detach().double() for t in model.weights + model.scales + model.shifts])
+        momenta.append([t.double() for t in optimiser.momenta])
+    start = train.Sage(W.cfg.feat_dim, 64, 8, len(W.cfg.fanout), W.local_rows.dtype)
+    before = [t.detach().double() for t in start.weights + start.scales + start.shifts]
+    assert len(before) == 3 * len(W.cfg.fanout)
+    for k, (a, b, s) in enumerate(zip(*models, before)):
+        assert float((b - s).norm()) > 0 and float((a - b).norm()) <= bound * float((b - s).norm()), k
+    for k, (a, b) in enumerate(zip(*momenta)):
+        assert float((a - b).norm()) <= bound * float(b.norm()), k
