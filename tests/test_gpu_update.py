@@ -420,3 +420,11 @@ def test_many_launches_recorded_into_a_graph(rg, dtype):
             t.fill_(7.0)
         step()
         assert all(torch.equal(a, b) for a, b in zip(got, w2 + m2))
+
+
+def test_the_largest_matrix(rg):
+    """RG_MAX_SIDE both ways: operands of 1 GiB, whose offsets are 32 bits."""
+    g = torch.randn((16_384, 16_384), generator=torch.Generator(device="cuda").manual_seed(23), device="cuda").bfloat16()
+    got, = rg.rg_orthogonalize([g], steps=2)
+    want = definition_there(g, steps=2)
+    assert off(got, want) <= 2 * SQUARE + off(want.to(g.dtype), want)
