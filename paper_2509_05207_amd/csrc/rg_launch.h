@@ -188,8 +188,8 @@ inline UpdateKind update_kind(uint64_t rows, uint64_t cols, bool wide_type, int 
     if (n <= 64 && m <= TINY_WIDE) return UpdateKind{true, true, 0, 0};
     UpdateKind k{false, wide_type || n <= UPDATE_NARROW, 0, 0};
     // Shared tiles where there are so few that they do not fill the chip anyway.
-    if (whole_tiles(n, m, 64) <= 256) k.whole_tile = UPDATE_TILE_SHARED;
-    if (k.whole_tile || half_tiles(n, 32) <= 256) k.half_tile = UPDATE_TILE_SHARED;
+    if (whole_tiles(n, m, 64) <= (uint64_t)n_cu) k.whole_tile = UPDATE_TILE_SHARED;
+    if (k.whole_tile || half_tiles(n, 32) <= (uint64_t)n_cu) k.half_tile = UPDATE_TILE_SHARED;
     else if (k.split) k.half_tile = update_tile([&](int tile) { return half_tiles(n, tile); }, n_cu, true);
     return k;
 }

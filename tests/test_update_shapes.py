@@ -120,3 +120,28 @@ def test_matrices_that_are_cut_otherwise_beside_others(tiles):
     alone, beside = tiles([(r, c, 1) for r, c, _ in CUT_OTHERWISE]), tiles(CUT_OTHERWISE)
     for (_, h, w), (_, half, whole) in zip(alone, beside):
         assert h == half and w != whole and not {w, whole} & {32, SHARED}
+
+
+UNITS = r"""
+#include "rg_launch.h"
+#include <cstdio>
+int main()
+{
+    for (int n_cu : {32, 64, 256})
+        for (unsigned n : {100u, 300u, 500u, 700u, 1000u, 1100u})
+            for (unsigned m : {100u, 1000u, 4000u, 16000u}) {
+                const rg::UpdateKind k = rg::update_kind(n, m, true, n_cu);
+                const unsigned long long least = n < m ? n : m, most = n < m ? m : n, units = n_cu;
+                const bool whole = rg::whole_tiles(least, most, 64) <= units, half = whole || rg::half_tiles(least, 32) <= units;
+                if (k.tiny) continue;
+                printf("%d %d\n", (k.whole_tile == rg::UPDATE_TILE_SHARED) == whole, (k.half_tile == rg::UPDATE_TILE_SHARED) == half);
+            }
+}
+"""
+
+
+def test_tiles_are_shared_by_the_compute_units_that_there_are(tmp_path):
+    (tmp_path / "driver.cpp").write_text(UNITS)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-o", str(tmp_path / "driver"), str(tmp_path / "driver.cpp")])
+    lines = subprocess.run([str(tmp_path / "driver")], capture_output=True, text=True, check=True).stdout.split("\n")[:-1]
+    assert len(lines) >= 60 and set(lines) == {"1 1"}
