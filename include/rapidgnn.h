@@ -492,8 +492,9 @@ rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, const void 
  *
  * All matrices of a model go in one call: what is small is bound by launches,
  * of which there are 2 + 3 * steps for every RG_UPDATES_PER_LAUNCH matrices that
- * are cut alike, and one for as many of up to 64 x 256.  A matrix' result does not
- * depend on what else is in the call.
+ * are cut alike, one for as many of up to 64 x 256, and two for every six steps of as
+ * many of RG_F32 with up to 36 rows or columns (48, with more than 1,024 of the
+ * other).  A matrix' result does not depend on what else is in the call.
  *
  *   u        host, [n]: the matrices (the arrays on the device)
  *   type     of grad, weight and out; momenta are fp32
@@ -501,9 +502,12 @@ rg_status rg_layer_norm_backward(const void *dy, uint64_t dy_stride, const void 
  *   workspace  dev, 256-byte aligned, as many bytes as rg_update_workspace says for the same u
  * The state X is fp32 throughout and sums are in 32 bits; the operands of the
  * products have 22 bits, and none below 2^-38 of the matrix' norm, whatever the
- * type.  Before its rounding a result is off by 1e-5 and less of its 2-norm, or
- * 1.2e-4 where G's singular values lie further apart than a factor of a hundred.
- * A matrix with an infinity or a NaN comes out all NaN.  rows and cols up to RG_MAX_SIDE; matrices without elements are passed over.
+ * type.  Before its rounding the result of five steps is off by 1e-5 and less of
+ * its 2-norm, or 1.2e-4 where G's singular values lie further apart than a factor
+ * of a hundred.  RG_F32 matrices of few rows or columns (see above) have their
+ * products in 64 bits: six steps are off by their rounding alone.  A matrix with
+ * an infinity or a NaN comes out all NaN.  rows and cols up to RG_MAX_SIDE;
+ * matrices without elements are passed over.
  * Outputs may be the inputs that they replace, with the same stride; other
  * overlaps, also between matrices, are not allowed.
  */

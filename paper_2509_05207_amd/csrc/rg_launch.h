@@ -175,18 +175,32 @@ template <typename F> inline int shared_tile(F &&tiles, int n_cu) { return tiles
 // shared ones, so that whether tiles are shared goes by the matrix alone.  Operands in two parts have two cross terms, added in an order that is another one in a
 // tile's reflection: which elements are reflected, that is the symmetric products' tile, then goes by the matrix alone too.
 constexpr uint64_t TINY_WIDE = 256, UPDATE_NARROW = 32;
+// fp32 matrices whose products are made in 64 bits: where with operands of 22 bits and sums of 32 the results are further off than by fp32 products.  (Of 48 matrices of n x m so many by more than half: 4 x 50 26, 16 x 200
+// 38, 28 x 2,500 10, 33 x 200 3, 36 x 130 to 700 0, 36 x 1,204 9, 40 x 700 0, 40 x 1,204 4, from 44 on none.)
+constexpr uint64_t UPDATE_NARROW_SIDE = 48;
+inline bool narrow(uint64_t rows, uint64_t cols)
+{
+    const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);
+    return n <= 36 || (n <= UPDATE_NARROW_SIDE && m > 1024);
+}
+// Columns of a narrow matrix to a part of its first sums, and to a workgroup of the rest: at least as many as keep its waves busy, and 32 parts and workgroups at most (all of them read all parts).
+constexpr uint32_t narrow_part(uint64_t m) { return 256 * (uint32_t)((m + 256 * 32 - 1) / (256 * 32)); }
+constexpr uint32_t narrow_parts(uint64_t m) { return (uint32_t)((m + narrow_part(m) - 1) / narrow_part(m)); }
+constexpr uint32_t narrow_share(uint64_t m) { return std::max(64u, 16 * (uint32_t)((m + 16 * 32 - 1) / (16 * 32))); }
+constexpr uint32_t narrow_shares(uint64_t m) { return (uint32_t)((m + narrow_share(m) - 1) / narrow_share(m)); }
 struct UpdateKind {
     bool tiny;                           // up to 64 x TINY_WIDE: a workgroup does it all
     bool split;                          // operands in two parts
     int half_tile, whole_tile;           // of the symmetric products and of the others; 0: by all matrices of a launch
-    bool operator==(const UpdateKind &o) const { return tiny == o.tiny && split == o.split && half_tile == o.half_tile && whole_tile == o.whole_tile; }
+    bool narrow;                         // products in 64 bits (fp32 alone: set by who knows the type)
+    bool operator==(const UpdateKind &o) const { return narrow == o.narrow && tiny == o.tiny && split == o.split && half_tile == o.half_tile && whole_tile == o.whole_tile; }
 };
 // wide_type: two parts whatever the size, which is what a result that is rounded once takes, of any type (rg_update.hip asks for nothing else).
 inline UpdateKind update_kind(uint64_t rows, uint64_t cols, bool wide_type, int n_cu)
 {
     const uint64_t n = std::min(rows, cols), m = std::max(rows, cols);
-    if (n <= 64 && m <= TINY_WIDE) return UpdateKind{true, true, 0, 0};
-    UpdateKind k{false, wide_type || n <= UPDATE_NARROW, 0, 0};
+    if (n <= 64 && m <= TINY_WIDE) return UpdateKind{true, true, 0, 0, false};
+    UpdateKind k{false, wide_type || n <= UPDATE_NARROW, 0, 0, false};
     // Shared tiles where there are so few that they do not fill the chip anyway.
     if (whole_tiles(n, m, 64) <= (uint64_t)n_cu) k.whole_tile = UPDATE_TILE_SHARED;
     if (k.whole_tile || half_tiles(n, 32) <= (uint64_t)n_cu) k.half_tile = UPDATE_TILE_SHARED;

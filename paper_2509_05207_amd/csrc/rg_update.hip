@@ -7,8 +7,8 @@
 // Precision.  A rounding of X itself is noise in the directions of X's small singular values, which every step
 // multiplies by 3.4; a rounding of P only tilts the directions that are there.  So the state X is kept in fp32 and a X is added from it.  The operands of
 // the products are fp16 numbers, scaled by 2^14, since nothing here is four or more (singular values stay below 1.21, A's entries below 1.46, P's below 2.9), and
-// always the sum of two, 22 bits, with no digits below 2^-38 of the matrix' norm; a product is three, hi hi + hi lo + lo hi.  Results are 1e-7 to 6e-6 off so (relative, 2-norm), as much as by
-// fp32 products, whatever the type; its own rounding comes last, once.  One part, 11 bits, is not enough for matrices of 16 bits either: roundings of singular values that are alike
+// always the sum of two, 22 bits, with no digits below 2^-38 of the matrix' norm; a product is three, hi hi + hi lo + lo hi.  Results are 1e-7 to 3e-6 off so (relative, 2-norm), as much as by
+// fp32 products, whatever the type; its own rounding comes last, once.  (fp32 matrices of few rows, of which that is not so, have products in 64 bits: see narrow matrices.)  One part, 11 bits, is not enough for matrices of 16 bits either: roundings of singular values that are alike
 // do not average out (43 rows of a unit matrix 8e-3 off, 48 x 4,096 orthonormal rows 4e-3, 400 x 500 of noise 1.6e-3, where rounding to bf16 costs 1.7e-3 and to fp16 2e-4).
 //
 // The division by the norm is exact: X starts as G 2^-e with a norm in [1/2, 1), and the factor f = 2^e / (|G| + eps) that is left
@@ -49,8 +49,8 @@ struct Matrix {
     rg_update u;
     int32_t n, m, n_pad, m_pad;          // narrower and wider side, and padded
     bool tall;                           // rows > cols: X is the transpose
-    uint32_t sum_blocks;                 // workgroups of the first pass
-    double *sums;                        // [sum_blocks]
+    uint32_t sum_blocks;                 // workgroups of the first pass; of a narrow matrix, parts of its columns
+    double *sums;                        // [sum_blocks]; of a narrow matrix, of tiles of A
     float *factor;                       // f
     float *x;                            // [n_pad][m_pad]
     f16 *xr, *xt[2];                     // operands: X's rows [n_pad][m_pad], its columns [m_pad][n_pad] before and after a step
@@ -818,6 +818,253 @@ __global__ void __launch_bounds__(TINY_THREADS) update_tiny_kernel(Group g, uint
     }
 }
 
+// ---------------------------------------------------------------- narrow matrices
+// Of few rows A and P have so few entries that their roundings do not average out, as they do over the singular values of larger matrices: with operands of 22 bits and sums of 32, fp32 results
+// were 1e-6 to 5e-6 off, two to three times as much as by fp32 products (see narrow in rg_launch.h; to 16 bits a result is rounded 50 times as far and more).  But there all of it is cheap but X itself, and every X is a
+// polynomial of A in front of the first one: with B = U U^T, r = 1 / (|U| + eps), A = r^2 B,
+//     Q = a + b A + c A^2,   M <- Q M,   A <- Q^2 A,   and at last X = r M U.
+// These few n x n products are made in 64 bits, and X is rounded once: results are off by that rounding alone, 3e-8.  Everything is symmetric and commutes, so that
+// only the lower half of a product is computed, and both operands are read along their rows.  A direction that U lacks has an A of 1e-16 instead of none, of either sign, which grows 12 times a step: up to
+// NARROW_STEPS steps are taken at once, in which that stays nothing, and then X is kept, in fp32, and B made of it again.
+//
+// One launch sums B up, by parts of X's columns; in another every workgroup adds the parts up in their order, makes M, and has its own columns of X.  (All workgroups make the same M, which takes as long as one that the
+// others would wait for, and a launch less.)  What is up to TINY_WIDE has one part, and one workgroup and one launch for all of it.  Bound by the 64-bit matrix operations, of about 115 cycles each on
+// a vector unit, and the latency of five barriers a step (16 x 256, us: 16, of which 1.6 a step; 32 x 256 24, 2.5 a step;
+// 48 x 4,096 48, 16 x 16,384 28; with operands of 22 bits 17, 20, 116 and 304).
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+constexpr double EXACT_A = 3.4445, EXACT_B = -4.7750, EXACT_C = 2.0315;
+constexpr int NARROW_THREADS = 1024, NARROW_WAVES = 16;
+constexpr uint32_t NARROW_STEPS = 6;
+constexpr int NARROW_PASS = 256;         // columns of U in LDS at a time
+
+struct Narrow {
+    int n, m, blocks, length, tiles;     // blocks of 16 rows; of a row in LDS; tiles of the lower half
+    __device__ __forceinline__ explicit Narrow(const Matrix &a) : n(a.n), m(a.m), blocks((a.n + 15) / 16), length(16 * (blocks | 1)), tiles(blocks * (blocks + 1) / 2) {}
+};
+// Rows of 16 or 48 numbers: two rows of 16 numbers of 64 bits, or four of 32, lie on all banks once.
+constexpr int NARROW_GRAM_LDS = NARROW_PASS * 48 * 4, NARROW_LDS = std::max(NARROW_GRAM_LDS, 3 * 48 * 48 * 8);
+static_assert(UPDATE_NARROW_SIDE == 48, "three blocks of rows at most");
+
+// Where element e of a lane lies in a tile of 16 x 16 that a 64-bit matrix operation leaves.
+__device__ __forceinline__ int row64(int e) { return 4 * e + (((int)threadIdx.x & 63) >> 4); }
+
+// U at (row of X, column of X).
+__device__ __forceinline__ float narrow_at(const Group &g, const Matrix &m, bool first, int i, int c)
+{
+    if (!first) return m.x[(uint64_t)i * m.m_pad + c];
+    const int r = m.tall ? c : i, k = m.tall ? i : c;
+    const float v = row_at<float>(m.u.grad, m.u.grad_stride, r)[k];
+    return g.muon ? update_of(g, v, row_at<float>(m.u.momentum_out, m.u.momentum_out_stride, r)[k]) : v;
+}
+
+// The part's share of B, and (muon) the new momentum of its columns.
+__device__ __forceinline__ void narrow_gram(const Group &g, const Matrix &m, bool first, uint32_t part, uint8_t *lds_bytes)
+{
+    const Narrow s(m);
+    float *columns = reinterpret_cast<float *>(lds_bytes);         // [NARROW_PASS][length]: a column of U after another
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const int slices = NARROW_WAVES / s.tiles, slice = wave / s.tiles, tile = wave % s.tiles, quads = s.blocks * 4;      // a tile has several waves, each with its own columns
+    int32_t ti, tj;
+    half_tile((uint32_t)tile, ti, tj);
+    f64x4 acc = {0.0, 0.0, 0.0, 0.0};
+    const int each = (int)narrow_part((uint64_t)s.m), from = (int)part * each, to = min(s.m, from + each);
+    for (int c0 = from; c0 < to; c0 += NARROW_PASS) {
+        const int count = min(NARROW_PASS, to - c0);
+        // Four rows of a column a thread; neighbours along G's rows.
+        for (int u = threadIdx.x; u < NARROW_PASS * quads; u += NARROW_THREADS) {
+            const int quad = m.tall ? u % quads : u / NARROW_PASS, c = m.tall ? u / quads : u % NARROW_PASS;
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+            if (c < count) {
+                if (first && g.muon) {
+                    float old[4] = {}, grad[4] = {};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = quad * 4 + e, r = m.tall ? c0 + c : i, k = m.tall ? i : c0 + c;
+                        if (i >= s.n) continue;
+                        grad[e] = row_at<float>(m.u.grad, m.u.grad_stride, r)[k];
+                        old[e] = row_at<float>(m.u.momentum, m.u.momentum_stride, r)[k];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = quad * 4 + e, r = m.tall ? c0 + c : i, k = m.tall ? i : c0 + c;
+                        if (i >= s.n) continue;
+                        const float next = g.momentum * old[e] + grad[e];
+                        row_at<float>(m.u.momentum_out, m.u.momentum_out_stride, r)[k] = next;
+                        v[e] = update_of(g, grad[e], next);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (quad * 4 + e < s.n) v[e] = narrow_at(g, m, first, quad * 4 + e, c0 + c);
+                }
+            }
+            *reinterpret_cast<f32x4 *>(columns + c * s.length + quad * 4) = v;
+        }
+        __syncthreads();
+        if (slice < slices)
+            for (int k = slice * 4; k < count; k += slices * 4) {
+                const float *at = columns + (k + (lane >> 4)) * s.length + (lane & 15);
+                acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)at[ti * 16], (double)at[tj * 16], acc, 0, 0, 0);
+            }
+        __syncthreads();
+    }
+    double *sums = reinterpret_cast<double *>(lds_bytes);
+    if (slice < slices)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[(slice * s.tiles + tile) * 256 + e * 64 + lane] = acc[e];
+    __syncthreads();
+    const int all = s.tiles * 256;
+    for (int q = threadIdx.x; q < all; q += NARROW_THREADS) {
+        double v = sums[q];
+        for (int k = 1; k < slices; ++k) v += sums[k * all + q];
+        m.sums[(uint64_t)part * all + q] = v;
+    }
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(NARROW_THREADS) narrow_gram_kernel(Group g, bool first)
+{
+    extern __shared__ __align__(16) uint8_t lds_bytes[];
+    uint32_t part;
+    const Matrix &m = g.mat[matrix_of(g.starts, blockIdx.x, part)];
+    narrow_gram(g, m, first, part, lds_bytes);
+}
+
+// Tile (ti, tj) of the product of two symmetric matrices in LDS.  All operands are read ahead of the operations, which are in two chains: each waits for the one before it in its chain.
+template <int BLOCKS> __device__ __forceinline__ f64x4 narrow_product(const double *x, const double *y, int ti, int tj)
+{
+    constexpr int LENGTH = 16 * (BLOCKS | 1);
+    const int lane = threadIdx.x & 63, at = (lane >> 4) * LENGTH + (lane & 15);
+    double l[BLOCKS * 4], r[BLOCKS * 4];
+#pragma unroll
+    for (int k = 0; k < BLOCKS * 4; ++k) {
+        l[k] = x[at + k * 4 * LENGTH + ti * 16];
+        r[k] = y[at + k * 4 * LENGTH + tj * 16];
+    }
+    f64x4 acc[2] = {{0.0, 0.0, 0.0, 0.0}, {0.0, 0.0, 0.0, 0.0}};
+#pragma unroll
+    for (int k = 0; k < BLOCKS * 4; ++k) acc[k & 1] = __builtin_amdgcn_mfma_f64_16x16x4f64(l[k], r[k], acc[k & 1], 0, 0, 0);
+    return acc[0] + acc[1];
+}
+__device__ __forceinline__ f64x4 narrow_product(const double *x, const double *y, int ti, int tj, const Narrow &s)
+{
+    switch (s.blocks) {
+    case 1: return narrow_product<1>(x, y, ti, tj);
+    case 2: return narrow_product<2>(x, y, ti, tj);
+    default: return narrow_product<3>(x, y, ti, tj);
+    }
+}
+
+// A tile and its reflection.
+__device__ __forceinline__ void narrow_put(double *to, int ti, int tj, const Narrow &s, const f64x4 &v)
+{
+    const int j = tj * 16 + ((int)threadIdx.x & 15);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int i = ti * 16 + row64(e);
+        to[i * s.length + j] = v[e];
+        if (ti != tj) to[j * s.length + i] = v[e];
+    }
+}
+
+// ALONE: the matrix' only workgroup, which makes B too.
+template <bool MUON, bool ALONE>
+__global__ void __launch_bounds__(NARROW_THREADS) narrow_apply_kernel(Group g, uint32_t steps, bool first, bool last)
+{
+    extern __shared__ __align__(16) uint8_t lds_bytes[];
+    uint32_t group;
+    const Matrix &m = g.mat[matrix_of(g.whole, blockIdx.x, group)];
+    if (ALONE) narrow_gram(g, m, first, 0, lds_bytes);
+    const Narrow s(m);
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, all = s.tiles * 256;
+    const int size = s.blocks * 16 * s.length;
+    double *a = reinterpret_cast<double *>(lds_bytes), *q = a + size, *p = q + size;                     // B and then A, Q, M
+    for (int x = threadIdx.x; x < all; x += NARROW_THREADS) {
+        double v = 0.0;
+        for (uint32_t k = 0; k < m.sum_blocks; ++k) v += m.sums[(uint64_t)k * all + x];
+        int32_t ti, tj;
+        half_tile((uint32_t)x / 256, ti, tj);
+        const int i = ti * 16 + row64((x >> 6) & 3), j = tj * 16 + (x & 15);
+        a[i * s.length + j] = v;
+        if (ti != tj) a[j * s.length + i] = v;
+    }
+    __syncthreads();
+    double r = 1.0;
+    if (first) {
+        double squares = lane < s.n ? a[lane * s.length + lane] : 0.0;
+        for (int k = 1; k < 64; k <<= 1) squares += __shfl_xor(squares, k);
+        r = squares < INFINITY ? 1.0 / (sqrt(squares) + (double)g.eps) : NAN;                            // nothing over nothing is a NaN by B
+    }
+    double scale = r * r;                                          // of the first step, whose A is this times B
+    for (uint32_t step = 0; step < steps; ++step) {
+        const bool more = step + 1 < steps;
+        if (wave < s.tiles) {
+            int32_t ti, tj;
+            half_tile((uint32_t)wave, ti, tj);
+            f64x4 v = narrow_product(a, a, ti, tj, s);
+            const int j = tj * 16 + (lane & 15);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = ti * 16 + row64(e);
+                v[e] = (i == j ? EXACT_A : 0.0) + scale * (EXACT_B * a[i * s.length + j] + scale * EXACT_C * v[e]);
+            }
+            narrow_put(q, ti, tj, s, v);
+            if (step == 0) narrow_put(p, ti, tj, s, v);
+        }
+        __syncthreads();
+        // Q A and Q M, in the places of A and M: a wave a tile, 12 of them at most
+        const int from = more ? 0 : s.tiles, units = s.tiles * (step == 0 ? 1 : 2);
+        const int unit = from + wave;
+        int32_t ti = 0, tj = 0;
+        f64x4 v = {0.0, 0.0, 0.0, 0.0};
+        if (unit < units) {
+            half_tile((uint32_t)(unit % s.tiles), ti, tj);
+            v = narrow_product(q, unit < s.tiles ? a : p, ti, tj, s);
+        }
+        __syncthreads();
+        if (unit < units) narrow_put(unit < s.tiles ? a : p, ti, tj, s, v);
+        __syncthreads();
+        if (!more) break;
+        if (wave < s.tiles) {
+            half_tile((uint32_t)wave, ti, tj);
+            v = narrow_product(q, a, ti, tj, s);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] *= scale;
+        }
+        __syncthreads();
+        if (wave < s.tiles) narrow_put(a, ti, tj, s, v);
+        __syncthreads();
+        scale = 1.0;
+    }
+    // X = r M U, 16 columns of it a wave at a time: it reads all of them before it writes the first, which may be in their place.
+    const float grow = MUON ? g.lr * sqrtf(fmaxf(1.f, (float)m.u.rows / (float)m.u.cols)) : 0.f;
+    const int each = ALONE ? s.m : (int)narrow_share((uint64_t)s.m), to = min(s.m, ((int)group + 1) * each);
+    for (int c0 = (int)group * each + wave * 16; c0 < to; c0 += NARROW_WAVES * 16) {
+        const int c = c0 + (lane & 15);
+        float u[12];
+#pragma unroll
+        for (int k = 0; k < 12; ++k) {
+            const int i = k * 4 + (lane >> 4);
+            u[k] = i < s.n && c < to ? narrow_at(g, m, first, i, c) : 0.f;
+        }
+        for (int t = 0; t < s.blocks; ++t) {
+            f64x4 v = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+            for (int k = 0; k < 12; ++k)
+                if (k < s.blocks * 4) v = __builtin_amdgcn_mfma_f64_16x16x4f64(p[(k * 4 + (lane >> 4)) * s.length + t * 16 + (lane & 15)], (double)u[k], v, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = t * 16 + row64(e), row = m.tall ? c : i, col = m.tall ? i : c;
+                if (i >= s.n || c >= to) continue;
+                const float x = (float)(r * v[e]);
+                if (!last) m.x[(uint64_t)i * m.m_pad + c] = x;
+                else if constexpr (MUON) row_at<float>(m.u.out, m.u.out_stride, row)[col] = g.keep * row_at<float>(m.u.weight, m.u.weight_stride, row)[col] - grow * x;
+                else row_at<float>(m.u.out, m.u.out_stride, row)[col] = x;
+            }
+        }
+    }
+}
+
 // ---------------------------------------------------------------- launches
 // LDS beyond 64 KB has to be asked for, once per kernel and device.
 template <typename K> rg_status allow_lds(K kernel, int bytes, std::atomic<uint64_t> &known)
@@ -905,6 +1152,20 @@ template <typename T, bool MUON> rg_status launch_tiny(const Group &g, uint32_t 
     return RG_OK;
 }
 
+template <bool MUON, bool ALONE> rg_status launch_narrow(const Group &g, uint32_t steps, const Shape &s, hipStream_t st)
+{
+    static_assert(NARROW_GRAM_LDS <= 64 * 1024 && NARROW_LDS <= 64 * 1024, "more has to be asked for");
+    for (uint32_t k = 0; k < steps; k += NARROW_STEPS) {
+        if (!ALONE) {
+            hipLaunchKernelGGL(narrow_gram_kernel, dim3(s.starts), dim3(NARROW_THREADS), NARROW_GRAM_LDS, st, g, k == 0);
+            RG_HIP(hipGetLastError());
+        }
+        hipLaunchKernelGGL((narrow_apply_kernel<MUON, ALONE>), dim3(s.whole), dim3(NARROW_THREADS), NARROW_LDS, st, g, std::min(NARROW_STEPS, steps - k), k == 0, k + NARROW_STEPS >= steps);
+        RG_HIP(hipGetLastError());
+    }
+    return RG_OK;
+}
+
 // Hands out the workspace; with no workspace it only counts.
 struct Carver {
     uint8_t *base;
@@ -925,6 +1186,13 @@ void lay_out(Matrix &m, const rg_update &u, const UpdateKind &kind, Carver &c)
     m.n_pad = (m.n + UPDATE_PAD - 1) / UPDATE_PAD * UPDATE_PAD;
     m.m_pad = (m.m + UPDATE_PAD - 1) / UPDATE_PAD * UPDATE_PAD;
     const uint64_t nm = (uint64_t)m.n_pad * m.m_pad, nn = (uint64_t)m.n_pad * m.n_pad;
+    if (kind.narrow) {
+        m.sum_blocks = narrow_parts((uint64_t)m.m);
+        const uint64_t blocks = (uint64_t)(m.n + 15) / 16;
+        c.take(m.sums, m.sum_blocks * (blocks * (blocks + 1) / 2) * 256);
+        c.take(m.x, nm);                                           // where there are more than NARROW_STEPS steps
+        return;
+    }
     c.take(m.sums, SUM_BLOCKS);
     c.take(m.factor, 1);
     if (kind.tiny) return;                                         // all the rest in registers and LDS
@@ -933,15 +1201,22 @@ void lay_out(Matrix &m, const rg_update &u, const UpdateKind &kind, Carver &c)
     for (f16 **p : {&m.a, &m.p}) c.take(*p, nn * 2);
 }
 
+UpdateKind kind_of_matrix(const rg_update &u, uint32_t type, int n_cu)
+{
+    UpdateKind k = update_kind(u.rows, u.cols, true, n_cu);
+    k.narrow = type == RG_F32 && narrow(u.rows, u.cols);
+    return k;
+}
+
 // Groups of matrices of a size class, in order, each with the whole workspace to itself.
 struct Options { bool muon, nesterov; float momentum, lr, weight_decay, eps; uint32_t steps; };
 
-template <typename F> rg_status each_group(const rg_update *u, uint32_t n, F &&body)
+template <typename F> rg_status each_group(const rg_update *u, uint32_t n, uint32_t type, F &&body)
 {
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
     const auto empty = [&](uint32_t k) { return u[k].rows == 0 || u[k].cols == 0; };
-    const auto kind_of = [&](uint32_t k) { return update_kind(u[k].rows, u[k].cols, true, n_cu); };
+    const auto kind_of = [&](uint32_t k) { return kind_of_matrix(u[k], type, n_cu); };
     for (uint32_t first = 0; first < n; ++first) {
         if (empty(first)) continue;
         const UpdateKind kind = kind_of(first);
@@ -969,21 +1244,31 @@ rg_status run_group(const UpdateKind &kind, int n_cu, const rg_update *const *u,
     g.eps = o.eps;
     Carver c{workspace};
     for (uint32_t k = 0; k < count; ++k) lay_out(g.mat[k], *u[k], kind, c);
+    Shape s{};
+    for (Starts *p : {&g.sums, &g.starts, &g.half, &g.whole})
+        for (uint32_t &x : p->first) x = UINT32_MAX;
+    if constexpr (std::is_same_v<T, float>)
+        if (kind.narrow) {
+            for (uint32_t k = 0; k < count; ++k) {
+                g.starts.first[k] = s.starts; g.whole.first[k] = s.whole;
+                s.starts += g.mat[k].sum_blocks;
+                s.whole += kind.tiny ? 1u : narrow_shares((uint64_t)g.mat[k].m);
+            }
+            if (kind.tiny) return g.muon ? launch_narrow<true, true>(g, o.steps, s, st) : launch_narrow<false, true>(g, o.steps, s, st);
+            return g.muon ? launch_narrow<true, false>(g, o.steps, s, st) : launch_narrow<false, false>(g, o.steps, s, st);
+        }
     if (kind.tiny) return g.muon ? launch_tiny<T, true>(g, count, o.steps, st) : launch_tiny<T, false>(g, count, o.steps, st);
     const auto tiles = [&](int tile, bool half) {
         uint64_t all = 0;
         for (uint32_t k = 0; k < count; ++k) all += half ? half_tiles(g.mat[k].n_pad, tile_side(tile)) : whole_tiles(g.mat[k].n_pad, g.mat[k].m_pad, tile_side(tile));
         return all;
     };
-    Shape s{};
     const auto pick = [&](int asked, bool half) {
         const auto count_of = [&](int tile) { return tiles(tile, half); };
         return asked == UPDATE_TILE_SHARED ? shared_tile(count_of, n_cu) : asked ? asked : update_tile(count_of, n_cu, kind.split);
     };
     s.half_tile = pick(kind.half_tile, true);
     s.whole_tile = pick(kind.whole_tile, false);
-    for (Starts *p : {&g.sums, &g.starts, &g.half, &g.whole})
-        for (uint32_t &x : p->first) x = UINT32_MAX;
     for (uint32_t k = 0; k < count; ++k) {
         Matrix &m = g.mat[k];
         m.sum_blocks = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(SUM_BLOCKS, (uint64_t)m.n * m.m / 4096));
@@ -1022,10 +1307,10 @@ rg_status check_place(uint32_t k, const char *what, const void *out, uint64_t ou
     return RG_EINVAL;
 }
 
-rg_status workspace_of(const rg_update *u, uint32_t n, uint64_t *bytes)
+rg_status workspace_of(const rg_update *u, uint32_t n, uint32_t type, uint64_t *bytes)
 {
     uint64_t most = 0;
-    RG_TRY(each_group(u, n, [&](const UpdateKind &kind, int, const rg_update *const *picked, uint32_t count) {
+    RG_TRY(each_group(u, n, type, [&](const UpdateKind &kind, int, const rg_update *const *picked, uint32_t count) {
         Carver c{nullptr};
         for (uint32_t k = 0; k < count; ++k) {
             Matrix m;
@@ -1058,12 +1343,12 @@ rg_status run_updates(const rg_update *u, uint32_t n, uint32_t type, const Optio
         RG_TRY(check_place(k, "momentum_out", u[k].momentum_out, u[k].momentum_out_stride, u[k].momentum, u[k].momentum_stride, u[k]));
     }
     uint64_t want = 0;
-    RG_TRY(workspace_of(u, n, &want));
+    RG_TRY(workspace_of(u, n, type, &want));
     if (want && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256)) { set_error("the workspace is null or not aligned to 256 bytes"); return RG_EINVAL; }
     if (workspace_bytes < want) { set_error("the workspace holds %llu bytes of %llu", (unsigned long long)workspace_bytes, (unsigned long long)want); return RG_ERANGE; }
     const hipStream_t st = as_stream(stream);
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    return each_group(u, n, [&](const UpdateKind &kind, int n_cu, const rg_update *const *picked, uint32_t count) {
+    return each_group(u, n, type, [&](const UpdateKind &kind, int n_cu, const rg_update *const *picked, uint32_t count) {
         return type == RG_F32 ? run_group<float>(kind, n_cu, picked, count, o, ws, st) : type == RG_BF16 ? run_group<bf16>(kind, n_cu, picked, count, o, ws, st) : run_group<f16>(kind, n_cu, picked, count, o, ws, st);
     });
 }
@@ -1077,7 +1362,7 @@ extern "C" rg_status rg_update_workspace(const rg_update *u, uint32_t n, uint32_
 {
     if (!bytes) { set_error("null argument"); return RG_EINVAL; }
     RG_TRY(check_updates(u, n, type));
-    return workspace_of(u, n, bytes);
+    return workspace_of(u, n, type, bytes);
 }
 
 extern "C" rg_status rg_orthogonalize(const rg_update *u, uint32_t n, uint32_t type, uint32_t steps, float eps, void *workspace, uint64_t workspace_bytes, void *stream)

@@ -428,3 +428,95 @@ def test_the_largest_matrix(rg):
     got, = rg.rg_orthogonalize([g], steps=2)
     want = definition_there(g, steps=2)
     assert off(got, want) <= 2 * SQUARE + off(want.to(g.dtype), want)
+
+
+# fp32 matrices of few rows.  The polynomial in 64 bits: 1e-9 (singular values that come of nothing, 1e-16, grow 12 times a step); its product with U rounded to fp32, 2^-24.
+NARROW = 2.0 ** -24 + 1e-9
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 15, 16, 17, 31, 32, 33, 36, 37, 47, 48])
+@pytest.mark.parametrize("tall", [False, True])
+def test_narrow_matrices_are_exact(rg, n, tall):
+    """Every number of blocks, passes of columns, parts and shares, just full and one more or less; a result is its rounding alone off."""
+    for m in (n, n + 1, 3 * n + 2, 64, 65, 100, 255, 256, 257, 1023, 1025, 2049, 9001, 16_384):
+        if m < n or (n > 36 and m <= 1024):
+            continue
+        for kind in ("noise", "sizes", "low", "unit"):
+            g = structured(kind, m if tall else n, n if tall else m, torch.float32)
+            want = definition_there(g)
+            assert off(rg.rg_orthogonalize([g])[0], want) <= 2 * NARROW + off(want.float(), want), (m, kind)
+
+
+@pytest.mark.parametrize("n", [1, 2, 17, 36, 37, 48, 49, 64])
+@pytest.mark.parametrize("dtype", list(BOUND))
+@pytest.mark.parametrize("tall", [False, True])
+def test_few_rows_of_every_type(rg, dtype, n, tall):
+    """Either side of what is made in 64 bits, and of what is made in one launch."""
+    for m in (n, 100, 255, 256, 257, 1024, 1025, 9001):
+        if m < n:
+            continue
+        g = structured("sizes", m if tall else n, n if tall else m, dtype)
+        want = definition_there(g)
+        assert off(rg.rg_orthogonalize([g])[0], want) <= 2e-5 + off(want.to(dtype), want), m
+
+
+@pytest.mark.parametrize("steps", [1, 2, 6, 7, 12, 13, 32])
+@pytest.mark.parametrize("rows,cols", [(1, 9), (5, 400), (700, 30), (32, 256), (48, 1100), (20, 30)])
+def test_steps_of_narrow_matrices(rg, rows, cols, steps):
+    """Beyond six steps the state is rounded to fp32 between them: the bounds of fp32, as for other matrices."""
+    g = made(rows, cols, torch.float32, 24)
+    want = definition(g, steps)
+    assert off(rg.rg_orthogonalize([g], steps=steps)[0], want) <= (2 * NARROW + 2.0 ** -24 if steps <= 6 else BOUND[torch.float32] * 3.5)
+
+
+@pytest.mark.parametrize("steps", [5, 13, 32])
+@pytest.mark.parametrize("rows,cols", [(30, 80), (48, 1300), (300, 7), (2, 300)])
+def test_narrow_matrices_without_rank(rg, rows, cols, steps):
+    """Rows that are multiples of one row, or empty: directions that the matrix lacks stay out of the result, whose singular values stay below 1.21 however many steps there are."""
+    g = torch.zeros((rows, cols), device="cuda")
+    g[: (rows + 1) // 2] = made(1, cols, torch.float32, 25) * torch.arange(1, (rows + 1) // 2 + 1, device="cuda")[:, None]
+    got = rg.rg_orthogonalize([g], steps=steps)[0]
+    assert bool(got.isfinite().all()) and float(torch.linalg.svdvals(got.double().cpu()).max()) <= 1.25
+    assert not got[(rows + 1) // 2:].any()
+    if steps == 5:
+        assert off(got, definition(g)) <= 2 * NARROW + 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", list(BOUND))
+@pytest.mark.parametrize("rows,cols", [(3, 5), (41, 512), (1000, 24), (32, 200), (1100, 48), (16, 16_384)])
+@pytest.mark.parametrize("steps", [5, 8])
+def test_optimiser_step_on_few_rows(rg, dtype, rows, cols, steps):
+    """In other tensors, in place, in the gradient's place, and beside others: the same bits; what they are, by the definition of the update that fp32 gives."""
+    w, g, m = made(rows, cols, dtype, 26), made(rows, cols, dtype, 27, "sizes"), made(rows, cols, torch.float32, 28) * 4
+    options = dict(lr=0.5, weight_decay=0.1, momentum=0.9, steps=steps)
+    w2, m2 = torch.empty_like(w), torch.empty_like(m)
+    rg.rg_muon_step([w], [g], [m], out_weights=[w2], out_momenta=[m2], **options)
+    want_m = 0.9 * m.double() + g.double()
+    assert off(m2, want_m) <= 2.0 ** -23
+    change = 0.5 * math.sqrt(max(1.0, rows / cols)) * definition_there(g.double() + 0.9 * want_m, steps)
+    want = w.double() * (1 - 0.5 * 0.1) - change
+    # the update (of which, in 64 bits or not, three roundings make what is orthogonalised); then the sum's roundings, two of them
+    e = (3.5e-5 if steps > 6 else 1e-5) * float(change.norm()) + 2.0 ** -23 * float(want.norm())
+    assert float((w2.double() - want).norm()) <= 2 * e + float((want.to(dtype).double() - want).norm())
+    others = [made(r, c, dtype, 29) for r, c in ((500, 300), (7, 700), (20, 20))]
+    w3, m3 = [w.clone()] + [t.clone() for t in others], [m.clone()] + [t.float() for t in others]
+    rg.rg_muon_step(w3, [g] + others, m3, **options)
+    assert torch.equal(w3[0], w2) and torch.equal(m3[0], m2)
+    rg.rg_muon_step([w], [g], [m], out_weights=[g], **options)                  # the result where the gradient was
+    assert torch.equal(g, w2) and torch.equal(m, m2)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (16, 70), (48, 3000), (9000, 32)])
+def test_narrow_matrices_of_nothing_and_of_no_numbers(rg, rows, cols):
+    z = torch.zeros((rows, cols), device="cuda")
+    assert not rg.rg_orthogonalize([z])[0].any() and bool(rg.rg_orthogonalize([z], eps=0.0)[0].isnan().all())
+    for steps in (1, 5, 9):
+        for bad in (float("nan"), float("inf"), float("-inf")):
+            g = made(rows, cols, torch.float32, 30)
+            g[rows // 2, cols // 2] = bad
+            assert bool(rg.rg_orthogonalize([g], steps=steps)[0].isnan().all())
+    for size in (1e-38, 1e-44, 1e36):
+        g = (made(rows, cols, torch.float64, 31) / 0.01 * size).float()
+        if g.any():
+            want = definition_there(g, eps=0.0)
+            assert off(rg.rg_orthogonalize([g], eps=0.0)[0], want) <= 2 * NARROW + 2.0 ** -24

@@ -145,3 +145,41 @@ def test_tiles_are_shared_by_the_compute_units_that_there_are(tmp_path):
     subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-o", str(tmp_path / "driver"), str(tmp_path / "driver.cpp")])
     lines = subprocess.run([str(tmp_path / "driver")], capture_output=True, text=True, check=True).stdout.split("\n")[:-1]
     assert len(lines) >= 60 and set(lines) == {"1 1"}
+
+
+NARROW = r"""
+#include "rg_launch.h"
+#include <cstdio>
+int main()
+{
+    for (unsigned long long m = 1; m <= 16384; ++m)
+        printf("%llu %u %u %u %u\n", m, rg::narrow_part(m), rg::narrow_parts(m), rg::narrow_share(m), rg::narrow_shares(m));
+}
+"""
+
+
+def test_columns_of_narrow_matrices_are_all_shared_out(tmp_path):
+    """Parts of whole passes, shares of whole tiles, none of them empty, 32 at most, and one part where one workgroup does it all."""
+    (tmp_path / "driver.cpp").write_text(NARROW)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-o", str(tmp_path / "driver"), str(tmp_path / "driver.cpp")])
+    for line in subprocess.run([str(tmp_path / "driver")], capture_output=True, text=True, check=True).stdout.split("\n")[:-1]:
+        m, part, parts, share, shares = (int(x) for x in line.split())
+        assert part % 256 == 0 and share % 16 == 0
+        assert (parts - 1) * part < m <= parts * part and (shares - 1) * share < m <= shares * share
+        assert 1 <= parts <= 32 and 1 <= shares <= 32 and (parts == 1) == (m <= 256)
+
+
+def test_what_is_narrow(tmp_path):
+    """Either way round, and no wider than what the kernels hold."""
+    (tmp_path / "driver.cpp").write_text(NARROW.split("int main")[0] + """int main()
+{
+    for (unsigned n = 1; n <= 70; ++n)
+        for (unsigned m : {1u, 32u, 33u, 48u, 49u, 256u, 257u, 1024u, 1025u, 16384u})
+            printf("%u %u %d %d\\n", n, m, rg::narrow(n, m), rg::narrow(m, n));
+}
+""")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-o", str(tmp_path / "driver"), str(tmp_path / "driver.cpp")])
+    for line in subprocess.run([str(tmp_path / "driver")], capture_output=True, text=True, check=True).stdout.split("\n")[:-1]:
+        a, b, is_narrow, turned = (int(x) for x in line.split())
+        n, m = min(a, b), max(a, b)
+        assert is_narrow == turned == int(n <= 36 or (n <= 48 and m > 1024))
