@@ -152,7 +152,7 @@ inline uint64_t whole_tiles(uint64_t n, uint64_t m, uint64_t tile) { return (n +
 constexpr int UPDATE_TILE_SHARED = 65, UPDATE_TILE_PAIR = 129;
 inline int tile_side(int tile) { return tile / 32 * 32; }
 // Of the tiles that no waves share the one whose launch is done first: so many tiles to the fullest compute unit, each at what it takes of one that is full (us a step of 64 along K, measured
-// on products of 1024 to 4096 a side), but no less than a tile that has the unit to itself.
+// on products of 1024 to 4096 a side, of operands in one part and in two), but no less than a tile that has the unit to itself.
 template <typename F> inline int update_tile(F &&tiles, int n_cu, bool split)
 {
     struct Cost { int tile; double full, alone; };

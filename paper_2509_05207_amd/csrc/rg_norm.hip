@@ -113,7 +113,7 @@ struct RowLane {
 
 constexpr int norm_threads(int lanes) { return lanes > 256 ? lanes : 256; }
 
-// y, and the rows' statistics.  (us: 199,000 x 602 fp32 171, 5.6 TB/s; 150,000 x 256 bf16 25, 6.1 TB/s; 8,192 x 8,192 bf16 50, 5.4 TB/s; 256 x 64 fp32 2.7,
+// y, and the rows' statistics.  (us: 199,000 x 602 fp32 181, 5.3 TB/s; 150,000 x 256 bf16 29, 5.2 TB/s; 8,192 x 8,192 bf16 52, 5.2 TB/s; 256 x 64 fp32 3.0,
 // a launch's latency.)
 template <typename T, int V, int LANES, int NV>
 __global__ void __launch_bounds__(norm_threads(LANES)) norm_rows_kernel(NormArgs a)
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(norm_threads(LANES)) norm_rows_kernel(NormArgs
 }
 
 // dx and the workgroup's sums of dy xhat and dy, from x, dy and the rows' statistics.  A wave has the next row under way while it works on one: without that a row's
-// way from memory and its sums follow one another.  (us: 199,000 x 602 fp32 without dx 198, 4.8 TB/s; 150,000 x 256 bf16 38, 6.0 TB/s; 8,192 x 8,192 bf16 83, 4.8 TB/s.)
+// way from memory and its sums follow one another.  (us: 199,000 x 602 fp32 without dx 199, 4.8 TB/s; 150,000 x 256 bf16 40, 5.8 TB/s; 8,192 x 8,192 bf16 86, 4.7 TB/s.)
 template <typename T, int V, int LANES, int NV>
 __global__ void __launch_bounds__(norm_threads(LANES), LANES > 256 ? 1 : V * NV > 8 ? 3 : 4) norm_grad_kernel(NormArgs a)
 {
@@ -296,7 +296,7 @@ __device__ __forceinline__ Moments join(const Moments &p, const Moments &q)
 }
 
 // Few rows are shared out among `parts` workgroups each: all of them take the row's sums (which they read from their L2: workgroup g runs on XCD g mod
-// 8, and a row's workgroups are on one), and each writes its own part.  (61 rows of 131,071 fp32, us: a workgroup a row 35, four 20.)
+// 8, and a row's workgroups are on one), and each writes its own part.  (61 rows of 131,071 fp32, us: a workgroup a row 26, four 21.)
 struct Part {
     int64_t row, rows;                   // the first row, and how far the next one is
     int64_t from, to;                    // packs of the part
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(LONG_THREADS) norm_long_dx_kernel(NormArgs a)
     }
 }
 
-// Partial column sums of the rows blockIdx.y, blockIdx.y + gridDim.y, ...: a pack of columns a thread.  (512 x 65,536 bf16, us: 30, 4.5 TB/s.)
+// Partial column sums of the rows blockIdx.y, blockIdx.y + gridDim.y, ...: a pack of columns a thread.  (512 x 65,536 bf16, us: 31, 4.3 TB/s.)
 template <typename T>
 __global__ void __launch_bounds__(256) norm_columns_kernel(NormArgs a)
 {
@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(NormArgs a)
 }
 
 // ---------------------------------------------------------------- the partial sums put together
-// 32 columns a workgroup at a time, 32 threads to a column; blockIdx.y 0: dweight, 1: dbias.  (4 to 5 us for up to 8,192 columns, most of it a launch's latency.)
+// 32 columns a workgroup at a time, 32 threads to a column; blockIdx.y 0: dweight, 1: dbias.  (4 to 5 us for up to 8,192 columns, most of it a launch's latency; 13 for 65,536.)
 __global__ void __launch_bounds__(NORM_SUM_THREADS) norm_partials_kernel(const float *__restrict__ partial, uint32_t n_partial, int64_t n_cols, void *dweight, void *dbias, uint32_t type)
 {
     static_assert(NORM_SUM_COLUMNS == 32 && NORM_SUM_THREADS == 32 * 32, "");

@@ -163,7 +163,7 @@ __device__ __forceinline__ float factor_of(double norm, float eps, int &e2)
     return norm == 0.0 && eps > 0.f ? 0.f : (float)(ldexp(1.0, e2) / (norm + (double)eps));
 }
 
-// A workgroup takes 64 x 64 elements of the padded X, which go through LDS to be written by columns too.  Bound by HBM.  (The same six, us: 68; 352 MB, 5.2 TB/s.)
+// A workgroup takes 64 x 64 elements of the padded X, which go through LDS to be written by columns too.  Bound by HBM.  (The same six, us: 83; 453 MB, 5.5 TB/s.)
 template <typename T>
 __global__ void __launch_bounds__(256) update_start_kernel(Group g)
 {
@@ -233,10 +233,10 @@ __global__ void __launch_bounds__(256) update_start_kernel(Group g)
 // chunk of each) fall on all banks once.
 //
 // A step is what LDS takes in, what the waves read from it and the matrix operations, which overlap in part: all waves stand at about the same point of a
-// step (4,096 x 4,096 bf16, X X^T by tiles of 192, us: 80; without matrix operations 51, without reads from LDS 59, without loads 68, matrix operations alone 51, loads
-// alone 51).  Larger tiles read less for the same products (the same matrix, tiles of 64, 96, 128, 192, us: X X^T 160, 119, 109, 80, P X 236, 206, 172, 174, and 168 by pairs of 128,
-// of which one finishes while the other multiplies); smaller ones fill the chip with less work (2,048 x 2,048, X X^T 25, 18, 21, 33, P X 41, 34, 30, 44).  Waves of 96 x 96 and 128 x 128,
-// one to a vector unit, read half as much and are slower: nothing else runs while such a wave waits (X X^T by tiles of 192 130).
+// step (4,096 x 4,096, X X^T by tiles of 192, us: 191; without matrix operations 108, without reads from LDS 146, without loads 141, matrix operations alone 125, loads
+// alone 109; the matrix units are busy for 60 % of it).  Larger tiles read less for the same products (the same matrix, tiles of 64, 96, 128, 192, us: X X^T 333, 239, 270, 191, P X 510, 445, 403, 412, and 386 by
+// pairs of 128, of which one finishes while the other multiplies); smaller ones fill the chip with less work (2,048 x 2,048, X X^T 49, 43, 53, 85, P X 80, 69, 62, 100).  Waves of 96 x 96 and 128 x 128,
+// one to a vector unit, read half as much and are slower: nothing else runs while such a wave waits (operands of one part, X X^T by tiles of 192: 80, so 130).
 //
 // Where there are no more tiles than compute units a wave alone on its vector unit waits for LDS most of a step.  KG > 1: KG waves share a block, each with
 // its own slices of a step; their sums meet in LDS at the end, and each finishes one block of the wave's BI x BJ (or one of them the only block).  There the cross terms
@@ -376,7 +376,7 @@ struct Product {
 #pragma unroll
             for (int s = 0; s < SLICES; ++s) {
                 // What was read is there.  What comes next goes out a few reads and loads at a time, between the products of one row of blocks and the next: a wave that
-                // issued them all at once would wait for the units that take them, and its matrix operations with it (4096 x 4096 bf16, X X^T, us: 99 so, 85 in turns).
+                // issued them all at once would wait for the units that take them, and its matrix operations with it (4,096 x 4,096, operands of one part, X X^T, us: 99 so, 85 in turns).
                 // (The wait is explicit because the compiler, with loads into LDS under way, would wait for the next reads too.)
                 __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));
@@ -505,8 +505,8 @@ __device__ __forceinline__ void half_tile(uint32_t t, int32_t &row, int32_t &col
     column = (int32_t)(t - r * (r + 1) / 2);
 }
 
-// A = X X^T (POLY false), P = b f^2 A + c f^4 A^2 (POLY true): the tiles of the lower half, and their reflections.  (4,096 x 4,096 bf16, us: 81 and 86, 850 and 800 TFLOP/s;
-// six of 1,024 x 4,096 41 and 18, 630 and 360.)
+// A = X X^T (POLY false), P = b f^2 A + c f^4 A^2 (POLY true): the tiles of the lower half, and their reflections.  (4,096 x 4,096 bf16, us: 194 and 208, 1,060 and 990 TFLOP/s of three
+// products; six of 1,024 x 4,096 129 and 46, 600 and 420.)
 template <typename Prod, bool POLY>
 __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, bool first)
 {
@@ -549,8 +549,8 @@ __global__ void __launch_bounds__(Prod::THREADS) update_half_kernel(Group g, boo
     });
 }
 
-// X <- f (a X + P X); behind the last step the result goes out instead.  What a tile's results read and write (12 bytes an element, 16 in two parts) overlaps with another tile's
-// product where two share a compute unit.  (4,096 x 4,096 bf16, us: 175, 780 TFLOP/s; six of 1,024 x 4,096 134, 380 TFLOP/s beside 2.6 TB/s.)  Reads of X ahead of the
+// X <- f (a X + P X); behind the last step the result goes out instead.  What a tile's results read and write (16 bytes an element) overlaps with another tile's
+// product where two share a compute unit.  (4,096 x 4,096 bf16, us: 394, 1,050 TFLOP/s of three products; six of 1,024 x 4,096 230, 670 TFLOP/s beside 2.2 TB/s.)  Reads of X ahead of the
 // product gained nothing (1999 x 517 fp32, us: 17.6 so, 18.4 ahead).
 template <typename T, typename Prod, bool LAST, bool MUON>
 __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, uint32_t step)
@@ -626,7 +626,7 @@ __global__ void __launch_bounds__(Prod::THREADS) update_apply_kernel(Group g, ui
 }
 
 // ---------------------------------------------------------------- small matrices
-// Matrices of up to 64 x TINY_WIDE, one workgroup each, all of it in one launch (47 x 256 bf16, us: 25 so, 78 by 17 launches).  Each of 16 waves keeps strips of 16
+// Matrices of up to 64 x TINY_WIDE (but for fp32 ones of few rows), one workgroup each, all of it in one launch (47 x 256 bf16, us: 25 so, 78 by 17 launches).  Each of 16 waves keeps strips of 16
 // columns of X in registers, laid out as matrix operations leave their results: a lane has a column, and of each block of 16 rows the
 // four from 4 (lane / 16) on.  P X needs X with eight rows of a column to a lane, and which eight is free as long as P is read to match: a lane's fours
 // of two blocks, so that X never leaves the registers for it.  For X X^T its rows go through LDS, as A and P do, in two parts always (products cost little here).
