@@ -512,9 +512,8 @@ _ELEMENT = {torch.float32: RG_F32, torch.bfloat16: RG_BF16, torch.float16: RG_F1
 
 
 def _rows(name, t, device, shape=None, dtype=None):
-    """(address, stride in bytes) of a matrix on `device` whose rows are contiguous."""
-    assert t.is_cuda and t.dim() == 2, f"{name}: expected a device matrix"
-    assert t.device == device, f"{name}: expected it on {device}, got {t.device}"
+    """(address, stride in bytes) of a matrix on `device` (any GPU, if None) whose rows are contiguous."""
+    assert t.dim() == 2 and (t.is_cuda if device is None else t.device == device), f"{name}: expected a matrix on {device or 'the device'}"
     assert shape is None or t.shape == shape, f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}"
     assert (dtype is None and t.dtype in _ELEMENT) or t.dtype == dtype, f"{name}: got {t.dtype}"
     along, across = t.stride()
@@ -568,10 +567,10 @@ def _stream_and_use(device, stream, *made):
 def rg_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """(y, mean, rstd) of the rows of `x` (device matrix; rows may be padded).  out: where y goes (x itself: in place)."""
     shape, dt, device = x.shape, x.dtype, x.device
-    xp, xs = _rows("x", x, device)
+    xp, xs = _rows("x", x, None)
     n, d = shape
     y = x.new_empty(shape) if out is None else out
-    yp, ys = _rows("out", y, device, shape, dt)
+    yp, ys = (y.data_ptr(), d * y.element_size()) if out is None else _rows("out", y, device, shape, dt)
     wt = (weight if weight is not None else bias if bias is not None else x).dtype
     stats = torch.empty((2, n), dtype=torch.float32, device=device)
     sp = stats.data_ptr()
@@ -594,7 +593,7 @@ def rg_layer_norm_backward(dy, x, weight, mean, rstd, want_dx=True, want_dweight
     """(dx, dweight, dbias); None for what is not wanted.  weight None: all ones (the gradients of weight and bias are then fp32).
     out: where dx goes (dy or x itself: in place); workspace: a device tensor of rg_layer_norm_workspace bytes, made here if None."""
     shape, dt, device = x.shape, x.dtype, x.device
-    xp, xs = _rows("x", x, device)
+    xp, xs = _rows("x", x, None)
     gp, gs = _rows("dy", dy, device, shape, dt)
     n, d = shape
     wt = weight.dtype if weight is not None else torch.float32
@@ -629,7 +628,7 @@ def _updates(grads, outs, weights=None, momenta=None, out_momenta=None):
     dt, device = (grads[0].dtype, grads[0].device) if grads else (torch.float32, None)
     for k, (e, g, o) in enumerate(zip(u, grads, outs)):
         e.rows, e.cols = g.shape
-        e.grad, e.grad_stride = _rows("grad", g, device, None, dt)
+        e.grad, e.grad_stride = _rows("grad", g, device if k else None, None, dt)
         e.out, e.out_stride = _rows("out", o, device, g.shape, dt)
         if weights is not None:
             e.weight, e.weight_stride = _rows("weight", weights[k], device, g.shape, dt)
