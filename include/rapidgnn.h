@@ -528,6 +528,75 @@ rg_status rg_orthogonalize(const rg_update *u, uint32_t n, uint32_t type, uint32
 rg_status rg_muon_step(const rg_update *u, uint32_t n, uint32_t type, float lr, float weight_decay, float momentum, int nesterov,
                        uint32_t steps, float eps, void *workspace, uint64_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Rows held in 8 bits, and the products on them: features in the store, the
+ * cache and on the host link in a quarter of the bytes of fp32, layers' products
+ * in 8-bit integers, and activations kept in 8 bits for the backward pass.  The
+ * same rules hold as for the operators above.
+ *
+ * A held row of n_cols elements is rg_rows8_bytes = 16 * ceil((n_cols + 4) / 16)
+ * bytes: n_cols codes (int8, -127 to 127), zeros, and in the last four bytes the
+ * row's scale s (fp32).  Element c stands for code[c] * s.  Held rows lie at
+ * multiples of 16 bytes, at any stride that is one and at least their size;
+ * for rg_gather_batch and what is built on it they are rows of that many bytes.
+ * 1 <= n_cols <= RG_MAX_HELD_COLS (beyond, sums of products would leave 32 bits).
+ */
+#define RG_MAX_HELD_COLS 131072u
+rg_status rg_rows8_bytes(uint64_t n_cols, uint64_t *bytes);
+
+/*
+ * rg_quantize_rows -- rows as they are written to a store, a cache or a checkpoint:
+ *     s = |x|_max / 127 in fp32, no less than 2^-126 and no more than 0x1.020406p+121, of which 127 are still a number,
+ *     code = the whole number nearest to x / s (of the exact quotient; ties to even).
+ * A row with an infinity or a NaN is held as codes of zero and a scale of NaN: all of it reads back as NaN.
+ * rg_dequantize_rows -- rows as they are read back: code * s, of `type`.
+ *
+ *   x            dev-visible, [n_rows][n_cols] of `type`
+ *   rows         dev, [n_out], or NULL: row i of the result is made of row rows[i]; -1 for a row of zeros, any other position
+ *                outside [0, n_rows) for a row that reads back as NaN.  NULL: n_out = n_rows, every row in its place
+ *   held         dev (rg_dequantize_rows: dev-visible), held rows
+ * n_rows, n_out < 2^40; n_out may be 0.  The result overlaps neither the rows nor their positions.
+ */
+rg_status rg_quantize_rows(const void *x, uint64_t x_stride, uint64_t n_rows, uint64_t n_cols, uint32_t type,
+                           const int64_t *rows, uint64_t n_out, void *held, uint64_t held_stride, void *stream);
+rg_status rg_dequantize_rows(const void *held, uint64_t held_stride, uint64_t n_rows, uint64_t n_cols,
+                             const int64_t *rows, uint64_t n_out, uint32_t type, void *out, uint64_t out_stride, void *stream);
+
+/*
+ * rg_rows8_product -- y = x w^T + bias of held rows x [n_rows] and held weights w [n_outs], a scale for each row of either:
+ *     y[n][m] = s_x[n] * s_w[m] * (sum over c of code_x[n][c] * code_w[m][c]) + bias[m].
+ * The sum is exact, and what follows is in 64 bits.  A row with a scale of NaN makes its results NaN.
+ *
+ *   bias         dev, [n_outs] of bias_type (RG_F32, or the same as `type`), or NULL
+ *   y            dev, [n_rows][n_outs] of `type`
+ *   workspace    dev, 16-byte aligned, as many bytes as rg_rows8_product_workspace says (often none; then it may be NULL)
+ * n_rows, n_outs <= 2^30, either may be 0; RG_ERANGE where a launch cannot hold the result's tiles (beyond 2^37 results).
+ */
+rg_status rg_rows8_product_workspace(uint64_t n_rows, uint64_t n_outs, uint64_t n_cols, uint64_t *bytes);
+rg_status rg_rows8_product(const void *x, uint64_t x_stride, uint64_t n_rows, const void *w, uint64_t w_stride, uint64_t n_outs, uint64_t n_cols,
+                           const void *bias, uint32_t bias_type, void *y, uint64_t y_stride, uint32_t type,
+                           void *workspace, uint64_t workspace_bytes, void *stream);
+
+/*
+ * rg_rows8_product_backward -- what dy gives of it, x and w as what they stand for (the rounding to codes counts as the identity):
+ *     dx[n][c] = sum over m of dy[n][m] * s_w[m] * code_w[m][c],
+ *     dweight[m][c] = sum over n of dy[n][m] * s_x[n] * code_x[n][c],   dbias[m] = sum over n of dy[n][m].
+ * All that it takes of the forward pass are the held rows.  dy times the scale goes into the products in 16 bits (24 where dy is fp32); sums are in 32.
+ *
+ *   dy           dev, [n_rows][n_outs] of `type`
+ *   dx           dev, [n_rows][n_cols] of `type`, or NULL: not wanted (then w may be NULL)
+ *   dweight      dev, [n_outs][n_cols] of weight_type (RG_F32, or the same as `type`), or NULL (then x may be NULL)
+ *   dbias        dev, [n_outs] of weight_type, or NULL
+ *   workspace    dev, 16-byte aligned, as many bytes as rg_rows8_product_backward_workspace says for the same sizes and the same results wanted
+ * n_rows, n_outs <= 2^30, either may be 0: sums of nothing are zero.
+ */
+rg_status rg_rows8_product_backward_workspace(uint64_t n_rows, uint64_t n_outs, uint64_t n_cols, uint32_t type, int want_dx, int want_dweight, int want_dbias,
+                                              uint64_t *bytes);
+rg_status rg_rows8_product_backward(const void *dy, uint64_t dy_stride, const void *x, uint64_t x_stride, const void *w, uint64_t w_stride,
+                                    uint64_t n_rows, uint64_t n_outs, uint64_t n_cols, uint32_t type, void *dx, uint64_t dx_stride,
+                                    void *dweight, uint64_t dweight_stride, void *dbias, uint32_t weight_type,
+                                    void *workspace, uint64_t workspace_bytes, void *stream);
+
 /* Timing aid for benchmarks: sums, since the last reset, the device time spent
  * in the named kernel group when profiling is enabled (HIP events around each
  * launch on the launch stream; adds a little latency).  Groups: 0 sampler

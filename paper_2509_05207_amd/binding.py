@@ -28,7 +28,9 @@ EXPORTS = ("rg_last_error", "rg_graph_validate", "rg_build_schedule", "rg_schedu
            "rg_classify_batch", "rg_build_schedule_with", "rg_gather_batches",
            "rg_schedule_save", "rg_schedule_load", "rg_gather_batch_noalloc", "rg_schedule_seeds", "rg_schedule_load_range",
            "rg_layer_norm", "rg_layer_norm_workspace", "rg_layer_norm_backward",
-           "rg_update_workspace", "rg_orthogonalize", "rg_muon_step")
+           "rg_update_workspace", "rg_orthogonalize", "rg_muon_step",
+           "rg_rows8_bytes", "rg_quantize_rows", "rg_dequantize_rows", "rg_rows8_product_workspace", "rg_rows8_product",
+           "rg_rows8_product_backward_workspace", "rg_rows8_product_backward")
 
 
 class RgError(RuntimeError):
@@ -129,6 +131,16 @@ def lib():
         L.rg_update_workspace.argtypes = [P(rg_update), u32, u32, P(u64)]
         L.rg_orthogonalize.argtypes = [P(rg_update), u32, u32, u32, C.c_float, vp, u64, vp]
         L.rg_muon_step.argtypes = [P(rg_update), u32, u32, C.c_float, C.c_float, C.c_float, C.c_int, u32, C.c_float, vp, u64, vp]
+        L.rg_rows8_bytes.argtypes = [u64, P(u64)]
+        L.rg_quantize_rows.argtypes = [vp, u64, u64, u64, u32, vp, u64, vp, u64, vp]
+        L.rg_dequantize_rows.argtypes = [vp, u64, u64, u64, vp, u64, u32, vp, u64, vp]
+        L.rg_rows8_product_workspace.argtypes = [u64, u64, u64, P(u64)]
+        L.rg_rows8_product.argtypes = [vp, u64, u64, vp, u64, u64, u64, vp, u32, vp, u64, u32, vp, u64, vp]
+        L.rg_rows8_product_backward_workspace.argtypes = [u64, u64, u64, u32, C.c_int, C.c_int, C.c_int, P(u64)]
+        L.rg_rows8_product_backward.argtypes = [vp, u64, vp, u64, vp, u64, u64, u64, u64, u32, vp, u64, vp, u64, vp, u32, vp, u64, vp]
+        for name in ("rg_rows8_bytes", "rg_quantize_rows", "rg_dequantize_rows", "rg_rows8_product_workspace", "rg_rows8_product",
+                     "rg_rows8_product_backward_workspace", "rg_rows8_product_backward"):
+            getattr(L, name).restype = C.c_int32
         for name in ("rg_layer_norm", "rg_layer_norm_workspace", "rg_layer_norm_backward", "rg_update_workspace", "rg_orthogonalize", "rg_muon_step"):
             getattr(L, name).restype = C.c_int32
         for name in ("rg_graph_validate", "rg_build_schedule", "rg_schedule_info", "rg_schedule_frontier", "rg_schedule_samples",
@@ -685,6 +697,153 @@ def rg_muon_step(weights, grads, momenta, lr, weight_decay=0.0, momentum=0.95, n
     p, b, st, _mine = _update_scratch(u, len(grads), t, workspace, device, stream)
     _call(device, lib().rg_muon_step, u, len(grads), t, lr, weight_decay, momentum, 1 if nesterov else 0, int(steps), eps, p, b, st)
     _written(*out_weights, *out_momenta)
+
+
+# ---------------------------------------------------------------- rows held in 8 bits, and the products on them
+RG_MAX_HELD_COLS = 131072
+
+
+def rg_rows8_bytes(cols):
+    """Bytes of a held row of `cols` elements: its codes, zeros, its scale in the last four."""
+    b = C.c_uint64()
+    _check(lib().rg_rows8_bytes(int(cols), C.byref(b)))
+    return b.value
+
+
+def _held(name, t, device, cols):
+    """(address, stride in bytes, rows) of held rows on `device` (any GPU, if None): a uint8 matrix of rg_rows8_bytes(cols) a row."""
+    assert t.dim() == 2 and t.dtype == torch.uint8 and (t.is_cuda if device is None else t.device == device), f"{name}: expected a uint8 matrix on {device or 'the device'}"
+    assert t.shape[1] == (cols + 19) // 16 * 16, f"{name}: rows of {t.shape[1]} bytes do not hold {cols} elements"
+    along, across = t.stride()
+    assert across == 1, f"{name}: the bytes of a row have to be contiguous"
+    return t.data_ptr(), along, t.shape[0]
+
+
+def _positions(rows, device):
+    if rows is None:
+        return None
+    assert rows.device == device and rows.dtype == torch.int64 and rows.dim() == 1 and rows.is_contiguous(), f"rows: expected contiguous int64 positions on {device}"
+    return rows.data_ptr()
+
+
+def _made_scratch(device, entry, *args):
+    """A workspace of the bytes that `entry` says, None where it says none."""
+    b = C.c_uint64()
+    _call(device, entry, *args, C.byref(b))
+    return None if b.value == 0 else torch.empty(b.value, dtype=torch.uint8, device=device)
+
+
+def _place(x, rows, out):
+    """Where the result of rows that may lie in pinned host memory goes."""
+    if x.is_cuda:
+        return x.device
+    assert x.is_pinned(), "expected device or pinned host memory"
+    return out.device if out is not None else rows.device if rows is not None else torch.device("cuda", torch.cuda.current_device())
+
+
+def rg_quantize_rows(x, rows=None, out=None, stream=None):
+    """The rows of `x` (device or pinned matrix; rows may be padded), or those at the positions `rows` (int64; -1: a row of zeros), as
+    held rows: a uint8 matrix of rg_rows8_bytes(x.shape[1]) a row.  out: where they go."""
+    device = _place(x, rows, out)
+    xp, xs = _rows("x", x, x.device if not x.is_cuda else None)
+    n, d = x.shape
+    n_out = n if rows is None else rows.shape[0]
+    made = out is None
+    if made:
+        out = torch.empty((n_out, (d + 19) // 16 * 16), dtype=torch.uint8, device=device)
+    hp, hs, got = _held("out", out, device, d)
+    assert got == n_out, f"out: expected {n_out} rows, got {got}"
+    st = _stream_and_use(device, stream, out if made else None)
+    _call(device, lib().rg_quantize_rows, xp, xs, n, d, _ELEMENT[x.dtype], _positions(rows, device), n_out, hp, hs, st)
+    if not made:
+        _written(out)
+    return out
+
+
+def rg_dequantize_rows(held, cols, dtype=torch.float32, rows=None, out=None, stream=None):
+    """What held rows of `cols` elements stand for, all of them or those at the positions `rows` (int64; -1: a row of zeros).  out: where it goes."""
+    device = _place(held, rows, out)
+    hp, hs, n = _held("held", held, held.device if not held.is_cuda else None, cols)
+    n_out = n if rows is None else rows.shape[0]
+    made = out is None
+    if made:
+        out = torch.empty((n_out, cols), dtype=dtype, device=device)
+    else:
+        dtype = out.dtype
+    op, os_ = _rows("out", out, device, (n_out, cols))
+    st = _stream_and_use(device, stream, out if made else None)
+    _call(device, lib().rg_dequantize_rows, hp, hs, n, cols, _positions(rows, device), n_out, _ELEMENT[dtype], op, os_, st)
+    if not made:
+        _written(out)
+    return out
+
+
+def rg_rows8_product_workspace(n_rows, n_outs, cols):
+    """Bytes of scratch that the product takes."""
+    b = C.c_uint64()
+    _check(lib().rg_rows8_product_workspace(int(n_rows), int(n_outs), int(cols), C.byref(b)))
+    return b.value
+
+
+def rg_rows8_product(x, w, cols, bias=None, dtype=torch.float32, out=None, workspace=None, stream=None):
+    """x w^T + bias of held rows x and held weights w, both of `cols` elements a row; bias: fp32, or of the result's type.  out: where it
+    goes; workspace: a device tensor of rg_rows8_product_workspace bytes, made here if None."""
+    device = x.device
+    xp, xs, n = _held("x", x, None, cols)
+    wp, ws, m = _held("w", w, device, cols)
+    made, mine = out is None, None
+    if made:
+        out = torch.empty((n, m), dtype=dtype, device=device)
+        yp, ys = out.data_ptr(), m * out.element_size()
+    else:
+        yp, ys = _rows("out", out, device, (n, m))
+        dtype = out.dtype
+    bt = dtype if bias is None else bias.dtype
+    bp = _vector("bias", bias, device, m, bt)
+    if workspace is None:
+        workspace = mine = _made_scratch(device, lib().rg_rows8_product_workspace, n, m, cols)
+    sp, sb = (None, 0) if workspace is None else _scratch(workspace, device)
+    st = _stream_and_use(device, stream, out if made else None, mine)
+    _call(device, lib().rg_rows8_product, xp, xs, n, wp, ws, m, cols, bp, _ELEMENT[bt], yp, ys, _ELEMENT[dtype], sp, sb, st)
+    if not made:
+        _written(out)
+    return out
+
+
+def rg_rows8_product_backward_workspace(n_rows, n_outs, cols, dtype, want_dx=True, want_dweight=True, want_dbias=True):
+    """Bytes of scratch that the backward pass takes."""
+    b = C.c_uint64()
+    _check(lib().rg_rows8_product_backward_workspace(int(n_rows), int(n_outs), int(cols), _ELEMENT[dtype], int(want_dx), int(want_dweight), int(want_dbias), C.byref(b)))
+    return b.value
+
+
+def rg_rows8_product_backward(dy, x, w, cols, want_dx=True, want_dweight=True, want_dbias=True, weight_dtype=None, out=None, workspace=None, stream=None):
+    """(dx, dweight, dbias) of the product of held rows x and held weights w; None for what is not wanted.  x may be None where no dweight is, w where no dx
+    is.  weight_dtype: of dweight and dbias, fp32 or dy's (the default).  out: where dx goes; workspace: a device tensor of rg_rows8_product_backward_workspace bytes, made here if None."""
+    device, dt = dy.device, dy.dtype
+    gp, gs = _rows("dy", dy, None)
+    n, m = dy.shape
+    wt = dt if weight_dtype is None else weight_dtype
+    xp, xs, nx = (None, 0, n) if x is None else _held("x", x, device, cols)
+    wp, ws, mw = (None, 0, m) if w is None else _held("w", w, device, cols)
+    assert (nx, mw) == (n, m), f"dy of {n} x {m} does not belong to {nx} rows and {mw} weights"
+    dx, op, os_, dw, db, mine = None, None, 0, None, None, None
+    if want_dx:
+        dx = torch.empty((n, cols), dtype=dt, device=device) if out is None else out
+        op, os_ = _rows("out", dx, device, (n, cols), dt)
+    if want_dweight:
+        dw = torch.empty((m, cols), dtype=wt, device=device)
+    if want_dbias:
+        db = torch.empty(m, dtype=wt, device=device)
+    if workspace is None:
+        workspace = mine = _made_scratch(device, lib().rg_rows8_product_backward_workspace, n, m, cols, _ELEMENT[dt], int(want_dx), int(want_dweight), int(want_dbias))
+    sp, sb = (None, 0) if workspace is None else _scratch(workspace, device)
+    st = _stream_and_use(device, stream, dx if out is None else None, dw, db, mine)
+    _call(device, lib().rg_rows8_product_backward, gp, gs, xp, xs, wp, ws, n, m, cols, _ELEMENT[dt], op, os_, dw.data_ptr() if want_dweight else None,
+          cols * wt.itemsize, db.data_ptr() if want_dbias else None, _ELEMENT[wt], sp, sb, st)
+    if want_dx and out is not None:
+        _written(dx)
+    return dx, dw, db
 
 
 def rg_trim_memory():

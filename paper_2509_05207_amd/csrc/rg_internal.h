@@ -280,6 +280,12 @@ extern thread_local std::atomic<uint64_t> *tls_table_bytes_sink;
 // The current device's compute units (asked of the runtime once per device).
 rg_status compute_units(int *n_cu);
 
+// A matrix of held rows: address, alignment and stride; an output's rows apart from each other.
+rg_status check_held(const char *what, const void *p, uint64_t stride, uint64_t n_rows, uint64_t n_cols, bool output);
+
+// A matrix of elements of `bytes` each: address and stride in whole elements; an output's rows apart from each other.
+rg_status check_elements(const char *what, const void *p, uint64_t stride, uint64_t n_rows, uint64_t n_cols, uint32_t bytes, bool output);
+
 // True when p is device memory on the current device (false for pinned host memory).
 bool is_device_memory(const void *p);
 

@@ -208,4 +208,34 @@ inline UpdateKind update_kind(uint64_t rows, uint64_t cols, bool wide_type, int 
     return k;
 }
 
+// ---------------------------------------------------------------- rows held in 8 bits
+constexpr uint64_t held_bytes(uint64_t n_cols) { return (n_cols + 4 + 15) / 16 * 16; }      // codes, zeros, the scale
+struct HoldShape {
+    int pack;                            // elements of an access
+    int lanes;                           // of a row: 8 to 64, or a workgroup of 256 or 1,024; 0: the row is longer than that
+    int packs;                           // of a lane
+    uint32_t grid;                       // workgroups; their waves, or they, take rows by turns
+};
+// Rows as they are written: packs over all of a held row's bytes, one code to a byte.
+inline HoldShape hold_shape(int64_t n_out, int64_t n_cols, int element_bytes, int n_cu)
+{
+    HoldShape s{16 / element_bytes, 0, 0, 0};
+    const int64_t need = (int64_t)held_bytes((uint64_t)n_cols) / s.pack;
+    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : need <= 64 * 4 ? 64 : need <= 256 * 4 ? 256 : need <= 1024 * 4 ? 1024 : 0;
+    s.packs = s.lanes ? (int)((need + s.lanes - 1) / s.lanes) : 0;
+    const int64_t groups = s.lanes == 0 || s.lanes > 64 ? 1 : 256 / s.lanes;
+    s.grid = (uint32_t)std::max<int64_t>(1, std::min((int64_t)n_cu * (s.lanes == 1024 || s.lanes == 0 ? 2 : 8), (n_out + groups - 1) / groups));
+    return s;
+}
+// Rows as they are read back: single elements where a row has fewer than an access.
+inline HoldShape read_shape(int64_t n_out, int64_t n_cols, int element_bytes, int n_cu)
+{
+    HoldShape s{n_cols < 16 / element_bytes ? 1 : 16 / element_bytes, 0, 0, 0};
+    const int64_t need = (n_cols + s.pack - 1) / s.pack;
+    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : need <= 64 * 8 ? 64 : 256;
+    const int64_t groups = 256 / s.lanes;
+    s.grid = (uint32_t)std::max<int64_t>(1, std::min((int64_t)n_cu * 8, (n_out + groups - 1) / groups));
+    return s;
+}
+
 }  // namespace rg

@@ -1,0 +1,125 @@
+"""What the calls on held rows refuse, and the launch shapes they take: neither needs a GPU, since nothing is launched."""
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2509_05207_amd", "csrc")
+F32, BF16, F16 = 0, 1, 2
+P = 4096                                   # an address that suits everything; nothing reads it
+
+
+@pytest.fixture(scope="module")
+def rg():
+    from paper_2509_05207_amd import binding, build
+    build.build(force=False)
+    binding.lib()
+    return binding
+
+
+def test_bytes(rg):
+    for cols in list(range(1, 300)) + [602, 4096, rg.RG_MAX_HELD_COLS]:
+        b = rg.rg_rows8_bytes(cols)
+        assert b % 16 == 0 and cols + 4 <= b < cols + 20
+    for cols, status in ((0, rg.RG_EINVAL), (rg.RG_MAX_HELD_COLS + 1, rg.RG_ERANGE)):
+        with pytest.raises(rg.RgError) as e:
+            rg.rg_rows8_bytes(cols)
+        assert e.value.status == status
+    assert rg.lib().rg_rows8_bytes(5, None) == rg.RG_EINVAL
+
+
+def call(rg, name, order, good, **change):
+    args = dict(good, **change)
+    return getattr(rg.lib(), name)(*[args[k] for k in order])
+
+
+QUANTIZE = ("x", "x_stride", "n", "d", "type", "rows", "n_out", "held", "held_stride", "stream")
+GOOD_Q = dict(x=P, x_stride=400, n=5, d=100, type=F32, rows=P, n_out=3, held=P, held_stride=112, stream=None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(type=3), "RG_EINVAL"), (dict(d=0), "RG_EINVAL"), (dict(d=131_073), "RG_ERANGE"), (dict(n=2**40), "RG_ERANGE"), (dict(n_out=2**40), "RG_ERANGE"), (dict(x=None), "RG_EINVAL"),
+    (dict(x=P + 2), "RG_EINVAL"), (dict(x_stride=402), "RG_EINVAL"), (dict(x_stride=2**41), "RG_ERANGE"), (dict(rows=None), "RG_EINVAL"), (dict(rows=P + 4), "RG_EINVAL"), (dict(held=None), "RG_EINVAL"),
+    (dict(held=P + 8), "RG_EINVAL"), (dict(held_stride=120), "RG_EINVAL"), (dict(held_stride=96), "RG_EINVAL"), (dict(held_stride=2**41), "RG_ERANGE")])
+def test_quantize(rg, change, status):
+    assert call(rg, "rg_quantize_rows", QUANTIZE, GOOD_Q, **change) == getattr(rg, status)
+    assert rg.lib().rg_last_error()
+
+
+DEQUANTIZE = ("held", "held_stride", "n", "d", "rows", "n_out", "type", "out", "out_stride", "stream")
+GOOD_D = dict(held=P, held_stride=112, n=5, d=100, rows=P, n_out=3, type=BF16, out=P, out_stride=200, stream=None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(type=9), "RG_EINVAL"), (dict(d=0), "RG_EINVAL"), (dict(d=131_073), "RG_ERANGE"), (dict(held=None), "RG_EINVAL"), (dict(held=P + 1), "RG_EINVAL"), (dict(held_stride=104), "RG_EINVAL"),
+    (dict(rows=None), "RG_EINVAL"), (dict(out=None), "RG_EINVAL"), (dict(out=P + 1), "RG_EINVAL"), (dict(out_stride=201), "RG_EINVAL"), (dict(out_stride=198), "RG_EINVAL")])
+def test_dequantize(rg, change, status):
+    assert call(rg, "rg_dequantize_rows", DEQUANTIZE, GOOD_D, **change) == getattr(rg, status)
+
+
+PRODUCT = ("x", "x_stride", "n", "w", "w_stride", "m", "d", "bias", "bias_type", "y", "y_stride", "type", "ws", "ws_bytes", "stream")
+GOOD_P = dict(x=P, x_stride=112, n=5, w=P, w_stride=112, m=7, d=100, bias=P, bias_type=F32, y=P, y_stride=14, type=BF16, ws=None, ws_bytes=0, stream=None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(type=3), "RG_EINVAL"), (dict(bias_type=F16), "RG_EINVAL"), (dict(bias_type=7), "RG_EINVAL"), (dict(bias=P + 2), "RG_EINVAL"), (dict(d=0), "RG_EINVAL"), (dict(d=131_073), "RG_ERANGE"),
+    (dict(n=2**30 + 1), "RG_ERANGE"), (dict(m=2**30 + 1), "RG_ERANGE"), (dict(x=None), "RG_EINVAL"), (dict(w=None), "RG_EINVAL"), (dict(x=P + 4), "RG_EINVAL"), (dict(w_stride=100), "RG_EINVAL"),
+    (dict(y=None), "RG_EINVAL"), (dict(y=P + 1), "RG_EINVAL"), (dict(y_stride=12), "RG_EINVAL"), (dict(y_stride=15), "RG_EINVAL")])
+def test_product(rg, change, status):
+    assert call(rg, "rg_rows8_product", PRODUCT, GOOD_P, **change) == getattr(rg, status)
+
+
+BACKWARD = ("dy", "dy_stride", "x", "x_stride", "w", "w_stride", "n", "m", "d", "type", "dx", "dx_stride", "dw", "dw_stride", "db", "weight_type", "ws", "ws_bytes", "stream")
+GOOD_B = dict(dy=P, dy_stride=14, x=P, x_stride=112, w=P, w_stride=112, n=5, m=7, d=100, type=BF16, dx=P, dx_stride=200, dw=P, dw_stride=400, db=P, weight_type=F32, ws=P, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(type=3), "RG_EINVAL"), (dict(weight_type=F16), "RG_EINVAL"), (dict(d=0), "RG_EINVAL"), (dict(d=131_073), "RG_ERANGE"), (dict(n=2**30 + 1), "RG_ERANGE"), (dict(m=2**30 + 1), "RG_ERANGE"),
+    (dict(dy=None), "RG_EINVAL"), (dict(dy=P + 1), "RG_EINVAL"), (dict(dy_stride=13), "RG_EINVAL"), (dict(x=None), "RG_EINVAL"), (dict(w=None), "RG_EINVAL"), (dict(x_stride=104), "RG_EINVAL"),
+    (dict(w=P + 8), "RG_EINVAL"), (dict(dx=P + 1), "RG_EINVAL"), (dict(dx_stride=198), "RG_EINVAL"), (dict(dw=P + 2), "RG_EINVAL"), (dict(dw_stride=396), "RG_EINVAL"), (dict(db=P + 2), "RG_EINVAL")])
+def test_backward(rg, change, status):
+    assert call(rg, "rg_rows8_product_backward", BACKWARD, GOOD_B, **change) == getattr(rg, status)
+
+
+def test_workspaces(rg):
+    b = C.c_uint64()
+    L = rg.lib()
+    assert L.rg_rows8_product_workspace(5, 5, 5, None) == rg.RG_EINVAL and L.rg_rows8_product_workspace(5, 5, 0, C.byref(b)) == rg.RG_EINVAL
+    assert L.rg_rows8_product_workspace(2**31, 5, 5, C.byref(b)) == rg.RG_ERANGE
+    assert L.rg_rows8_product_backward_workspace(5, 5, 5, F32, 1, 1, 1, None) == rg.RG_EINVAL
+    assert L.rg_rows8_product_backward_workspace(5, 5, 5, 3, 1, 1, 1, C.byref(b)) == rg.RG_EINVAL
+
+
+DRIVER = r"""
+#include "rg_launch.h"
+#include <cstdio>
+int main()
+{
+    long long rows, cols, bytes, cu, read;
+    while (scanf("%lld %lld %lld %lld %lld", &rows, &cols, &bytes, &cu, &read) == 5) {
+        const rg::HoldShape s = read ? rg::read_shape(rows, cols, (int)bytes, (int)cu) : rg::hold_shape(rows, cols, (int)bytes, (int)cu);
+        printf("%d %d %d %u %llu\n", s.pack, s.lanes, s.packs, s.grid, (unsigned long long)rg::held_bytes(cols));
+    }
+}
+"""
+HOLD_KERNELS = {(8, 1), (16, 1), (32, 1), (64, 1), (64, 2), (64, 3), (64, 4), (256, 2), (256, 3), (256, 4), (1024, 2), (1024, 3), (1024, 4)}
+
+
+def test_every_width_has_a_kernel_that_holds_it(tmp_path):
+    (tmp_path / "driver.cpp").write_text(DRIVER)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-o", str(tmp_path / "driver"), str(tmp_path / "driver.cpp")])
+    widths = list(range(1, 2100)) + [k * 256 + d for k in range(9, 140) for d in (-5, -4, -3, -1, 0, 1, 7)] + [65_535, 131_071, 131_072]
+    cases = [(r, c, b, 256, 0) for c in widths for b in (2, 4) for r in (1, 100_000)] + [(r, c, b, 256, 1) for c in widths for b in (2, 4) for r in (1, 2**40 - 1)]
+    out = subprocess.run([str(tmp_path / "driver")], input="\n".join(" ".join(map(str, c)) for c in cases) + "\n", capture_output=True, text=True, check=True).stdout.split("\n")
+    for (rows, cols, element, cu, read), line in zip(cases, out):
+        pack, lanes, packs, grid, held = map(int, line.split())
+        assert held == (cols + 19) // 16 * 16 and 1 <= grid <= 8 * cu
+        if read:
+            assert pack == (16 // element if cols >= 16 // element else 1) and lanes in (8, 16, 32, 64, 256) and packs == 0
+        else:
+            assert pack == 16 // element and held % pack == 0
+            if lanes == 0:
+                assert held // pack > 4096
+            else:
+                assert (lanes, packs) in HOLD_KERNELS and (packs - 1) * lanes * pack < held <= packs * lanes * pack, (cols, lanes, packs)
