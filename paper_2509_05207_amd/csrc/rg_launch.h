@@ -238,4 +238,47 @@ inline HoldShape read_shape(int64_t n_out, int64_t n_cols, int element_bytes, in
     return s;
 }
 
+// y = x w^T of held rows: n rows, m outputs, d codes.
+constexpr uint32_t THIN_THREADS = 512, THIN_LDS = 160 * 1024;
+constexpr uint64_t THIN_COLS = 768;       // codes of a row in a lane's registers, at most: twelve chunks of 16, and as many of the next row (with 16 of each they spill)
+struct ThinShape {
+    uint32_t outs, shares, lds, grid;     // outputs of a workgroup, as many as LDS holds with their scales and bias; workgroups side by side over the outputs; of LDS; workgroups
+};
+inline ThinShape thin_shape(uint64_t n, uint64_t m, uint64_t d, int n_cu)
+{
+    const uint64_t each = (d + 15) / 16 * 16 + 8, most = (THIN_LDS - 16) / each / 32 * 32;
+    ThinShape s{};
+    s.shares = (uint32_t)((m + most - 1) / most);
+    s.outs = (uint32_t)(((m + s.shares - 1) / s.shares + 31) / 32 * 32);
+    s.lds = (uint32_t)(s.outs * each + 16);
+    const uint64_t rows = 16 * THIN_THREADS / 64, at_once = (uint64_t)n_cu * (s.lds * 2 <= THIN_LDS ? 2 : 1);
+    s.grid = (uint32_t)std::min((n + rows - 1) / rows, std::max<uint64_t>(1, at_once / s.shares)) * s.shares;
+    return s;
+}
+enum class ProductWay { FEW, FEW_LONG, THIN, TILES_64, TILES_128, TILES_256 };
+// The way that is done first, in us by what each takes (measured on 1 to 150,000 rows of 64 to 8,192 codes, 47 to 4,096 outputs in bf16; 64 x 4,096 to 4,096
+// takes 17.0 so and 14.8 in tiles of 64, 10,000 x 64 to 4,096 33 and 32, 150,000 x 602 to 47 29.7 and 28.8).  FEW: a launch, and workgroups of 16 x 16 by their steps of 64 codes.  Tiles: a tile alone on its compute unit,
+// or as many as the fullest has, by their starts and ends and their steps of 128.  THIN: w's way into LDS, then the rows' and results' bytes, or a wave's blocks one after the other.
+inline ProductWay product_way(uint64_t n, uint64_t m, uint64_t d, uint64_t element_bytes, int n_cu)
+{
+    const double cu = (double)n_cu, steps = (double)((d + 127) / 128);
+    const auto tiles = [&](uint64_t side) { return (double)((n + side - 1) / side) * (double)((m + side - 1) / side); };
+    const auto fullest = [&](uint64_t side) { return (double)(uint64_t)((tiles(side) + cu - 1) / cu); };
+    double best = std::max(10 + 1.75 * steps, 4 + fullest(256) * (9 + 2.08 * steps));
+    ProductWay way = ProductWay::TILES_256;
+    const auto offer = [&](ProductWay other, double us, double work_items = 0) {
+        if (us < best && work_items <= (double)MAX_WORK_ITEMS) { best = us; way = other; }
+    };
+    offer(ProductWay::TILES_128, std::max(5.5 + 0.93 * steps, 3.5 + fullest(128) * (2.7 + 0.69 * steps)), tiles(128) * 512);
+    offer(ProductWay::TILES_64, std::max(4.3 + 0.43 * steps, 3.5 + fullest(64) * (0.84 + 0.26 * steps)), tiles(64) * 256);
+    offer(steps >= 16 && tiles(16) <= 4 * cu ? ProductWay::FEW_LONG : ProductWay::FEW, 3.3 + tiles(16) / cu * (0.15 + 0.085 * steps) + 0.02 * steps, tiles(16) * 256);
+    if (d <= THIN_COLS && m <= 1ull << 16) {
+        const ThinShape s = thin_shape(n, m, d, n_cu);
+        const double blocks = (double)((n + 15) / 16), waves = (double)(s.grid / s.shares) * (THIN_THREADS / 64);
+        const double bytes = (double)n * ((double)s.shares * (double)(d + 4) + (double)(m * element_bytes));
+        offer(ProductWay::THIN, 4 + 0.03 * (double)s.lds / 1024 + std::max(1.25 * bytes / 5.1e6 * 256 / cu, 0.3 * (double)(uint64_t)((blocks + waves - 1) / waves) * (double)(s.outs / 32)));
+    }
+    return way;
+}
+
 }  // namespace rg

@@ -4,11 +4,14 @@
 #include "rg_elements.h"
 #include "rg_launch.h"
 
+#include <atomic>
+
 namespace rg {
 
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -35,46 +38,409 @@ __device__ __forceinline__ float bias_at(const ProductArgs &a, int32_t m)
     return a.bias_type == RG_F32 ? static_cast<const float *>(a.bias)[m] : a.bias_type == RG_BF16 ? (float)static_cast<const bf16 *>(a.bias)[m] : (float)static_cast<const f16 *>(a.bias)[m];
 }
 
-// What a sum of codes stands for.  In 64 bits: the sum has up to 31 bits, and two scales' product may leave fp32's range where the result does not.
-__device__ __forceinline__ float product_value(int32_t sum, uint32_t sx, uint32_t sw, float bias, bool scales_in)
+// A product that is rounded before it goes into a sum or a difference.
+__device__ __forceinline__ float rounded(float a, float b)
 {
-    if (scales_in) sum = sum - __builtin_amdgcn_sdot4((int)sx, (int)sw, 0, false);
+#pragma clang fp contract(off)
+    return a * b;
+}
+
+__device__ __forceinline__ int32_t sum_of_codes(int32_t sum, uint32_t sx, uint32_t sw, bool scales_in)
+{
+    return scales_in ? sum - __builtin_amdgcn_sdot4((int)sx, (int)sw, 0, false) : sum;
+}
+
+// What a sum of codes stands for: sum s_x s_w + bias, in 64 bits.
+__device__ __forceinline__ float wide_value(int32_t sum, uint32_t sx, uint32_t sw, float bias)
+{
     return (float)((double)sum * ((double)__builtin_bit_cast(float, sx) * (double)__builtin_bit_cast(float, sw)) + (double)bias);
 }
 
-// Sixteen rows by sixteen outputs to a workgroup, whose waves share out the steps of 64 codes.
-template <typename T>
-__global__ void __launch_bounds__(256) product_few_kernel(ProductArgs a)
+// The same in 32.  T of 16 bits: the sum and the scales' product are rounded, and so is the result before it is rounded to T.  T of 32 bits: the sum has up to 31 bits, the scales' product 48,
+// and both have a part that 32 bits leave over, as have their product and the sum with the bias; with these the result is off by its own rounding and no more than 2^-23 of that.
+template <typename T> __device__ __forceinline__ float product_value(int32_t sum, float sx, float sw, float bias)
 {
-    constexpr int WAVES = 4;
+    const float p = rounded(sx, sw), hi = (float)sum;
+    if constexpr (sizeof(T) == 2) return fmaf(hi, p, bias);
+    const float p_rest = fmaf(sx, sw, -p), lo = (float)(sum - (int32_t)hi), t = rounded(hi, p), t_rest = fmaf(hi, p, -t);
+    const float whole = t + bias, of_bias = whole - t;
+    return whole + (fmaf(hi, p_rest, fmaf(lo, p, t_rest)) + ((t - (whole - of_bias)) + (bias - of_bias)));
+}
+// Scales and biases of which no part of the above leaves the range.
+__device__ __forceinline__ bool moderate(float scale) { return fabsf(scale) >= 0x1p-38f && fabsf(scale) <= 0x1p48f; }
+__device__ __forceinline__ bool moderate_bias(float b) { return fabsf(b) < 0x1p120f; }
+// Others: the scales' mantissas and the powers of two apart, the bias added last.
+template <typename T> __device__ __forceinline__ float product_value_apart(int32_t sum, float sx, float sw, float bias)
+{
+    return ldexpf(product_value<T>(sum, __builtin_amdgcn_frexp_mantf(sx), __builtin_amdgcn_frexp_mantf(sw), 0.f), __builtin_amdgcn_frexp_expf(sx) + __builtin_amdgcn_frexp_expf(sw)) + bias;
+}
+
+__device__ const i32x4 ZERO_CHUNK = {0, 0, 0, 0};
+
+// Few results: 16 rows by 16 outputs to a workgroup, whose waves share out the steps of 64 codes, straight from memory into registers, and add their sums up in LDS.  Bound by w's way
+// from memory, and where that is short by a launch and what follows one another in it (bf16, 4 and 16 waves, us: 1 x 4,096 to 4,096 6.3 and 5.0, 100 x 512 to 256 3.6 and 4.9).  Up to 64 rows a
+// workgroup, w read once for all of them: 12.9 for 64 x 4,096 to 4,096, 15.8 so, but 14.6 for 11.7 with 8,192 to 1,000, and later for 300 rows than tiles.
+template <typename T, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64) product_few_kernel(ProductArgs a)
+{
+    constexpr int AT_ONCE = 4;                                     // steps whose loads are under way together
     __shared__ i32x4 sums[WAVES][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int32_t down = (a.n_rows + 15) / 16;
     const int32_t n0 = (int32_t)(blockIdx.x % (uint32_t)down) * 16, m0 = (int32_t)(blockIdx.x / (uint32_t)down) * 16;
-    const uint8_t *x = a.x + (uint64_t)min(n0 + (lane & 15), a.n_rows - 1) * a.x_stride, *w = a.w + (uint64_t)min(m0 + (lane & 15), a.n_outs - 1) * a.w_stride;
+    const uint8_t *w = a.w + (uint64_t)min(m0 + (lane & 15), a.n_outs - 1) * a.w_stride, *x = a.x + (uint64_t)min(n0 + (lane & 15), a.n_rows - 1) * a.x_stride;
     const int32_t chunks = (a.n_cols + 15) / 16, steps = (chunks + 3) / 4;
     i32x4 acc = {0, 0, 0, 0};
-    for (int32_t t = wave; t < steps; t += WAVES) {
-        const int32_t c = t * 4 + (lane >> 4);
-        i32x4 u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-        if (c < chunks) {
-            u = *reinterpret_cast<const i32x4 *>(w + c * 16);
-            v = *reinterpret_cast<const i32x4 *>(x + c * 16);
+    for (int32_t t0 = wave; t0 < steps; t0 += WAVES * AT_ONCE) {
+        i32x4 u[AT_ONCE], v[AT_ONCE];
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) {
+            // Chunks beyond the row: its last one's codes of w, and zeros in place of x'.
+            const int32_t c = (t0 + q * WAVES) * 4 + (lane >> 4);
+            u[q] = *reinterpret_cast<const i32x4 *>(w + min(c, chunks - 1) * 16);
+            v[q] = *reinterpret_cast<const i32x4 *>(c < chunks ? x + c * 16 : reinterpret_cast<const uint8_t *>(&ZERO_CHUNK));
         }
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(u, v, acc, 0, 0, 0);
+#pragma unroll
+        for (int q = 0; q < AT_ONCE; ++q) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(u[q], v[q], acc, 0, 0, 0);
     }
     sums[wave][lane] = acc;
     __syncthreads();
     if (wave) return;
+#pragma unroll
     for (int k = 1; k < WAVES; ++k) acc += sums[k][lane];
     const int32_t n = n0 + (lane & 15), m = m0 + (lane >> 4) * 4;
-    if (n >= a.n_rows) return;
+    if (n >= a.n_rows || m >= a.n_outs) return;
     const uint32_t sx = *reinterpret_cast<const uint32_t *>(x + a.held_bytes - 4);
-    T *y = row_at<T>(a.y, a.y_stride, n);
+    T *y = row_at<T>(a.y, a.y_stride, n) + m;
+    float v[4];
+#pragma unroll
     for (int e = 0; e < 4; ++e) {
-        if (m + e >= a.n_outs) return;
-        const uint32_t s = *row_at<uint32_t>(a.w + a.held_bytes - 4, a.w_stride, m + e);
-        y[m + e] = (T)product_value(acc[e], sx, s, bias_at(a, m + e), scale_in_sum(a.n_cols));
+        const int32_t at = min(m + e, a.n_outs - 1);
+        const uint32_t sw = *row_at<uint32_t>(a.w + a.held_bytes - 4, a.w_stride, at);
+        v[e] = wide_value(sum_of_codes(acc[e], sx, sw, scale_in_sum(a.n_cols)), sx, sw, bias_at(a, at));
+    }
+    if (m + 4 <= a.n_outs) {
+        store_pack<T, 4>(y, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (m + e < a.n_outs) y[e] = (T)v[e];
+    }
+}
+
+// Tiles of TM rows by TN outputs, by WM x WN waves of BM x BN blocks of 16 x 16.  Steps of 128 codes pass through LDS, two of them there: one is multiplied while the other
+// arrives, written into LDS by the loads themselves.  A row of a step is eight chunks of 16 bytes, stored in an order that depends on the row, so that the 16 lanes that
+// LDS serves at a time (16 rows, one chunk of each) fall on all banks once.
+// Workgroup g runs on XCD g mod 8, and every XCD has an L2 of its own: tiles that share operands, which follow one another, go to one XCD.
+__device__ __forceinline__ uint32_t tile_of_workgroup()
+{
+    constexpr uint32_t XCDS = 8;
+    const uint32_t x = blockIdx.x % XCDS, each = gridDim.x / XCDS, rest = gridDim.x % XCDS;
+    return x * each + min(x, rest) + blockIdx.x / XCDS;
+}
+
+template <int WM_, int WN_, int BM_, int BN_, int PACK_>
+struct Tiles {
+    static constexpr int WM = WM_, WN = WN_, BM = BM_, BN = BN_, PACK = PACK_;
+    static constexpr int THREADS = WM * WN * 64, TM = WM * BM * 16, TN = WN * BN * 16, DEPTH = 128;
+    static constexpr int ROWS = TM + TN, STAGE = ROWS * DEPTH, LOADS = ROWS * 8 / THREADS;
+    static constexpr int LDS_BYTES = 2 * STAGE + ROWS * 4;          // behind the stages the scales
+    static_assert(ROWS * 8 % THREADS == 0 && TM * 8 % THREADS == 0 && LDS_BYTES <= 160 * 1024, "");
+    typedef i32x4 Acc[BM][BN];
+    typedef const __attribute__((address_space(1))) uint8_t *Global;
+
+    static __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
+
+    // Waits until this wave's loads have arrived, and then for every wave to be there.  The fences keep the compiler to the order and cost no instruction.
+    static __device__ __forceinline__ void arrive()
+    {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0 | (7 << 4));                  // vmcnt 0, lgkmcnt 0
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+    // Rows of w lie in a stage in an order by which a lane, which comes to hold four outputs of each block, holds PACK that follow one another, and the four lanes of a row 4 PACK: 64 bytes.
+    static __device__ __forceinline__ int output_of(int row)
+    {
+        const int in = row % (4 * PACK), r = in % 16;
+        return row - in + r / 4 * PACK + in / 16 * 4 + r % 4;
+    }
+    static __device__ __forceinline__ int of_output(int m)         // the row of a stage
+    {
+        const int in = m % (4 * PACK), r = in % PACK;
+        return TM + m - in + r / 4 * 16 + in / PACK * 4 + r % 4;
+    }
+
+    // Eight columns of tiles at a time, row by row: what an XCD works on at once is about square.
+    struct Place { int32_t n0, m0; };
+    static __device__ __forceinline__ Place place_of(const ProductArgs &a, uint32_t t)
+    {
+        constexpr uint32_t ABREAST = 8;
+        const uint32_t down = ((uint32_t)a.n_rows + TM - 1) / TM, across = ((uint32_t)a.n_outs + TN - 1) / TN;
+        const uint32_t band = t / (down * ABREAST), in_band = t - band * down * ABREAST, width = min(ABREAST, across - band * ABREAST);
+        return {(int32_t)(in_band / width) * TM, (int32_t)(band * ABREAST + in_band % width) * TN};
+    }
+
+    struct Source {
+        Global base[2];                                            // of the tile's first row of x, of w
+        uint32_t offset[LOADS];
+        int32_t chunks, last;                                      // of a row; the step that has the last of them
+        __device__ __forceinline__ Source(const ProductArgs &a, const Place &p) : chunks((a.n_cols + 15) / 16), last((chunks - 1) / 8)
+        {
+            base[0] = (Global)(a.x + (uint64_t)p.n0 * a.x_stride);
+            base[1] = (Global)(a.w + (uint64_t)p.m0 * a.w_stride);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int q = i * THREADS + (int)threadIdx.x, row = q / 8;
+                offset[i] = row_offset(a, p, row) + (uint32_t)slot_of(row, q % 8) * 16u;
+            }
+        }
+        static __device__ __forceinline__ uint32_t row_offset(const ProductArgs &a, const Place &p, int row)
+        {
+            return row < TM ? (uint32_t)min(row, a.n_rows - 1 - p.n0) * (uint32_t)a.x_stride : (uint32_t)min(output_of(row - TM), a.n_outs - 1 - p.m0) * (uint32_t)a.w_stride;
+        }
+        __device__ __forceinline__ void load(int32_t step, uint8_t *stage) const
+        {
+            constexpr int OF_X = TM * 8 / THREADS;
+            step = min(step, last);                                // behind the last step that step again
+            const bool ragged = step == last && (chunks & 7);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                Global from = base[i < OF_X ? 0 : 1] + (int64_t)step * DEPTH + offset[i];
+                if (ragged) {                                      // chunks beyond the row are zeros
+                    const int q = i * THREADS + (int)threadIdx.x;
+                    if (step * 8 + slot_of(q / 8, q % 8) >= chunks) from = (Global)reinterpret_cast<const uint8_t *>(&ZERO_CHUNK);
+                }
+                __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void *)(stage + (i * THREADS + (int)(threadIdx.x & ~63u)) * 16), 16, 0, 0);
+            }
+        }
+    };
+};
+
+// Bias of V outputs from each of m, m + 4 V, ..., read in one go.
+template <int N, int V, typename B> __device__ __forceinline__ void load_bias(const B *bias, int32_t m, int32_t n_outs, float (&b)[N])
+{
+#pragma unroll
+    for (int e = 0; e < N; ++e) b[e] = (float)bias[min(m + e / V * V * 4 + e % V, n_outs - 1)];
+}
+
+// The tile's results.
+template <typename T, typename Tile, bool APART> __device__ __forceinline__ void store_tile(const ProductArgs &a, const typename Tile::Place &p, const typename Tile::Acc &acc, const float *scales,
+                                                                                           const float (&b)[Tile::BN * 4])
+{
+    constexpr int V = Tile::PACK;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = (wave % Tile::WN) * Tile::BN * 16 + (lane >> 4) * V;
+    const float *sx = scales + (wave / Tile::WN) * Tile::BM * 16 + (lane & 15);
+    const int32_t n0 = p.n0 + (wave / Tile::WN) * Tile::BM * 16 + (lane & 15);
+    const bool scales_in = scale_in_sum(a.n_cols);
+#pragma unroll
+    for (int k = 0; k < Tile::BN * 4; k += V) {                    // V outputs that lie side by side
+        const int32_t m = p.m0 + first + k * 4;
+        float sw[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) sw[e] = scales[Tile::of_output(first + k * 4 + e)];
+        if (m >= a.n_outs) continue;
+#pragma unroll
+        for (int i = 0; i < Tile::BM; ++i) {
+            if (n0 + i * 16 >= a.n_rows) continue;
+            float v[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float x = sx[i * 16];
+                const int32_t sum = sum_of_codes(acc[i][(k + e) / 4][(k + e) % 4], __builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, sw[e]), scales_in);
+                v[e] = APART ? product_value_apart<T>(sum, x, sw[e], b[k + e]) : product_value<T>(sum, x, sw[e], b[k + e]);
+            }
+            T *y = row_at<T>(a.y, a.y_stride, n0 + i * 16) + m;
+            if (m + V <= a.n_outs) {
+                store_pack<T, V>(y, v);
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (m + e < a.n_outs) y[e] = (T)v[e];
+            }
+        }
+    }
+}
+
+template <typename T, typename Tile> __device__ __forceinline__ void finish_tile(const ProductArgs &a, const typename Tile::Place &p, const typename Tile::Acc &acc, const float *scales)
+{
+    constexpr int V = Tile::PACK;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = (wave % Tile::WN) * Tile::BN * 16 + (lane >> 4) * V;
+    float b[Tile::BN * 4] = {};
+    if (a.bias) {
+        if (a.bias_type == RG_F32) load_bias<Tile::BN * 4, V>(static_cast<const float *>(a.bias), p.m0 + first, a.n_outs, b);
+        else if (a.bias_type == RG_BF16) load_bias<Tile::BN * 4, V>(static_cast<const bf16 *>(a.bias), p.m0 + first, a.n_outs, b);
+        else load_bias<Tile::BN * 4, V>(static_cast<const f16 *>(a.bias), p.m0 + first, a.n_outs, b);
+    }
+    bool fine = true;
+#pragma unroll
+    for (int i = 0; i < Tile::BM; ++i) fine = fine && moderate(scales[(wave / Tile::WN) * Tile::BM * 16 + (lane & 15) + i * 16]);
+#pragma unroll
+    for (int k = 0; k < Tile::BN * 4; ++k) fine = fine && moderate(scales[Tile::of_output(first + k / V * V * 4 + k % V)]) && moderate_bias(b[k]);
+    if (__ballot(!fine)) store_tile<T, Tile, true>(a, p, acc, scales, b);
+    else store_tile<T, Tile, false>(a, p, acc, scales, b);
+}
+
+template <typename T, typename Tile>
+__global__ void __launch_bounds__(Tile::THREADS, 2) product_tiles_kernel(ProductArgs a)
+{
+    extern __shared__ __align__(16) uint8_t lds[];
+    constexpr int BM = Tile::BM, BN = Tile::BN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const typename Tile::Place place = Tile::place_of(a, tile_of_workgroup());
+    const typename Tile::Source src(a, place);
+    src.load(0, lds);
+    src.load(1, lds + Tile::STAGE);
+    float *scales = reinterpret_cast<float *>(lds + 2 * Tile::STAGE);
+    for (int row = threadIdx.x; row < Tile::ROWS; row += Tile::THREADS) {
+        const auto *from = (const __attribute__((address_space(1))) float *)(src.base[row < Tile::TM ? 0 : 1] + Tile::Source::row_offset(a, place, row) + (a.held_bytes - 4));
+        scales[row] = *from;
+    }
+    typename Tile::Acc acc;
+#pragma unroll
+    for (int i = 0; i < BM; ++i)
+#pragma unroll
+        for (int j = 0; j < BN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    const int row_x = (wave / Tile::WN) * BM * 16 + (lane & 15), row_w = Tile::TM + (wave % Tile::WN) * BN * 16 + (lane & 15);
+    const auto read = [&](const uint8_t *stage, int s, i32x4 (&x)[BM], i32x4 (&w)[BN]) {
+        const int slot = Tile::slot_of(lane & 15, s * 4 + (lane >> 4)) * 16;              // the rows of a block begin at multiples of 16
+#pragma unroll
+        for (int i = 0; i < BM; ++i) x[i] = *reinterpret_cast<const i32x4 *>(stage + (row_x + i * 16) * Tile::DEPTH + slot);
+#pragma unroll
+        for (int j = 0; j < BN; ++j) w[j] = *reinterpret_cast<const i32x4 *>(stage + (row_w + j * 16) * Tile::DEPTH + slot);
+    };
+    const auto multiply = [&](const i32x4 (&x)[BM], const i32x4 (&w)[BN]) {
+#pragma unroll
+        for (int i = 0; i < BM; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], x[i], acc[i][j], 0, 0, 0);
+    };
+    Tile::arrive();
+    i32x4 x0[BM], w0[BN], x1[BM], w1[BN];
+    read(lds, 0, x0, w0);
+    for (int32_t t = 0; t <= src.last; ++t) {
+        uint8_t *stage = lds + (t & 1) * Tile::STAGE, *next = lds + (~t & 1) * Tile::STAGE;
+        read(stage, 1, x1, w1);
+        multiply(x0, w0);
+        Tile::arrive();                                            // the stage is read, and the next one there
+        src.load(t + 2, stage);
+        read(next, 0, x0, w0);
+        multiply(x1, w1);
+    }
+    Tile::arrive();                                                // a workgroup's LDS is not left with loads under way
+    finish_tile<T, Tile>(a, place, acc, scales);
+}
+
+// Many rows of few codes: what bounds them is the rows' and the results' way from and to HBM, and tiles spend most of their time on it at their start and end.  Here w lies in LDS, once
+// for all rows that a workgroup does (where it has more than that holds, each workgroup has a share of the outputs), and a wave by itself takes 16 rows at a time into registers, the next
+// ones under way meanwhile: no barrier behind the first.  w lies as the matrix operations take it: of a block of 16 outputs chunk by chunk, 16 rows side by side.
+struct ThinArgs {
+    ProductArgs p;
+    int32_t outs;                    // of a workgroup, a multiple of 32
+    int32_t shares;                  // of the outputs
+};
+
+// The row of w that lies at place r (0 to 31) of two blocks, so that a lane holds V outputs side by side.
+template <int V> __device__ __forceinline__ int thin_output(int r) { return V == 8 ? r % 16 / 4 * 8 + r / 16 * 4 + r % 4 : r; }
+
+template <typename T, int KS>
+__global__ void __launch_bounds__(THIN_THREADS) product_thin_kernel(ThinArgs t)
+{
+    constexpr int V = 16 / sizeof(T), WAVES = THIN_THREADS / 64;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const ProductArgs &a = t.p;
+    typedef const __attribute__((address_space(1))) uint8_t *Global;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int32_t chunks = (a.n_cols + 15) / 16, m0 = (int32_t)(blockIdx.x % (uint32_t)t.shares) * t.outs, mine = min(t.outs, a.n_outs - m0);
+    const int32_t blocks = (mine + 31) / 32 * 2;
+    // Blocks of 16 rows; behind the last block's rows its last row, which nothing is made of.
+    const int32_t turns = (int32_t)(gridDim.x / (uint32_t)t.shares) * WAVES;
+    int32_t rb = (int32_t)(blockIdx.x / (uint32_t)t.shares) * WAVES + wave;
+    i32x4 x[KS], next[KS];
+    float sx, next_sx;
+    const auto load = [&](int32_t b, i32x4 (&to)[KS], float &s) {
+        const uint8_t *row = a.x + (uint64_t)min((int64_t)b * 16 + (lane & 15), (int64_t)a.n_rows - 1) * a.x_stride;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int32_t c = k * 4 + (lane >> 4);
+            Global from = c < chunks ? (Global)(row + c * 16) : (Global)reinterpret_cast<const uint8_t *>(&ZERO_CHUNK);
+            to[k] = *(const __attribute__((address_space(1))) i32x4 *)from;
+        }
+        s = *(const __attribute__((address_space(1))) float *)(Global)(row + a.held_bytes - 4);
+    };
+    load(rb, x, sx);
+    float *scales = reinterpret_cast<float *>(lds + (uint32_t)(t.outs / 16 * chunks) * 256), *bias = scales + t.outs;
+    int *all_fine = reinterpret_cast<int *>(bias + t.outs);
+    if (threadIdx.x == 0) *all_fine = 1;
+    for (int32_t block = wave; block < blocks; block += WAVES) {
+        const int32_t m = block / 2 * 32 + thin_output<V>(block % 2 * 16 + (lane & 15));
+        Global row = (Global)(a.w + (uint64_t)(m0 + min(m, mine - 1)) * a.w_stride);
+        uint8_t *to = lds + (uint32_t)(block * chunks) * 256;
+        int32_t c = 0;
+        for (; c + 4 <= chunks; c += 4) __builtin_amdgcn_global_load_lds(row + (c + (lane >> 4)) * 16, (__attribute__((address_space(3))) void *)(to + c * 256), 16, 0, 0);
+        if (c + (lane >> 4) < chunks) *reinterpret_cast<i32x4 *>(to + c * 256 + lane * 16) = *(const __attribute__((address_space(1))) i32x4 *)(row + (c + (lane >> 4)) * 16);
+    }
+    bool w_fine = true;
+    for (int32_t m = threadIdx.x; m < blocks * 16; m += THIN_THREADS) {
+        const int32_t at = m0 + min(m, mine - 1);
+        scales[m] = *row_at<float>(a.w + a.held_bytes - 4, a.w_stride, at);
+        bias[m] = bias_at(a, at);
+        w_fine = w_fine && moderate(scales[m]) && moderate_bias(bias[m]);
+    }
+    __syncthreads();                                               // and what was loaded is there
+    if (!w_fine) *all_fine = 0;
+    __syncthreads();
+    w_fine = *all_fine;
+    const bool scales_in = scale_in_sum(a.n_cols);
+    const int32_t n_blocks = (a.n_rows + 15) / 16;
+    while (rb < n_blocks) {
+        if (rb + turns < n_blocks) load(rb + turns, next, next_sx);
+        const bool fine = !__ballot(!(w_fine && moderate(sx)));
+        const int32_t n = rb * 16 + (lane & 15);
+        T *y = row_at<T>(a.y, a.y_stride, n) + m0;
+        for (int32_t pair = 0; pair < blocks; pair += 2) {
+            i32x4 acc[2] = {};
+            const uint8_t *w = lds + (uint32_t)(pair * chunks) * 256 + (lane & 15) * 16;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int32_t c = min(k * 4 + (lane >> 4), chunks - 1) * 256;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4 *>(w + j * chunks * 256 + c), x[k], acc[j], 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; k += V) {
+                const int32_t m = pair * 16 + k * 4 + (lane >> 4) * V;
+                if (n >= a.n_rows || m >= mine) continue;
+                float v[V], sw[V];
+                int32_t sum[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    sw[e] = scales[m + e];
+                    sum[e] = sum_of_codes(acc[(k + e) / 4][(k + e) % 4], __builtin_bit_cast(uint32_t, sx), __builtin_bit_cast(uint32_t, sw[e]), scales_in);
+                }
+                if (fine) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[e] = product_value<T>(sum[e], sx, sw[e], bias[m + e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[e] = product_value_apart<T>(sum[e], sx, sw[e], bias[m + e]);
+                }
+                if (m + V <= mine) {
+                    store_pack<T, V>(y + m, v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (m + e < mine) y[m + e] = (T)v[e];
+                }
+            }
+        }
+        rb += turns;
+        sx = next_sx;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) x[k] = next[k];
     }
 }
 
@@ -217,11 +583,89 @@ rg_status check_workspace(const void *workspace, uint64_t got, uint64_t want)
     return RG_OK;
 }
 
+// Offsets within a tile's rows have 32 bits.
+rg_status check_steps(const char *what, uint64_t stride)
+{
+    if (stride < 1ull << 24) return RG_OK;
+    set_error("%s: a stride of %llu bytes is beyond the products' limit (2^24)", what, (unsigned long long)stride);
+    return RG_ERANGE;
+}
+
 rg_status check_grid(uint64_t groups, uint32_t threads)
 {
     if (groups <= MAX_WORK_ITEMS / threads) return RG_OK;
     set_error("a result of %llu tiles is more than a launch holds", (unsigned long long)groups);
     return RG_ERANGE;
+}
+
+// LDS beyond 64 KB has to be asked for, once per kernel and device.
+template <typename K> rg_status allow_lds(K kernel, int bytes, std::atomic<uint64_t> &known)
+{
+    if (bytes <= 64 * 1024) return RG_OK;
+    int dev = 0;
+    RG_HIP(hipGetDevice(&dev));
+    const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (known.load(std::memory_order_relaxed) & bit) return RG_OK;
+    RG_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    known.fetch_or(bit, std::memory_order_relaxed);
+    return RG_OK;
+}
+
+template <typename T, typename Tile> rg_status launch_tiles(const ProductArgs &a, hipStream_t st)
+{
+    const uint64_t tiles = ((uint64_t)a.n_rows + Tile::TM - 1) / Tile::TM * (((uint64_t)a.n_outs + Tile::TN - 1) / Tile::TN);
+    RG_TRY(check_grid(tiles, Tile::THREADS));
+    static std::atomic<uint64_t> known{0};
+    RG_TRY(allow_lds(product_tiles_kernel<T, Tile>, Tile::LDS_BYTES, known));
+    hipLaunchKernelGGL((product_tiles_kernel<T, Tile>), dim3((uint32_t)tiles), dim3(Tile::THREADS), Tile::LDS_BYTES, st, a);
+    RG_HIP(hipGetLastError());
+    return RG_OK;
+}
+
+template <typename T, int KS> rg_status launch_thin(const ProductArgs &a, int n_cu, hipStream_t st)
+{
+    const ThinShape s = thin_shape((uint64_t)a.n_rows, (uint64_t)a.n_outs, (uint64_t)a.n_cols, n_cu);
+    static std::atomic<uint64_t> known{0};
+    RG_TRY(allow_lds(product_thin_kernel<T, KS>, (int)THIN_LDS, known));
+    hipLaunchKernelGGL((product_thin_kernel<T, KS>), dim3(s.grid), dim3(THIN_THREADS), s.lds, st, ThinArgs{a, (int32_t)s.outs, (int32_t)s.shares});
+    RG_HIP(hipGetLastError());
+    return RG_OK;
+}
+
+template <typename T> rg_status launch_thin_of(const ProductArgs &a, int n_cu, hipStream_t st)
+{
+    const int steps = (a.n_cols + 63) / 64;
+    if (steps <= 1) return launch_thin<T, 1>(a, n_cu, st);
+    if (steps <= 2) return launch_thin<T, 2>(a, n_cu, st);
+    if (steps <= 4) return launch_thin<T, 4>(a, n_cu, st);
+    if (steps <= 6) return launch_thin<T, 6>(a, n_cu, st);
+    if (steps <= 8) return launch_thin<T, 8>(a, n_cu, st);
+    if (steps <= 10) return launch_thin<T, 10>(a, n_cu, st);
+    return launch_thin<T, THIN_COLS / 64>(a, n_cu, st);
+}
+
+template <typename T, int WAVES> rg_status launch_few(const ProductArgs &a, hipStream_t st)
+{
+    const uint64_t tiles = ((uint64_t)a.n_rows + 15) / 16 * (((uint64_t)a.n_outs + 15) / 16);
+    RG_TRY(check_grid(tiles, WAVES * 64));
+    hipLaunchKernelGGL((product_few_kernel<T, WAVES>), dim3((uint32_t)tiles), dim3(WAVES * 64), 0, st, a);
+    RG_HIP(hipGetLastError());
+    return RG_OK;
+}
+
+template <typename T> rg_status launch_product(const ProductArgs &a, hipStream_t st)
+{
+    constexpr int PACK = 16 / sizeof(T);
+    int n_cu = 0;
+    RG_TRY(compute_units(&n_cu));
+    switch (product_way((uint64_t)a.n_rows, (uint64_t)a.n_outs, (uint64_t)a.n_cols, sizeof(T), n_cu)) {
+    case ProductWay::FEW: return launch_few<T, 4>(a, st);
+    case ProductWay::FEW_LONG: return launch_few<T, 16>(a, st);
+    case ProductWay::THIN: return launch_thin_of<T>(a, n_cu, st);
+    case ProductWay::TILES_64: return launch_tiles<T, Tiles<2, 2, 2, 2, PACK>>(a, st);
+    case ProductWay::TILES_128: return launch_tiles<T, Tiles<4, 2, 2, 4, PACK>>(a, st);
+    default: return launch_tiles<T, Tiles<2, 4, 8, 4, PACK>>(a, st);
+    }
 }
 
 // How the backward pass is cut, and where its scratch lies.
@@ -308,7 +752,8 @@ extern "C" rg_status rg_rows8_product(const void *x, uint64_t x_stride, uint64_t
     RG_TRY(check_held("x", x, x_stride, n_rows, n_cols, false));
     RG_TRY(check_held("w", w, w_stride, n_outs, n_cols, false));
     RG_TRY(check_elements("y", y, y_stride, n_rows, n_outs, element_bytes(type), true));
-    RG_TRY(check_workspace(workspace, workspace_bytes, 0));
+    RG_TRY(check_steps("x", x_stride));
+    RG_TRY(check_steps("w", w_stride));
     ProductArgs a{};
     a.x = static_cast<const uint8_t *>(x); a.x_stride = x_stride;
     a.w = static_cast<const uint8_t *>(w); a.w_stride = w_stride;
@@ -316,12 +761,9 @@ extern "C" rg_status rg_rows8_product(const void *x, uint64_t x_stride, uint64_t
     a.y = static_cast<uint8_t *>(y); a.y_stride = y_stride;
     a.n_rows = (int32_t)n_rows; a.n_outs = (int32_t)n_outs; a.n_cols = (int32_t)n_cols; a.held_bytes = (int32_t)held_bytes(n_cols);
     const hipStream_t st = as_stream(stream);
-    const uint64_t tiles = (n_rows + 15) / 16 * ((n_outs + 15) / 16);
-    RG_TRY(check_grid(tiles, 256));
-    if (type == RG_F32) hipLaunchKernelGGL(product_few_kernel<float>, dim3((uint32_t)tiles), dim3(256), 0, st, a);
-    else if (type == RG_BF16) hipLaunchKernelGGL(product_few_kernel<bf16>, dim3((uint32_t)tiles), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(product_few_kernel<f16>, dim3((uint32_t)tiles), dim3(256), 0, st, a);
-    RG_HIP(hipGetLastError());
+    if (type == RG_F32) RG_TRY(launch_product<float>(a, st));
+    else if (type == RG_BF16) RG_TRY(launch_product<bf16>(a, st));
+    else RG_TRY(launch_product<f16>(a, st));
     return RG_OK;
 }
 

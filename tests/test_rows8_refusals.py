@@ -123,3 +123,39 @@ def test_every_width_has_a_kernel_that_holds_it(tmp_path):
                 assert held // pack > 4096
             else:
                 assert (lanes, packs) in HOLD_KERNELS and (packs - 1) * lanes * pack < held <= packs * lanes * pack, (cols, lanes, packs)
+
+
+WAYS = r"""
+#include "rg_launch.h"
+#include <cstdio>
+int main()
+{
+    unsigned long long n, m, d, bytes;
+    int cu;
+    while (scanf("%llu %llu %llu %llu %d", &n, &m, &d, &bytes, &cu) == 5) {
+        const rg::ProductWay way = rg::product_way(n, m, d, bytes, cu);
+        const rg::ThinShape s = way == rg::ProductWay::THIN ? rg::thin_shape(n, m, d, cu) : rg::ThinShape{};
+        printf("%d %u %u %u %u\n", (int)way, s.outs, s.shares, s.lds, s.grid);
+    }
+}
+"""
+
+
+def test_ways_of_the_product(tmp_path):
+    """Each way is taken somewhere, launches hold its tiles, and what THIN puts into LDS fits and covers the outputs."""
+    (tmp_path / "driver.cpp").write_text(WAYS)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-o", str(tmp_path / "driver"), str(tmp_path / "driver.cpp")])
+    sizes = [1, 2, 15, 16, 17, 64, 100, 999, 4096, 40_000, 150_000, 1_000_000, 2**24, 2**30]
+    cases = [(n, m, d, b, cu) for n in sizes for m in sizes for d in (1, 16, 61, 64, 500, 602, 768, 769, 4096, 131_072) for b in (2, 4) for cu in (64, 256) if n * m <= 2**37]
+    out = subprocess.run([str(tmp_path / "driver")], input="\n".join(" ".join(map(str, c)) for c in cases) + "\n", capture_output=True, text=True, check=True).stdout.split("\n")
+    seen = set()
+    for (n, m, d, b, cu), line in zip(cases, out):
+        way, outs, shares, lds, grid = map(int, line.split())
+        seen.add(way)
+        if way == 2:
+            assert d <= 768 and outs % 32 == 0 and outs * shares >= m > outs * (shares - 1) and lds <= 160 * 1024 and outs * ((d + 15) // 16 * 16 + 8) + 16 == lds
+            assert grid % shares == 0 and 0 < grid // shares <= (n + 127) // 128 and grid <= max(2 * cu, shares)
+        else:
+            side, threads = {0: (16, 256), 1: (16, 1024), 3: (64, 256), 4: (128, 512), 5: (256, 512)}[way]
+            assert -(-n // side) * -(-m // side) * threads < 2**32, (n, m, d)
+    assert seen == set(range(6))
