@@ -5,6 +5,7 @@
 #include "rg_launch.h"
 
 #include <atomic>
+#include <cstdlib>
 
 namespace rg {
 
@@ -453,23 +454,57 @@ struct GradArgs {
     uint8_t *out;
     uint64_t out_stride;
     uint32_t out_type;
+    const float *scales;             // of the held rows (dx)
     float *partial;                  // [splits][n_i][n_j], or NULL: a sum is done by one workgroup
     int32_t n_i, n_j, n_k, held_bytes;
     int32_t k_each;                  // of a split
+    uint32_t tiles;
 };
 
+// A number as a sum of bf16 numbers: cut off, not rounded, but for the last, so that no part is beyond the range.  What an infinity or a NaN leaves is nothing.
 template <int PARTS> __device__ __forceinline__ void parts_of(float v, bf16 (&p)[PARTS])
 {
+    const bool number = (__builtin_bit_cast(uint32_t, v) & 0x7F800000u) != 0x7F800000u;
 #pragma unroll
     for (int q = 0; q < PARTS; ++q) {
-        // cut off, not rounded, but for the last: no part is beyond the range.  What an infinity leaves is nothing.
         const uint32_t bits = __builtin_bit_cast(uint32_t, v) & 0xFFFF0000u;
-        const float head = __builtin_bit_cast(float, bits);
-        if (q == PARTS - 1) p[q] = (bf16)v;
-        else p[q] = __builtin_bit_cast(bf16, (uint16_t)(bits >> 16));
-        const bool number = (__builtin_bit_cast(uint32_t, v) & 0x7F800000u) != 0x7F800000u;
-        if (!number && q != PARTS - 1) p[q] = (bf16)v;
-        v = number ? v - head : 0.f;
+        p[q] = q == PARTS - 1 || !number ? (bf16)v : __builtin_bit_cast(bf16, (uint16_t)(bits >> 16));
+        v = number ? v - __builtin_bit_cast(float, bits) : 0.f;
+    }
+}
+// Eight of them at once: as above, but that one test does for all.
+template <int PARTS> __device__ __forceinline__ void parts_of(const float (&from)[8], bf16x8 (&p)[PARTS])
+{
+    float v[8], most = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = from[e];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) most = fmaxf(fmaxf(most, fabsf(v[e])), fabsf(v[e + 1]));      // passes over NaN, of which something is left over and is NaN
+    if (__builtin_expect(most != __builtin_inff(), 1)) {
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+            if (q == PARTS - 1) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[q][e] = (bf16)v[e];
+            } else {
+                u32x4 heads;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    heads[e / 2] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, v[e + 1]), __builtin_bit_cast(uint32_t, v[e]), 0x07060302u);
+                    v[e] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v[e]) & 0xFFFF0000u);
+                    v[e + 1] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v[e + 1]) & 0xFFFF0000u);
+                }
+                p[q] = __builtin_bit_cast(bf16x8, heads);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            bf16 one[PARTS];
+            parts_of<PARTS>(v[e], one);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) p[q][e] = one[q];
+        }
     }
 }
 
@@ -479,65 +514,301 @@ __device__ __forceinline__ void store_as(void *p, uint32_t type, int64_t at, flo
     else if (type == RG_BF16) static_cast<bf16 *>(p)[at] = (bf16)v;
     else static_cast<f16 *>(p)[at] = (f16)v;
 }
-
-constexpr int GRAD_TILE = 64, GRAD_DEPTH = 32, GRAD_PITCH = GRAD_DEPTH + 8;
-
-// ALONG: dy's rows run along k (dx); otherwise along i (dweight).
-template <typename T, int PARTS, bool ALONG>
-__global__ void __launch_bounds__(256) grad_kernel(GradArgs a)
+// Four results side by side, of which n are inside.
+template <typename O> __device__ __forceinline__ void store_four(O *p, const f32x4 &v, int32_t n)
 {
-    __shared__ __align__(16) bf16 left[PARTS][GRAD_TILE][GRAD_PITCH];
-    __shared__ __align__(16) bf16 right[GRAD_TILE][GRAD_PITCH];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int32_t down = (a.n_i + GRAD_TILE - 1) / GRAD_TILE;
-    const int32_t i0 = (int32_t)(blockIdx.x % (uint32_t)down) * GRAD_TILE, j0 = (int32_t)(blockIdx.x / (uint32_t)down) * GRAD_TILE;
-    const int64_t k_first = (int64_t)blockIdx.y * a.k_each;
-    const int32_t k_end = (int32_t)min((int64_t)a.n_k, k_first + a.k_each);
-    f32x4 acc[2][2] = {};
-    for (int32_t k0 = (int32_t)k_first; k0 < k_end; k0 += GRAD_DEPTH) {
-        __syncthreads();
-        for (int e = 0; e < 8; ++e) {
-            const int q = (int)threadIdx.x * 8 + e;
-            const int i = ALONG ? q / GRAD_DEPTH : q % GRAD_TILE, k = ALONG ? q % GRAD_DEPTH : q / GRAD_TILE;
-            float v = 0.f;
-            if (i0 + i < a.n_i && k0 + k < k_end) {
-                const float s = *row_at<float>(a.held + a.held_bytes - 4, a.held_stride, k0 + k);
-                v = (float)(ALONG ? row_at<T>(a.dy, a.dy_stride, i0 + i)[k0 + k] : row_at<T>(a.dy, a.dy_stride, k0 + k)[i0 + i]) * s;
-            }
-            bf16 p[PARTS];
-            parts_of<PARTS>(v, p);
-            for (int x = 0; x < PARTS; ++x) left[x][i][k] = p[x];
-        }
-        for (int e = 0; e < 8; ++e) {
-            const int q = (int)threadIdx.x * 8 + e, j = q % GRAD_TILE, k = q / GRAD_TILE;
-            right[j][k] = (bf16)(float)(j0 + j < a.n_j && k0 + k < k_end ? row_at<int8_t>(a.held, a.held_stride, k0 + k)[j0 + j] : (int8_t)0);
-        }
-        __syncthreads();
-        for (int x = 0; x < PARTS; ++x)
-            for (int bi = 0; bi < 2; ++bi)
-                for (int bj = 0; bj < 2; ++bj) {
-                    const bf16x8 l = *reinterpret_cast<const bf16x8 *>(&left[x][(wave >> 1) * 32 + bi * 16 + (lane & 15)][(lane >> 4) * 8]);
-                    const bf16x8 r = *reinterpret_cast<const bf16x8 *>(&right[(wave & 1) * 32 + bj * 16 + (lane & 15)][(lane >> 4) * 8]);
-                    acc[bi][bj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r, l, acc[bi][bj], 0, 0, 0);
-                }
+    if (n >= 4) {
+        const float w[4] = {v[0], v[1], v[2], v[3]};
+        store_pack<O, 4>(p, w);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) p[e] = (O)v[e];
     }
-    for (int bi = 0; bi < 2; ++bi)
-        for (int bj = 0; bj < 2; ++bj)
-            for (int e = 0; e < 4; ++e) {
-                const int32_t i = i0 + (wave >> 1) * 32 + bi * 16 + (lane & 15), j = j0 + (wave & 1) * 32 + bj * 16 + (lane >> 4) * 4 + e;
-                if (i >= a.n_i || j >= a.n_j) continue;
-                if (a.partial) a.partial[((int64_t)blockIdx.y * a.n_i + i) * a.n_j + j] = acc[bi][bj][e];
-                else store_as(a.out + (uint64_t)i * a.out_stride, a.out_type, j, acc[bi][bj][e]);
-            }
 }
 
-// The splits' sums, added up in their order.
+// Tiles of TI x TJ by WI x WJ waves of BI x BJ blocks of 16 x 16, in steps of 32 along k.  ALONG: dy's rows run along k (dx); otherwise along i (dweight).  A step's elements of dy are read into registers
+// two steps ahead, and one step ahead are multiplied with their scales, parted, and written into LDS; the codes go there as they are.  Of operands that lie along the wrong axis LDS itself makes columns (reads
+// that transpose blocks of 16 x 8 bytes or 16 x 4 numbers).  What the lanes read at a time falls on all banks once: the order of the 16-byte chunks of a row, or of the 32-byte pieces of
+// one of dy's, depends on the row.
+template <typename T, int PARTS_, bool ALONG_, int WI_, int WJ_, int BI_, int BJ_>
+struct GradTile {
+    static constexpr int PARTS = PARTS_, WI = WI_, WJ = WJ_, BI = BI_, BJ = BJ_;
+    static constexpr bool ALONG = ALONG_;
+    static constexpr int THREADS = WI * WJ * 64, TI = WI * BI * 16, TJ = WJ * BJ * 16, DEPTH = 32;
+    static constexpr int LEFT = PARTS * TI * DEPTH * 2, RIGHT = DEPTH * TJ, STAGE = LEFT + RIGHT, LDS_BYTES = 2 * STAGE;
+    static constexpr int PACKS = TI * DEPTH / 8 / THREADS, CHUNKS = (DEPTH * TJ / 16 + THREADS - 1) / THREADS;
+    static_assert(PACKS * THREADS * 8 == TI * DEPTH && LDS_BYTES <= 160 * 1024 && TI >= 64 && TJ >= 64, "");
+    typedef typename PackOf<T, 8>::type Raw;
+
+    // Bytes into a part of the left operand, of the pack of eight elements that begins at (i, k), one of which runs.
+    static __device__ __forceinline__ uint32_t left_at(int i, int k)
+    {
+        if (ALONG) return (uint32_t)(i * 64 + ((k / 8) ^ (-(i >> 2) & 3)) * 16);
+        const int turn = TI >= 128 ? (k & 3) | ((k >> 1) & 4) : ((k >> 1) & 1) | ((k >> 2) & 2);      // of 64 elements two rows lie on all banks together
+        return (uint32_t)(k * TI * 2 + ((i / 16) ^ turn) * 32 + (i % 16) * 2);
+    }
+    // Bytes into the right one, of the chunk of 16 codes from j on of row k.
+    static __device__ __forceinline__ uint32_t right_at(int k, int j)
+    {
+        constexpr int N = TJ / 16, TURN = TJ >= 256 ? 0 : TJ >= 128 ? 1 : 2;       // rows of less than 256 bytes: several lie on all banks together
+        return (uint32_t)(k * TJ + ((j / 16) ^ ((k >> TURN) & (N < 16 ? N - 1 : 15))) * 16);
+    }
+
+    // What a thread reads of a step.
+    struct Step {
+        Raw dy[PACKS];
+        float scale[ALONG ? 8 : PACKS];
+        i32x4 codes[CHUNKS];
+    };
+    // Where it comes from: addresses of the next step's, as long as all of that is inside; else they are made anew, element by element.
+    struct Source {
+        const GradArgs &a;
+        const uint8_t *dy[PACKS], *scale[ALONG ? 1 : PACKS], *codes[CHUNKS];
+        int32_t i0, j0, k0, k_end;                                 // of the next step
+        bool whole;                                                // rows of i
+        __device__ __forceinline__ Source(const GradArgs &args, int32_t i, int32_t j, int32_t k, int32_t end) : a(args), i0(i), j0(j), k0(k), k_end(end), whole(ALONG || i + TI <= args.n_i)
+        {
+#pragma unroll
+            for (int p = 0; p < PACKS; ++p) {
+                const int q = p * THREADS + (int)threadIdx.x;
+                if constexpr (ALONG) {                             // (of a row beyond the last nothing is made: the last one's elements do)
+                    dy[p] = reinterpret_cast<const uint8_t *>(row_at<T>(a.dy, a.dy_stride, min(i0 + q / 4, a.n_i - 1)) + k0 + q % 4 * 8);
+                } else {
+                    const int32_t row = min(k0 + q / (TI / 8), k_end - 1);
+                    dy[p] = reinterpret_cast<const uint8_t *>(row_at<T>(a.dy, a.dy_stride, row) + i0 + q % (TI / 8) * 8);
+                    scale[p] = a.held + (uint64_t)row * a.held_stride + (a.held_bytes - 4);
+                }
+            }
+            if constexpr (ALONG) scale[0] = reinterpret_cast<const uint8_t *>(a.scales + k0 + (int32_t)(threadIdx.x % 4) * 8);
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) codes[c] = codes_at(k0, c);
+        }
+        __device__ __forceinline__ const uint8_t *codes_at(int32_t k, int c) const
+        {
+            const int q = min(c * THREADS + (int)threadIdx.x, DEPTH * TJ / 16 - 1);
+            return a.held + (uint64_t)min(k + q / (TJ / 16), k_end - 1) * a.held_stride + min(j0 + q % (TJ / 16) * 16, a.held_bytes - 16);
+        }
+        __device__ __forceinline__ void load(Step &s)
+        {
+            if (whole && k0 + DEPTH <= k_end) {
+#pragma unroll
+                for (int p = 0; p < PACKS; ++p) {
+                    s.dy[p] = load_raw<T, 8>(reinterpret_cast<const T *>(dy[p]));
+                    dy[p] += ALONG ? DEPTH * sizeof(T) : DEPTH * a.dy_stride;
+                }
+                if constexpr (ALONG) {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 4) {
+                        const f32x4 v = reinterpret_cast<const f32x4 *>(scale[0])[e / 4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) s.scale[e + x] = v[x];
+                    }
+                    scale[0] += DEPTH * sizeof(float);
+                } else {
+#pragma unroll
+                    for (int p = 0; p < PACKS; ++p) {
+                        s.scale[p] = *reinterpret_cast<const float *>(scale[p]);
+                        scale[p] += DEPTH * a.held_stride;
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) {
+                    s.codes[c] = *reinterpret_cast<const i32x4 *>(codes[c]);
+                    codes[c] += DEPTH * a.held_stride;
+                }
+            } else if (k0 < k_end) {
+                load_part(s);
+            }
+            k0 += DEPTH;
+        }
+        __device__ __forceinline__ void load_part(Step &s) const
+        {
+#pragma unroll
+            for (int p = 0; p < PACKS; ++p) {
+                const int q = p * THREADS + (int)threadIdx.x;
+                const int32_t i = i0 + (ALONG ? q / 4 : q % (TI / 8) * 8), k = k0 + (ALONG ? q % 4 * 8 : q / (TI / 8));
+                const int32_t row = ALONG ? i : k, first = ALONG ? k : i, rows = ALONG ? a.n_i : k_end, cols = ALONG ? k_end : a.n_i;
+                const T *from = row_at<T>(a.dy, a.dy_stride, min(row, rows - 1)) + first;
+                if (row < rows && first + 8 <= cols) {
+                    s.dy[p] = load_raw<T, 8>(from);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s.dy[p][e] = row < rows && first + e < cols ? from[e] : (T)0.f;
+                }
+                if constexpr (!ALONG) s.scale[p] = *row_at<float>(a.held + a.held_bytes - 4, a.held_stride, min(k, k_end - 1));
+            }
+            if constexpr (ALONG) {
+                const int32_t k = k0 + (int32_t)(threadIdx.x % 4) * 8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s.scale[e] = a.scales[min(k + e, a.n_k - 1)];
+            }
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) s.codes[c] = *reinterpret_cast<const i32x4 *>(codes_at(k0, c));
+        }
+    };
+    static __device__ __forceinline__ void put(const Step &s, uint8_t *stage)
+    {
+#pragma unroll
+        for (int p = 0; p < PACKS; ++p) {
+            const int q = p * THREADS + (int)threadIdx.x;
+            const int i = ALONG ? q / 4 : q % (TI / 8) * 8, k = ALONG ? q % 4 * 8 : q / (TI / 8);
+            float v[8];
+            unpack<T, 8>(s.dy[p], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = rounded(v[e], s.scale[ALONG ? e : p]);
+            bf16x8 parts[PARTS];
+            parts_of<PARTS>(v, parts);
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x) *reinterpret_cast<bf16x8 *>(stage + x * (TI * DEPTH * 2) + left_at(i, k)) = parts[x];
+        }
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int q = c * THREADS + (int)threadIdx.x;
+            if (DEPTH * TJ / 16 % THREADS == 0 || q < DEPTH * TJ / 16) *reinterpret_cast<i32x4 *>(stage + LEFT + right_at(q / (TJ / 16), q % (TJ / 16) * 16)) = s.codes[c];
+        }
+    }
+
+    // The operand of a matrix operation: 16 rows of i (columns of j), a lane has eight along k.
+    static __device__ __forceinline__ bf16x8 left(const uint8_t *part, int i, int lane)
+    {
+        if constexpr (ALONG) {
+            return *reinterpret_cast<const bf16x8 *>(part + left_at(i + (lane & 15), (lane >> 4) * 8));
+        } else {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const int k = (lane >> 4) * 8 + ((lane >> 2) & 3), at = i + (lane & 3) * 4;
+            const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(part + left_at(at, k)));
+            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(part + left_at(at, k + 4)));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+    static __device__ __forceinline__ bf16x8 right(const uint8_t *codes, int j, int lane)
+    {
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(codes + right_at((lane >> 4) * 8 + ((lane & 15) >> 1), j) + (lane & 1) * 8));
+        u32x4 out;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {                           // whole numbers of seven bits: bf16 is the upper half of fp32
+            const float lo = (float)(int8_t)(c[e / 4] >> (e % 4 * 8)), hi = (float)(int8_t)(c[e / 4] >> (e % 4 * 8 + 8));
+            out[e / 2] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+        }
+        return __builtin_bit_cast(bf16x8, out);
+    }
+
+    // Waits until what this wave wrote into LDS is there, and then for every wave.  (Loads stay under way, which __syncthreads would wait for.)
+    static __device__ __forceinline__ void arrive()
+    {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (3 << 14));     // lgkmcnt 0
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+};
+
+template <typename T, typename Tile>
+__global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
+{
+    extern __shared__ __align__(16) uint8_t lds[];
+    constexpr int BI = Tile::BI, BJ = Tile::BJ, PARTS = Tile::PARTS, DEPTH = Tile::DEPTH;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    // Tiles of one row of j follow one another, splits of k of a tile lie apart: what an XCD works on at once shares dy.
+    const uint32_t across = ((uint32_t)a.n_j + Tile::TJ - 1) / Tile::TJ, t = tile_of_workgroup();
+    const uint32_t tile = t % a.tiles, split = t / a.tiles;
+    const int32_t i0 = (int32_t)(tile / across) * Tile::TI, j0 = (int32_t)(tile % across) * Tile::TJ;
+    const int64_t k_first = (int64_t)split * a.k_each;
+    const int32_t k_end = (int32_t)min((int64_t)a.n_k, k_first + a.k_each);
+    const int wi = (wave / Tile::WJ) * BI * 16, wj = (wave % Tile::WJ) * BJ * 16;
+    // Of the two waves of a vector unit one prepares the next step before it multiplies, the other behind it: the one's conversions go beside the other's matrix operations.
+    const bool early = wave < 4;
+    f32x4 acc[BI][BJ] = {};
+    if (k_first < k_end) {
+        typename Tile::Step step;
+        typename Tile::Source src(a, i0, j0, (int32_t)k_first, k_end);
+        const int32_t last = (k_end - 1 - (int32_t)k_first) / DEPTH;
+        src.load(step);
+        Tile::put(step, lds);
+        src.load(step);
+        Tile::arrive();
+        for (int32_t s = 0; s <= last; ++s) {
+            const uint8_t *stage = lds + (s & 1) * Tile::STAGE;
+            const auto prepare = [&] {
+                Tile::put(step, lds + (~s & 1) * Tile::STAGE);
+                src.load(step);
+            };
+            if (early && s < last) prepare();
+            // The next blocks' elements are on their way out of LDS while one row of blocks is multiplied: left to itself the compiler asks for them when they are needed.
+            bf16x8 r[BJ], l[2][PARTS];
+            const auto read = [&](int i, bf16x8 (&to)[PARTS]) {
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) to[p] = Tile::left(stage + p * (Tile::TI * DEPTH * 2), wi + i * 16, lane);
+            };
+            read(0, l[0]);
+#pragma unroll
+            for (int j = 0; j < BJ; ++j) r[j] = Tile::right(stage + Tile::LEFT, wj + j * 16, lane);
+#pragma unroll
+            for (int i = 0; i < BI; ++i) {
+                if (i + 1 < BI) read(i + 1, l[(i + 1) & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int j = 0; j < BJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[j], l[i & 1][p], acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (!early && s < last) prepare();
+            Tile::arrive();
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < BI; ++i) {
+        const int32_t at = i0 + wi + i * 16 + (lane & 15);
+        if (at >= a.n_i) continue;
+#pragma unroll
+        for (int j = 0; j < BJ; ++j) {
+            const int32_t col = j0 + wj + j * 16 + (lane >> 4) * 4, n = a.n_j - col;
+            if (a.partial) store_four(a.partial + ((int64_t)split * a.n_i + at) * a.n_j + col, acc[i][j], n);
+            else if (a.out_type == RG_F32) store_four(row_at<float>(a.out, a.out_stride, at) + col, acc[i][j], n);
+            else if (a.out_type == RG_BF16) store_four(row_at<bf16>(a.out, a.out_stride, at) + col, acc[i][j], n);
+            else store_four(row_at<f16>(a.out, a.out_stride, at) + col, acc[i][j], n);
+        }
+    }
+}
+
+// The scales of held rows side by side.
+__global__ void __launch_bounds__(256) scales_kernel(const uint8_t *held, uint64_t stride, int32_t held_bytes, int32_t n, float *scales)
+{
+    const int32_t r = (int32_t)(blockIdx.x * 256 + threadIdx.x);
+    if (r < n) scales[r] = *row_at<float>(held + held_bytes - 4, stride, r);
+}
+
+// The splits' sums, added up in their order: four elements of a row to a thread.
 __global__ void __launch_bounds__(256) grad_join_kernel(const float *partial, int32_t splits, int64_t n_i, int64_t n_j, uint8_t *out, uint64_t out_stride, uint32_t type)
 {
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n_i * n_j; q += (int64_t)gridDim.x * 256) {
-        float v = 0.f;
-        for (int32_t s = 0; s < splits; ++s) v += partial[s * n_i * n_j + q];
-        store_as(out + (uint64_t)(q / n_j) * out_stride, type, q % n_j, v);
+    const int64_t quads = (n_j + 3) / 4;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n_i * quads; q += (int64_t)gridDim.x * 256) {
+        const int64_t i = q / quads, j = q % quads * 4;
+        const int32_t n = (int32_t)min((int64_t)4, n_j - j);
+        const float *from = partial + i * n_j + j;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (n == 4) {
+#pragma unroll 8
+            for (int32_t s = 0; s < splits; ++s) {
+                float w[4];
+                load_pack<float, 4>(from + s * n_i * n_j, w);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += w[e];
+            }
+        } else {
+            for (int32_t s = 0; s < splits; ++s)
+                for (int e = 0; e < n; ++e) v[e] += from[s * n_i * n_j + e];
+        }
+        uint8_t *row = out + (uint64_t)i * out_stride;
+        if (type == RG_F32) store_four(reinterpret_cast<float *>(row) + j, v, n);
+        else if (type == RG_BF16) store_four(reinterpret_cast<bf16 *>(row) + j, v, n);
+        else store_four(reinterpret_cast<f16 *>(row) + j, v, n);
     }
 }
 
@@ -670,36 +941,41 @@ template <typename T> rg_status launch_product(const ProductArgs &a, hipStream_t
 
 // How the backward pass is cut, and where its scratch lies.
 struct GradPlan {
+    int dx_tile, dw_tile;                // side
     uint64_t dx_tiles, dw_tiles;
     int32_t dx_splits, dx_each, dw_splits, dw_each, bias_parts, bias_each;
-    uint64_t bias_at, bytes;             // sums of dx, then of dweight in the same place; those of dbias
+    uint64_t scales_at, bias_at, bytes;  // sums of dx, then of dweight in the same place; w's scales; sums of dbias
 };
 
-int32_t splits_of(uint64_t tiles, uint64_t n_k, int n_cu, int32_t *each)
+void cut(uint64_t n_i, uint64_t n_j, uint64_t n_k, int n_cu, int *side, uint64_t *tiles, int32_t *splits, int32_t *each)
 {
-    const uint64_t steps = (n_k + GRAD_DEPTH - 1) / GRAD_DEPTH;
-    uint64_t splits = 1;
-    while (tiles * splits * 2 <= (uint64_t)n_cu * 2 && steps >= splits * 2 * 4) splits *= 2;
-    const uint64_t per = std::max<uint64_t>(1, (steps + splits - 1) / splits);
-    *each = (int32_t)(per * GRAD_DEPTH);
-    return (int32_t)std::max<uint64_t>(1, (steps + per - 1) / per);
+    const char *e = getenv("RG_G");
+    const uint64_t steps = (n_k + 31) / 32;
+    const auto count = [&](uint64_t s) { return (n_i + s - 1) / s * ((n_j + s - 1) / s); };
+    *side = e ? atoi(e) : 256;
+    *tiles = count((uint64_t)*side);
+    uint64_t n = 1;
+    const uint64_t slots = (uint64_t)n_cu * (*side == 256 ? 1 : *side == 128 ? 2 : 4);
+    if (*tiles && *tiles < slots) n = std::max<uint64_t>(1, std::min(slots / *tiles, steps / 8));
+    const uint64_t per = std::max<uint64_t>(1, (steps + n - 1) / n);
+    *each = (int32_t)(per * 32);
+    *splits = (int32_t)std::max<uint64_t>(1, (steps + per - 1) / per);
 }
 
 GradPlan grad_plan(uint64_t n, uint64_t m, uint64_t d, int n_cu, bool dx, bool dw, bool db)
 {
     GradPlan p{};
     uint64_t bytes = 0;
-    const auto tiles = [](uint64_t i, uint64_t j) { return (i + GRAD_TILE - 1) / GRAD_TILE * ((j + GRAD_TILE - 1) / GRAD_TILE); };
     if (dx) {
-        p.dx_tiles = tiles(n, d);
-        p.dx_splits = splits_of(p.dx_tiles, m, n_cu, &p.dx_each);
+        cut(n, d, m, n_cu, &p.dx_tile, &p.dx_tiles, &p.dx_splits, &p.dx_each);
         if (p.dx_splits > 1) bytes = std::max(bytes, (uint64_t)p.dx_splits * n * d * 4);
     }
     if (dw) {
-        p.dw_tiles = tiles(m, d);
-        p.dw_splits = splits_of(p.dw_tiles, n, n_cu, &p.dw_each);
+        cut(m, d, n, n_cu, &p.dw_tile, &p.dw_tiles, &p.dw_splits, &p.dw_each);
         if (p.dw_splits > 1) bytes = std::max(bytes, (uint64_t)p.dw_splits * m * d * 4);
     }
+    p.scales_at = (bytes + 15) / 16 * 16;
+    if (dx) bytes = p.scales_at + m * 4;
     p.bias_at = (bytes + 15) / 16 * 16;
     if (db) {
         p.bias_parts = (int32_t)std::max<uint64_t>(1, std::min<uint64_t>(256, n / 64));
@@ -710,20 +986,32 @@ GradPlan grad_plan(uint64_t n, uint64_t m, uint64_t d, int n_cu, bool dx, bool d
     return p;
 }
 
-template <typename T, int PARTS, bool ALONG> void launch_grad(uint64_t tiles, int32_t splits, const GradArgs &g, hipStream_t st)
+template <typename T, typename Tile> rg_status launch_grad(int32_t splits, const GradArgs &g, hipStream_t st)
 {
-    hipLaunchKernelGGL((grad_kernel<T, PARTS, ALONG>), dim3((uint32_t)tiles, (uint32_t)splits), dim3(256), 0, st, g);
+    RG_TRY(check_grid((uint64_t)g.tiles * (uint64_t)splits, Tile::THREADS));
+    static std::atomic<uint64_t> known{0};
+    RG_TRY(allow_lds(grad_kernel<T, Tile>, Tile::LDS_BYTES, known));
+    hipLaunchKernelGGL((grad_kernel<T, Tile>), dim3(g.tiles * (uint32_t)splits), dim3(Tile::THREADS), Tile::LDS_BYTES, st, g);
+    RG_HIP(hipGetLastError());
+    return RG_OK;
 }
 
-template <bool ALONG> rg_status launch_grad_of(uint32_t type, uint64_t tiles, int32_t splits, GradArgs g, void *workspace, hipStream_t st)
+template <typename T, int PARTS, bool ALONG> rg_status launch_grad_by(int side, int32_t splits, const GradArgs &g, hipStream_t st)
+{
+    if (side == 256) return launch_grad<T, GradTile<T, PARTS, ALONG, 2, 4, 8, 4>>(splits, g, st);
+    if (side == 128) return launch_grad<T, GradTile<T, PARTS, ALONG, 2, 2, 4, 4>>(splits, g, st);
+    return launch_grad<T, GradTile<T, PARTS, ALONG, 2, 2, 2, 2>>(splits, g, st);
+}
+
+template <bool ALONG> rg_status launch_grad_of(uint32_t type, int side, int32_t splits, GradArgs g, void *workspace, hipStream_t st)
 {
     g.partial = splits > 1 ? static_cast<float *>(workspace) : nullptr;
-    if (type == RG_F32) launch_grad<float, 3, ALONG>(tiles, splits, g, st);
-    else if (type == RG_BF16) launch_grad<bf16, 2, ALONG>(tiles, splits, g, st);
-    else launch_grad<f16, 2, ALONG>(tiles, splits, g, st);
-    RG_HIP(hipGetLastError());
+    if (type == RG_F32) RG_TRY((launch_grad_by<float, 3, ALONG>(side, splits, g, st)));
+    else if (type == RG_BF16) RG_TRY((launch_grad_by<bf16, 2, ALONG>(side, splits, g, st)));
+    else RG_TRY((launch_grad_by<f16, 2, ALONG>(side, splits, g, st)));
     if (splits > 1) {
-        hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)std::min<int64_t>(2048, ((int64_t)g.n_i * g.n_j + 255) / 256)), dim3(256), 0, st, g.partial, splits, (int64_t)g.n_i, (int64_t)g.n_j, g.out,
+        const int64_t quads = (int64_t)g.n_i * ((g.n_j + 3) / 4);
+        hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)std::min<int64_t>(4096, (quads + 255) / 256)), dim3(256), 0, st, g.partial, splits, (int64_t)g.n_i, (int64_t)g.n_j, g.out,
                            g.out_stride, g.out_type);
         RG_HIP(hipGetLastError());
     }
@@ -800,8 +1088,7 @@ extern "C" rg_status rg_rows8_product_backward(const void *dy, uint64_t dy_strid
     RG_TRY(compute_units(&n_cu));
     const GradPlan p = grad_plan(n_rows, n_outs, n_cols, n_cu, dx, dweight, dbias);
     RG_TRY(check_workspace(workspace, workspace_bytes, p.bytes));
-    RG_TRY(check_grid(p.dx_tiles, 256));
-    RG_TRY(check_grid(p.dw_tiles, 256));
+    RG_TRY(check_grid(std::max(p.dx_tiles * (uint64_t)std::max(p.dx_splits, 1), p.dw_tiles * (uint64_t)std::max(p.dw_splits, 1)), 512));
     RG_TRY(check_grid((n_outs + 63) / 64, 256));
     const hipStream_t st = as_stream(stream);
     GradArgs g{};
@@ -810,14 +1097,20 @@ extern "C" rg_status rg_rows8_product_backward(const void *dy, uint64_t dy_strid
     if (dx && n_rows) {
         g.held = static_cast<const uint8_t *>(w); g.held_stride = w_stride;
         g.out = static_cast<uint8_t *>(dx); g.out_stride = dx_stride; g.out_type = type;
-        g.n_i = (int32_t)n_rows; g.n_k = (int32_t)n_outs; g.k_each = p.dx_each;
-        RG_TRY(launch_grad_of<true>(type, p.dx_tiles, p.dx_splits, g, workspace, st));
+        g.n_i = (int32_t)n_rows; g.n_k = (int32_t)n_outs; g.k_each = p.dx_each; g.tiles = (uint32_t)p.dx_tiles;
+        if (n_outs) {
+            float *scales = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.scales_at);
+            hipLaunchKernelGGL(scales_kernel, dim3((uint32_t)((n_outs + 255) / 256)), dim3(256), 0, st, g.held, g.held_stride, g.held_bytes, g.n_k, scales);
+            RG_HIP(hipGetLastError());
+            g.scales = scales;
+        }
+        RG_TRY(launch_grad_of<true>(type, p.dx_tile, p.dx_splits, g, workspace, st));
     }
     if (dweight && n_outs) {
         g.held = static_cast<const uint8_t *>(x); g.held_stride = x_stride;
         g.out = static_cast<uint8_t *>(dweight); g.out_stride = dweight_stride; g.out_type = weight_type;
-        g.n_i = (int32_t)n_outs; g.n_k = (int32_t)n_rows; g.k_each = p.dw_each;
-        RG_TRY(launch_grad_of<false>(type, p.dw_tiles, p.dw_splits, g, workspace, st));
+        g.n_i = (int32_t)n_outs; g.n_k = (int32_t)n_rows; g.k_each = p.dw_each; g.tiles = (uint32_t)p.dw_tiles;
+        RG_TRY(launch_grad_of<false>(type, p.dw_tile, p.dw_splits, g, workspace, st));
     }
     if (dbias && n_outs) {
         float *partial = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.bias_at);
@@ -827,7 +1120,7 @@ extern "C" rg_status rg_rows8_product_backward(const void *dy, uint64_t dy_strid
         else if (type == RG_BF16) hipLaunchKernelGGL(bias_sums_kernel<bf16>, grid, dim3(256), 0, st, from, dy_stride, (int32_t)n_rows, (int32_t)n_outs, p.bias_each, partial);
         else hipLaunchKernelGGL(bias_sums_kernel<f16>, grid, dim3(256), 0, st, from, dy_stride, (int32_t)n_rows, (int32_t)n_outs, p.bias_each, partial);
         RG_HIP(hipGetLastError());
-        hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)std::min<uint64_t>(2048, (n_outs + 255) / 256)), dim3(256), 0, st, partial, p.bias_parts, (int64_t)1, (int64_t)n_outs,
+        hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)std::min<uint64_t>(2048, (n_outs + 1023) / 1024)), dim3(256), 0, st, partial, p.bias_parts, (int64_t)1, (int64_t)n_outs,
                            static_cast<uint8_t *>(dbias), (uint64_t)0, weight_type);
         RG_HIP(hipGetLastError());
     }
