@@ -281,4 +281,62 @@ inline ProductWay product_way(uint64_t n, uint64_t m, uint64_t d, uint64_t eleme
     return way;
 }
 
+// The backward pass' products: sums over n_k of n_i x n_j, in `parts` bf16 numbers.
+constexpr uint64_t GRAD_DEPTH = 32, GRAD_THIN_OUTS = 256;      // of a step along k; outputs that the thin way has registers for
+enum class GradWay { TILES_64, TILES_64_256, TILES_128, TILES_256, THIN };
+struct GradCut {
+    GradWay way;
+    uint64_t tiles;
+    int32_t splits, each;                 // of k, and elements of a split
+};
+// dx of many rows: k in LDS, padded to 32 columns; rows of a wave at a time.
+inline ThinShape grad_thin_shape(uint64_t n, uint64_t d, uint64_t k, uint64_t rows, int n_cu)
+{
+    const uint64_t most = (THIN_LDS / k - 4) / 32 * 32;
+    ThinShape s{};
+    s.shares = (uint32_t)((d + most - 1) / most);
+    s.outs = (uint32_t)(((d + s.shares - 1) / s.shares + 31) / 32 * 32);
+    s.lds = (uint32_t)((s.outs + 4) * k);
+    const uint64_t each = rows * THIN_THREADS / 64, at_once = (uint64_t)n_cu * (s.lds * 2 <= THIN_LDS ? 2 : 1);
+    s.grid = (uint32_t)std::min((n + each - 1) / each, std::max<uint64_t>(1, at_once / s.shares)) * s.shares;
+    return s;
+}
+// The way, and the splits of k, that are done first, in us by what each takes (measured on 1 to 150,000 rows and outputs of 47 to 4,096, sums over 1 to 150,000, in bf16): a tile alone on its
+// compute unit, or as many as the fullest has, by its start and end and its steps; splits write their sums and another launch adds them up.
+inline GradCut grad_cut(uint64_t n_i, uint64_t n_j, uint64_t n_k, int parts, int n_cu, bool along)
+{
+    struct Cost { GradWay way; uint64_t ti, tj; double alone, alone_step, start, step; };
+    static constexpr Cost COSTS[] = {{GradWay::TILES_64, 64, 64, 2.3, 0.7, 0.67, 0.25}, {GradWay::TILES_64_256, 64, 256, 3.5, 0.9, 1.5, 0.62},
+                                     {GradWay::TILES_128, 128, 128, 4, 1.05, 1.8, 0.64}, {GradWay::TILES_256, 256, 256, 8, 1.7, 10, 1.75}};
+    const double more = parts == 3 ? 1.37 : 1.0, cu = (double)n_cu;
+    const uint64_t steps = std::max<uint64_t>(1, (n_k + GRAD_DEPTH - 1) / GRAD_DEPTH);
+    GradCut best{GradWay::TILES_64, 0, 1, (int32_t)(steps * GRAD_DEPTH)};
+    double least = -1;
+    for (const Cost &c : COSTS) {
+        const uint64_t tiles = (n_i + c.ti - 1) / c.ti * ((n_j + c.tj - 1) / c.tj);
+        // None, and as many as leave one, two or four workgroups to a compute unit, or half of them.
+        for (uint64_t fill = 0; fill <= 4; ++fill) {
+            const uint64_t splits = fill == 0 ? 1 : tiles ? std::min(((uint64_t)n_cu << (fill - 1)) / 2 / tiles, steps / 2) : 0;
+            if (splits == 0 || (fill && splits == 1)) continue;
+            const uint64_t per = (steps + splits - 1) / splits, used = (steps + per - 1) / per;
+            const double fullest = (double)((tiles * used + (uint64_t)n_cu - 1) / (uint64_t)n_cu);
+            double us = std::max(c.alone + (double)per * c.alone_step * more, fullest * (c.start + (double)per * c.step * more));
+            if (used > 1) us += 4 + (double)(used * n_i * n_j) * 8 / 8e6 * 256 / cu;
+            if (least < 0 || us < least) {
+                least = us;
+                best = GradCut{c.way, tiles, (int32_t)used, (int32_t)(per * GRAD_DEPTH)};
+            }
+        }
+    }
+    if (along && n_k && n_i && n_k <= GRAD_THIN_OUTS) {
+        const uint64_t rows = parts == 2 ? 32 : 16, k = n_k <= 32 ? 32 : n_k <= 64 ? 64 : n_k <= 128 ? 128 : GRAD_THIN_OUTS;
+        const ThinShape s = grad_thin_shape(n_i, n_j, k, rows, n_cu);
+        const double blocks = (double)((n_i + rows - 1) / rows), waves = (double)(s.grid / s.shares) * (THIN_THREADS / 64);
+        const double turns = blocks / waves, work = (double)(s.outs / 32) * (double)(k / 32) * (parts == 2 ? 0.27 : 0.24);
+        const double us = 3 + 0.05 * (double)s.lds / 1024 + std::max(turns * (s.lds * 2 <= THIN_LDS ? 2 : 1), 0.6) * work;
+        if (us < least) best = GradCut{GradWay::THIN, 0, 1, (int32_t)(steps * GRAD_DEPTH)};
+    }
+    return best;
+}
+
 }  // namespace rg

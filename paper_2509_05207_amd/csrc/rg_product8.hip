@@ -5,7 +5,6 @@
 #include "rg_launch.h"
 
 #include <atomic>
-#include <cstdlib>
 
 namespace rg {
 
@@ -455,10 +454,16 @@ struct GradArgs {
     uint64_t out_stride;
     uint32_t out_type;
     const float *scales;             // of the held rows (dx)
+    float *sums;                     // [splits][n_i] of dy's columns (dweight's), or NULL
     float *partial;                  // [splits][n_i][n_j], or NULL: a sum is done by one workgroup
+    const uint8_t *gather;           // held rows whose scales are put side by side on the way, or NULL
+    uint64_t gather_stride;
+    float *gathered;
+    int32_t n_gather;
     int32_t n_i, n_j, n_k, held_bytes;
     int32_t k_each;                  // of a split
     uint32_t tiles;
+    bool rows_apart;                 // dy's rows: what lies behind a row's end, but for the last rows', may be read
 };
 
 // A number as a sum of bf16 numbers: cut off, not rounded, but for the last, so that no part is beyond the range.  What an infinity or a NaN leaves is nothing.
@@ -472,48 +477,45 @@ template <int PARTS> __device__ __forceinline__ void parts_of(float v, bf16 (&p)
         v = number ? v - __builtin_bit_cast(float, bits) : 0.f;
     }
 }
-// Eight of them at once: as above, but that one test does for all.
-template <int PARTS> __device__ __forceinline__ void parts_of(const float (&from)[8], bf16x8 (&p)[PARTS])
+// Eight of them at once, of numbers; the largest of their magnitudes (passing over NaN, of which something is left over and is NaN).
+template <int PARTS> __device__ __forceinline__ float parts_of_numbers(const float (&from)[8], bf16x8 (&p)[PARTS])
 {
     float v[8], most = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = from[e];
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) most = fmaxf(fmaxf(most, fabsf(v[e])), fabsf(v[e + 1]));      // passes over NaN, of which something is left over and is NaN
-    if (__builtin_expect(most != __builtin_inff(), 1)) {
+    for (int e = 0; e < 8; e += 2) most = fmaxf(fmaxf(most, fabsf(v[e])), fabsf(v[e + 1]));
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q) {
-            if (q == PARTS - 1) {
+    for (int q = 0; q < PARTS; ++q) {
+        if (q == PARTS - 1) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[q][e] = (bf16)v[e];
-            } else {
-                u32x4 heads;
+            for (int e = 0; e < 8; ++e) p[q][e] = (bf16)v[e];
+        } else {
+            u32x4 heads;
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    heads[e / 2] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, v[e + 1]), __builtin_bit_cast(uint32_t, v[e]), 0x07060302u);
-                    v[e] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v[e]) & 0xFFFF0000u);
-                    v[e + 1] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v[e + 1]) & 0xFFFF0000u);
-                }
-                p[q] = __builtin_bit_cast(bf16x8, heads);
+            for (int e = 0; e < 8; e += 2) {
+                heads[e / 2] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, v[e + 1]), __builtin_bit_cast(uint32_t, v[e]), 0x07060302u);
+                v[e] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v[e]) & 0xFFFF0000u);
+                v[e + 1] -= __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v[e + 1]) & 0xFFFF0000u);
             }
+            p[q] = __builtin_bit_cast(bf16x8, heads);
         }
-    } else {
+    }
+    return most;
+}
+// Whether a lane of the wave has an infinity, of which the above makes a NaN.
+__device__ __forceinline__ bool beyond_numbers(float most) { return __builtin_expect(__ballot(most == __builtin_inff()) != 0, 0); }
+template <int PARTS> __device__ __forceinline__ void parts_of_any(const float (&v)[8], bf16x8 (&p)[PARTS])
+{
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            bf16 one[PARTS];
-            parts_of<PARTS>(v[e], one);
+    for (int e = 0; e < 8; ++e) {
+        bf16 one[PARTS];
+        parts_of<PARTS>(v[e], one);
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) p[q][e] = one[q];
-        }
+        for (int q = 0; q < PARTS; ++q) p[q][e] = one[q];
     }
 }
 
-__device__ __forceinline__ void store_as(void *p, uint32_t type, int64_t at, float v)
-{
-    if (type == RG_F32) static_cast<float *>(p)[at] = v;
-    else if (type == RG_BF16) static_cast<bf16 *>(p)[at] = (bf16)v;
-    else static_cast<f16 *>(p)[at] = (f16)v;
-}
 // Four results side by side, of which n are inside.
 template <typename O> __device__ __forceinline__ void store_four(O *p, const f32x4 &v, int32_t n)
 {
@@ -527,16 +529,30 @@ template <typename O> __device__ __forceinline__ void store_four(O *p, const f32
     }
 }
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+// Eight codes of a column, of rows whose eight bytes 16 lanes point at.
+__device__ __forceinline__ i32x2 column_of_codes(const uint8_t *from) { return __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)from); }
+__device__ __forceinline__ bf16x8 codes_as_bf16(const i32x2 &c)
+{
+    u32x4 out;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {                               // whole numbers of seven bits: bf16 is the upper half of fp32
+        const float lo = (float)(int8_t)(c[e / 4] >> (e % 4 * 8)), hi = (float)(int8_t)(c[e / 4] >> (e % 4 * 8 + 8));
+        out[e / 2] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
+    }
+    return __builtin_bit_cast(bf16x8, out);
+}
+
 // Tiles of TI x TJ by WI x WJ waves of BI x BJ blocks of 16 x 16, in steps of 32 along k.  ALONG: dy's rows run along k (dx); otherwise along i (dweight).  A step's elements of dy are read into registers
 // two steps ahead, and one step ahead are multiplied with their scales, parted, and written into LDS; the codes go there as they are.  Of operands that lie along the wrong axis LDS itself makes columns (reads
 // that transpose blocks of 16 x 8 bytes or 16 x 4 numbers).  What the lanes read at a time falls on all banks once: the order of the 16-byte chunks of a row, or of the 32-byte pieces of
 // one of dy's, depends on the row.
-template <typename T, int PARTS_, bool ALONG_, int WI_, int WJ_, int BI_, int BJ_>
+template <typename T, int PARTS_, bool ALONG_, bool SUMS_, int WI_, int WJ_, int BI_, int BJ_>
 struct GradTile {
     static constexpr int PARTS = PARTS_, WI = WI_, WJ = WJ_, BI = BI_, BJ = BJ_;
-    static constexpr bool ALONG = ALONG_;
+    static constexpr bool ALONG = ALONG_, SUMS = SUMS_;              // SUMS: of dy's columns as well (dbias)
     static constexpr int THREADS = WI * WJ * 64, TI = WI * BI * 16, TJ = WJ * BJ * 16, DEPTH = 32;
-    static constexpr int LEFT = PARTS * TI * DEPTH * 2, RIGHT = DEPTH * TJ, STAGE = LEFT + RIGHT, LDS_BYTES = 2 * STAGE;
+    static constexpr int LEFT = PARTS * TI * DEPTH * 2, RIGHT = DEPTH * TJ * 2, STAGE = LEFT + RIGHT, LDS_BYTES = 2 * STAGE;
     static constexpr int PACKS = TI * DEPTH / 8 / THREADS, CHUNKS = (DEPTH * TJ / 16 + THREADS - 1) / THREADS;
     static_assert(PACKS * THREADS * 8 == TI * DEPTH && LDS_BYTES <= 160 * 1024 && TI >= 64 && TJ >= 64, "");
     typedef typename PackOf<T, 8>::type Raw;
@@ -545,15 +561,15 @@ struct GradTile {
     static __device__ __forceinline__ uint32_t left_at(int i, int k)
     {
         if (ALONG) return (uint32_t)(i * 64 + ((k / 8) ^ (-(i >> 2) & 3)) * 16);
-        const int turn = TI >= 128 ? (k & 3) | ((k >> 1) & 4) : ((k >> 1) & 1) | ((k >> 2) & 2);      // of 64 elements two rows lie on all banks together
-        return (uint32_t)(k * TI * 2 + ((i / 16) ^ turn) * 32 + (i % 16) * 2);
+        return across_at<TI>(k, i);
     }
-    // Bytes into the right one, of the chunk of 16 codes from j on of row k.
-    static __device__ __forceinline__ uint32_t right_at(int k, int j)
+    template <int N> static __device__ __forceinline__ uint32_t across_at(int k, int c)
     {
-        constexpr int N = TJ / 16, TURN = TJ >= 256 ? 0 : TJ >= 128 ? 1 : 2;       // rows of less than 256 bytes: several lie on all banks together
-        return (uint32_t)(k * TJ + ((j / 16) ^ ((k >> TURN) & (N < 16 ? N - 1 : 15))) * 16);
+        const int turn = N >= 128 ? (k & 3) | ((k >> 1) & 4) : ((k >> 1) & 1) | ((k >> 2) & 2);       // of 64 numbers two rows lie on all banks together
+        return (uint32_t)(k * N * 2 + ((c / 16) ^ turn) * 32 + (c % 16) * 2);
     }
+    // Bytes into the right one, of (k, j): rows of all columns of the tile.
+    static __device__ __forceinline__ uint32_t right_at(int k, int j) { return across_at<TJ>(k, j); }
 
     // What a thread reads of a step.
     struct Step {
@@ -565,10 +581,11 @@ struct GradTile {
     struct Source {
         const GradArgs &a;
         const uint8_t *dy[PACKS], *scale[ALONG ? 1 : PACKS], *codes[CHUNKS];
-        int32_t i0, j0, k0, k_end;                                 // of the next step
-        bool whole;                                                // rows of i
-        __device__ __forceinline__ Source(const GradArgs &args, int32_t i, int32_t j, int32_t k, int32_t end) : a(args), i0(i), j0(j), k0(k), k_end(end), whole(ALONG || i + TI <= args.n_i)
+        int32_t i0, j0, k0, k_end, k_whole;                        // of the next step; up to where a step's elements may be read whole
+        __device__ __forceinline__ Source(const GradArgs &args, int32_t i, int32_t j, int32_t k, int32_t end) : a(args), i0(i), j0(j), k0(k), k_end(end), k_whole(end)
         {
+            // Beyond the last column of i nothing is made of what is read, which are the next rows' elements.
+            if (!ALONG && i0 + TI > a.n_i) k_whole = a.rows_apart ? min(k_end, a.n_k - 8) : 0;
 #pragma unroll
             for (int p = 0; p < PACKS; ++p) {
                 const int q = p * THREADS + (int)threadIdx.x;
@@ -576,7 +593,8 @@ struct GradTile {
                     dy[p] = reinterpret_cast<const uint8_t *>(row_at<T>(a.dy, a.dy_stride, min(i0 + q / 4, a.n_i - 1)) + k0 + q % 4 * 8);
                 } else {
                     const int32_t row = min(k0 + q / (TI / 8), k_end - 1);
-                    dy[p] = reinterpret_cast<const uint8_t *>(row_at<T>(a.dy, a.dy_stride, row) + i0 + q % (TI / 8) * 8);
+                    const int32_t first = i0 + q % (TI / 8) * 8;
+                    dy[p] = reinterpret_cast<const uint8_t *>(row_at<T>(a.dy, a.dy_stride, row) + (first < a.n_i ? first : 0));
                     scale[p] = a.held + (uint64_t)row * a.held_stride + (a.held_bytes - 4);
                 }
             }
@@ -591,11 +609,11 @@ struct GradTile {
         }
         __device__ __forceinline__ void load(Step &s)
         {
-            if (whole && k0 + DEPTH <= k_end) {
+            if (k0 + DEPTH <= k_whole) {
 #pragma unroll
                 for (int p = 0; p < PACKS; ++p) {
                     s.dy[p] = load_raw<T, 8>(reinterpret_cast<const T *>(dy[p]));
-                    dy[p] += ALONG ? DEPTH * sizeof(T) : DEPTH * a.dy_stride;
+                    dy[p] += ALONG ? (uint64_t)DEPTH * sizeof(T) : DEPTH * a.dy_stride;
                 }
                 if constexpr (ALONG) {
 #pragma unroll
@@ -647,53 +665,73 @@ struct GradTile {
             for (int c = 0; c < CHUNKS; ++c) s.codes[c] = *reinterpret_cast<const i32x4 *>(codes_at(k0, c));
         }
     };
-    static __device__ __forceinline__ void put(const Step &s, uint8_t *stage)
+    static __device__ __forceinline__ void scaled(const Step &s, int p, float (&v)[8])
     {
+        unpack<T, 8>(s.dy[p], v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = rounded(v[e], s.scale[ALONG ? e : p]);
+    }
+    static __device__ __forceinline__ void put_parts(int p, const bf16x8 (&parts)[PARTS], uint8_t *stage)
+    {
+        const int q = p * THREADS + (int)threadIdx.x;
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x)
+            *reinterpret_cast<bf16x8 *>(stage + x * (TI * DEPTH * 2) + left_at(ALONG ? q / 4 : q % (TI / 8) * 8, ALONG ? q % 4 * 8 : q / (TI / 8))) = parts[x];
+    }
+    // A step into LDS, as if all were numbers; what they were is in `most`.  sums: of dy's columns.
+    static __device__ __forceinline__ float put(const Step &s, uint8_t *stage, float (&sums)[8])
+    {
+        float most = 0.f;
 #pragma unroll
         for (int p = 0; p < PACKS; ++p) {
-            const int q = p * THREADS + (int)threadIdx.x;
-            const int i = ALONG ? q / 4 : q % (TI / 8) * 8, k = ALONG ? q % 4 * 8 : q / (TI / 8);
             float v[8];
-            unpack<T, 8>(s.dy[p], v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = rounded(v[e], s.scale[ALONG ? e : p]);
             bf16x8 parts[PARTS];
-            parts_of<PARTS>(v, parts);
+            if constexpr (SUMS) {
+                unpack<T, 8>(s.dy[p], v);
 #pragma unroll
-            for (int x = 0; x < PARTS; ++x) *reinterpret_cast<bf16x8 *>(stage + x * (TI * DEPTH * 2) + left_at(i, k)) = parts[x];
+                for (int e = 0; e < 8; ++e) sums[e] += v[e];
+            }
+            scaled(s, p, v);
+            most = fmaxf(most, parts_of_numbers<PARTS>(v, parts));
+            put_parts(p, parts, stage);
         }
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             const int q = c * THREADS + (int)threadIdx.x;
-            if (DEPTH * TJ / 16 % THREADS == 0 || q < DEPTH * TJ / 16) *reinterpret_cast<i32x4 *>(stage + LEFT + right_at(q / (TJ / 16), q % (TJ / 16) * 16)) = s.codes[c];
+            if (DEPTH * TJ / 16 % THREADS && q >= DEPTH * TJ / 16) continue;
+            bf16x8 *to = reinterpret_cast<bf16x8 *>(stage + LEFT + right_at(q / (TJ / 16), q % (TJ / 16) * 16));
+            to[0] = codes_as_bf16(i32x2{s.codes[c][0], s.codes[c][1]});
+            to[1] = codes_as_bf16(i32x2{s.codes[c][2], s.codes[c][3]});
+        }
+        return most;
+    }
+    // And once more where they were not.
+    static __device__ __forceinline__ void put_any(const Step &s, uint8_t *stage)
+    {
+#pragma unroll
+        for (int p = 0; p < PACKS; ++p) {
+            float v[8];
+            bf16x8 parts[PARTS];
+            scaled(s, p, v);
+            parts_of_any<PARTS>(v, parts);
+            put_parts(p, parts, stage);
         }
     }
 
     // The operand of a matrix operation: 16 rows of i (columns of j), a lane has eight along k.
     static __device__ __forceinline__ bf16x8 left(const uint8_t *part, int i, int lane)
     {
-        if constexpr (ALONG) {
-            return *reinterpret_cast<const bf16x8 *>(part + left_at(i + (lane & 15), (lane >> 4) * 8));
-        } else {
-            typedef short s16x4 __attribute__((ext_vector_type(4)));
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
-            const int k = (lane >> 4) * 8 + ((lane >> 2) & 3), at = i + (lane & 3) * 4;
-            const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(part + left_at(at, k)));
-            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(part + left_at(at, k + 4)));
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
+        if constexpr (ALONG) return *reinterpret_cast<const bf16x8 *>(part + left_at(i + (lane & 15), (lane >> 4) * 8));
+        else return column<TI>(part, i, lane);
     }
-    static __device__ __forceinline__ bf16x8 right(const uint8_t *codes, int j, int lane)
+    static __device__ __forceinline__ bf16x8 right(const uint8_t *part, int j, int lane) { return column<TJ>(part, j, lane); }
+    template <int N> static __device__ __forceinline__ bf16x8 column(const uint8_t *part, int c, int lane)
     {
-        typedef int i32x2 __attribute__((ext_vector_type(2)));
-        const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2 *)(codes + right_at((lane >> 4) * 8 + ((lane & 15) >> 1), j) + (lane & 1) * 8));
-        u32x4 out;
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {                           // whole numbers of seven bits: bf16 is the upper half of fp32
-            const float lo = (float)(int8_t)(c[e / 4] >> (e % 4 * 8)), hi = (float)(int8_t)(c[e / 4] >> (e % 4 * 8 + 8));
-            out[e / 2] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, hi), __builtin_bit_cast(uint32_t, lo), 0x07060302u);
-        }
-        return __builtin_bit_cast(bf16x8, out);
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        const int k = (lane >> 4) * 8 + ((lane >> 2) & 3), at = c + (lane & 3) * 4;
+        const s16x4 u = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(part + across_at<N>(k, at)));
+        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(part + across_at<N>(k + 4, at)));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 
     // Waits until what this wave wrote into LDS is there, and then for every wave.  (Loads stay under way, which __syncthreads would wait for.)
@@ -714,6 +752,8 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
     extern __shared__ __align__(16) uint8_t lds[];
     constexpr int BI = Tile::BI, BJ = Tile::BJ, PARTS = Tile::PARTS, DEPTH = Tile::DEPTH;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t mine = blockIdx.x * Tile::THREADS + threadIdx.x;
+    if (!Tile::ALONG && a.gather && mine < (uint32_t)a.n_gather) a.gathered[mine] = *row_at<float>(a.gather + a.held_bytes - 4, a.gather_stride, mine);
     // Tiles of one row of j follow one another, splits of k of a tile lie apart: what an XCD works on at once shares dy.
     const uint32_t across = ((uint32_t)a.n_j + Tile::TJ - 1) / Tile::TJ, t = tile_of_workgroup();
     const uint32_t tile = t % a.tiles, split = t / a.tiles;
@@ -724,24 +764,25 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
     // Of the two waves of a vector unit one prepares the next step before it multiplies, the other behind it: the one's conversions go beside the other's matrix operations.
     const bool early = wave < 4;
     f32x4 acc[BI][BJ] = {};
+    float sums[8] = {};
     if (k_first < k_end) {
         typename Tile::Step step;
         typename Tile::Source src(a, i0, j0, (int32_t)k_first, k_end);
         const int32_t last = (k_end - 1 - (int32_t)k_first) / DEPTH;
+        const auto prepare = [&](uint8_t *stage) __attribute__((always_inline)) {
+            if (beyond_numbers(Tile::put(step, stage, sums))) Tile::put_any(step, stage);
+            src.load(step);
+        };
         src.load(step);
-        Tile::put(step, lds);
-        src.load(step);
+        prepare(lds);
         Tile::arrive();
         for (int32_t s = 0; s <= last; ++s) {
             const uint8_t *stage = lds + (s & 1) * Tile::STAGE;
-            const auto prepare = [&] {
-                Tile::put(step, lds + (~s & 1) * Tile::STAGE);
-                src.load(step);
-            };
-            if (early && s < last) prepare();
+            uint8_t *other = lds + (~s & 1) * Tile::STAGE;
+            if (early && s < last) prepare(other);
             // The next blocks' elements are on their way out of LDS while one row of blocks is multiplied: left to itself the compiler asks for them when they are needed.
             bf16x8 r[BJ], l[2][PARTS];
-            const auto read = [&](int i, bf16x8 (&to)[PARTS]) {
+            const auto read = [&](int i, bf16x8 (&to)[PARTS]) __attribute__((always_inline)) {
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) to[p] = Tile::left(stage + p * (Tile::TI * DEPTH * 2), wi + i * 16, lane);
             };
@@ -758,8 +799,23 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
                     for (int j = 0; j < BJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[j], l[i & 1][p], acc[i][j], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (!early && s < last) prepare();
+            if (!early && s < last) prepare(other);
             Tile::arrive();
+        }
+    }
+    if constexpr (Tile::SUMS) {
+        // What the threads have of a column, added up in their order.
+        if (a.sums && j0 == 0) {
+            float *parts = reinterpret_cast<float *>(lds);
+            constexpr int PACKS_ACROSS = Tile::TI / 8, GROUPS = Tile::THREADS / PACKS_ACROSS;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) parts[(threadIdx.x / PACKS_ACROSS) * Tile::TI + threadIdx.x % PACKS_ACROSS * 8 + e] = sums[e];
+            __syncthreads();
+            if (threadIdx.x < Tile::TI && i0 + (int32_t)threadIdx.x < a.n_i) {
+                float v = 0.f;
+                for (int g = 0; g < GROUPS; ++g) v += parts[g * Tile::TI + threadIdx.x];
+                a.sums[(int64_t)split * a.n_i + i0 + threadIdx.x] = v;
+            }
         }
     }
 #pragma unroll
@@ -777,6 +833,139 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
     }
 }
 
+// dx of many rows and few outputs, which the tiles do at the pace of their starts and ends: w's codes lie in LDS, once for all rows that a workgroup does (where there is more than that holds, each
+// has a share of the columns), and a wave by itself takes R blocks of 16 rows of dy at a time, parted in registers (the next ones' elements on their way beside them spill).  The codes lie by blocks of 16 columns, row after row: what the
+// lanes read at a time is contiguous.
+struct ThinGradArgs {
+    GradArgs g;
+    int32_t cols;                    // of a workgroup, a multiple of 32
+    int32_t shares;                  // of the columns
+};
+
+template <typename T, int PARTS, int KS, int R>
+__global__ void __launch_bounds__(THIN_THREADS) grad_thin_kernel(ThinGradArgs t)
+{
+    constexpr int V = 16 / sizeof(T), WAVES = THIN_THREADS / 64, K = KS * 32;
+    typedef typename PackOf<T, 8>::type Raw;
+    extern __shared__ __align__(16) uint8_t lds[];
+    const GradArgs &a = t.g;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int32_t j0 = (int32_t)(blockIdx.x % (uint32_t)t.shares) * t.cols, mine = min(t.cols, a.n_j - j0);
+    const int32_t pairs = (mine + 31) / 32, turns = (int32_t)(gridDim.x / (uint32_t)t.shares) * WAVES, n_blocks = (a.n_i + 16 * R - 1) / (16 * R);
+    // Where few blocks are left for a last turn, several waves take one, each a part of the columns.
+    const int32_t number = (int32_t)(blockIdx.x / (uint32_t)t.shares) * WAVES + wave, left_over = n_blocks % turns, parts = left_over ? turns / left_over : 1;
+    const int32_t whole_turns = n_blocks - left_over;
+    int32_t rb = number, from_pair = 0, to_pair = pairs;
+    const auto place = [&] {
+        if (rb < whole_turns) return;
+        if (left_over == 0 || number >= left_over * parts) { rb = n_blocks; return; }
+        const int32_t part = number / left_over;
+        rb = whole_turns + number % left_over;
+        from_pair = part * pairs / parts;
+        to_pair = (part + 1) * pairs / parts;
+    };
+    place();
+    float *scales = reinterpret_cast<float *>(lds + (uint32_t)t.cols * K);
+    const bool even = a.n_k % 32 == 0 && a.n_k == K;
+    Raw next[R][KS];
+    const auto load = [&](int32_t b) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const T *row = row_at<T>(a.dy, a.dy_stride, min((int64_t)b * (16 * R) + i * 16 + (lane & 15), (int64_t)a.n_i - 1));
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int32_t k = s * 32 + (lane >> 4) * 8;
+                if (even || k + 8 <= a.n_k) {
+                    next[i][s] = load_raw<T, 8>(row + k);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) next[i][s][e] = k + e < a.n_k ? row[k + e] : (T)0.f;
+                }
+            }
+        }
+    };
+    load(rb);
+    // Units of 32 columns of a row of w, eight rows by eight units to a wave.  Of results of 16 bits a lane comes to hold eight side by side, four of either block.
+    const int32_t down = (a.n_k + 7) / 8;
+    for (int32_t u = wave; u < down * ((pairs + 7) / 8); u += WAVES) {
+        const int32_t k = u % down * 8 + (lane >> 3), pair = u / down * 8 + (lane & 7);
+        if (k >= a.n_k || pair >= pairs) continue;
+        const uint8_t *row = a.held + (uint64_t)k * a.held_stride;
+        const int32_t at = j0 + pair * 32;
+        const i32x4 u0 = *reinterpret_cast<const i32x4 *>(row + at), u1 = *reinterpret_cast<const i32x4 *>(row + min(at + 16, a.held_bytes - 16));
+        i32x4 *to = reinterpret_cast<i32x4 *>(lds + (uint32_t)(pair * 2) * (K * 16) + k * 16);
+        if constexpr (V == 8) {
+            to[0] = __builtin_shufflevector(u0, u1, 0, 2, 4, 6);
+            to[K] = __builtin_shufflevector(u0, u1, 1, 3, 5, 7);
+        } else {
+            to[0] = u0;
+            to[K] = u1;
+        }
+    }
+    for (int32_t k = threadIdx.x; k < K; k += THIN_THREADS) scales[k] = k < a.n_k ? *row_at<float>(a.held + a.held_bytes - 4, a.held_stride, k) : 0.f;
+    __syncthreads();
+    while (rb < n_blocks) {
+        bf16x8 l[R][KS][PARTS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const f32x4 lo = *reinterpret_cast<const f32x4 *>(scales + s * 32 + (lane >> 4) * 8), hi = *reinterpret_cast<const f32x4 *>(scales + s * 32 + (lane >> 4) * 8 + 4);
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                float v[8];
+                unpack<T, 8>(next[i][s], v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = rounded(v[e], e < 4 ? lo[e] : hi[e - 4]);
+                if (beyond_numbers(parts_of_numbers<PARTS>(v, l[i][s]))) parts_of_any<PARTS>(v, l[i][s]);
+            }
+        }
+        const int32_t i0 = rb * (16 * R) + (lane & 15);
+        for (int32_t pair = from_pair; pair < to_pair; ++pair) {
+            f32x4 acc[R][2] = {};
+            // The next step's codes are on their way out of LDS while one is multiplied, and no more: all at once they spill.
+            const uint8_t *codes = lds + (uint32_t)(pair * 2) * (K * 16) + ((lane >> 4) * 8 + ((lane & 15) >> 1)) * 16 + (lane & 1) * 8;
+            i32x2 now[2] = {column_of_codes(codes), column_of_codes(codes + K * 16)};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bf16x8 r[2] = {codes_as_bf16(now[0]), codes_as_bf16(now[1])};
+                if (s + 1 < KS) {
+                    now[0] = column_of_codes(codes + (s + 1) * 512);
+                    now[1] = column_of_codes(codes + (K * 16) + (s + 1) * 512);
+                }
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int i = 0; i < R; ++i) acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[b], l[i][s][p], acc[i][b], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                if (i0 + i * 16 >= a.n_i) continue;
+                T *row = row_at<T>(a.out, a.out_stride, i0 + i * 16) + j0;
+#pragma unroll
+                for (int k = 0; k < 8; k += V) {
+                    const int32_t j = pair * 32 + k * 4 + (lane >> 4) * V;
+                    float v[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[e] = acc[i][(k + e) / 4][(k + e) % 4];
+                    if (j + V <= mine) {
+                        store_pack<T, V>(row + j, v);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; ++e)
+                            if (j + e < mine) row[j + e] = (T)v[e];
+                    }
+                }
+            }
+        }
+        if (rb >= whole_turns) return;
+        rb += turns;
+        place();
+        if (rb < n_blocks) load(rb);
+    }
+}
+
 // The scales of held rows side by side.
 __global__ void __launch_bounds__(256) scales_kernel(const uint8_t *held, uint64_t stride, int32_t held_bytes, int32_t n, float *scales)
 {
@@ -784,28 +973,49 @@ __global__ void __launch_bounds__(256) scales_kernel(const uint8_t *held, uint64
     if (r < n) scales[r] = *row_at<float>(held + held_bytes - 4, stride, r);
 }
 
-// The splits' sums, added up in their order: four elements of a row to a thread.
-__global__ void __launch_bounds__(256) grad_join_kernel(const float *partial, int32_t splits, int64_t n_i, int64_t n_j, uint8_t *out, uint64_t out_stride, uint32_t type)
+// The splits' sums of a matrix and, in the workgroups behind it, of a vector, added up in a fixed order: four elements of a row to sixteen threads, each of which has every sixteenth
+// split.  (All splits to a thread 27 us for 67 MB of them, so 14.)
+struct Join {
+    const float *partial;            // [splits][n_i][n_j]
+    int32_t splits;
+    int64_t n_i, n_j;
+    uint8_t *out;
+    uint64_t out_stride;
+};
+constexpr int JOIN_GROUPS = 16, JOIN_QUADS = 256 / JOIN_GROUPS;
+inline uint32_t join_grid(const Join &j) { return j.out ? (uint32_t)std::min<int64_t>(8192, (j.n_i * ((j.n_j + 3) / 4) + JOIN_QUADS - 1) / JOIN_QUADS) : 0; }
+__global__ void __launch_bounds__(256) grad_join_kernel(Join first, Join second, uint32_t first_grid, uint32_t type)
 {
-    const int64_t quads = (n_j + 3) / 4;
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n_i * quads; q += (int64_t)gridDim.x * 256) {
-        const int64_t i = q / quads, j = q % quads * 4;
-        const int32_t n = (int32_t)min((int64_t)4, n_j - j);
-        const float *from = partial + i * n_j + j;
+    __shared__ f32x4 sums[JOIN_GROUPS][JOIN_QUADS];
+    const bool one = blockIdx.x < first_grid;
+    const Join &a = one ? first : second;
+    const uint32_t block = one ? blockIdx.x : blockIdx.x - first_grid, grid = one ? first_grid : gridDim.x - first_grid;
+    const int at = threadIdx.x % JOIN_QUADS, group = threadIdx.x / JOIN_QUADS;
+    const int64_t across = (a.n_j + 3) / 4, quads = a.n_i * across;
+    for (int64_t q0 = (int64_t)block * JOIN_QUADS; q0 < quads; q0 += (int64_t)grid * JOIN_QUADS) {
+        const int64_t q = min(q0 + at, quads - 1), i = q / across, j = q % across * 4;
+        const int32_t n = (int32_t)min((int64_t)4, a.n_j - j);
+        const float *from = a.partial + i * a.n_j + j;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
         if (n == 4) {
 #pragma unroll 8
-            for (int32_t s = 0; s < splits; ++s) {
+            for (int32_t s = group; s < a.splits; s += JOIN_GROUPS) {
                 float w[4];
-                load_pack<float, 4>(from + s * n_i * n_j, w);
+                load_pack<float, 4>(from + s * a.n_i * a.n_j, w);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += w[e];
             }
         } else {
-            for (int32_t s = 0; s < splits; ++s)
-                for (int e = 0; e < n; ++e) v[e] += from[s * n_i * n_j + e];
+            for (int32_t s = group; s < a.splits; s += JOIN_GROUPS)
+                for (int e = 0; e < n; ++e) v[e] += from[s * a.n_i * a.n_j + e];
         }
-        uint8_t *row = out + (uint64_t)i * out_stride;
+        __syncthreads();
+        sums[group][at] = v;
+        __syncthreads();
+        if (group || q0 + at >= quads) continue;
+#pragma unroll
+        for (int g = 1; g < JOIN_GROUPS; ++g) v += sums[g][at];
+        uint8_t *row = a.out + (uint64_t)i * a.out_stride;
         if (type == RG_F32) store_four(reinterpret_cast<float *>(row) + j, v, n);
         else if (type == RG_BF16) store_four(reinterpret_cast<bf16 *>(row) + j, v, n);
         else store_four(reinterpret_cast<f16 *>(row) + j, v, n);
@@ -941,44 +1151,29 @@ template <typename T> rg_status launch_product(const ProductArgs &a, hipStream_t
 
 // How the backward pass is cut, and where its scratch lies.
 struct GradPlan {
-    int dx_tile, dw_tile;                // side
-    uint64_t dx_tiles, dw_tiles;
-    int32_t dx_splits, dx_each, dw_splits, dw_each, bias_parts, bias_each;
-    uint64_t scales_at, bias_at, bytes;  // sums of dx, then of dweight in the same place; w's scales; sums of dbias
+    GradCut dx, dw;
+    int32_t bias_parts, bias_each;
+    uint64_t scales_at, bias_at, bytes;  // sums of dweight, then of dx in the same place; w's scales; sums of dbias
 };
 
-void cut(uint64_t n_i, uint64_t n_j, uint64_t n_k, int n_cu, int *side, uint64_t *tiles, int32_t *splits, int32_t *each)
-{
-    const char *e = getenv("RG_G");
-    const uint64_t steps = (n_k + 31) / 32;
-    const auto count = [&](uint64_t s) { return (n_i + s - 1) / s * ((n_j + s - 1) / s); };
-    *side = e ? atoi(e) : 256;
-    *tiles = count((uint64_t)*side);
-    uint64_t n = 1;
-    const uint64_t slots = (uint64_t)n_cu * (*side == 256 ? 1 : *side == 128 ? 2 : 4);
-    if (*tiles && *tiles < slots) n = std::max<uint64_t>(1, std::min(slots / *tiles, steps / 8));
-    const uint64_t per = std::max<uint64_t>(1, (steps + n - 1) / n);
-    *each = (int32_t)(per * 32);
-    *splits = (int32_t)std::max<uint64_t>(1, (steps + per - 1) / per);
-}
-
-GradPlan grad_plan(uint64_t n, uint64_t m, uint64_t d, int n_cu, bool dx, bool dw, bool db)
+GradPlan grad_plan(uint64_t n, uint64_t m, uint64_t d, uint32_t type, int n_cu, bool dx, bool dw, bool db)
 {
     GradPlan p{};
     uint64_t bytes = 0;
+    const int parts = type == RG_F32 ? 3 : 2;
     if (dx) {
-        cut(n, d, m, n_cu, &p.dx_tile, &p.dx_tiles, &p.dx_splits, &p.dx_each);
-        if (p.dx_splits > 1) bytes = std::max(bytes, (uint64_t)p.dx_splits * n * d * 4);
+        p.dx = grad_cut(n, d, m, parts, n_cu, true);
+        if (p.dx.splits > 1) bytes = std::max(bytes, (uint64_t)p.dx.splits * n * d * 4);
     }
     if (dw) {
-        cut(m, d, n, n_cu, &p.dw_tile, &p.dw_tiles, &p.dw_splits, &p.dw_each);
-        if (p.dw_splits > 1) bytes = std::max(bytes, (uint64_t)p.dw_splits * m * d * 4);
+        p.dw = grad_cut(m, d, n, parts, n_cu, false);
+        if (p.dw.splits > 1) bytes = std::max(bytes, (uint64_t)p.dw.splits * m * d * 4);
     }
     p.scales_at = (bytes + 15) / 16 * 16;
-    if (dx) bytes = p.scales_at + m * 4;
+    if (dx && p.dx.way != GradWay::THIN) bytes = p.scales_at + m * 4;
     p.bias_at = (bytes + 15) / 16 * 16;
     if (db) {
-        p.bias_parts = (int32_t)std::max<uint64_t>(1, std::min<uint64_t>(256, n / 64));
+        p.bias_parts = dw ? p.dw.splits : (int32_t)std::max<uint64_t>(1, std::min<uint64_t>(256, n / 64));
         p.bias_each = (int32_t)((n + p.bias_parts - 1) / p.bias_parts);
         bytes = p.bias_at + (uint64_t)p.bias_parts * m * 4;
     }
@@ -988,7 +1183,6 @@ GradPlan grad_plan(uint64_t n, uint64_t m, uint64_t d, int n_cu, bool dx, bool d
 
 template <typename T, typename Tile> rg_status launch_grad(int32_t splits, const GradArgs &g, hipStream_t st)
 {
-    RG_TRY(check_grid((uint64_t)g.tiles * (uint64_t)splits, Tile::THREADS));
     static std::atomic<uint64_t> known{0};
     RG_TRY(allow_lds(grad_kernel<T, Tile>, Tile::LDS_BYTES, known));
     hipLaunchKernelGGL((grad_kernel<T, Tile>), dim3(g.tiles * (uint32_t)splits), dim3(Tile::THREADS), Tile::LDS_BYTES, st, g);
@@ -996,25 +1190,48 @@ template <typename T, typename Tile> rg_status launch_grad(int32_t splits, const
     return RG_OK;
 }
 
-template <typename T, int PARTS, bool ALONG> rg_status launch_grad_by(int side, int32_t splits, const GradArgs &g, hipStream_t st)
+template <typename T, int PARTS, bool ALONG, bool SUMS> rg_status launch_grad_by(const GradCut &c, const GradArgs &g, hipStream_t st)
 {
-    if (side == 256) return launch_grad<T, GradTile<T, PARTS, ALONG, 2, 4, 8, 4>>(splits, g, st);
-    if (side == 128) return launch_grad<T, GradTile<T, PARTS, ALONG, 2, 2, 4, 4>>(splits, g, st);
-    return launch_grad<T, GradTile<T, PARTS, ALONG, 2, 2, 2, 2>>(splits, g, st);
+    switch (c.way) {
+    case GradWay::TILES_256: return launch_grad<T, GradTile<T, PARTS, ALONG, SUMS, 2, 4, 8, 4>>(c.splits, g, st);
+    case GradWay::TILES_128: return launch_grad<T, GradTile<T, PARTS, ALONG, SUMS, 2, 2, 4, 4>>(c.splits, g, st);
+    case GradWay::TILES_64_256: return launch_grad<T, GradTile<T, PARTS, ALONG, SUMS, 1, 4, 4, 4>>(c.splits, g, st);
+    default: return launch_grad<T, GradTile<T, PARTS, ALONG, SUMS, 2, 2, 2, 2>>(c.splits, g, st);
+    }
 }
 
-template <bool ALONG> rg_status launch_grad_of(uint32_t type, int side, int32_t splits, GradArgs g, void *workspace, hipStream_t st)
+template <typename T, int PARTS, int KS, int R> rg_status launch_grad_thin(const GradArgs &g, int n_cu, hipStream_t st)
 {
-    g.partial = splits > 1 ? static_cast<float *>(workspace) : nullptr;
-    if (type == RG_F32) RG_TRY((launch_grad_by<float, 3, ALONG>(side, splits, g, st)));
-    else if (type == RG_BF16) RG_TRY((launch_grad_by<bf16, 2, ALONG>(side, splits, g, st)));
-    else RG_TRY((launch_grad_by<f16, 2, ALONG>(side, splits, g, st)));
-    if (splits > 1) {
-        const int64_t quads = (int64_t)g.n_i * ((g.n_j + 3) / 4);
-        hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)std::min<int64_t>(4096, (quads + 255) / 256)), dim3(256), 0, st, g.partial, splits, (int64_t)g.n_i, (int64_t)g.n_j, g.out,
-                           g.out_stride, g.out_type);
-        RG_HIP(hipGetLastError());
-    }
+    const ThinShape s = grad_thin_shape((uint64_t)g.n_i, (uint64_t)g.n_j, KS * 32, 16 * R, n_cu);
+    static std::atomic<uint64_t> known{0};
+    RG_TRY(allow_lds(grad_thin_kernel<T, PARTS, KS, R>, (int)THIN_LDS, known));
+    hipLaunchKernelGGL((grad_thin_kernel<T, PARTS, KS, R>), dim3(s.grid), dim3(THIN_THREADS), s.lds, st, ThinGradArgs{g, (int32_t)s.outs, (int32_t)s.shares});
+    RG_HIP(hipGetLastError());
+    return RG_OK;
+}
+template <typename T, int PARTS> rg_status launch_grad_thin_of(const GradArgs &g, int n_cu, hipStream_t st)
+{
+    constexpr int R = PARTS == 2 ? 2 : 1;
+    if (g.n_k <= 32) return launch_grad_thin<T, PARTS, 1, R>(g, n_cu, st);
+    if (g.n_k <= 64) return launch_grad_thin<T, PARTS, 2, R>(g, n_cu, st);
+    if (g.n_k <= 128) return launch_grad_thin<T, PARTS, 4, R>(g, n_cu, st);
+    return launch_grad_thin<T, PARTS, GRAD_THIN_OUTS / 32, R>(g, n_cu, st);
+}
+
+template <bool ALONG> rg_status launch_grad_of(uint32_t type, const GradCut &c, const GradArgs &g, hipStream_t st)
+{
+    constexpr bool MAY = !ALONG;
+    if (type == RG_F32) return g.sums ? (launch_grad_by<float, 3, ALONG, MAY>(c, g, st)) : (launch_grad_by<float, 3, ALONG, false>(c, g, st));
+    if (type == RG_BF16) return g.sums ? (launch_grad_by<bf16, 2, ALONG, MAY>(c, g, st)) : (launch_grad_by<bf16, 2, ALONG, false>(c, g, st));
+    return g.sums ? (launch_grad_by<f16, 2, ALONG, MAY>(c, g, st)) : (launch_grad_by<f16, 2, ALONG, false>(c, g, st));
+}
+
+rg_status launch_join(const Join &first, const Join &second, uint32_t type, hipStream_t st)
+{
+    const uint32_t grid = join_grid(first), more = join_grid(second);
+    if (grid + more == 0) return RG_OK;
+    hipLaunchKernelGGL(grad_join_kernel, dim3(grid + more), dim3(256), 0, st, first, second, grid, type);
+    RG_HIP(hipGetLastError());
     return RG_OK;
 }
 
@@ -1063,7 +1280,7 @@ extern "C" rg_status rg_rows8_product_backward_workspace(uint64_t n_rows, uint64
     RG_TRY(check_types("dy", nullptr, RG_F32, type));
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
-    *bytes = grad_plan(n_rows, n_outs, n_cols, n_cu, want_dx, want_dweight, want_dbias).bytes;
+    *bytes = grad_plan(n_rows, n_outs, n_cols, type, n_cu, want_dx, want_dweight, want_dbias).bytes;
     return RG_OK;
 }
 
@@ -1086,43 +1303,56 @@ extern "C" rg_status rg_rows8_product_backward(const void *dy, uint64_t dy_strid
     }
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
-    const GradPlan p = grad_plan(n_rows, n_outs, n_cols, n_cu, dx, dweight, dbias);
+    const GradPlan p = grad_plan(n_rows, n_outs, n_cols, type, n_cu, dx, dweight, dbias);
     RG_TRY(check_workspace(workspace, workspace_bytes, p.bytes));
-    RG_TRY(check_grid(std::max(p.dx_tiles * (uint64_t)std::max(p.dx_splits, 1), p.dw_tiles * (uint64_t)std::max(p.dw_splits, 1)), 512));
+    RG_TRY(check_grid(p.dx.tiles * (uint64_t)p.dx.splits, 512));
+    RG_TRY(check_grid(p.dw.tiles * (uint64_t)p.dw.splits, 512));
     RG_TRY(check_grid((n_outs + 63) / 64, 256));
     const hipStream_t st = as_stream(stream);
-    GradArgs g{};
-    g.dy = static_cast<const uint8_t *>(dy); g.dy_stride = dy_stride;
-    g.n_j = (int32_t)n_cols; g.held_bytes = (int32_t)held_bytes(n_cols);
-    if (dx && n_rows) {
-        g.held = static_cast<const uint8_t *>(w); g.held_stride = w_stride;
-        g.out = static_cast<uint8_t *>(dx); g.out_stride = dx_stride; g.out_type = type;
-        g.n_i = (int32_t)n_rows; g.n_k = (int32_t)n_outs; g.k_each = p.dx_each; g.tiles = (uint32_t)p.dx_tiles;
-        if (n_outs) {
-            float *scales = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.scales_at);
-            hipLaunchKernelGGL(scales_kernel, dim3((uint32_t)((n_outs + 255) / 256)), dim3(256), 0, st, g.held, g.held_stride, g.held_bytes, g.n_k, scales);
-            RG_HIP(hipGetLastError());
-            g.scales = scales;
-        }
-        RG_TRY(launch_grad_of<true>(type, p.dx_tile, p.dx_splits, g, workspace, st));
-    }
+    uint8_t *scratch = static_cast<uint8_t *>(workspace);
+    float *sums = reinterpret_cast<float *>(scratch), *scales = reinterpret_cast<float *>(scratch + p.scales_at), *bias = reinterpret_cast<float *>(scratch + p.bias_at);
+    const bool by_tiles = dx && n_rows && n_outs && p.dx.way != GradWay::THIN;        // which take w's scales side by side
+    GradArgs common{};
+    common.dy = static_cast<const uint8_t *>(dy); common.dy_stride = dy_stride;
+    common.rows_apart = dy_stride >= n_outs * bytes;
+    common.n_j = (int32_t)n_cols; common.held_bytes = (int32_t)held_bytes(n_cols);
+    Join of_weight{}, of_bias{};
+    if (dbias && n_outs) of_bias = Join{bias, p.bias_parts, 1, (int64_t)n_outs, static_cast<uint8_t *>(dbias), 0};
     if (dweight && n_outs) {
+        GradArgs g = common;
         g.held = static_cast<const uint8_t *>(x); g.held_stride = x_stride;
         g.out = static_cast<uint8_t *>(dweight); g.out_stride = dweight_stride; g.out_type = weight_type;
-        g.n_i = (int32_t)n_outs; g.n_k = (int32_t)n_rows; g.k_each = p.dw_each; g.tiles = (uint32_t)p.dw_tiles;
-        RG_TRY(launch_grad_of<false>(type, p.dw_tile, p.dw_splits, g, workspace, st));
-    }
-    if (dbias && n_outs) {
-        float *partial = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.bias_at);
+        g.n_i = (int32_t)n_outs; g.n_k = (int32_t)n_rows; g.k_each = p.dw.each; g.tiles = (uint32_t)p.dw.tiles;
+        g.sums = dbias ? bias : nullptr;
+        if (by_tiles) { g.gather = static_cast<const uint8_t *>(w); g.gather_stride = w_stride; g.gathered = scales; g.n_gather = (int32_t)n_outs; }
+        if (p.dw.splits > 1) { g.partial = sums; of_weight = Join{sums, p.dw.splits, (int64_t)n_outs, (int64_t)n_cols, g.out, g.out_stride}; }
+        RG_TRY(launch_grad_of<false>(type, p.dw, g, st));
+    } else if (of_bias.out) {
         const dim3 grid((uint32_t)((n_outs + 63) / 64), (uint32_t)p.bias_parts);
-        const uint8_t *from = static_cast<const uint8_t *>(dy);
-        if (type == RG_F32) hipLaunchKernelGGL(bias_sums_kernel<float>, grid, dim3(256), 0, st, from, dy_stride, (int32_t)n_rows, (int32_t)n_outs, p.bias_each, partial);
-        else if (type == RG_BF16) hipLaunchKernelGGL(bias_sums_kernel<bf16>, grid, dim3(256), 0, st, from, dy_stride, (int32_t)n_rows, (int32_t)n_outs, p.bias_each, partial);
-        else hipLaunchKernelGGL(bias_sums_kernel<f16>, grid, dim3(256), 0, st, from, dy_stride, (int32_t)n_rows, (int32_t)n_outs, p.bias_each, partial);
+        if (type == RG_F32) hipLaunchKernelGGL(bias_sums_kernel<float>, grid, dim3(256), 0, st, common.dy, dy_stride, (int32_t)n_rows, (int32_t)n_outs, p.bias_each, bias);
+        else if (type == RG_BF16) hipLaunchKernelGGL(bias_sums_kernel<bf16>, grid, dim3(256), 0, st, common.dy, dy_stride, (int32_t)n_rows, (int32_t)n_outs, p.bias_each, bias);
+        else hipLaunchKernelGGL(bias_sums_kernel<f16>, grid, dim3(256), 0, st, common.dy, dy_stride, (int32_t)n_rows, (int32_t)n_outs, p.bias_each, bias);
         RG_HIP(hipGetLastError());
-        hipLaunchKernelGGL(grad_join_kernel, dim3((uint32_t)std::min<uint64_t>(2048, (n_outs + 1023) / 1024)), dim3(256), 0, st, partial, p.bias_parts, (int64_t)1, (int64_t)n_outs,
-                           static_cast<uint8_t *>(dbias), (uint64_t)0, weight_type);
-        RG_HIP(hipGetLastError());
+    }
+    RG_TRY(launch_join(of_weight, of_bias, weight_type, st));
+    if (dx && n_rows) {
+        GradArgs g = common;
+        g.held = static_cast<const uint8_t *>(w); g.held_stride = w_stride;
+        g.out = static_cast<uint8_t *>(dx); g.out_stride = dx_stride; g.out_type = type;
+        g.n_i = (int32_t)n_rows; g.n_k = (int32_t)n_outs; g.k_each = p.dx.each; g.tiles = (uint32_t)p.dx.tiles;
+        g.scales = scales;
+        if (p.dx.way == GradWay::THIN) {
+            if (type == RG_F32) return launch_grad_thin_of<float, 3>(g, n_cu, st);
+            return type == RG_BF16 ? launch_grad_thin_of<bf16, 2>(g, n_cu, st) : launch_grad_thin_of<f16, 2>(g, n_cu, st);
+        }
+        if (by_tiles && !dweight) {
+            hipLaunchKernelGGL(scales_kernel, dim3((uint32_t)((n_outs + 255) / 256)), dim3(256), 0, st, g.held, g.held_stride, g.held_bytes, g.n_k, scales);
+            RG_HIP(hipGetLastError());
+        }
+        Join of_rows{};
+        if (p.dx.splits > 1) { g.partial = sums; of_rows = Join{sums, p.dx.splits, (int64_t)n_rows, (int64_t)n_cols, g.out, g.out_stride}; }
+        RG_TRY(launch_grad_of<true>(type, p.dx, g, st));
+        RG_TRY(launch_join(of_rows, Join{}, type, st));
     }
     return RG_OK;
 }

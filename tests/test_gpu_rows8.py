@@ -311,7 +311,7 @@ def gradient_bounds(dy, qx, sx, qw, sw):
 
 
 GRADIENTS = [(1, 1, 1), (1, 300, 200), (300, 1, 33), (2, 3, 13), (64, 64, 64), (65, 63, 129), (130, 257, 1001), (1000, 41, 602), (33, 700, 28), (256, 256, 256), (5000, 17, 60), (513, 255, 300), (4099, 130, 515),
-             (20_000, 64, 128), (16, 2048, 1024), (300, 3000, 96)]
+             (20_000, 64, 128), (16, 2048, 1024), (300, 3000, 96), (40_000, 47, 256), (33_000, 130, 64), (70_001, 256, 130), (600, 1030, 770)]
 
 
 @pytest.mark.parametrize("n,m,d", GRADIENTS)
@@ -364,6 +364,29 @@ def test_strides_of_the_backward_pass(rg, dtype, n, m, d):
     assert got[0] is out and all(torch.equal(a, b) for a, b in zip(got, want))
     out.fill_(3.0)
     assert bool((buf == 3).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n,m,d", [(300, 70, 100), (5000, 517, 64), (40, 3, 602)])
+def test_gradients_of_a_broadcast(rg, dtype, n, m, d):
+    """One row of dy for all rows: a stride of zero."""
+    x, w = random_held(n, d, 1)[0], random_held(m, d, 2)[0]
+    dy = made(1, m, dtype, 7).expand(n, m)
+    assert dy.stride(0) == 0
+    for a, b in zip(rg.rg_rows8_product_backward(dy, x, w, d), rg.rg_rows8_product_backward(dy.contiguous(), x, w, d)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("n,m,d", [(70, 5, 33), (1000, 70, 100), (3000, 517, 300)])
+def test_nothing_beyond_a_row_counts(rg, dtype, n, m, d):
+    """What lies between dy's rows, and beside codes that a row's end cuts off, is not a number."""
+    x, qx, sx = random_held(n, d, 1)
+    w, qw, sw = random_held(m, d, 2)
+    buf, dy = strided(n, m, dtype, 11, 3, fill=float("nan"))
+    dy.copy_(made(n, m, dtype, 7))
+    for name, got in zip(("dx", "dweight", "dbias"), rg.rg_rows8_product_backward(dy, x, w, d)):
+        check(name, got, gradient_reference(dy, qx, sx, qw, sw)[name], gradient_bounds(dy, qx, sx, qw, sw)[name])
 
 
 @pytest.mark.parametrize("wanted", [(1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1), (0, 1, 1), (0, 0, 0)])

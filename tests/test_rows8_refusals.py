@@ -159,3 +159,40 @@ def test_ways_of_the_product(tmp_path):
             side, threads = {0: (16, 256), 1: (16, 1024), 3: (64, 256), 4: (128, 512), 5: (256, 512)}[way]
             assert -(-n // side) * -(-m // side) * threads < 2**32, (n, m, d)
     assert seen == set(range(6))
+
+
+CUTS = r"""
+#include "rg_launch.h"
+#include <cstdio>
+int main()
+{
+    unsigned long long i, j, k;
+    int parts, cu, along;
+    while (scanf("%llu %llu %llu %d %d %d", &i, &j, &k, &parts, &cu, &along) == 6) {
+        const rg::GradCut c = rg::grad_cut(i, j, k, parts, cu, along != 0);
+        const rg::ThinShape s = c.way == rg::GradWay::THIN ? rg::grad_thin_shape(i, j, k <= 32 ? 32 : k <= 64 ? 64 : k <= 128 ? 128 : 256, parts == 2 ? 32 : 16, cu) : rg::ThinShape{};
+        printf("%d %llu %d %d %u %u %u %u\n", (int)c.way, (unsigned long long)c.tiles, c.splits, c.each, s.outs, s.shares, s.lds, s.grid);
+    }
+}
+"""
+
+
+def test_cuts_of_the_backward_pass(tmp_path):
+    """Every split has a part of the sum and together they have all of it; launches hold the tiles; what the thin way puts into LDS fits and covers the columns."""
+    (tmp_path / "driver.cpp").write_text(CUTS)
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", CSRC, "-o", str(tmp_path / "driver"), str(tmp_path / "driver.cpp")])
+    sizes = [0, 1, 31, 32, 33, 64, 255, 256, 257, 999, 4096, 40_000, 150_000, 2**24, 2**30]
+    cases = [(i, j, k, p, cu, a) for i in sizes for j in (1, 60, 256, 602, 4096, 131_072) for k in sizes for p in (2, 3) for cu in (64, 256) for a in (0, 1) if i * j <= 2**37]
+    out = subprocess.run([str(tmp_path / "driver")], input="\n".join(" ".join(map(str, c)) for c in cases) + "\n", capture_output=True, text=True, check=True).stdout.split("\n")
+    seen = set()
+    for (i, j, k, p, cu, a), line in zip(cases, out):
+        way, tiles, splits, each, outs, shares, lds, grid = map(int, line.split())
+        seen.add(way)
+        if way == 4:
+            assert a and 0 < k <= 256 and outs % 32 == 0 and outs * shares >= j > outs * (shares - 1) and lds <= 160 * 1024 and grid % shares == 0 and grid > 0
+            continue
+        ti, tj = {0: (64, 64), 1: (64, 256), 2: (128, 128), 3: (256, 256)}[way]
+        assert tiles == -(-i // ti) * -(-j // tj) and 1 <= splits and each % 32 == 0 and each > 0
+        assert (splits - 1) * each < max(k, 1) <= splits * each and each < 2**31
+        assert splits == 1 or splits * tiles <= 4 * cu
+    assert seen == set(range(5))
