@@ -750,9 +750,12 @@ def rg_quantize_rows(x, rows=None, out=None, stream=None):
     n_out = n if rows is None else rows.shape[0]
     made = out is None
     if made:
-        out = torch.empty((n_out, (d + 19) // 16 * 16), dtype=torch.uint8, device=device)
-    hp, hs, got = _held("out", out, device, d)
-    assert got == n_out, f"out: expected {n_out} rows, got {got}"
+        hs = (d + 19) // 16 * 16
+        out = torch.empty((n_out, hs), dtype=torch.uint8, device=device)
+        hp = out.data_ptr()
+    else:
+        hp, hs, got = _held("out", out, device, d)
+        assert got == n_out, f"out: expected {n_out} rows, got {got}"
     st = _stream_and_use(device, stream, out if made else None)
     _call(device, lib().rg_quantize_rows, xp, xs, n, d, _ELEMENT[x.dtype], _positions(rows, device), n_out, hp, hs, st)
     if not made:
@@ -768,9 +771,10 @@ def rg_dequantize_rows(held, cols, dtype=torch.float32, rows=None, out=None, str
     made = out is None
     if made:
         out = torch.empty((n_out, cols), dtype=dtype, device=device)
+        op, os_ = out.data_ptr(), cols * dtype.itemsize
     else:
         dtype = out.dtype
-    op, os_ = _rows("out", out, device, (n_out, cols))
+        op, os_ = _rows("out", out, device, (n_out, cols))
     st = _stream_and_use(device, stream, out if made else None)
     _call(device, lib().rg_dequantize_rows, hp, hs, n, cols, _positions(rows, device), n_out, _ELEMENT[dtype], op, os_, st)
     if not made:

@@ -216,25 +216,29 @@ struct HoldShape {
     int packs;                           // of a lane
     uint32_t grid;                       // workgroups; their waves, or they, take rows by turns
 };
+// Lanes to a row, of half a wave up to as many packs a lane as leave fewer idle than a wave does (602 elements, packs of four and eight: 160 and 96 of 192 and 128).
+inline void lanes_of(int64_t need, HoldShape &s)
+{
+    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 * 5 ? 32 : need <= 64 * 4 ? 64 : need <= 256 * 4 ? 256 : need <= 1024 * 4 ? 1024 : 0;
+    s.packs = s.lanes ? (int)((need + s.lanes - 1) / s.lanes) : 0;
+}
 // Rows as they are written: packs over all of a held row's bytes, one code to a byte.
 inline HoldShape hold_shape(int64_t n_out, int64_t n_cols, int element_bytes, int n_cu)
 {
     HoldShape s{16 / element_bytes, 0, 0, 0};
-    const int64_t need = (int64_t)held_bytes((uint64_t)n_cols) / s.pack;
-    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : need <= 64 * 4 ? 64 : need <= 256 * 4 ? 256 : need <= 1024 * 4 ? 1024 : 0;
-    s.packs = s.lanes ? (int)((need + s.lanes - 1) / s.lanes) : 0;
+    lanes_of((int64_t)held_bytes((uint64_t)n_cols) / s.pack, s);
     const int64_t groups = s.lanes == 0 || s.lanes > 64 ? 1 : 256 / s.lanes;
-    s.grid = (uint32_t)std::max<int64_t>(1, std::min((int64_t)n_cu * (s.lanes == 1024 || s.lanes == 0 ? 2 : 8), (n_out + groups - 1) / groups));
+    s.grid = s.lanes == 0 ? grid_for(n_out, 1024) : (uint32_t)std::max<int64_t>(1, std::min((int64_t)n_cu * (s.lanes == 1024 ? 2 : 8), (n_out + groups - 1) / groups));
     return s;
 }
-// Rows as they are read back: single elements where a row has fewer than an access.
+// Rows as they are read back: single elements where a row has fewer than an access; longer ones than a wave's by parts.
 inline HoldShape read_shape(int64_t n_out, int64_t n_cols, int element_bytes, int n_cu)
 {
     HoldShape s{n_cols < 16 / element_bytes ? 1 : 16 / element_bytes, 0, 0, 0};
-    const int64_t need = (n_cols + s.pack - 1) / s.pack;
-    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 ? 32 : need <= 64 * 8 ? 64 : 256;
-    const int64_t groups = 256 / s.lanes;
-    s.grid = (uint32_t)std::max<int64_t>(1, std::min((int64_t)n_cu * 8, (n_out + groups - 1) / groups));
+    lanes_of((n_cols + s.pack - 1) / s.pack, s);
+    if (s.lanes > 64) s.lanes = s.packs = 0;
+    const int64_t groups = s.lanes ? 256 / s.lanes : 1;
+    s.grid = s.lanes ? (uint32_t)std::max<int64_t>(1, std::min((int64_t)n_cu * 8, (n_out + groups - 1) / groups)) : grid_for(n_out * ((n_cols + 1024 * s.pack - 1) / (1024 * s.pack)), 256);
     return s;
 }
 

@@ -103,7 +103,8 @@ int main()
     }
 }
 """
-HOLD_KERNELS = {(8, 1), (16, 1), (32, 1), (64, 1), (64, 2), (64, 3), (64, 4), (256, 2), (256, 3), (256, 4), (1024, 2), (1024, 3), (1024, 4)}
+READ_KERNELS = {(8, 1), (16, 1), (32, 1), (32, 2), (32, 3), (32, 4), (32, 5), (64, 3), (64, 4)}
+HOLD_KERNELS = READ_KERNELS | {(256, 2), (256, 3), (256, 4), (1024, 2), (1024, 3), (1024, 4)}
 
 
 def test_every_width_has_a_kernel_that_holds_it(tmp_path):
@@ -114,9 +115,11 @@ def test_every_width_has_a_kernel_that_holds_it(tmp_path):
     out = subprocess.run([str(tmp_path / "driver")], input="\n".join(" ".join(map(str, c)) for c in cases) + "\n", capture_output=True, text=True, check=True).stdout.split("\n")
     for (rows, cols, element, cu, read), line in zip(cases, out):
         pack, lanes, packs, grid, held = map(int, line.split())
-        assert held == (cols + 19) // 16 * 16 and 1 <= grid <= 8 * cu
+        assert held == (cols + 19) // 16 * 16 and 1 <= grid and (grid <= 8 * cu if lanes else grid * (256 if read else 1024) < 2**32)
         if read:
-            assert pack == (16 // element if cols >= 16 // element else 1) and lanes in (8, 16, 32, 64, 256) and packs == 0
+            assert pack == (16 // element if cols >= 16 // element else 1)
+            assert (lanes, packs) in READ_KERNELS and (packs - 1) * lanes * pack < cols <= packs * lanes * pack if lanes else cols > 256 * pack
+            assert pack > 1 or (lanes, packs) == (8, 1)
         else:
             assert pack == 16 // element and held % pack == 0
             if lanes == 0:
