@@ -22,7 +22,6 @@ struct HoldArgs {
     const int64_t *rows;             // positions in `from`, or NULL: every row in its place
     int64_t n_from, n_out;
     int32_t n_cols, held_bytes;
-    bool past;                       // results past the caches
 };
 
 // The position of output i's row.
@@ -226,26 +225,25 @@ __global__ void __launch_bounds__(1024) quantize_long_rows_kernel(HoldArgs a)
 }
 
 // V codes of a held row at a time.  The last pack of a row is the one that ends at the row's end: it overlaps its predecessor, and both write the same there.
-template <typename T, int V> __device__ __forceinline__ void store_values(T *to, const typename PackOf<int8_t, V>::type &q, float s, bool past)
+// PAST: past the caches.
+template <typename T, int V, bool PAST> __device__ __forceinline__ void store_values(T *to, const typename PackOf<int8_t, V>::type &q, float s)
 {
     typedef typename PackOf<T, V>::type P __attribute__((aligned(alignof(T))));
     float v[V];
     unpack<int8_t, V>(q, v);
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] *= s;
-    if constexpr (V > 1) {
-        if (past) {
-            P raw;
+    if constexpr (PAST && V > 1) {
+        P raw;
 #pragma unroll
-            for (int e = 0; e < V; ++e) raw[e] = (T)v[e];
-            __builtin_nontemporal_store(raw, reinterpret_cast<P *>(to));
-            return;
-        }
+        for (int e = 0; e < V; ++e) raw[e] = (T)v[e];
+        __builtin_nontemporal_store(raw, reinterpret_cast<P *>(to));
+    } else {
+        store_pack<T, V>(to, v);
     }
-    store_pack<T, V>(to, v);
 }
 
-template <typename T, int V, int LANES, int NV>
+template <typename T, int V, int LANES, int NV, bool PAST>
 __global__ void __launch_bounds__(256) dequantize_rows_kernel(HoldArgs a)
 {
     constexpr int GROUPS = 256 / LANES;
@@ -281,13 +279,13 @@ __global__ void __launch_bounds__(256) dequantize_rows_kernel(HoldArgs a)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int32_t at = (j * LANES + lane) * V;
-            if (at < a.n_cols) store_values<T, V>(to + min(at, a.n_cols - V), now[j], s, a.past);
+            if (at < a.n_cols) store_values<T, V, PAST>(to + min(at, a.n_cols - V), now[j], s);
         }
     }
 }
 
 // Long rows, by parts of four packs a thread.
-template <typename T, int V>
+template <typename T, int V, bool PAST>
 __global__ void __launch_bounds__(256) dequantize_long_rows_kernel(HoldArgs a)
 {
     typedef typename PackOf<int8_t, V>::type Codes;
@@ -308,7 +306,7 @@ __global__ void __launch_bounds__(256) dequantize_long_rows_kernel(HoldArgs a)
         }
 #pragma unroll
         for (int j = 0; j < PACKS; ++j)
-            if (at + j * 256 * V < a.n_cols) store_values<T, V>(to + min(at + j * 256 * V, a.n_cols - V), q[j], s, a.past);
+            if (at + j * 256 * V < a.n_cols) store_values<T, V, PAST>(to + min(at + j * 256 * V, a.n_cols - V), q[j], s);
     }
 }
 
@@ -341,29 +339,34 @@ template <typename T> bool launch_quantize_of(const HoldShape &s, const HoldArgs
     return false;
 }
 
-template <typename T, int V, int LANES, int NV> bool launch_dequantize(const HoldShape &s, const HoldArgs &a, hipStream_t st)
+template <typename T, int V, int LANES, int NV, bool PAST> bool launch_dequantize(const HoldShape &s, const HoldArgs &a, hipStream_t st)
 {
-    hipLaunchKernelGGL((dequantize_rows_kernel<T, V, LANES, NV>), dim3(s.grid), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((dequantize_rows_kernel<T, V, LANES, NV, PAST>), dim3(s.grid), dim3(256), 0, st, a);
     return true;
 }
 
-template <typename T> bool launch_dequantize_of(const HoldShape &s, const HoldArgs &a, hipStream_t st)
+template <typename T, bool PAST> bool launch_dequantize_of(const HoldShape &s, const HoldArgs &a, hipStream_t st)
 {
     constexpr int V = 16 / sizeof(T);
-    if (s.pack == 1) return launch_dequantize<T, 1, 8, 1>(s, a, st);
+    if (s.pack == 1) return launch_dequantize<T, 1, 8, 1, false>(s, a, st);
     switch (s.lanes * 16 + s.packs) {
-    case 0: hipLaunchKernelGGL((dequantize_long_rows_kernel<T, V>), dim3(s.grid), dim3(256), 0, st, a); return true;
-    case 8 * 16 + 1: return launch_dequantize<T, V, 8, 1>(s, a, st);
-    case 16 * 16 + 1: return launch_dequantize<T, V, 16, 1>(s, a, st);
-    case 32 * 16 + 1: return launch_dequantize<T, V, 32, 1>(s, a, st);
-    case 32 * 16 + 2: return launch_dequantize<T, V, 32, 2>(s, a, st);
-    case 32 * 16 + 3: return launch_dequantize<T, V, 32, 3>(s, a, st);
-    case 32 * 16 + 4: return launch_dequantize<T, V, 32, 4>(s, a, st);
-    case 32 * 16 + 5: return launch_dequantize<T, V, 32, 5>(s, a, st);
-    case 64 * 16 + 3: return launch_dequantize<T, V, 64, 3>(s, a, st);
-    case 64 * 16 + 4: return launch_dequantize<T, V, 64, 4>(s, a, st);
+    case 0: hipLaunchKernelGGL((dequantize_long_rows_kernel<T, V, PAST>), dim3(s.grid), dim3(256), 0, st, a); return true;
+    case 8 * 16 + 1: return launch_dequantize<T, V, 8, 1, PAST>(s, a, st);
+    case 16 * 16 + 1: return launch_dequantize<T, V, 16, 1, PAST>(s, a, st);
+    case 32 * 16 + 1: return launch_dequantize<T, V, 32, 1, PAST>(s, a, st);
+    case 32 * 16 + 2: return launch_dequantize<T, V, 32, 2, PAST>(s, a, st);
+    case 32 * 16 + 3: return launch_dequantize<T, V, 32, 3, PAST>(s, a, st);
+    case 32 * 16 + 4: return launch_dequantize<T, V, 32, 4, PAST>(s, a, st);
+    case 32 * 16 + 5: return launch_dequantize<T, V, 32, 5, PAST>(s, a, st);
+    case 64 * 16 + 3: return launch_dequantize<T, V, 64, 3, PAST>(s, a, st);
+    case 64 * 16 + 4: return launch_dequantize<T, V, 64, 4, PAST>(s, a, st);
     }
     return false;
+}
+
+template <typename T> bool launch_dequantize_as(bool past, const HoldShape &s, const HoldArgs &a, hipStream_t st)
+{
+    return past ? launch_dequantize_of<T, true>(s, a, st) : launch_dequantize_of<T, false>(s, a, st);
 }
 
 rg_status check_hold(uint64_t n_rows, uint64_t n_cols, uint32_t type, const int64_t *rows, uint64_t n_out)
@@ -452,13 +455,13 @@ extern "C" rg_status rg_dequantize_rows(const void *held, uint64_t held_stride, 
     if (n_out == 0) return RG_OK;
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
-    HoldArgs a = hold_args(held, held_stride, n_rows, rows, n_out, n_cols, out, out_stride);
+    const HoldArgs a = hold_args(held, held_stride, n_rows, rows, n_out, n_cols, out, out_stride);
     // Results that fill more than half of the caches (256 MB) are read from memory by whoever takes them, and go there faster past them (199,000 x 602, us: fp32 164, past
     // them 142; bf16 picked by positions 90 and 84; 700 x 131,072 fp32 83 and 68).
-    a.past = n_out * n_cols * bytes > 128ull << 20;
+    const bool past = n_out * n_cols * bytes > 128ull << 20;
     const HoldShape s = read_shape((int64_t)n_out, (int64_t)n_cols, (int)bytes, n_cu);
     const hipStream_t st = as_stream(stream);
-    const bool found = type == RG_F32 ? launch_dequantize_of<float>(s, a, st) : type == RG_BF16 ? launch_dequantize_of<bf16>(s, a, st) : launch_dequantize_of<f16>(s, a, st);
+    const bool found = type == RG_F32 ? launch_dequantize_as<float>(past, s, a, st) : type == RG_BF16 ? launch_dequantize_as<bf16>(past, s, a, st) : launch_dequantize_as<f16>(past, s, a, st);
     if (!found) { set_error("no kernel for rows of %llu elements", (unsigned long long)n_cols); return RG_EHIP; }
     RG_HIP(hipGetLastError());
     return RG_OK;
