@@ -1,11 +1,14 @@
 """A small GraphSAGE trainer on the data path (Sec. 4 par. (8); Eq. 1): node classification on a synthetic graph, every
 step from a batch's gathered feature block and its computation blocks to new weights.
 
-    python -m paper_2509_05207_amd.train --workload tiny --epochs 4
+    python -m paper_2509_05207_amd.train --workload tiny --epochs 4 [--rows8]
 
 The schedule, the cache, the blocks and the feature rows come from the library, and so do the layers' norms with their gradients
 (rg_layer_norm, on the gathered rows as they are, padding and all) and the weights' update (rg_muon_step, all matrices in
-one call).  Means over neighbours, products and the loss are torch's."""
+one call).  Means over neighbours, products and the loss are torch's.
+
+--rows8: features are held in 8 bits in the store, and come through the cache and the gather so (rg_quantize_rows, rg_dequantize_rows), and the layers' products
+are those of held rows and held weights (rg_rows8_product), whose backward pass has nothing but the held rows of the forward pass (rg_rows8_product_backward)."""
 import argparse
 import sys
 import time
@@ -34,6 +37,30 @@ def layer_norm(rg, eps=1e-5):
     return Norm.apply
 
 
+def linear8(rg):
+    """x w^T of rows and weights held in 8 bits, as a function that torch can differentiate, once: gradients are those of what the held rows stand for, and the rounding to codes
+    counts as the identity.  Only the held rows are kept for the backward pass."""
+    class Linear(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight):
+            held, held_weight = rg.rg_quantize_rows(x), rg.rg_quantize_rows(weight)
+            ctx.save_for_backward(held, held_weight)
+            ctx.cols, ctx.weight_dtype = x.shape[1], weight.dtype
+            return rg.rg_rows8_product(held, held_weight, ctx.cols, dtype=x.dtype)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dy):
+            held, held_weight = ctx.saved_tensors
+            dx, dweight = ctx.needs_input_grad
+            return rg.rg_rows8_product_backward(dy.contiguous(), held, held_weight, ctx.cols, want_dx=dx, want_dweight=dweight, want_dbias=False, weight_dtype=ctx.weight_dtype)[:2]
+    return Linear.apply
+
+
+def plain_linear(x, weight):
+    return x @ weight.t()
+
+
 class Sage:
     """L layers h_v <- W [h_v, mean of the sampled neighbours' h], each on normed rows; relu between them."""
 
@@ -44,14 +71,14 @@ class Sage:
         self.scales = [torch.ones(i, device=device).requires_grad_() for i in dims[:-1]]
         self.shifts = [torch.zeros(i, device=device).requires_grad_() for i in dims[:-1]]
 
-    def forward(self, norm, rows, blocks):
-        """rows: the batch's feature block; blocks: outermost hop first, (destinations, each edge's destination, each edge's source)."""
+    def forward(self, norm, rows, blocks, linear=plain_linear):
+        """rows: the batch's feature block; blocks: outermost hop first, (destinations, each edge's destination, each edge's source); linear: a layer's product."""
         h = rows
         for k, (n_dst, dst, src) in enumerate(blocks):
             h = norm(h, self.scales[k], self.shifts[k])
             near = torch.zeros((n_dst, h.shape[1]), dtype=torch.float32, device=h.device).index_add(0, dst, h[src].float())
             degree = torch.bincount(dst, minlength=n_dst).clamp(min=1)
-            h = torch.cat([h[:n_dst], (near / degree[:, None]).to(h.dtype)], dim=1) @ self.weights[k].t()
+            h = linear(torch.cat([h[:n_dst], (near / degree[:, None]).to(h.dtype)], dim=1), self.weights[k])
             if k + 1 < len(blocks):
                 h = torch.relu(h)
         return h
@@ -75,14 +102,26 @@ class Muon:
             p.grad = None
 
 
-class Batches:
-    """The batches of one epoch: feature rows, computation blocks and seeds."""
+def held_tables(rg, W):
+    """The feature tables held in 8 bits, where they were: local rows on the device, remote ones there or in pinned host memory."""
+    tables = []
+    for table in (W.local_rows, W.remote_rows):
+        held = rg.rg_quantize_rows(table[:, : W.cfg.feat_dim])
+        tables.append(held if table.is_cuda else held.cpu().pin_memory())
+    return tables
 
-    def __init__(self, rg, W, epoch=0):
+
+class Batches:
+    """The batches of one epoch: feature rows, computation blocks and seeds.  held: the feature tables held in 8 bits (held_tables), to be gathered as they are and read back."""
+
+    def __init__(self, rg, W, epoch=0, held=None):
         cfg = W.cfg
-        self.rg, self.W = rg, W
+        self.rg, self.W, self.held = rg, W, held
         self.schedule = rg.rg_build_schedule(W.indptr, W.indices, W.train, cfg.batch_size, cfg.fanout, cfg.s0, cfg.worker, cfg.epoch + epoch)
-        self.features = rg.make_features(W.is_local, W.row_of, W.local_rows, W.remote_rows, W.row_bytes)
+        if held is None:
+            self.features = rg.make_features(W.is_local, W.row_of, W.local_rows, W.remote_rows, W.row_bytes)
+        else:
+            self.features = rg.make_features(W.is_local, W.row_of, *held, rg.rg_rows8_bytes(cfg.feat_dim))
         self.cache = rg.rg_build_cache([self.schedule], self.features, W.K)
         rg.rg_schedule_build_blocks(self.schedule)
         s = self.schedule
@@ -93,14 +132,24 @@ class Batches:
     def __len__(self):
         return self.schedule.n_batches
 
-    def rows(self, b):
-        """The batch's feature block: a matrix over the padded rows that the gather leaves."""
-        dtype, stride = self.W.local_rows.dtype, self.W.stride_bytes
+    def gathered(self, b):
+        """The batch's rows as the gather leaves them: a matrix over padded rows, or held rows."""
+        if self.held is None:
+            dtype, stride = self.W.local_rows.dtype, self.W.stride_bytes
+        else:
+            dtype, stride = torch.uint8, self.rg.rg_rows8_bytes(self.W.cfg.feat_dim)
         off = self.ids[-1][2]
         n = int(off[b + 1] - off[b])
         block = torch.empty((n, stride // dtype.itemsize), dtype=dtype, device="cuda")
         self.rg.rg_gather_batch(self.schedule, self.cache, self.features, b, block, out_stride=stride, out_capacity_rows=n, want_stats=False)
-        return block[:, : self.W.cfg.feat_dim]
+        return block
+
+    def rows(self, b):
+        """The batch's feature block."""
+        block = self.gathered(b)
+        if self.held is None:
+            return block[:, : self.W.cfg.feat_dim]
+        return self.rg.rg_dequantize_rows(block, self.W.cfg.feat_dim, dtype=self.W.local_rows.dtype)
 
     def blocks(self, b):
         out = []
@@ -129,11 +178,11 @@ def labels_of(W, n_classes, seed=1):
     return out
 
 
-def train_epoch(rg, batches, model, optimiser, labels, norm):
+def train_epoch(rg, batches, model, optimiser, labels, norm, linear=plain_linear):
     """One pass; the losses of its batches."""
     losses = []
     for b in range(len(batches)):
-        out = model.forward(norm, batches.rows(b), batches.blocks(b))
+        out = model.forward(norm, batches.rows(b), batches.blocks(b), linear)
         loss = torch.nn.functional.cross_entropy(out.float(), labels[batches.seeds(b)])
         loss.backward()
         optimiser.step()
@@ -147,6 +196,7 @@ def main():
     ap.add_argument("--epochs", type=int, default=4)
     ap.add_argument("--hidden", type=int, default=256)
     ap.add_argument("--classes", type=int, default=16)
+    ap.add_argument("--rows8", action="store_true", help="features held in 8 bits, layers' products in 8-bit integers")
     args = ap.parse_args()
     if not torch.cuda.is_available():
         sys.exit("train: no GPU visible; the HIP path has no CPU fallback")
@@ -155,9 +205,10 @@ def main():
     W = synth.make_workload(args.workload, device="cuda", feature_device="cuda", remote_device="cuda")
     model = Sage(W.cfg.feat_dim, args.hidden, args.classes, len(W.cfg.fanout), W.local_rows.dtype)
     optimiser, norm, labels = Muon(rg, model), layer_norm(rg), labels_of(W, args.classes)
+    held, linear = (held_tables(rg, W), linear8(rg)) if args.rows8 else (None, plain_linear)
     for epoch in range(args.epochs):
         t0 = time.perf_counter()
-        losses = train_epoch(rg, Batches(rg, W, epoch), model, optimiser, labels, norm)
+        losses = train_epoch(rg, Batches(rg, W, epoch, held), model, optimiser, labels, norm, linear)
         print(f"epoch {epoch}: loss {losses[0]:.3f} -> {losses[-1]:.3f}, {len(losses)} batches, {time.perf_counter() - t0:.2f} s", flush=True)
 
 
