@@ -565,14 +565,15 @@ rg_status rg_dequantize_rows(const void *held, uint64_t held_stride, uint64_t n_
 /*
  * rg_rows8_product -- y = x w^T + bias of held rows x [n_rows] and held weights w [n_outs], a scale for each row of either:
  *     y[n][m] = s_x[n] * s_w[m] * (sum over c of code_x[n][c] * code_w[m][c]) + bias[m].
- * The sum is exact, and what follows is in 64 bits.  A row with a scale of NaN makes its results NaN.
+ * The sum is exact.  Results of RG_F32 are off by their own rounding and a few units of 2^-47 of the product; for 16 bits the sum and the scales' product are rounded to fp32 first.  A row
+ * with a scale of NaN makes its results NaN.
  *
  *   bias         dev, [n_outs] of bias_type (RG_F32, or the same as `type`), or NULL
  *   y            dev, [n_rows][n_outs] of `type`
- *   workspace    dev, 16-byte aligned, as many bytes as rg_rows8_product_workspace says (often none; then it may be NULL)
- * n_rows, n_outs <= 2^30, either may be 0; RG_ERANGE where a launch cannot hold the result's tiles (beyond 2^37 results).
+ *   workspace    dev, 16-byte aligned, as many bytes as rg_rows8_product_workspace says for the same sizes and type of y (often none; then it may be NULL)
+ * n_rows, n_outs <= 2^30, either may be 0; strides of x and w below 2^24; RG_ERANGE where a launch cannot hold the result's tiles (beyond 2^37 results).  y overlaps no input.
  */
-rg_status rg_rows8_product_workspace(uint64_t n_rows, uint64_t n_outs, uint64_t n_cols, uint64_t *bytes);
+rg_status rg_rows8_product_workspace(uint64_t n_rows, uint64_t n_outs, uint64_t n_cols, uint32_t type, uint64_t *bytes);
 rg_status rg_rows8_product(const void *x, uint64_t x_stride, uint64_t n_rows, const void *w, uint64_t w_stride, uint64_t n_outs, uint64_t n_cols,
                            const void *bias, uint32_t bias_type, void *y, uint64_t y_stride, uint32_t type,
                            void *workspace, uint64_t workspace_bytes, void *stream);
@@ -588,7 +589,7 @@ rg_status rg_rows8_product(const void *x, uint64_t x_stride, uint64_t n_rows, co
  *   dweight      dev, [n_outs][n_cols] of weight_type (RG_F32, or the same as `type`), or NULL (then x may be NULL)
  *   dbias        dev, [n_outs] of weight_type, or NULL
  *   workspace    dev, 16-byte aligned, as many bytes as rg_rows8_product_backward_workspace says for the same sizes and the same results wanted
- * n_rows, n_outs <= 2^30, either may be 0: sums of nothing are zero.
+ * n_rows, n_outs <= 2^30, either may be 0: sums of nothing are zero.  Results overlap neither the inputs nor one another.
  */
 rg_status rg_rows8_product_backward_workspace(uint64_t n_rows, uint64_t n_outs, uint64_t n_cols, uint32_t type, int want_dx, int want_dweight, int want_dbias,
                                               uint64_t *bytes);

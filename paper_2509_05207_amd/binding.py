@@ -134,7 +134,7 @@ def lib():
         L.rg_rows8_bytes.argtypes = [u64, P(u64)]
         L.rg_quantize_rows.argtypes = [vp, u64, u64, u64, u32, vp, u64, vp, u64, vp]
         L.rg_dequantize_rows.argtypes = [vp, u64, u64, u64, vp, u64, u32, vp, u64, vp]
-        L.rg_rows8_product_workspace.argtypes = [u64, u64, u64, P(u64)]
+        L.rg_rows8_product_workspace.argtypes = [u64, u64, u64, u32, P(u64)]
         L.rg_rows8_product.argtypes = [vp, u64, u64, vp, u64, u64, u64, vp, u32, vp, u64, u32, vp, u64, vp]
         L.rg_rows8_product_backward_workspace.argtypes = [u64, u64, u64, u32, C.c_int, C.c_int, C.c_int, P(u64)]
         L.rg_rows8_product_backward.argtypes = [vp, u64, vp, u64, vp, u64, u64, u64, u64, u32, vp, u64, vp, u64, vp, u32, vp, u64, vp]
@@ -782,10 +782,10 @@ def rg_dequantize_rows(held, cols, dtype=torch.float32, rows=None, out=None, str
     return out
 
 
-def rg_rows8_product_workspace(n_rows, n_outs, cols):
-    """Bytes of scratch that the product takes."""
+def rg_rows8_product_workspace(n_rows, n_outs, cols, dtype=torch.float32):
+    """Bytes of scratch that the product takes; dtype: of its result."""
     b = C.c_uint64()
-    _check(lib().rg_rows8_product_workspace(int(n_rows), int(n_outs), int(cols), C.byref(b)))
+    _check(lib().rg_rows8_product_workspace(int(n_rows), int(n_outs), int(cols), _ELEMENT[dtype], C.byref(b)))
     return b.value
 
 
@@ -805,7 +805,7 @@ def rg_rows8_product(x, w, cols, bias=None, dtype=torch.float32, out=None, works
     bt = dtype if bias is None else bias.dtype
     bp = _vector("bias", bias, device, m, bt)
     if workspace is None:
-        workspace = mine = _made_scratch(device, lib().rg_rows8_product_workspace, n, m, cols)
+        workspace = mine = _made_scratch(device, lib().rg_rows8_product_workspace, n, m, cols, _ELEMENT[dtype])
     sp, sb = (None, 0) if workspace is None else _scratch(workspace, device)
     st = _stream_and_use(device, stream, out if made else None, mine)
     _call(device, lib().rg_rows8_product, xp, xs, n, wp, ws, m, cols, bp, _ELEMENT[bt], yp, ys, _ELEMENT[dtype], sp, sb, st)

@@ -259,30 +259,52 @@ inline ThinShape thin_shape(uint64_t n, uint64_t m, uint64_t d, int n_cu)
     s.grid = (uint32_t)std::min((n + rows - 1) / rows, std::max<uint64_t>(1, at_once / s.shares)) * s.shares;
     return s;
 }
-enum class ProductWay { FEW, FEW_LONG, THIN, TILES_64, TILES_128, TILES_256 };
-// The way that is done first, in us by what each takes (measured on 1 to 150,000 rows of 64 to 8,192 codes, 47 to 4,096 outputs in bf16; 64 x 4,096 to 4,096
-// takes 17.0 so and 14.8 in tiles of 64, 10,000 x 64 to 4,096 33 and 32, 150,000 x 602 to 47 29.7 and 28.8).  FEW: a launch, and workgroups of 16 x 16 by their steps of 64 codes.  Tiles: a tile alone on its compute unit,
-// or as many as the fullest has, by their starts and ends and their steps of 128.  THIN: w's way into LDS, then the rows' and results' bytes, or a wave's blocks one after the other.
-inline ProductWay product_way(uint64_t n, uint64_t m, uint64_t d, uint64_t element_bytes, int n_cu)
+enum class ProductWay { FEW, FEW_LONG, THIN, TILES_64, TILES_128, TILES_128_DEEP, TILES_256 };
+struct ProductCut {
+    ProductWay way;
+    int32_t splits, each;                 // of the codes, for tiles, and steps of 128 of a split
+};
+// The way that is done first, in us by what each takes (measured on 1 to 150,000 rows of 64 to 8,192 codes, 47 to 4,096 outputs in bf16).  FEW: a launch, and
+// workgroups of 16 x 16 by their steps of 64 codes.  Tiles: one alone on its compute unit, or as many as the fullest has, by their starts and ends and their
+// steps of 128; splits of the codes write their sums, and another launch adds them up (300 x 8,192 to 1,000: 24.9 whole and 17.2 in three; 1,000 rows of
+// them 24.9 and 34.8).  Four stages in LDS hide more of a step's way than two and leave a compute unit one tile (4,000 x 8,192 to 1,000: 63.1 by two and 47.4 by four; 4,000 x 4,096 to
+// 4,096: 93.0 and 103.9).  THIN: w's way into LDS, then the rows' and results' bytes, or a wave's blocks one after the other.
+inline ProductCut product_cut(uint64_t n, uint64_t m, uint64_t d, uint64_t element_bytes, int n_cu)
 {
-    const double cu = (double)n_cu, steps = (double)((d + 127) / 128);
-    const auto tiles = [&](uint64_t side) { return (double)((n + side - 1) / side) * (double)((m + side - 1) / side); };
-    const auto fullest = [&](uint64_t side) { return (double)(uint64_t)((tiles(side) + cu - 1) / cu); };
-    double best = std::max(10 + 1.75 * steps, 4 + fullest(256) * (9 + 2.08 * steps));
-    ProductWay way = ProductWay::TILES_256;
-    const auto offer = [&](ProductWay other, double us, double work_items = 0) {
-        if (us < best && work_items <= (double)MAX_WORK_ITEMS) { best = us; way = other; }
+    struct Cost { ProductWay way; uint64_t side, threads; double alone, alone_step, base, start, step; };
+    static constexpr Cost COSTS[] = {{ProductWay::TILES_256, 256, 512, 10, 1.75, 4, 9, 2.08},
+                                     {ProductWay::TILES_128, 128, 512, 5.2, 0.65, 3.5, 2.7, 0.69},
+                                     {ProductWay::TILES_128_DEEP, 128, 512, 5.9, 0.58, 0, 0, 0},
+                                     {ProductWay::TILES_64, 64, 256, 4.3, 0.32, 3.5, 0.84, 0.29}};
+    const uint64_t steps = (d + 127) / 128, units = (uint64_t)n_cu;
+    const double cu = (double)n_cu;
+    const auto tiles = [&](uint64_t side) { return (n + side - 1) / side * ((m + side - 1) / side); };
+    ProductCut best{ProductWay::TILES_256, 1, (int32_t)steps};
+    if (n == 0 || m == 0) return best;                             // nothing is launched
+    double least = -1;
+    const auto offer = [&](ProductWay way, uint64_t splits, uint64_t each, double us, uint64_t work_items) {
+        if (work_items > MAX_WORK_ITEMS && way != ProductWay::TILES_256) return;
+        if (least < 0 || us < least) { least = us; best = ProductCut{way, (int32_t)splits, (int32_t)each}; }
     };
-    offer(ProductWay::TILES_128, std::max(5.5 + 0.93 * steps, 3.5 + fullest(128) * (2.7 + 0.69 * steps)), tiles(128) * 512);
-    offer(ProductWay::TILES_64, std::max(4.3 + 0.43 * steps, 3.5 + fullest(64) * (0.84 + 0.26 * steps)), tiles(64) * 256);
-    offer(steps >= 16 && tiles(16) <= 4 * cu ? ProductWay::FEW_LONG : ProductWay::FEW, 3.3 + tiles(16) / cu * (0.15 + 0.085 * steps) + 0.02 * steps, tiles(16) * 256);
+    for (const Cost &c : COSTS) {
+        const uint64_t all = tiles(c.side);
+        for (uint64_t want = 1; want <= std::min<uint64_t>(64, std::max<uint64_t>(steps / 4, 1)); want += std::max<uint64_t>(1, want / 4)) {
+            const uint64_t each = (steps + want - 1) / want, splits = (steps + each - 1) / each, fullest = (all * splits + units - 1) / units;
+            if (splits > 1 && fullest > 4) break;
+            if (fullest > 1 && c.way == ProductWay::TILES_128_DEEP) break;
+            double us = std::max(c.alone + c.alone_step * (double)each, c.base + (double)fullest * (c.start + c.step * (double)each));
+            if (splits > 1) us += 3.5 + (double)(splits * n * m) * 8 / 2.85e6 * 256 / cu;
+            offer(c.way, splits, each, us, all * splits * c.threads);
+        }
+    }
+    offer(steps >= 16 && tiles(16) <= 4 * units ? ProductWay::FEW_LONG : ProductWay::FEW, 1, steps, 3.3 + (double)tiles(16) / cu * (0.15 + 0.085 * (double)steps) + 0.02 * (double)steps, tiles(16) * 256);
     if (d <= THIN_COLS && m <= 1ull << 16) {
         const ThinShape s = thin_shape(n, m, d, n_cu);
         const double blocks = (double)((n + 15) / 16), waves = (double)(s.grid / s.shares) * (THIN_THREADS / 64);
         const double bytes = (double)n * ((double)s.shares * (double)(d + 4) + (double)(m * element_bytes));
-        offer(ProductWay::THIN, 4 + 0.03 * (double)s.lds / 1024 + std::max(1.25 * bytes / 5.1e6 * 256 / cu, 0.3 * (double)(uint64_t)((blocks + waves - 1) / waves) * (double)(s.outs / 32)));
+        offer(ProductWay::THIN, 1, steps, 4 + 0.03 * (double)s.lds / 1024 + std::max(1.25 * bytes / 5.1e6 * 256 / cu, 0.3 * (double)(uint64_t)((blocks + waves - 1) / waves) * (double)(s.outs / 32)), 0);
     }
-    return way;
+    return best;
 }
 
 // The backward pass' products: sums over n_k of n_i x n_j, in `parts` bf16 numbers.

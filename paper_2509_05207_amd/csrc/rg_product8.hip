@@ -18,6 +18,19 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 template <typename T> __device__ __forceinline__ T *row_at(void *p, uint64_t stride, int64_t r) { return reinterpret_cast<T *>(static_cast<uint8_t *>(p) + (uint64_t)r * stride); }
 template <typename T> __device__ __forceinline__ const T *row_at(const void *p, uint64_t stride, int64_t r) { return reinterpret_cast<const T *>(static_cast<const uint8_t *>(p) + (uint64_t)r * stride); }
 
+// Four results side by side, of which n are inside.
+template <typename O> __device__ __forceinline__ void store_four(O *p, const f32x4 &v, int32_t n)
+{
+    if (n >= 4) {
+        const float w[4] = {v[0], v[1], v[2], v[3]};
+        store_pack<O, 4>(p, w);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) p[e] = (O)v[e];
+    }
+}
+
 // ---------------------------------------------------------------- y = x w^T + bias
 struct ProductArgs {
     const uint8_t *x, *w;
@@ -27,6 +40,9 @@ struct ProductArgs {
     uint8_t *y;
     uint64_t y_stride;
     int32_t n_rows, n_outs, n_cols, held_bytes;
+    int32_t *partial;                // [splits][n_rows][n_outs], or NULL: a sum is done by one workgroup
+    int32_t each;                    // steps of 128 codes of a split
+    uint32_t tiles;
 };
 
 // A chunk of 16 bytes with codes in it may have the scale's four behind them: where that is so, the scales' own bytes have gone into a sum, and are taken off again.
@@ -139,23 +155,24 @@ __device__ __forceinline__ uint32_t tile_of_workgroup()
     return x * each + min(x, rest) + blockIdx.x / XCDS;
 }
 
-template <int WM_, int WN_, int BM_, int BN_, int PACK_>
+template <int WM_, int WN_, int BM_, int BN_, int STAGES_, int PACK_>
 struct Tiles {
-    static constexpr int WM = WM_, WN = WN_, BM = BM_, BN = BN_, PACK = PACK_;
+    static constexpr int WM = WM_, WN = WN_, BM = BM_, BN = BN_, STAGES = STAGES_, PACK = PACK_;
     static constexpr int THREADS = WM * WN * 64, TM = WM * BM * 16, TN = WN * BN * 16, DEPTH = 128;
     static constexpr int ROWS = TM + TN, STAGE = ROWS * DEPTH, LOADS = ROWS * 8 / THREADS;
-    static constexpr int LDS_BYTES = 2 * STAGE + ROWS * 4;          // behind the stages the scales
+    static constexpr int LDS_BYTES = STAGES * STAGE + ROWS * 4;          // behind the stages the scales
     static_assert(ROWS * 8 % THREADS == 0 && TM * 8 % THREADS == 0 && LDS_BYTES <= 160 * 1024, "");
     typedef i32x4 Acc[BM][BN];
     typedef const __attribute__((address_space(1))) uint8_t *Global;
 
     static __device__ __forceinline__ int slot_of(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
 
-    // Waits until this wave's loads have arrived, and then for every wave to be there.  The fences keep the compiler to the order and cost no instruction.
-    static __device__ __forceinline__ void arrive()
+    // Waits until no more than the newest AWAY of this wave's loads are under way, and then for every wave to be there.  The fences keep the compiler to the order and cost no instruction.
+    template <int AWAY> static __device__ __forceinline__ void arrive()
     {
+        static_assert(AWAY < 64, "");
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0 | (7 << 4));                  // vmcnt 0, lgkmcnt 0
+        __builtin_amdgcn_s_waitcnt((AWAY & 15) | (AWAY >> 4 << 14) | (7 << 4));           // vmcnt AWAY, lgkmcnt 0
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -187,8 +204,8 @@ struct Tiles {
     struct Source {
         Global base[2];                                            // of the tile's first row of x, of w
         uint32_t offset[LOADS];
-        int32_t chunks, last;                                      // of a row; the step that has the last of them
-        __device__ __forceinline__ Source(const ProductArgs &a, const Place &p) : chunks((a.n_cols + 15) / 16), last((chunks - 1) / 8)
+        int32_t chunks, row_last, first, last;                     // of a row; the step that has the last of them; the workgroup's steps
+        __device__ __forceinline__ Source(const ProductArgs &a, const Place &p, int32_t split) : chunks((a.n_cols + 15) / 16), row_last((chunks - 1) / 8), first(split * a.each), last(min(first + a.each - 1, row_last))
         {
             base[0] = (Global)(a.x + (uint64_t)p.n0 * a.x_stride);
             base[1] = (Global)(a.w + (uint64_t)p.m0 * a.w_stride);
@@ -206,7 +223,7 @@ struct Tiles {
         {
             constexpr int OF_X = TM * 8 / THREADS;
             step = min(step, last);                                // behind the last step that step again
-            const bool ragged = step == last && (chunks & 7);
+            const bool ragged = step == row_last && (chunks & 7);
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 Global from = base[i < OF_X ? 0 : 1] + (int64_t)step * DEPTH + offset[i];
@@ -284,17 +301,39 @@ template <typename T, typename Tile> __device__ __forceinline__ void finish_tile
     else store_tile<T, Tile, false>(a, p, acc, scales, b);
 }
 
+// A split's sums as they are, rows of a multiple of 4 apart.
+__host__ __device__ constexpr int64_t sums_pitch(int64_t n_outs) { return (n_outs + 3) / 4 * 4; }
+template <typename Tile> __device__ __forceinline__ void store_sums(const ProductArgs &a, const typename Tile::Place &p, int32_t split, const typename Tile::Acc &acc)
+{
+    constexpr int V = Tile::PACK;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int32_t n0 = p.n0 + (wave / Tile::WN) * Tile::BM * 16 + (lane & 15), m0 = p.m0 + (wave % Tile::WN) * Tile::BN * 16 + (lane >> 4) * V;
+#pragma unroll
+    for (int i = 0; i < Tile::BM; ++i) {
+        if (n0 + i * 16 >= a.n_rows) continue;
+        int32_t *to = a.partial + ((int64_t)split * a.n_rows + n0 + i * 16) * sums_pitch(a.n_outs);
+#pragma unroll
+        for (int j = 0; j < Tile::BN; ++j) {
+            const int32_t m = m0 + j * 4 / V * V * 4 + j * 4 % V;
+            if (m < a.n_outs) *reinterpret_cast<i32x4 *>(to + m) = acc[i][j];
+        }
+    }
+}
+
 template <typename T, typename Tile>
 __global__ void __launch_bounds__(Tile::THREADS, 2) product_tiles_kernel(ProductArgs a)
 {
     extern __shared__ __align__(16) uint8_t lds[];
     constexpr int BM = Tile::BM, BN = Tile::BN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const typename Tile::Place place = Tile::place_of(a, tile_of_workgroup());
-    const typename Tile::Source src(a, place);
-    src.load(0, lds);
-    src.load(1, lds + Tile::STAGE);
-    float *scales = reinterpret_cast<float *>(lds + 2 * Tile::STAGE);
+    const uint32_t number = tile_of_workgroup();
+    const int32_t split = (int32_t)(number / a.tiles);
+    const typename Tile::Place place = Tile::place_of(a, number % a.tiles);
+    const typename Tile::Source src(a, place, split);
+    constexpr int STAGES = Tile::STAGES;
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s) src.load(src.first + s, lds + s * Tile::STAGE);
+    float *scales = reinterpret_cast<float *>(lds + STAGES * Tile::STAGE);
     for (int row = threadIdx.x; row < Tile::ROWS; row += Tile::THREADS) {
         const auto *from = (const __attribute__((address_space(1))) float *)(src.base[row < Tile::TM ? 0 : 1] + Tile::Source::row_offset(a, place, row) + (a.held_bytes - 4));
         scales[row] = *from;
@@ -318,20 +357,46 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) product_tiles_kernel(Product
 #pragma unroll
             for (int j = 0; j < BN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], x[i], acc[i][j], 0, 0, 0);
     };
-    Tile::arrive();
+    Tile::template arrive<0>();
     i32x4 x0[BM], w0[BN], x1[BM], w1[BN];
     read(lds, 0, x0, w0);
-    for (int32_t t = 0; t <= src.last; ++t) {
-        uint8_t *stage = lds + (t & 1) * Tile::STAGE, *next = lds + (~t & 1) * Tile::STAGE;
+    uint8_t *stage = lds;
+    for (int32_t t = 0; t <= src.last - src.first; ++t) {
+        uint8_t *next = stage == lds + (STAGES - 1) * Tile::STAGE ? lds : stage + Tile::STAGE;
         read(stage, 1, x1, w1);
         multiply(x0, w0);
-        Tile::arrive();                                            // the stage is read, and the next one there
-        src.load(t + 2, stage);
+        Tile::template arrive<(STAGES - 2) * Tile::LOADS>();      // the stage is read, and the next one there
+        src.load(src.first + t + STAGES, stage);
         read(next, 0, x0, w0);
         multiply(x1, w1);
+        stage = next;
     }
-    Tile::arrive();                                                // a workgroup's LDS is not left with loads under way
-    finish_tile<T, Tile>(a, place, acc, scales);
+    Tile::template arrive<0>();                                    // a workgroup's LDS is not left with loads under way
+    if (a.partial) store_sums<Tile>(a, place, split, acc);
+    else finish_tile<T, Tile>(a, place, acc, scales);
+}
+
+// The splits' sums, added up, and what they stand for: four results of a row to a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) product_join_kernel(ProductArgs a, int32_t splits)
+{
+    const int32_t across = (a.n_outs + 3) / 4;
+    const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x, n = q / across;
+    if (n >= a.n_rows) return;
+    const int32_t m = (int32_t)(q - n * across) * 4, count = min(4, a.n_outs - m);
+    const int64_t pitch = sums_pitch(a.n_outs);
+    const int32_t *from = a.partial + n * pitch + m;
+    i32x4 sum{0, 0, 0, 0};                                         // (behind the last output whatever the tile made of that output's codes)
+    for (int32_t s = 0; s < splits; ++s) sum += *reinterpret_cast<const i32x4 *>(from + s * a.n_rows * pitch);
+    const uint32_t sx = *row_at<uint32_t>(a.x + a.held_bytes - 4, a.x_stride, n);
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int32_t at = m + min(e, count - 1);
+        const uint32_t sw = *row_at<uint32_t>(a.w + a.held_bytes - 4, a.w_stride, at);
+        v[e] = wide_value(sum_of_codes(sum[e], sx, sw, scale_in_sum(a.n_cols)), sx, sw, bias_at(a, at));
+    }
+    store_four(row_at<T>(a.y, a.y_stride, n) + m, f32x4{v[0], v[1], v[2], v[3]}, count);
 }
 
 // Many rows of few codes: what bounds them is the rows' and the results' way from and to HBM, and tiles spend most of their time on it at their start and end.  Here w lies in LDS, once
@@ -513,19 +578,6 @@ template <int PARTS> __device__ __forceinline__ void parts_of_any(const float (&
         parts_of<PARTS>(v[e], one);
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) p[q][e] = one[q];
-    }
-}
-
-// Four results side by side, of which n are inside.
-template <typename O> __device__ __forceinline__ void store_four(O *p, const f32x4 &v, int32_t n)
-{
-    if (n >= 4) {
-        const float w[4] = {v[0], v[1], v[2], v[3]};
-        store_pack<O, 4>(p, w);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (e < n) p[e] = (O)v[e];
     }
 }
 
@@ -1092,14 +1144,19 @@ template <typename K> rg_status allow_lds(K kernel, int bytes, std::atomic<uint6
     return RG_OK;
 }
 
-template <typename T, typename Tile> rg_status launch_tiles(const ProductArgs &a, hipStream_t st)
+template <typename T, typename Tile> rg_status launch_tiles(ProductArgs a, int32_t splits, hipStream_t st)
 {
     const uint64_t tiles = ((uint64_t)a.n_rows + Tile::TM - 1) / Tile::TM * (((uint64_t)a.n_outs + Tile::TN - 1) / Tile::TN);
-    RG_TRY(check_grid(tiles, Tile::THREADS));
+    RG_TRY(check_grid(tiles * (uint64_t)splits, Tile::THREADS));
+    a.tiles = (uint32_t)tiles;
     static std::atomic<uint64_t> known{0};
     RG_TRY(allow_lds(product_tiles_kernel<T, Tile>, Tile::LDS_BYTES, known));
-    hipLaunchKernelGGL((product_tiles_kernel<T, Tile>), dim3((uint32_t)tiles), dim3(Tile::THREADS), Tile::LDS_BYTES, st, a);
+    hipLaunchKernelGGL((product_tiles_kernel<T, Tile>), dim3((uint32_t)tiles * (uint32_t)splits), dim3(Tile::THREADS), Tile::LDS_BYTES, st, a);
     RG_HIP(hipGetLastError());
+    if (splits > 1) {
+        hipLaunchKernelGGL(product_join_kernel<T>, dim3((uint32_t)(((uint64_t)a.n_rows * (((uint64_t)a.n_outs + 3) / 4) + 255) / 256)), dim3(256), 0, st, a, splits);
+        RG_HIP(hipGetLastError());
+    }
     return RG_OK;
 }
 
@@ -1134,20 +1191,21 @@ template <typename T, int WAVES> rg_status launch_few(const ProductArgs &a, hipS
     return RG_OK;
 }
 
-template <typename T> rg_status launch_product(const ProductArgs &a, hipStream_t st)
+template <typename T> rg_status launch_product(const ProductArgs &a, const ProductCut &c, int n_cu, hipStream_t st)
 {
     constexpr int PACK = 16 / sizeof(T);
-    int n_cu = 0;
-    RG_TRY(compute_units(&n_cu));
-    switch (product_way((uint64_t)a.n_rows, (uint64_t)a.n_outs, (uint64_t)a.n_cols, sizeof(T), n_cu)) {
+    switch (c.way) {
     case ProductWay::FEW: return launch_few<T, 4>(a, st);
     case ProductWay::FEW_LONG: return launch_few<T, 16>(a, st);
     case ProductWay::THIN: return launch_thin_of<T>(a, n_cu, st);
-    case ProductWay::TILES_64: return launch_tiles<T, Tiles<2, 2, 2, 2, PACK>>(a, st);
-    case ProductWay::TILES_128: return launch_tiles<T, Tiles<4, 2, 2, 4, PACK>>(a, st);
-    default: return launch_tiles<T, Tiles<2, 4, 8, 4, PACK>>(a, st);
+    case ProductWay::TILES_64: return launch_tiles<T, Tiles<2, 2, 2, 2, 3, PACK>>(a, c.splits, st);
+    case ProductWay::TILES_128: return launch_tiles<T, Tiles<4, 2, 2, 4, 2, PACK>>(a, c.splits, st);
+    case ProductWay::TILES_128_DEEP: return launch_tiles<T, Tiles<4, 2, 2, 4, 4, PACK>>(a, c.splits, st);
+    default: return launch_tiles<T, Tiles<2, 4, 8, 4, 2, PACK>>(a, c.splits, st);
     }
 }
+
+uint64_t product_scratch(uint64_t n, uint64_t m, const ProductCut &c) { return c.splits > 1 ? (uint64_t)c.splits * n * (uint64_t)sums_pitch((int64_t)m) * 4 : 0; }
 
 // How the backward pass is cut, and where its scratch lies.
 struct GradPlan {
@@ -1240,11 +1298,16 @@ rg_status launch_join(const Join &first, const Join &second, uint32_t type, hipS
 
 using namespace rg;
 
-extern "C" rg_status rg_rows8_product_workspace(uint64_t n_rows, uint64_t n_outs, uint64_t n_cols, uint64_t *bytes)
+extern "C" rg_status rg_rows8_product_workspace(uint64_t n_rows, uint64_t n_outs, uint64_t n_cols, uint32_t type, uint64_t *bytes)
 {
     if (!bytes) { set_error("null argument"); return RG_EINVAL; }
     RG_TRY(check_product_sizes(n_rows, n_outs, n_cols));
+    RG_TRY(check_types("y", nullptr, RG_F32, type));
     *bytes = 0;
+    if (n_rows == 0 || n_outs == 0) return RG_OK;
+    int n_cu = 0;
+    RG_TRY(compute_units(&n_cu));
+    *bytes = product_scratch(n_rows, n_outs, product_cut(n_rows, n_outs, n_cols, element_bytes(type), n_cu));
     return RG_OK;
 }
 
@@ -1266,9 +1329,15 @@ extern "C" rg_status rg_rows8_product(const void *x, uint64_t x_stride, uint64_t
     a.y = static_cast<uint8_t *>(y); a.y_stride = y_stride;
     a.n_rows = (int32_t)n_rows; a.n_outs = (int32_t)n_outs; a.n_cols = (int32_t)n_cols; a.held_bytes = (int32_t)held_bytes(n_cols);
     const hipStream_t st = as_stream(stream);
-    if (type == RG_F32) RG_TRY(launch_product<float>(a, st));
-    else if (type == RG_BF16) RG_TRY(launch_product<bf16>(a, st));
-    else RG_TRY(launch_product<f16>(a, st));
+    int n_cu = 0;
+    RG_TRY(compute_units(&n_cu));
+    const ProductCut c = product_cut(n_rows, n_outs, n_cols, element_bytes(type), n_cu);
+    RG_TRY(check_workspace(workspace, workspace_bytes, product_scratch(n_rows, n_outs, c)));
+    a.partial = c.splits > 1 ? static_cast<int32_t *>(workspace) : nullptr;
+    a.each = c.each;
+    if (type == RG_F32) RG_TRY(launch_product<float>(a, c, n_cu, st));
+    else if (type == RG_BF16) RG_TRY(launch_product<bf16>(a, c, n_cu, st));
+    else RG_TRY(launch_product<f16>(a, c, n_cu, st));
     return RG_OK;
 }
 

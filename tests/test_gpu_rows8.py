@@ -203,6 +203,20 @@ def test_a_table_beyond_32_bits(rg):
     assert bool((held[:-1, :-4] == 0).all())
 
 
+@pytest.mark.parametrize("dtype,cols", [(torch.float32, 601), (torch.bfloat16, 1203), (torch.float16, 40_001)], ids=str)
+def test_results_larger_than_the_caches(rg, dtype, cols):
+    rows = 150_000_000 // (cols * dtype.itemsize)
+    held, codes, scale = random_held(500, cols, 5)
+    at = torch.randint(-1, 500, (rows,), generator=torch.Generator().manual_seed(1)).cuda()
+    buf, out = strided(rows, cols, dtype, 1, 1)
+    rg.rg_dequantize_rows(held, cols, rows=at, out=out)
+    values = torch.cat([(codes.float() * scale[:, None]).to(dtype), torch.zeros((1, cols), dtype=dtype, device="cuda")])
+    for first in range(0, rows, 10_000):
+        assert torch.equal(out[first: first + 10_000], values[at[first: first + 10_000]])
+    out.fill_(3.0)
+    assert bool((buf == 3).all())
+
+
 def rounding(ref, dtype):
     rel, least = HALF_ULP[dtype]
     return ref.abs() * rel + least
@@ -225,7 +239,8 @@ def product_sum(x, w):
 
 
 PRODUCTS = [(1, 1, 1), (1, 4096, 4096), (3, 5, 13), (16, 16, 64), (17, 33, 12), (2, 1000, 8191), (64, 64, 128), (65, 63, 129), (130, 257, 1001), (128, 256, 16), (1, 1, 131_072), (200, 3, 20_011), (33, 700, 28),
-            (1000, 41, 602), (511, 513, 256), (48, 2048, 512), (300, 300, 140), (1025, 129, 384), (2048, 1024, 272), (5000, 17, 60), (4099, 515, 1300)]
+            (1000, 41, 602), (511, 513, 256), (48, 2048, 512), (300, 300, 140), (1025, 129, 384), (2048, 1024, 272), (5000, 17, 60), (4099, 515, 1300), (300, 1000, 8192), (130, 127, 20_011), (257, 65, 6001), (700, 515, 4100), (30_011, 70, 300),
+            (20_000, 333, 700)]
 
 
 @pytest.mark.parametrize("n,m,d", PRODUCTS)
@@ -486,7 +501,7 @@ def run_all(rg, x32, rows, w, bias, dy, d, **kw):
     return held, y, dx, dw, db, rg.rg_dequantize_rows(held, d, dtype=dy.dtype, **kw)
 
 
-SIZES = [(1500, 96, 200), (3, 700, 1001), (700, 300, 64)]
+SIZES = [(1500, 96, 200), (3, 700, 1001), (700, 300, 64), (300, 200, 9000)]
 
 
 def inputs(n, m, d, seed=0):
@@ -521,7 +536,7 @@ def test_captured_and_replayed(rg, n, m, d):
     """Two graphs that share their workspaces, replayed by turns on changed inputs, with eager work between."""
     a = inputs(n, m, d)
     dt = a[4].dtype
-    works = [torch.empty(max(rg.rg_rows8_product_workspace(n, m, d), 16), dtype=torch.uint8, device="cuda"),
+    works = [torch.empty(max(rg.rg_rows8_product_workspace(n, m, d, dt), 16), dtype=torch.uint8, device="cuda"),
              torch.empty(max(rg.rg_rows8_product_backward_workspace(n, m, d, dt), 16), dtype=torch.uint8, device="cuda")]
 
     def step():
@@ -569,8 +584,8 @@ def test_workspaces(rg):
     for n, m, d in SIZES + [(30_000, 64, 100)]:
         x, rows, w, bias, dy = inputs(n, m, d)
         held = rg.rg_quantize_rows(x, rows=rows)
-        sizes = rg.rg_rows8_product_workspace(n, m, d), rg.rg_rows8_product_backward_workspace(n, m, d, dy.dtype)
-        for size, call in zip(sizes, (lambda ws: [rg.rg_rows8_product(held, w, d, workspace=ws)], lambda ws: rg.rg_rows8_product_backward(dy, held, w, d, workspace=ws))):
+        sizes = rg.rg_rows8_product_workspace(n, m, d, dy.dtype), rg.rg_rows8_product_backward_workspace(n, m, d, dy.dtype)
+        for size, call in zip(sizes, (lambda ws: [rg.rg_rows8_product(held, w, d, dtype=dy.dtype, workspace=ws)], lambda ws: rg.rg_rows8_product_backward(dy, held, w, d, workspace=ws))):
             buf = torch.full((size + 4096,), 171, dtype=torch.uint8, device="cuda")
             for u, v in zip(call(buf[:size]), call(None)):
                 assert torch.equal(u, v)

@@ -85,8 +85,11 @@ def test_backward(rg, change, status):
 def test_workspaces(rg):
     b = C.c_uint64()
     L = rg.lib()
-    assert L.rg_rows8_product_workspace(5, 5, 5, None) == rg.RG_EINVAL and L.rg_rows8_product_workspace(5, 5, 0, C.byref(b)) == rg.RG_EINVAL
-    assert L.rg_rows8_product_workspace(2**31, 5, 5, C.byref(b)) == rg.RG_ERANGE
+    assert L.rg_rows8_product_workspace(5, 5, 5, F32, None) == rg.RG_EINVAL and L.rg_rows8_product_workspace(5, 5, 0, F32, C.byref(b)) == rg.RG_EINVAL
+    for n, m in ((0, 5), (5, 0), (0, 0)):
+        b.value = 7
+        assert L.rg_rows8_product_workspace(n, m, 64, F32, C.byref(b)) == rg.RG_OK and b.value == 0
+    assert L.rg_rows8_product_workspace(2**31, 5, 5, F32, C.byref(b)) == rg.RG_ERANGE and L.rg_rows8_product_workspace(5, 5, 5, 9, C.byref(b)) == rg.RG_EINVAL
     assert L.rg_rows8_product_backward_workspace(5, 5, 5, F32, 1, 1, 1, None) == rg.RG_EINVAL
     assert L.rg_rows8_product_backward_workspace(5, 5, 5, 3, 1, 1, 1, C.byref(b)) == rg.RG_EINVAL
 
@@ -136,9 +139,9 @@ int main()
     unsigned long long n, m, d, bytes;
     int cu;
     while (scanf("%llu %llu %llu %llu %d", &n, &m, &d, &bytes, &cu) == 5) {
-        const rg::ProductWay way = rg::product_way(n, m, d, bytes, cu);
-        const rg::ThinShape s = way == rg::ProductWay::THIN ? rg::thin_shape(n, m, d, cu) : rg::ThinShape{};
-        printf("%d %u %u %u %u\n", (int)way, s.outs, s.shares, s.lds, s.grid);
+        const rg::ProductCut c = rg::product_cut(n, m, d, bytes, cu);
+        const rg::ThinShape s = c.way == rg::ProductWay::THIN ? rg::thin_shape(n, m, d, cu) : rg::ThinShape{};
+        printf("%d %u %u %u %u %d %d\n", (int)c.way, s.outs, s.shares, s.lds, s.grid, c.splits, c.each);
     }
 }
 """
@@ -153,15 +156,18 @@ def test_ways_of_the_product(tmp_path):
     out = subprocess.run([str(tmp_path / "driver")], input="\n".join(" ".join(map(str, c)) for c in cases) + "\n", capture_output=True, text=True, check=True).stdout.split("\n")
     seen = set()
     for (n, m, d, b, cu), line in zip(cases, out):
-        way, outs, shares, lds, grid = map(int, line.split())
+        way, outs, shares, lds, grid, splits, each = map(int, line.split())
         seen.add(way)
+        steps = -(-d // 128)
+        assert splits >= 1 and (splits - 1) * each < steps <= splits * each and (splits == 1 or (way >= 3 and each >= 4))
         if way == 2:
             assert d <= 768 and outs % 32 == 0 and outs * shares >= m > outs * (shares - 1) and lds <= 160 * 1024 and outs * ((d + 15) // 16 * 16 + 8) + 16 == lds
             assert grid % shares == 0 and 0 < grid // shares <= (n + 127) // 128 and grid <= max(2 * cu, shares)
         else:
-            side, threads = {0: (16, 256), 1: (16, 1024), 3: (64, 256), 4: (128, 512), 5: (256, 512)}[way]
-            assert -(-n // side) * -(-m // side) * threads < 2**32, (n, m, d)
-    assert seen == set(range(6))
+            side, threads = {0: (16, 256), 1: (16, 1024), 3: (64, 256), 4: (128, 512), 5: (128, 512), 6: (256, 512)}[way]
+            assert -(-n // side) * -(-m // side) * threads * splits < 2**32, (n, m, d)
+            assert splits == 1 or (-(-n // side) * -(-m // side) * splits <= 4 * cu and n * -(-m // 4) < 2**32)
+    assert seen == set(range(7))
 
 
 CUTS = r"""
