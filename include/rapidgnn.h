@@ -546,7 +546,8 @@ rg_status rg_rows8_bytes(uint64_t n_cols, uint64_t *bytes);
 
 /*
  * rg_quantize_rows -- rows as they are written to a store, a cache or a checkpoint:
- *     s = |x|_max / 127 in fp32, no less than 2^-126 and no more than 0x1.020406p+121, of which 127 are still a number,
+ *     s = |x|_max * 0x1.020408p-7 (the fp32 number next to 1 / 127) rounded to fp32, no less than 2^-126 and no more
+ *         than 0x1.020406p+121, of which 127 are still a number,
  *     code = the whole number nearest to x / s (of the exact quotient; ties to even).
  * A row with an infinity or a NaN is held as codes of zero and a scale of NaN: all of it reads back as NaN.
  * rg_dequantize_rows -- rows as they are read back: code * s, of `type`.

@@ -1,7 +1,8 @@
 // Rows held in 8 bits: written (rg_quantize_rows) and read back (rg_dequantize_rows).
 //
 // A held row is its codes, zeros, and its scale in the last four bytes, so that everything that moves rows moves held ones: a quarter of the bytes of fp32 through the
-// cache, the gather and the host link.  With s = max|x| / 127 (rounded to fp32; at least 2^-126, and 127 s is a number) a code is the whole number nearest to the exact quotient x / s, ties to
+// cache, the gather and the host link.  With s = max|x| / 127 (the fp32 product with the fp32 number next to 1 / 127, as torch divides by 127 on this
+// device, so that rows held by either are the same; at least 2^-126, and 127 s is a number) a code is the whole number nearest to the exact quotient x / s, ties to
 // even: what is read back is off by s / 2 at most.
 //
 // Both directions are bound by HBM: a row is read once into registers and written once.  It belongs to 8 to 64 lanes of a wave, or to a workgroup, whatever holds
@@ -68,6 +69,7 @@ template <int LANES> __device__ __forceinline__ uint32_t row_max(uint32_t v, uin
     return v;
 }
 
+constexpr float ONE_127TH = 0x1.020408p-7f;         // the largest element over the scale stays within 2^-22 of 127, so codes do
 constexpr float SCALE_MOST = 0x1.020406p+121f;      // the largest of which 127 are a number
 constexpr float ROUNDER = 12582912.f;               // 1.5 * 2^23: a sum with it is a whole number, which is in its last bits
 struct Scale {
@@ -76,7 +78,7 @@ struct Scale {
     __device__ __forceinline__ explicit Scale(uint32_t largest)
     {
         finite = largest < 0x7F800000u;
-        s = fminf(fmaxf(__builtin_bit_cast(float, largest) / 127.f, 0x1p-126f), SCALE_MOST);
+        s = fminf(fmaxf(__builtin_bit_cast(float, largest) * ONE_127TH, 0x1p-126f), SCALE_MOST);
         inverse = __builtin_amdgcn_rcpf(s);
         half = 0.5f * s;
     }

@@ -40,11 +40,14 @@ def made(rows, cols, dtype, seed, pad=0, lead=0):
     return v
 
 
+ONE_127TH = torch.tensor(float.fromhex("0x1.020408p-7"), dtype=torch.float32)
+
+
 def definition(x):
     """(codes, scale) of rows in 64 bits."""
     x = x.detach().cpu()
     largest = x.float().abs().amax(1)
-    scale = (largest / 127).clamp(min=2.0 ** -126, max=float.fromhex("0x1.020406p+121"))
+    scale = (largest * ONE_127TH).clamp(min=2.0 ** -126, max=float.fromhex("0x1.020406p+121"))
     q = x.double() / scale.double()[:, None]
     low = torch.floor(q)
     part = q - low
@@ -145,7 +148,7 @@ def test_quotients_next_to_a_border(rg):
     """Elements at and one unit beside (k + 1/2) s, of scales with all 24 bits."""
     g = torch.Generator().manual_seed(3)
     largest = (torch.rand(64, generator=g) * 4 + 0.1).float()
-    scale = (largest / 127).float()
+    scale = largest * ONE_127TH
     x = torch.zeros((64, 3 * 126 + 1), dtype=torch.float32)
     x[:, 0] = largest
     for k in range(126):
