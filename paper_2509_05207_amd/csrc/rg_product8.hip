@@ -144,10 +144,12 @@ __global__ void __launch_bounds__(WAVES * 64) product_few_kernel(ProductArgs a)
     }
 }
 
-// Tiles of TM rows by TN outputs, by WM x WN waves of BM x BN blocks of 16 x 16.  Steps of 128 codes pass through LDS, two of them there: one is multiplied while the other
-// arrives, written into LDS by the loads themselves.  A row of a step is eight chunks of 16 bytes, stored in an order that depends on the row, so that the 16 lanes that
+// Tiles of TM rows by TN outputs, by WM x WN waves of BM x BN blocks of 16 x 16.  Steps of 128 codes pass through LDS, two to four of them there: one is multiplied while the others
+// arrive, written into LDS by the loads themselves.  A row of a step is eight chunks of 16 bytes, stored in an order that depends on the row, so that the 16 lanes that
 // LDS serves at a time (16 rows, one chunk of each) fall on all banks once.
 // Workgroup g runs on XCD g mod 8, and every XCD has an L2 of its own: tiles that share operands, which follow one another, go to one XCD.
+// Large products are bound by the matrix operations and by what waves read of LDS: 8,192 x 8,192 to 8,192 in bf16 499 us by tiles of 256 (2,200 TOPS; the matrix units are busy for 56 %), 545 behind other
+// work.  Where that is a fraction of a tile's start and end, by these: 10,007 x 1,001 to 517 in fp32 18.5 by tiles of 128.  Workgroups that stay and take one tile after the other have no registers left for it (560).
 __device__ __forceinline__ uint32_t tile_of_workgroup()
 {
     constexpr uint32_t XCDS = 8;
@@ -376,7 +378,7 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) product_tiles_kernel(Product
     else finish_tile<T, Tile>(a, place, acc, scales);
 }
 
-// The splits' sums, added up, and what they stand for: four results of a row to a thread.
+// The splits' sums, added up, and what they stand for: four results of a row to a thread.  Bound by the sums' way through the caches; with it 300 x 8,192 to 1,000 takes 16.8 us in three splits.
 template <typename T>
 __global__ void __launch_bounds__(256) product_join_kernel(ProductArgs a, int32_t splits)
 {
@@ -401,7 +403,8 @@ __global__ void __launch_bounds__(256) product_join_kernel(ProductArgs a, int32_
 
 // Many rows of few codes: what bounds them is the rows' and the results' way from and to HBM, and tiles spend most of their time on it at their start and end.  Here w lies in LDS, once
 // for all rows that a workgroup does (where it has more than that holds, each workgroup has a share of the outputs), and a wave by itself takes 16 rows at a time into registers, the next
-// ones under way meanwhile: no barrier behind the first.  w lies as the matrix operations take it: of a block of 16 outputs chunk by chunk, 16 rows side by side.
+// ones under way meanwhile: no barrier behind the first.  w lies as the matrix operations take it: of a block of 16 outputs chunk by chunk, 16 rows side by side.  150,000 x 512 to 256 in bf16: 45 us,
+// 3.4 TB/s; the matrix units are busy for 24 % of it.
 struct ThinArgs {
     ProductArgs p;
     int32_t outs;                    // of a workgroup, a multiple of 32
@@ -599,6 +602,9 @@ __device__ __forceinline__ bf16x8 codes_as_bf16(const i32x2 &c)
 // two steps ahead, and one step ahead are multiplied with their scales, parted, and written into LDS; the codes go there as they are.  Of operands that lie along the wrong axis LDS itself makes columns (reads
 // that transpose blocks of 16 x 8 bytes or 16 x 4 numbers).  What the lanes read at a time falls on all banks once: the order of the 16-byte chunks of a row, or of the 32-byte pieces of
 // one of dy's, depends on the row.
+// Bound by the vector units: matrix operations keep them for 41 to 56 % of the time, and what parts dy hardly overlaps with them.  In tiles of 256:
+// dweight and the sums of 199,000 x 602 to 256 in fp32, three parts, 199 us behind other work (920 TFLOP/s of bf16) and 17 for the join; 150,000 x 512 to 256 in bf16 94 and 17; 8,192 x 4,096 to 4,096
+// 450 each way (1,220).  
 template <typename T, int PARTS_, bool ALONG_, bool SUMS_, int WI_, int WJ_, int BI_, int BJ_>
 struct GradTile {
     static constexpr int PARTS = PARTS_, WI = WI_, WJ = WJ_, BI = BI_, BJ = BJ_;
@@ -887,7 +893,8 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
 
 // dx of many rows and few outputs, which the tiles do at the pace of their starts and ends: w's codes lie in LDS, once for all rows that a workgroup does (where there is more than that holds, each
 // has a share of the columns), and a wave by itself takes R blocks of 16 rows of dy at a time, parted in registers (the next ones' elements on their way beside them spill).  The codes lie by blocks of 16 columns, row after row: what the
-// lanes read at a time is contiguous.
+// lanes read at a time is contiguous.  Bound as the tiles are: 150,000 x 256 to 512 in bf16 97 us (810 TFLOP/s of bf16), the matrix units
+// busy for 40 %.
 struct ThinGradArgs {
     GradArgs g;
     int32_t cols;                    // of a workgroup, a multiple of 32
@@ -1074,7 +1081,7 @@ __global__ void __launch_bounds__(256) grad_join_kernel(Join first, Join second,
     }
 }
 
-// Sums of dy's columns over a part of its rows: 64 columns to a workgroup, four rows at a time.
+// Sums of dy's columns over a part of its rows, for calls that want no dweight, whose tiles make them on the way: 64 columns to a workgroup, four rows at a time.  Bound by HBM.
 template <typename T>
 __global__ void __launch_bounds__(256) bias_sums_kernel(const uint8_t *dy, uint64_t dy_stride, int32_t n_rows, int32_t n_outs, int32_t each, float *partial)
 {
