@@ -566,7 +566,7 @@ rg_status rg_dequantize_rows(const void *held, uint64_t held_stride, uint64_t n_
 /*
  * rg_rows8_product -- y = x w^T + bias of held rows x [n_rows] and held weights w [n_outs], a scale for each row of either:
  *     y[n][m] = s_x[n] * s_w[m] * (sum over c of code_x[n][c] * code_w[m][c]) + bias[m].
- * The sum is exact.  Results of RG_F32 are off by their own rounding and a few units of 2^-47 of the product; for 16 bits the sum and the scales' product are rounded to fp32 first.  A row
+ * The sum is exact.  Results of RG_F32 are off by half a step, and 2^-23 of that; for 16 bits what follows the sum is in fp32.  A row
  * with a scale of NaN makes its results NaN.
  *
  *   bias         dev, [n_outs] of bias_type (RG_F32, or the same as `type`), or NULL

@@ -216,10 +216,11 @@ struct HoldShape {
     int packs;                           // of a lane
     uint32_t grid;                       // workgroups; their waves, or they, take rows by turns
 };
-// Lanes to a row, of half a wave up to as many packs a lane as leave fewer idle than a wave does (602 elements, packs of four and eight: 160 and 96 of 192 and 128).
+// Lanes to a row, of half a wave up to as many packs a lane as leave fewer idle than a wave does (602 elements, packs of four and eight: 160 and 96 of 192 and 128); of others five, so that the scale behind a
+// power of two of codes does not take twice or four times the lanes (written, us: 8,192 x 8,192 bf16 64 by four of 1,024 and 39 by five of 256, 16,384 x 4,096 fp32 75 and 67, 32,768 x 2,048 bf16 53 and 37).
 inline void lanes_of(int64_t need, HoldShape &s)
 {
-    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 * 5 ? 32 : need <= 64 * 4 ? 64 : need <= 256 * 4 ? 256 : need <= 1024 * 4 ? 1024 : 0;
+    s.lanes = need <= 8 ? 8 : need <= 16 ? 16 : need <= 32 * 5 ? 32 : need <= 64 * 5 ? 64 : need <= 256 * 5 ? 256 : need <= 1024 * 5 ? 1024 : 0;
     s.packs = s.lanes ? (int)((need + s.lanes - 1) / s.lanes) : 0;
 }
 // Rows as they are written: packs over all of a held row's bytes, one code to a byte.
@@ -231,12 +232,12 @@ inline HoldShape hold_shape(int64_t n_out, int64_t n_cols, int element_bytes, in
     s.grid = s.lanes == 0 ? grid_for(n_out, 1024) : (uint32_t)std::max<int64_t>(1, std::min((int64_t)n_cu * (s.lanes == 1024 ? 2 : 8), (n_out + groups - 1) / groups));
     return s;
 }
-// Rows as they are read back: single elements where a row has fewer than an access; longer ones than a wave's by parts.
+// Rows as they are read back: single elements where a row has fewer than an access; longer ones than four of a wave's by parts (60,000 x 1,100 fp32 53, by five 69).
 inline HoldShape read_shape(int64_t n_out, int64_t n_cols, int element_bytes, int n_cu)
 {
     HoldShape s{n_cols < 16 / element_bytes ? 1 : 16 / element_bytes, 0, 0, 0};
-    lanes_of((n_cols + s.pack - 1) / s.pack, s);
-    if (s.lanes > 64) s.lanes = s.packs = 0;
+    const int64_t need = (n_cols + s.pack - 1) / s.pack;
+    if (need <= 64 * 4) lanes_of(need, s);
     const int64_t groups = s.lanes ? 256 / s.lanes : 1;
     s.grid = s.lanes ? (uint32_t)std::max<int64_t>(1, std::min((int64_t)n_cu * 8, (n_out + groups - 1) / groups)) : grid_for(n_out * ((n_cols + 1024 * s.pack - 1) / (1024 * s.pack)), 256);
     return s;

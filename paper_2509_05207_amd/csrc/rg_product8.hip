@@ -604,7 +604,7 @@ __device__ __forceinline__ bf16x8 codes_as_bf16(const i32x2 &c)
 // one of dy's, depends on the row.
 // Bound by the vector units: matrix operations keep them for 41 to 56 % of the time, and what parts dy hardly overlaps with them.  In tiles of 256:
 // dweight and the sums of 199,000 x 602 to 256 in fp32, three parts, 199 us behind other work (920 TFLOP/s of bf16) and 17 for the join; 150,000 x 512 to 256 in bf16 94 and 17; 8,192 x 4,096 to 4,096
-// 450 each way (1,220).  
+// 450 each way (1,220).
 template <typename T, int PARTS_, bool ALONG_, bool SUMS_, int WI_, int WJ_, int BI_, int BJ_>
 struct GradTile {
     static constexpr int PARTS = PARTS_, WI = WI_, WJ = WJ_, BI = BI_, BJ = BJ_;

@@ -6,7 +6,7 @@
 // even: what is read back is off by s / 2 at most.
 //
 // Both directions are bound by HBM: a row is read once into registers and written once.  It belongs to 8 to 64 lanes of a wave, or to a workgroup, whatever holds
-// it in 32 elements a lane or fewer; rows beyond that are read twice.
+// it in 40 elements a lane or fewer; rows beyond that are read twice.
 // 199,000 x 602 in fp32: written 112 us (5.4 TB/s), read back 140 (4.3 TB/s; results past the caches), where a copy reaches 5.1; 200,000 x 256 in bf16 by positions out of a million rows
 // 48 and 25; 199,000 x 602 to bf16 out of 233,000 rows 79 (4.6 TB/s).
 #include "rg_internal.h"
@@ -334,12 +334,15 @@ template <typename T> bool launch_quantize_of(const HoldShape &s, const HoldArgs
     case 32 * 16 + 5: return launch_quantize<T, 32, 5>(s, a, st);
     case 64 * 16 + 3: return launch_quantize<T, 64, 3>(s, a, st);
     case 64 * 16 + 4: return launch_quantize<T, 64, 4>(s, a, st);
+    case 64 * 16 + 5: return launch_quantize<T, 64, 5>(s, a, st);
     case 256 * 16 + 2: return launch_quantize<T, 256, 2>(s, a, st);
     case 256 * 16 + 3: return launch_quantize<T, 256, 3>(s, a, st);
     case 256 * 16 + 4: return launch_quantize<T, 256, 4>(s, a, st);
+    case 256 * 16 + 5: return launch_quantize<T, 256, 5>(s, a, st);
     case 1024 * 16 + 2: return launch_quantize<T, 1024, 2>(s, a, st);
     case 1024 * 16 + 3: return launch_quantize<T, 1024, 3>(s, a, st);
     case 1024 * 16 + 4: return launch_quantize<T, 1024, 4>(s, a, st);
+    case 1024 * 16 + 5: return launch_quantize<T, 1024, 5>(s, a, st);
     }
     return false;
 }

@@ -65,7 +65,8 @@ GOOD_P = dict(x=P, x_stride=112, n=5, w=P, w_stride=112, m=7, d=100, bias=P, bia
 @pytest.mark.parametrize("change,status", [
     (dict(type=3), "RG_EINVAL"), (dict(bias_type=F16), "RG_EINVAL"), (dict(bias_type=7), "RG_EINVAL"), (dict(bias=P + 2), "RG_EINVAL"), (dict(d=0), "RG_EINVAL"), (dict(d=131_073), "RG_ERANGE"),
     (dict(n=2**30 + 1), "RG_ERANGE"), (dict(m=2**30 + 1), "RG_ERANGE"), (dict(x=None), "RG_EINVAL"), (dict(w=None), "RG_EINVAL"), (dict(x=P + 4), "RG_EINVAL"), (dict(w_stride=100), "RG_EINVAL"),
-    (dict(y=None), "RG_EINVAL"), (dict(y=P + 1), "RG_EINVAL"), (dict(y_stride=12), "RG_EINVAL"), (dict(y_stride=15), "RG_EINVAL")])
+    (dict(y=None), "RG_EINVAL"), (dict(y=P + 1), "RG_EINVAL"), (dict(y_stride=12), "RG_EINVAL"), (dict(y_stride=15), "RG_EINVAL"),
+    (dict(x_stride=2**24), "RG_ERANGE"), (dict(w_stride=2**24), "RG_ERANGE"), (dict(y_stride=2**41), "RG_ERANGE")])
 def test_product(rg, change, status):
     assert call(rg, "rg_rows8_product", PRODUCT, GOOD_P, **change) == getattr(rg, status)
 
@@ -107,7 +108,7 @@ int main()
 }
 """
 READ_KERNELS = {(8, 1), (16, 1), (32, 1), (32, 2), (32, 3), (32, 4), (32, 5), (64, 3), (64, 4)}
-HOLD_KERNELS = READ_KERNELS | {(256, 2), (256, 3), (256, 4), (1024, 2), (1024, 3), (1024, 4)}
+HOLD_KERNELS = READ_KERNELS | {(64, 5), (256, 2), (256, 3), (256, 4), (256, 5), (1024, 2), (1024, 3), (1024, 4), (1024, 5)}
 
 
 def test_every_width_has_a_kernel_that_holds_it(tmp_path):
