@@ -40,7 +40,7 @@ struct ProductArgs {
     uint8_t *y;
     uint64_t y_stride;
     int32_t n_rows, n_outs, n_cols, held_bytes;
-    int32_t *partial;                // [splits][n_rows][n_outs], or NULL: a sum is done by one workgroup
+    int32_t *partial;                // [splits][n_rows][n_outs to a multiple of 4], or NULL: a sum is done by one workgroup
     int32_t each;                    // steps of 128 codes of a split
     uint32_t tiles;
 };
