@@ -308,8 +308,9 @@ inline ProductCut product_cut(uint64_t n, uint64_t m, uint64_t d, uint64_t eleme
     return best;
 }
 
-// The backward pass' products: sums over n_k of n_i x n_j, in `parts` bf16 numbers.
-constexpr uint64_t GRAD_DEPTH = 32, GRAD_THIN_OUTS = 256;      // of a step along k; outputs that the thin way has registers for
+// The backward pass' products: sums over n_k of n_i x n_j, of numbers in `parts` bf16 numbers.
+constexpr uint64_t GRAD_DEPTH = 32, GRAD_THIN_OUTS = 256, GRAD_THIN_ROWS = 16;      // of a step along k; outputs that the thin way has registers for, rows of a wave of it at a time
+constexpr int GRAD_PARTS = 3;
 enum class GradWay { TILES_64, TILES_64_256, TILES_128, TILES_256, THIN };
 struct GradCut {
     GradWay way;
@@ -335,7 +336,7 @@ inline GradCut grad_cut(uint64_t n_i, uint64_t n_j, uint64_t n_k, int parts, int
     struct Cost { GradWay way; uint64_t ti, tj; double alone, alone_step, start, step; };
     static constexpr Cost COSTS[] = {{GradWay::TILES_64, 64, 64, 2.3, 0.7, 0.67, 0.25}, {GradWay::TILES_64_256, 64, 256, 3.5, 0.9, 1.5, 0.62},
                                      {GradWay::TILES_128, 128, 128, 4, 1.05, 1.8, 0.64}, {GradWay::TILES_256, 256, 256, 8, 1.7, 10, 1.75}};
-    const double more = parts == 3 ? 1.37 : 1.0, cu = (double)n_cu;
+    const double more = 0.26 + 0.37 * parts, cu = (double)n_cu;          // measured with two and with three
     const uint64_t steps = std::max<uint64_t>(1, (n_k + GRAD_DEPTH - 1) / GRAD_DEPTH);
     GradCut best{GradWay::TILES_64, 0, 1, (int32_t)(steps * GRAD_DEPTH)};
     double least = -1;
@@ -356,10 +357,10 @@ inline GradCut grad_cut(uint64_t n_i, uint64_t n_j, uint64_t n_k, int parts, int
         }
     }
     if (along && n_k && n_i && n_k <= GRAD_THIN_OUTS) {
-        const uint64_t rows = parts == 2 ? 32 : 16, k = n_k <= 32 ? 32 : n_k <= 64 ? 64 : n_k <= 128 ? 128 : GRAD_THIN_OUTS;
+        const uint64_t rows = GRAD_THIN_ROWS, k = n_k <= 32 ? 32 : n_k <= 64 ? 64 : n_k <= 128 ? 128 : GRAD_THIN_OUTS;
         const ThinShape s = grad_thin_shape(n_i, n_j, k, rows, n_cu);
         const double blocks = (double)((n_i + rows - 1) / rows), waves = (double)(s.grid / s.shares) * (THIN_THREADS / 64);
-        const double turns = blocks / waves, work = (double)(s.outs / 32) * (double)(k / 32) * (parts == 2 ? 0.27 : 0.24);
+        const double turns = blocks / waves, work = (double)(s.outs / 32) * (double)(k / 32) * 0.08 * parts;
         const double us = 3 + 0.05 * (double)s.lds / 1024 + std::max(turns * (s.lds * 2 <= THIN_LDS ? 2 : 1), 0.6) * work;
         if (us < least) best = GradCut{GradWay::THIN, 0, 1, (int32_t)(steps * GRAD_DEPTH)};
     }

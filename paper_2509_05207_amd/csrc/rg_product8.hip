@@ -513,8 +513,10 @@ __global__ void __launch_bounds__(THIN_THREADS) product_thin_kernel(ThinArgs t)
 }
 
 // ---------------------------------------------------------------- the backward pass
-// C[i][j] = sum over k of A(i, k) s[k] code[k][j]: dx (i: rows, k: outputs, held rows w) and dweight (i: outputs, k: rows, held rows x).  A's elements times the scale
-// go in as sums of PARTS bf16 numbers.
+// C[i][j] = sum over k of A(i, k) s[k] code[k][j]: dx (i: rows, k: outputs, held rows w) and dweight (i: outputs, k: rows, held rows x).  A's elements times the scale, in fp32,
+// go in as sums of three bf16 numbers, which hold all 24 bits, for 16-bit A as well: with two, 16 bits, one result of 200 was another bf16 number than the exact one's (150,000 x 256 to 512; of
+// fp32 sums one of 4,600), and fp32 gradients of 16-bit rows had no more than those 16 bits.
+constexpr int PARTS = GRAD_PARTS;
 struct GradArgs {
     const uint8_t *dy, *held;
     uint64_t dy_stride, held_stride;
@@ -535,7 +537,7 @@ struct GradArgs {
 };
 
 // A number as a sum of bf16 numbers: cut off, not rounded, but for the last, so that no part is beyond the range.  What an infinity or a NaN leaves is nothing.
-template <int PARTS> __device__ __forceinline__ void parts_of(float v, bf16 (&p)[PARTS])
+__device__ __forceinline__ void parts_of(float v, bf16 (&p)[PARTS])
 {
     const bool number = (__builtin_bit_cast(uint32_t, v) & 0x7F800000u) != 0x7F800000u;
 #pragma unroll
@@ -546,7 +548,7 @@ template <int PARTS> __device__ __forceinline__ void parts_of(float v, bf16 (&p)
     }
 }
 // Eight of them at once, of numbers; the largest of their magnitudes (passing over NaN, of which something is left over and is NaN).
-template <int PARTS> __device__ __forceinline__ float parts_of_numbers(const float (&from)[8], bf16x8 (&p)[PARTS])
+__device__ __forceinline__ float parts_of_numbers(const float (&from)[8], bf16x8 (&p)[PARTS])
 {
     float v[8], most = 0.f;
 #pragma unroll
@@ -573,12 +575,12 @@ template <int PARTS> __device__ __forceinline__ float parts_of_numbers(const flo
 }
 // Whether a lane of the wave has an infinity, of which the above makes a NaN.
 __device__ __forceinline__ bool beyond_numbers(float most) { return __builtin_expect(__ballot(most == __builtin_inff()) != 0, 0); }
-template <int PARTS> __device__ __forceinline__ void parts_of_any(const float (&v)[8], bf16x8 (&p)[PARTS])
+__device__ __forceinline__ void parts_of_any(const float (&v)[8], bf16x8 (&p)[PARTS])
 {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         bf16 one[PARTS];
-        parts_of<PARTS>(v[e], one);
+        parts_of(v[e], one);
 #pragma unroll
         for (int q = 0; q < PARTS; ++q) p[q][e] = one[q];
     }
@@ -605,9 +607,9 @@ __device__ __forceinline__ bf16x8 codes_as_bf16(const i32x2 &c)
 // Bound by the vector units: matrix operations keep them for 41 to 56 % of the time, and what parts dy hardly overlaps with them.  In tiles of 256:
 // dweight and the sums of 199,000 x 602 to 256 in fp32, three parts, 199 us behind other work (920 TFLOP/s of bf16) and 17 for the join; 150,000 x 512 to 256 in bf16 94 and 17; 8,192 x 4,096 to 4,096
 // 450 each way (1,220).
-template <typename T, int PARTS_, bool ALONG_, bool SUMS_, int WI_, int WJ_, int BI_, int BJ_>
+template <typename T, bool ALONG_, bool SUMS_, int WI_, int WJ_, int BI_, int BJ_>
 struct GradTile {
-    static constexpr int PARTS = PARTS_, WI = WI_, WJ = WJ_, BI = BI_, BJ = BJ_;
+    static constexpr int WI = WI_, WJ = WJ_, BI = BI_, BJ = BJ_;
     static constexpr bool ALONG = ALONG_, SUMS = SUMS_;              // SUMS: of dy's columns as well (dbias)
     static constexpr int THREADS = WI * WJ * 64, TI = WI * BI * 16, TJ = WJ * BJ * 16, DEPTH = 32;
     static constexpr int LEFT = PARTS * TI * DEPTH * 2, RIGHT = DEPTH * TJ * 2, STAGE = LEFT + RIGHT, LDS_BYTES = 2 * STAGE;
@@ -750,7 +752,7 @@ struct GradTile {
                 for (int e = 0; e < 8; ++e) sums[e] += v[e];
             }
             scaled(s, p, v);
-            most = fmaxf(most, parts_of_numbers<PARTS>(v, parts));
+            most = fmaxf(most, parts_of_numbers(v, parts));
             put_parts(p, parts, stage);
         }
 #pragma unroll
@@ -771,7 +773,7 @@ struct GradTile {
             float v[8];
             bf16x8 parts[PARTS];
             scaled(s, p, v);
-            parts_of_any<PARTS>(v, parts);
+            parts_of_any(v, parts);
             put_parts(p, parts, stage);
         }
     }
@@ -808,7 +810,7 @@ template <typename T, typename Tile>
 __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
 {
     extern __shared__ __align__(16) uint8_t lds[];
-    constexpr int BI = Tile::BI, BJ = Tile::BJ, PARTS = Tile::PARTS, DEPTH = Tile::DEPTH;
+    constexpr int BI = Tile::BI, BJ = Tile::BJ, DEPTH = Tile::DEPTH;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t mine = blockIdx.x * Tile::THREADS + threadIdx.x;
     if (!Tile::ALONG && a.gather && mine < (uint32_t)a.n_gather) a.gathered[mine] = *row_at<float>(a.gather + a.held_bytes - 4, a.gather_stride, mine);
@@ -892,7 +894,7 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
 }
 
 // dx of many rows and few outputs, which the tiles do at the pace of their starts and ends: w's codes lie in LDS, once for all rows that a workgroup does (where there is more than that holds, each
-// has a share of the columns), and a wave by itself takes R blocks of 16 rows of dy at a time, parted in registers (the next ones' elements on their way beside them spill).  The codes lie by blocks of 16 columns, row after row: what the
+// has a share of the columns), and a wave by itself takes 16 rows of dy at a time, parted in registers (the next ones' elements on their way beside them spill, and so do 32 rows).  The codes lie by blocks of 16 columns, row after row: what the
 // lanes read at a time is contiguous.  Bound as the tiles are: 150,000 x 256 to 512 in bf16 97 us (810 TFLOP/s of bf16), the matrix units
 // busy for 40 %.
 struct ThinGradArgs {
@@ -901,7 +903,7 @@ struct ThinGradArgs {
     int32_t shares;                  // of the columns
 };
 
-template <typename T, int PARTS, int KS, int R>
+template <typename T, int KS>
 __global__ void __launch_bounds__(THIN_THREADS) grad_thin_kernel(ThinGradArgs t)
 {
     constexpr int V = 16 / sizeof(T), WAVES = THIN_THREADS / 64, K = KS * 32;
@@ -910,7 +912,7 @@ __global__ void __launch_bounds__(THIN_THREADS) grad_thin_kernel(ThinGradArgs t)
     const GradArgs &a = t.g;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int32_t j0 = (int32_t)(blockIdx.x % (uint32_t)t.shares) * t.cols, mine = min(t.cols, a.n_j - j0);
-    const int32_t pairs = (mine + 31) / 32, turns = (int32_t)(gridDim.x / (uint32_t)t.shares) * WAVES, n_blocks = (a.n_i + 16 * R - 1) / (16 * R);
+    const int32_t pairs = (mine + 31) / 32, turns = (int32_t)(gridDim.x / (uint32_t)t.shares) * WAVES, n_blocks = (a.n_i + (int32_t)GRAD_THIN_ROWS - 1) / (int32_t)GRAD_THIN_ROWS;
     // Where few blocks are left for a last turn, several waves take one, each a part of the columns.
     const int32_t number = (int32_t)(blockIdx.x / (uint32_t)t.shares) * WAVES + wave, left_over = n_blocks % turns, parts = left_over ? turns / left_over : 1;
     const int32_t whole_turns = n_blocks - left_over;
@@ -926,20 +928,17 @@ __global__ void __launch_bounds__(THIN_THREADS) grad_thin_kernel(ThinGradArgs t)
     place();
     float *scales = reinterpret_cast<float *>(lds + (uint32_t)t.cols * K);
     const bool even = a.n_k % 32 == 0 && a.n_k == K;
-    Raw next[R][KS];
+    Raw next[KS];
     const auto load = [&](int32_t b) {
+        const T *row = row_at<T>(a.dy, a.dy_stride, min((int64_t)b * (int64_t)GRAD_THIN_ROWS + (lane & 15), (int64_t)a.n_i - 1));
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const T *row = row_at<T>(a.dy, a.dy_stride, min((int64_t)b * (16 * R) + i * 16 + (lane & 15), (int64_t)a.n_i - 1));
+        for (int s = 0; s < KS; ++s) {
+            const int32_t k = s * 32 + (lane >> 4) * 8;
+            if (even || k + 8 <= a.n_k) {
+                next[s] = load_raw<T, 8>(row + k);
+            } else {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const int32_t k = s * 32 + (lane >> 4) * 8;
-                if (even || k + 8 <= a.n_k) {
-                    next[i][s] = load_raw<T, 8>(row + k);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) next[i][s][e] = k + e < a.n_k ? row[k + e] : (T)0.f;
-                }
+                for (int e = 0; e < 8; ++e) next[s][e] = k + e < a.n_k ? row[k + e] : (T)0.f;
             }
         }
     };
@@ -964,22 +963,19 @@ __global__ void __launch_bounds__(THIN_THREADS) grad_thin_kernel(ThinGradArgs t)
     for (int32_t k = threadIdx.x; k < K; k += THIN_THREADS) scales[k] = k < a.n_k ? *row_at<float>(a.held + a.held_bytes - 4, a.held_stride, k) : 0.f;
     __syncthreads();
     while (rb < n_blocks) {
-        bf16x8 l[R][KS][PARTS];
+        bf16x8 l[KS][PARTS];
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const f32x4 lo = *reinterpret_cast<const f32x4 *>(scales + s * 32 + (lane >> 4) * 8), hi = *reinterpret_cast<const f32x4 *>(scales + s * 32 + (lane >> 4) * 8 + 4);
+            float v[8];
+            unpack<T, 8>(next[s], v);
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                float v[8];
-                unpack<T, 8>(next[i][s], v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = rounded(v[e], e < 4 ? lo[e] : hi[e - 4]);
-                if (beyond_numbers(parts_of_numbers<PARTS>(v, l[i][s]))) parts_of_any<PARTS>(v, l[i][s]);
-            }
+            for (int e = 0; e < 8; ++e) v[e] = rounded(v[e], e < 4 ? lo[e] : hi[e - 4]);
+            if (beyond_numbers(parts_of_numbers(v, l[s]))) parts_of_any(v, l[s]);
         }
-        const int32_t i0 = rb * (16 * R) + (lane & 15);
+        const int32_t i = rb * (int32_t)GRAD_THIN_ROWS + (lane & 15);
         for (int32_t pair = from_pair; pair < to_pair; ++pair) {
-            f32x4 acc[R][2] = {};
+            f32x4 acc[2] = {};
             // The next step's codes are on their way out of LDS while one is multiplied, and no more: all at once they spill.
             const uint8_t *codes = lds + (uint32_t)(pair * 2) * (K * 16) + ((lane >> 4) * 8 + ((lane & 15) >> 1)) * 16 + (lane & 1) * 8;
             i32x2 now[2] = {column_of_codes(codes), column_of_codes(codes + K * 16)};
@@ -993,28 +989,23 @@ __global__ void __launch_bounds__(THIN_THREADS) grad_thin_kernel(ThinGradArgs t)
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-                    for (int b = 0; b < 2; ++b)
-#pragma unroll
-                        for (int i = 0; i < R; ++i) acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[b], l[i][s][p], acc[i][b], 0, 0, 0);
+                    for (int b = 0; b < 2; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[b], l[s][p], acc[b], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if (i >= a.n_i) continue;
+            T *row = row_at<T>(a.out, a.out_stride, i) + j0;
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                if (i0 + i * 16 >= a.n_i) continue;
-                T *row = row_at<T>(a.out, a.out_stride, i0 + i * 16) + j0;
+            for (int k = 0; k < 8; k += V) {
+                const int32_t j = pair * 32 + k * 4 + (lane >> 4) * V;
+                float v[V];
 #pragma unroll
-                for (int k = 0; k < 8; k += V) {
-                    const int32_t j = pair * 32 + k * 4 + (lane >> 4) * V;
-                    float v[V];
+                for (int e = 0; e < V; ++e) v[e] = acc[(k + e) / 4][(k + e) % 4];
+                if (j + V <= mine) {
+                    store_pack<T, V>(row + j, v);
+                } else {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) v[e] = acc[i][(k + e) / 4][(k + e) % 4];
-                    if (j + V <= mine) {
-                        store_pack<T, V>(row + j, v);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < V; ++e)
-                            if (j + e < mine) row[j + e] = (T)v[e];
-                    }
+                    for (int e = 0; e < V; ++e)
+                        if (j + e < mine) row[j + e] = (T)v[e];
                 }
             }
         }
@@ -1221,17 +1212,16 @@ struct GradPlan {
     uint64_t scales_at, bias_at, bytes;  // sums of dweight, then of dx in the same place; w's scales; sums of dbias
 };
 
-GradPlan grad_plan(uint64_t n, uint64_t m, uint64_t d, uint32_t type, int n_cu, bool dx, bool dw, bool db)
+GradPlan grad_plan(uint64_t n, uint64_t m, uint64_t d, int n_cu, bool dx, bool dw, bool db)
 {
     GradPlan p{};
     uint64_t bytes = 0;
-    const int parts = type == RG_F32 ? 3 : 2;
     if (dx) {
-        p.dx = grad_cut(n, d, m, parts, n_cu, true);
+        p.dx = grad_cut(n, d, m, PARTS, n_cu, true);
         if (p.dx.splits > 1) bytes = std::max(bytes, (uint64_t)p.dx.splits * n * d * 4);
     }
     if (dw) {
-        p.dw = grad_cut(m, d, n, parts, n_cu, false);
+        p.dw = grad_cut(m, d, n, PARTS, n_cu, false);
         if (p.dw.splits > 1) bytes = std::max(bytes, (uint64_t)p.dw.splits * m * d * 4);
     }
     p.scales_at = (bytes + 15) / 16 * 16;
@@ -1255,40 +1245,39 @@ template <typename T, typename Tile> rg_status launch_grad(int32_t splits, const
     return RG_OK;
 }
 
-template <typename T, int PARTS, bool ALONG, bool SUMS> rg_status launch_grad_by(const GradCut &c, const GradArgs &g, hipStream_t st)
+template <typename T, bool ALONG, bool SUMS> rg_status launch_grad_by(const GradCut &c, const GradArgs &g, hipStream_t st)
 {
     switch (c.way) {
-    case GradWay::TILES_256: return launch_grad<T, GradTile<T, PARTS, ALONG, SUMS, 2, 4, 8, 4>>(c.splits, g, st);
-    case GradWay::TILES_128: return launch_grad<T, GradTile<T, PARTS, ALONG, SUMS, 2, 2, 4, 4>>(c.splits, g, st);
-    case GradWay::TILES_64_256: return launch_grad<T, GradTile<T, PARTS, ALONG, SUMS, 1, 4, 4, 4>>(c.splits, g, st);
-    default: return launch_grad<T, GradTile<T, PARTS, ALONG, SUMS, 2, 2, 2, 2>>(c.splits, g, st);
+    case GradWay::TILES_256: return launch_grad<T, GradTile<T, ALONG, SUMS, 2, 4, 8, 4>>(c.splits, g, st);
+    case GradWay::TILES_128: return launch_grad<T, GradTile<T, ALONG, SUMS, 2, 2, 4, 4>>(c.splits, g, st);
+    case GradWay::TILES_64_256: return launch_grad<T, GradTile<T, ALONG, SUMS, 1, 4, 4, 4>>(c.splits, g, st);
+    default: return launch_grad<T, GradTile<T, ALONG, SUMS, 2, 2, 2, 2>>(c.splits, g, st);
     }
 }
 
-template <typename T, int PARTS, int KS, int R> rg_status launch_grad_thin(const GradArgs &g, int n_cu, hipStream_t st)
+template <typename T, int KS> rg_status launch_grad_thin(const GradArgs &g, int n_cu, hipStream_t st)
 {
-    const ThinShape s = grad_thin_shape((uint64_t)g.n_i, (uint64_t)g.n_j, KS * 32, 16 * R, n_cu);
+    const ThinShape s = grad_thin_shape((uint64_t)g.n_i, (uint64_t)g.n_j, KS * 32, GRAD_THIN_ROWS, n_cu);
     static std::atomic<uint64_t> known{0};
-    RG_TRY(allow_lds(grad_thin_kernel<T, PARTS, KS, R>, (int)THIN_LDS, known));
-    hipLaunchKernelGGL((grad_thin_kernel<T, PARTS, KS, R>), dim3(s.grid), dim3(THIN_THREADS), s.lds, st, ThinGradArgs{g, (int32_t)s.outs, (int32_t)s.shares});
+    RG_TRY(allow_lds(grad_thin_kernel<T, KS>, (int)THIN_LDS, known));
+    hipLaunchKernelGGL((grad_thin_kernel<T, KS>), dim3(s.grid), dim3(THIN_THREADS), s.lds, st, ThinGradArgs{g, (int32_t)s.outs, (int32_t)s.shares});
     RG_HIP(hipGetLastError());
     return RG_OK;
 }
-template <typename T, int PARTS> rg_status launch_grad_thin_of(const GradArgs &g, int n_cu, hipStream_t st)
+template <typename T> rg_status launch_grad_thin_of(const GradArgs &g, int n_cu, hipStream_t st)
 {
-    constexpr int R = PARTS == 2 ? 2 : 1;
-    if (g.n_k <= 32) return launch_grad_thin<T, PARTS, 1, R>(g, n_cu, st);
-    if (g.n_k <= 64) return launch_grad_thin<T, PARTS, 2, R>(g, n_cu, st);
-    if (g.n_k <= 128) return launch_grad_thin<T, PARTS, 4, R>(g, n_cu, st);
-    return launch_grad_thin<T, PARTS, GRAD_THIN_OUTS / 32, R>(g, n_cu, st);
+    if (g.n_k <= 32) return launch_grad_thin<T, 1>(g, n_cu, st);
+    if (g.n_k <= 64) return launch_grad_thin<T, 2>(g, n_cu, st);
+    if (g.n_k <= 128) return launch_grad_thin<T, 4>(g, n_cu, st);
+    return launch_grad_thin<T, GRAD_THIN_OUTS / 32>(g, n_cu, st);
 }
 
 template <bool ALONG> rg_status launch_grad_of(uint32_t type, const GradCut &c, const GradArgs &g, hipStream_t st)
 {
     constexpr bool MAY = !ALONG;
-    if (type == RG_F32) return g.sums ? (launch_grad_by<float, 3, ALONG, MAY>(c, g, st)) : (launch_grad_by<float, 3, ALONG, false>(c, g, st));
-    if (type == RG_BF16) return g.sums ? (launch_grad_by<bf16, 2, ALONG, MAY>(c, g, st)) : (launch_grad_by<bf16, 2, ALONG, false>(c, g, st));
-    return g.sums ? (launch_grad_by<f16, 2, ALONG, MAY>(c, g, st)) : (launch_grad_by<f16, 2, ALONG, false>(c, g, st));
+    if (type == RG_F32) return g.sums ? (launch_grad_by<float, ALONG, MAY>(c, g, st)) : (launch_grad_by<float, ALONG, false>(c, g, st));
+    if (type == RG_BF16) return g.sums ? (launch_grad_by<bf16, ALONG, MAY>(c, g, st)) : (launch_grad_by<bf16, ALONG, false>(c, g, st));
+    return g.sums ? (launch_grad_by<f16, ALONG, MAY>(c, g, st)) : (launch_grad_by<f16, ALONG, false>(c, g, st));
 }
 
 rg_status launch_join(const Join &first, const Join &second, uint32_t type, hipStream_t st)
@@ -1356,7 +1345,7 @@ extern "C" rg_status rg_rows8_product_backward_workspace(uint64_t n_rows, uint64
     RG_TRY(check_types("dy", nullptr, RG_F32, type));
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
-    *bytes = grad_plan(n_rows, n_outs, n_cols, type, n_cu, want_dx, want_dweight, want_dbias).bytes;
+    *bytes = grad_plan(n_rows, n_outs, n_cols, n_cu, want_dx, want_dweight, want_dbias).bytes;
     return RG_OK;
 }
 
@@ -1379,7 +1368,7 @@ extern "C" rg_status rg_rows8_product_backward(const void *dy, uint64_t dy_strid
     }
     int n_cu = 0;
     RG_TRY(compute_units(&n_cu));
-    const GradPlan p = grad_plan(n_rows, n_outs, n_cols, type, n_cu, dx, dweight, dbias);
+    const GradPlan p = grad_plan(n_rows, n_outs, n_cols, n_cu, dx, dweight, dbias);
     RG_TRY(check_workspace(workspace, workspace_bytes, p.bytes));
     RG_TRY(check_grid(p.dx.tiles * (uint64_t)p.dx.splits, 512));
     RG_TRY(check_grid(p.dw.tiles * (uint64_t)p.dw.splits, 512));
@@ -1418,8 +1407,8 @@ extern "C" rg_status rg_rows8_product_backward(const void *dy, uint64_t dy_strid
         g.n_i = (int32_t)n_rows; g.n_k = (int32_t)n_outs; g.k_each = p.dx.each; g.tiles = (uint32_t)p.dx.tiles;
         g.scales = scales;
         if (p.dx.way == GradWay::THIN) {
-            if (type == RG_F32) return launch_grad_thin_of<float, 3>(g, n_cu, st);
-            return type == RG_BF16 ? launch_grad_thin_of<bf16, 2>(g, n_cu, st) : launch_grad_thin_of<f16, 2>(g, n_cu, st);
+            if (type == RG_F32) return launch_grad_thin_of<float>(g, n_cu, st);
+            return type == RG_BF16 ? launch_grad_thin_of<bf16>(g, n_cu, st) : launch_grad_thin_of<f16>(g, n_cu, st);
         }
         if (by_tiles && !dweight) {
             hipLaunchKernelGGL(scales_kernel, dim3((uint32_t)((n_outs + 255) / 256)), dim3(256), 0, st, g.held, g.held_stride, g.held_bytes, g.n_k, scales);

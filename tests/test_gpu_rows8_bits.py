@@ -1,0 +1,44 @@
+"""How many bits of dy the gradients on held rows have, whatever its type.
+
+With one element of a row of dy (of a column, for dweight) that is not zero, a gradient is that element times its scale, which is rounded to 24 bits (2^-24 of it), times a code.  Of the parts that the
+product goes in as, which hold all 24 bits, each gives an exact term, and two of three additions may round, in whatever direction: 2^-23 of the sum of parts, which the first two exceed by 2^-7 at
+most.  Sums with zeros are exact.  So a result before it is rounded to its type is off by no more than 2^-24 + 2 2^-23 (1 + 2^-7) < 3 2^-23 of itself, and rounding does not change an order: it lies
+between what both ends of that range are rounded to."""
+import pytest
+import torch
+
+from test_gpu_rows8 import made, random_held
+
+pytestmark = pytest.mark.gpu
+OFF = 3 * 2.0 ** -23
+
+
+@pytest.fixture(scope="module")
+def rg():
+    from paper_2509_05207_amd import binding
+    binding.lib()
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return binding
+
+
+def between(what, got, ref):
+    lo, hi = (ref - OFF * ref.abs()).to(got.dtype), (ref + OFF * ref.abs()).to(got.dtype)
+    bad = ~((lo <= got) & (got <= hi))
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} of {bad.numel()}, first at {bad.nonzero()[0].tolist()}: {float(got[bad][0])!r} for {float(ref[bad][0])!r}"
+
+
+@pytest.mark.parametrize("n,m,d", [(4, 64, 256), (65, 33, 130), (300, 270, 602), (5000, 257, 130), (20_000, 64, 128), (70_001, 256, 96)])
+@pytest.mark.parametrize("dtype,weight", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float16, torch.float16), (torch.float16, torch.float32)], ids=str)
+def test_single_terms(rg, n, m, d, dtype, weight):
+    x, qx, sx = random_held(n, d, 1)
+    w, qw, sw = random_held(m, d, 2)
+    values = made(n, m, dtype, 7)
+    at = torch.randint(m, (n,), generator=torch.Generator().manual_seed(3)).cuda()
+    dy = torch.zeros_like(values).scatter_(1, at[:, None], values.gather(1, at[:, None]))
+    dx, _, _ = rg.rg_rows8_product_backward(dy, x, w, d)
+    between("dx", dx, (values.gather(1, at[:, None]).double() * sw.double()[at][:, None]) * qw[at])
+    at = torch.randint(n, (m,), generator=torch.Generator().manual_seed(4)).cuda()
+    dy = torch.zeros_like(values).scatter_(0, at[None], values.gather(0, at[None]))
+    _, dw, db = rg.rg_rows8_product_backward(dy, x, w, d, weight_dtype=weight)
+    between("dweight", dw, (values.gather(0, at[None])[0].double() * sx.double()[at])[:, None] * qx[at])
+    assert torch.equal(db, values.gather(0, at[None])[0].to(weight))
