@@ -566,8 +566,9 @@ rg_status rg_dequantize_rows(const void *held, uint64_t held_stride, uint64_t n_
 /*
  * rg_rows8_product -- y = x w^T + bias of held rows x [n_rows] and held weights w [n_outs], a scale for each row of either:
  *     y[n][m] = s_x[n] * s_w[m] * (sum over c of code_x[n][c] * code_w[m][c]) + bias[m].
- * The sum is exact.  Results of RG_F32 are off by half a step, and 2^-23 of that; for 16 bits what follows the sum is in fp32.  A row
- * with a scale of NaN makes its results NaN.
+ * The sum is exact.  Results of RG_F32 are off by half a step and 2^-44 of what the product and the bias are by themselves (2^-149 at
+ * least); for 16 bits what follows the sum is in fp32.  A result's bits do not depend on other rows' values.  A row with a scale of NaN makes its
+ * results NaN.
  *
  *   bias         dev, [n_outs] of bias_type (RG_F32, or the same as `type`), or NULL
  *   y            dev, [n_rows][n_outs] of `type`

@@ -72,24 +72,51 @@ __device__ __forceinline__ float wide_value(int32_t sum, uint32_t sx, uint32_t s
     return (float)((double)sum * ((double)__builtin_bit_cast(float, sx) * (double)__builtin_bit_cast(float, sw)) + (double)bias);
 }
 
+// A result of 16 bits before its rounding to them.  (Where that is fp16 the compiler makes one instruction of some of these and their rounding, which rounds once, so that bits would depend on a result's place.)
+template <typename T> __device__ __forceinline__ float in_32_bits(float a, float b, float c)
+{
+    float v = fmaf(a, b, c);
+    if constexpr (__is_same(T, f16)) asm("" : "+v"(v));
+    return v;
+}
+
+// A product in two parts and the bias, added up.
+__device__ __forceinline__ float with_bias(float t, float rest, float bias)
+{
+    const float whole = t + bias, of_bias = whole - t;
+    return whole + (rest + ((t - (whole - of_bias)) + (bias - of_bias)));
+}
+
 // The same in 32.  T of 16 bits: the sum and the scales' product are rounded, and so is the result before it is rounded to T.  T of 32 bits: the sum has up to 31 bits, the scales' product 48,
-// and both have a part that 32 bits leave over, as have their product and the sum with the bias; with these the result is off by its own rounding and no more than 2^-23 of that.
+// and both have a part that 32 bits leave over, as have their product and the sum with the bias; with these the result is off by its own rounding and less than ten times 2^-48 of what the product and the
+// bias are by themselves.
 template <typename T> __device__ __forceinline__ float product_value(int32_t sum, float sx, float sw, float bias)
 {
     const float p = rounded(sx, sw), hi = (float)sum;
-    if constexpr (sizeof(T) == 2) return fmaf(hi, p, bias);
-    const float p_rest = fmaf(sx, sw, -p), lo = (float)(sum - (int32_t)hi), t = rounded(hi, p), t_rest = fmaf(hi, p, -t);
-    const float whole = t + bias, of_bias = whole - t;
-    return whole + (fmaf(hi, p_rest, fmaf(lo, p, t_rest)) + ((t - (whole - of_bias)) + (bias - of_bias)));
+    if constexpr (sizeof(T) == 2) return in_32_bits<T>(hi, p, bias);
+    const float lo = (float)(sum - (int32_t)hi), t = rounded(hi, p);
+    return with_bias(t, fmaf(hi, fmaf(sx, sw, -p), fmaf(lo, p, fmaf(hi, p, -t))), bias);
 }
 // Scales and biases of which no part of the above leaves the range.
 __device__ __forceinline__ bool moderate(float scale) { return fabsf(scale) >= 0x1p-38f && fabsf(scale) <= 0x1p48f; }
 __device__ __forceinline__ bool moderate_bias(float b) { return fabsf(b) < 0x1p120f; }
-// Others: the scales' mantissas and the powers of two apart, the bias added last.
+// Others: the same steps on the scales' mantissas, whose powers of two come in before the bias does; what is near the end of the range is added up 2^8 below it.  Powers of two are exact, so that results of moderate
+// scales are the same to the bit either way, and do not depend on what is done beside them.
 template <typename T> __device__ __forceinline__ float product_value_apart(int32_t sum, float sx, float sw, float bias)
 {
-    return ldexpf(product_value<T>(sum, __builtin_amdgcn_frexp_mantf(sx), __builtin_amdgcn_frexp_mantf(sw), 0.f), __builtin_amdgcn_frexp_expf(sx) + __builtin_amdgcn_frexp_expf(sw)) + bias;
+    const float mx = __builtin_amdgcn_frexp_mantf(sx), mw = __builtin_amdgcn_frexp_mantf(sw), p = rounded(mx, mw), hi = (float)sum;
+    const int power = __builtin_amdgcn_frexp_expf(sx) + __builtin_amdgcn_frexp_expf(sw);
+    if constexpr (sizeof(T) == 2) {
+        const int of_p = min(max(power, -100), 100);
+        return in_32_bits<T>(ldexpf(hi, power - of_p), ldexpf(p, of_p), bias);
+    }
+    const float lo = (float)(sum - (int32_t)hi), t = rounded(hi, p);
+    const int down = fabsf(ldexpf(t, power)) >= 0x1p120f || fabsf(bias) >= 0x1p120f ? 8 : 0;
+    const float at = ldexpf(t, power - down), b = ldexpf(bias, -down), v = with_bias(at, ldexpf(fmaf(hi, fmaf(mx, mw, -p), fmaf(lo, p, fmaf(hi, p, -t))), power - down), b);
+    return fabsf(at + b) < __builtin_inff() ? ldexpf(v, down) : at + b;              // (an infinity has no rest)
 }
+// A row of zeros has the least scale that there is.  Of a sum of zero the first way makes the bias whatever the scales, so rows of that scale go it too, where their codes, or all their sums, are zero.
+__device__ __forceinline__ bool least_scale(float scale) { return scale == 0x1p-126f; }
 
 __device__ const i32x4 ZERO_CHUNK = {0, 0, 0, 0};
 
@@ -294,12 +321,41 @@ template <typename T, typename Tile> __device__ __forceinline__ void finish_tile
         else if (a.bias_type == RG_BF16) load_bias<Tile::BN * 4, V>(static_cast<const bf16 *>(a.bias), p.m0 + first, a.n_outs, b);
         else load_bias<Tile::BN * 4, V>(static_cast<const f16 *>(a.bias), p.m0 + first, a.n_outs, b);
     }
-    bool fine = true;
+    const float *sx = scales + (wave / Tile::WN) * Tile::BM * 16 + (lane & 15);
+    const auto sw = [&](int k) { return scales[Tile::of_output(first + k / V * V * 4 + k % V)]; };
+    const auto sums = [&](int i, int k, float x, float w) { return sum_of_codes(acc[i][k / 4][k % 4], __builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, w), scale_in_sum(a.n_cols)); };
+    uint32_t far = 0, least = 0;                                   // (bits, so that the compiler makes no branches of them)
 #pragma unroll
-    for (int i = 0; i < Tile::BM; ++i) fine = fine && moderate(scales[(wave / Tile::WN) * Tile::BM * 16 + (lane & 15) + i * 16]);
+    for (int i = 0; i < Tile::BM; ++i) {
+        least |= (uint32_t)least_scale(sx[i * 16]);
+        far |= (uint32_t)!moderate(sx[i * 16]) & (uint32_t)!least_scale(sx[i * 16]);
+    }
 #pragma unroll
-    for (int k = 0; k < Tile::BN * 4; ++k) fine = fine && moderate(scales[Tile::of_output(first + k / V * V * 4 + k % V)]) && moderate_bias(b[k]);
-    if (__ballot(!fine)) store_tile<T, Tile, true>(a, p, acc, scales, b);
+    for (int k = 0; k < Tile::BN * 4; ++k) {
+        least |= (uint32_t)least_scale(sw(k));
+        far |= ((uint32_t)!moderate(sw(k)) & (uint32_t)!least_scale(sw(k))) | (uint32_t)!moderate_bias(b[k]);
+    }
+    if (__ballot(least)) {                                         // (by rows and outputs, of which most have none: all at once they spill)
+#pragma unroll
+        for (int i = 0; i < Tile::BM; ++i) {
+            const float x = sx[i * 16];
+            if (!__ballot(least_scale(x))) continue;
+            int32_t left = 0;
+#pragma unroll
+            for (int k = 0; k < Tile::BN * 4; ++k) left |= sums(i, k, x, sw(k));
+            far |= (uint32_t)least_scale(x) & (uint32_t)(left != 0);
+        }
+#pragma unroll
+        for (int k = 0; k < Tile::BN * 4; ++k) {
+            const float w = sw(k);
+            if (!__ballot(least_scale(w))) continue;
+            int32_t left = 0;
+#pragma unroll
+            for (int i = 0; i < Tile::BM; ++i) left |= sums(i, k, sx[i * 16], w);
+            far |= (uint32_t)least_scale(w) & (uint32_t)(left != 0);
+        }
+    }
+    if (__ballot(far)) store_tile<T, Tile, true>(a, p, acc, scales, b);
     else store_tile<T, Tile, false>(a, p, acc, scales, b);
 }
 
@@ -451,22 +507,41 @@ __global__ void __launch_bounds__(THIN_THREADS) product_thin_kernel(ThinArgs t)
         for (; c + 4 <= chunks; c += 4) __builtin_amdgcn_global_load_lds(row + (c + (lane >> 4)) * 16, (__attribute__((address_space(3))) void *)(to + c * 256), 16, 0, 0);
         if (c + (lane >> 4) < chunks) *reinterpret_cast<i32x4 *>(to + c * 256 + lane * 16) = *(const __attribute__((address_space(1))) i32x4 *)(row + (c + (lane >> 4)) * 16);
     }
-    bool w_fine = true;
+    const bool scales_in = scale_in_sum(a.n_cols);
+    // Whether a row of the least scale has other codes than zeros, by its words in this lane's chunks; behind the last ones in a row lies its scale.
+    constexpr uint32_t LEAST_BITS = 0x00800000u;
+    const auto words_of = [&](const i32x4 &v, int32_t c) { return v[0] | v[1] | v[2] | (scales_in && c == chunks - 1 ? v[3] ^ (int)LEAST_BITS : v[3]); };
     for (int32_t m = threadIdx.x; m < blocks * 16; m += THIN_THREADS) {
         const int32_t at = m0 + min(m, mine - 1);
         scales[m] = *row_at<float>(a.w + a.held_bytes - 4, a.w_stride, at);
         bias[m] = bias_at(a, at);
-        w_fine = w_fine && moderate(scales[m]) && moderate_bias(bias[m]);
     }
     __syncthreads();                                               // and what was loaded is there
+    bool w_fine = true;
+    for (int32_t r = threadIdx.x; r < blocks * 16; r += THIN_THREADS) {
+        const int32_t m = r / 32 * 32 + thin_output<V>(r % 32);
+        bool fine = moderate(scales[m]);
+        if (least_scale(scales[m])) {
+            int words = 0;
+            for (int32_t c = 0; c < chunks; ++c) words |= words_of(*reinterpret_cast<const i32x4 *>(lds + (uint32_t)(r / 16 * chunks + c) * 256 + r % 16 * 16), c);
+            fine = words == 0;
+        }
+        w_fine = w_fine && fine && moderate_bias(bias[m]);
+    }
     if (!w_fine) *all_fine = 0;
     __syncthreads();
     w_fine = *all_fine;
-    const bool scales_in = scale_in_sum(a.n_cols);
     const int32_t n_blocks = (a.n_rows + 15) / 16;
     while (rb < n_blocks) {
         if (rb + turns < n_blocks) load(rb + turns, next, next_sx);
-        const bool fine = !__ballot(!(w_fine && moderate(sx)));
+        bool x_fine = moderate(sx);
+        if (__ballot(least_scale(sx))) {
+            int words = 0;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) words |= words_of(x[k], k * 4 + (lane >> 4));
+            x_fine = x_fine || (least_scale(sx) && words == 0);
+        }
+        const bool fine = !__ballot(!(w_fine && x_fine));
         const int32_t n = rb * 16 + (lane & 15);
         T *y = row_at<T>(a.y, a.y_stride, n) + m0;
         for (int32_t pair = 0; pair < blocks; pair += 2) {
