@@ -687,7 +687,7 @@ struct GradTile {
     static constexpr int WI = WI_, WJ = WJ_, BI = BI_, BJ = BJ_;
     static constexpr bool ALONG = ALONG_, SUMS = SUMS_;              // SUMS: of dy's columns as well (dbias)
     static constexpr int THREADS = WI * WJ * 64, TI = WI * BI * 16, TJ = WJ * BJ * 16, DEPTH = 32;
-    static constexpr int LEFT = PARTS * TI * DEPTH * 2, RIGHT = DEPTH * TJ * 2, STAGE = LEFT + RIGHT, LDS_BYTES = 2 * STAGE;
+    static constexpr int LEFT = PARTS * TI * DEPTH * 2, RIGHT = DEPTH * TJ * 2, STAGE = LEFT + RIGHT, LDS_BYTES = 2 * STAGE + (SUMS ? THREADS * 32 : 0);      // behind the stages the threads' sums of dy's columns
     static constexpr int PACKS = TI * DEPTH / 8 / THREADS, CHUNKS = (DEPTH * TJ / 16 + THREADS - 1) / THREADS;
     static_assert(PACKS * THREADS * 8 == TI * DEPTH && LDS_BYTES <= 160 * 1024 && TI >= 64 && TJ >= 64, "");
     typedef typename PackOf<T, 8>::type Raw;
@@ -899,7 +899,16 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
     // Of the two waves of a vector unit one prepares the next step before it multiplies, the other behind it: the one's conversions go beside the other's matrix operations.
     const bool early = wave < 4;
     f32x4 acc[BI][BJ] = {};
+    // Sums of dy's columns in two levels, so that no more than 16 elements are added up in a row: what a thread has of eight steps goes onto what it has in LDS.  (The largest tile has no registers left.)
     float sums[8] = {};
+    f32x4 *const mine_of_sums = reinterpret_cast<f32x4 *>(lds + 2 * Tile::STAGE) + threadIdx.x * 2;
+    const auto keep_sums = [&] {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) mine_of_sums[h] += f32x4{sums[h * 4], sums[h * 4 + 1], sums[h * 4 + 2], sums[h * 4 + 3]};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[e] = 0.f;
+    };
+    if constexpr (Tile::SUMS) mine_of_sums[0] = mine_of_sums[1] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (k_first < k_end) {
         typename Tile::Step step;
         typename Tile::Source src(a, i0, j0, (int32_t)k_first, k_end);
@@ -935,16 +944,17 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (!early && s < last) prepare(other);
+            if constexpr (Tile::SUMS)
+                if ((s & 7) == 6) keep_sums();                     // (step s + 1 is in)
             Tile::arrive();
         }
     }
     if constexpr (Tile::SUMS) {
         // What the threads have of a column, added up in their order.
         if (a.sums && j0 == 0) {
-            float *parts = reinterpret_cast<float *>(lds);
-            constexpr int PACKS_ACROSS = Tile::TI / 8, GROUPS = Tile::THREADS / PACKS_ACROSS;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) parts[(threadIdx.x / PACKS_ACROSS) * Tile::TI + threadIdx.x % PACKS_ACROSS * 8 + e] = sums[e];
+            const float *parts = reinterpret_cast<const float *>(lds + 2 * Tile::STAGE);           // rows of TI, of which a thread has eight
+            constexpr int GROUPS = Tile::THREADS * 8 / Tile::TI;
+            keep_sums();
             __syncthreads();
             if (threadIdx.x < Tile::TI && i0 + (int32_t)threadIdx.x < a.n_i) {
                 float v = 0.f;

@@ -42,3 +42,14 @@ def test_single_terms(rg, n, m, d, dtype, weight):
     _, dw, db = rg.rg_rows8_product_backward(dy, x, w, d, weight_dtype=weight)
     between("dweight", dw, (values.gather(0, at[None])[0].double() * sx.double()[at])[:, None] * qx[at])
     assert torch.equal(db, values.gather(0, at[None])[0].to(weight))
+
+
+@pytest.mark.parametrize("n,m,d", [(16_384, 4096, 4096), (70_001, 256, 130), (30_011, 5, 40), (8192, 300, 64)])
+@pytest.mark.parametrize("want_dweight", [True, False])
+def test_long_sums_of_columns(rg, n, m, d, want_dweight):
+    """dbias is off by (64 + rows / 256) 2^-24 sum |dy| at most: no sum of it is longer than that.  The same number in all rows, whose last bits every addition beyond 512 of them loses, if they are added up one by one."""
+    value = 1 + 2.0 ** -15 - 2.0 ** -23
+    dy = torch.full((n, m), value, device="cuda")
+    x = torch.zeros((n, (d + 19) // 16 * 16), dtype=torch.uint8, device="cuda") if want_dweight else None
+    _, _, db = rg.rg_rows8_product_backward(dy, x, None, d, want_dx=False, want_dweight=want_dweight)
+    assert bool(((db.double() - n * value).abs() <= (64 + n / 256) * 2.0 ** -24 * n * value).all()), float((db.double() / (n * value) - 1).abs().max() * 2 ** 24)
