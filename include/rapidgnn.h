@@ -584,7 +584,8 @@ rg_status rg_rows8_product(const void *x, uint64_t x_stride, uint64_t n_rows, co
  * rg_rows8_product_backward -- what dy gives of it, x and w as what they stand for (the rounding to codes counts as the identity):
  *     dx[n][c] = sum over m of dy[n][m] * s_w[m] * code_w[m][c],
  *     dweight[m][c] = sum over n of dy[n][m] * s_x[n] * code_x[n][c],   dbias[m] = sum over n of dy[n][m].
- * All that it takes of the forward pass are the held rows.  dy times the scale goes into the products in 24 bits, whatever dy's type; sums are in 32.
+ * All that it takes of the forward pass are the held rows.  dy times the scale goes into the products in 24 bits, whatever dy's type; sums are in 32.  Where
+ * it is beyond fp32, and dy is not, codes other than zero make infinities of it, and codes of zero nothing; an infinity of dy makes a NaN of them.
  *
  *   dy           dev, [n_rows][n_outs] of `type`
  *   dx           dev, [n_rows][n_cols] of `type`, or NULL: not wanted (then w may be NULL)

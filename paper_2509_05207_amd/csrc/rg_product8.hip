@@ -650,14 +650,18 @@ __device__ __forceinline__ float parts_of_numbers(const float (&from)[8], bf16x8
 }
 // Whether a lane of the wave has an infinity, of which the above makes a NaN.
 __device__ __forceinline__ bool beyond_numbers(float most) { return __builtin_expect(__ballot(most == __builtin_inff()) != 0, 0); }
-__device__ __forceinline__ void parts_of_any(const float (&v)[8], bf16x8 (&p)[PARTS])
+// Eight products dy[e] * scale(e) of any kind.  Of numbers whose product is beyond the range every part is the largest bf16 number: a code other than zero makes an infinity of them, a code of zero leaves nothing, where an
+// infinity would make a NaN of it.
+template <typename S> __device__ __forceinline__ void parts_of_any(const float (&dy)[8], const S &scale, bf16x8 (&p)[PARTS])
 {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+        const float v = rounded(dy[e], scale(e));
+        const bool beyond = fabsf(v) == __builtin_inff() && fabsf(dy[e]) < __builtin_inff() && fabsf(scale(e)) < __builtin_inff();
         bf16 one[PARTS];
-        parts_of(v[e], one);
+        parts_of(v, one);
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q) p[q][e] = one[q];
+        for (int q = 0; q < PARTS; ++q) p[q][e] = beyond ? (bf16)copysignf(0x1.FEp+127f, v) : one[q];
     }
 }
 
@@ -800,12 +804,6 @@ struct GradTile {
             for (int c = 0; c < CHUNKS; ++c) s.codes[c] = *reinterpret_cast<const i32x4 *>(codes_at(k0, c));
         }
     };
-    static __device__ __forceinline__ void scaled(const Step &s, int p, float (&v)[8])
-    {
-        unpack<T, 8>(s.dy[p], v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = rounded(v[e], s.scale[ALONG ? e : p]);
-    }
     static __device__ __forceinline__ void put_parts(int p, const bf16x8 (&parts)[PARTS], uint8_t *stage)
     {
         const int q = p * THREADS + (int)threadIdx.x;
@@ -821,12 +819,13 @@ struct GradTile {
         for (int p = 0; p < PACKS; ++p) {
             float v[8];
             bf16x8 parts[PARTS];
+            unpack<T, 8>(s.dy[p], v);
             if constexpr (SUMS) {
-                unpack<T, 8>(s.dy[p], v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sums[e] += v[e];
             }
-            scaled(s, p, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = rounded(v[e], s.scale[ALONG ? e : p]);
             most = fmaxf(most, parts_of_numbers(v, parts));
             put_parts(p, parts, stage);
         }
@@ -847,8 +846,8 @@ struct GradTile {
         for (int p = 0; p < PACKS; ++p) {
             float v[8];
             bf16x8 parts[PARTS];
-            scaled(s, p, v);
-            parts_of_any(v, parts);
+            unpack<T, 8>(s.dy[p], v);
+            parts_of_any(v, [&](int e) { return s.scale[ALONG ? e : p]; }, parts);
             put_parts(p, parts, stage);
         }
     }
@@ -1052,11 +1051,12 @@ __global__ void __launch_bounds__(THIN_THREADS) grad_thin_kernel(ThinGradArgs t)
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             const f32x4 lo = *reinterpret_cast<const f32x4 *>(scales + s * 32 + (lane >> 4) * 8), hi = *reinterpret_cast<const f32x4 *>(scales + s * 32 + (lane >> 4) * 8 + 4);
-            float v[8];
-            unpack<T, 8>(next[s], v);
+            const auto scale = [&](int e) { return e < 4 ? lo[e] : hi[e - 4]; };
+            float dy[8], v[8];
+            unpack<T, 8>(next[s], dy);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = rounded(v[e], e < 4 ? lo[e] : hi[e - 4]);
-            if (beyond_numbers(parts_of_numbers(v, l[s]))) parts_of_any(v, l[s]);
+            for (int e = 0; e < 8; ++e) v[e] = rounded(dy[e], scale(e));
+            if (beyond_numbers(parts_of_numbers(v, l[s]))) parts_of_any(dy, scale, l[s]);
         }
         const int32_t i = rb * (int32_t)GRAD_THIN_ROWS + (lane & 15);
         for (int32_t pair = from_pair; pair < to_pair; ++pair) {

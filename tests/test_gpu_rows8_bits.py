@@ -7,7 +7,7 @@ between what both ends of that range are rounded to."""
 import pytest
 import torch
 
-from test_gpu_rows8 import made, random_held
+from test_gpu_rows8 import made, packed, random_held
 
 pytestmark = pytest.mark.gpu
 OFF = 3 * 2.0 ** -23
@@ -53,3 +53,27 @@ def test_long_sums_of_columns(rg, n, m, d, want_dweight):
     x = torch.zeros((n, (d + 19) // 16 * 16), dtype=torch.uint8, device="cuda") if want_dweight else None
     _, _, db = rg.rg_rows8_product_backward(dy, x, None, d, want_dx=False, want_dweight=want_dweight)
     assert bool(((db.double() - n * value).abs() <= (64 + n / 256) * 2.0 ** -24 * n * value).all()), float((db.double() / (n * value) - 1).abs().max() * 2 ** 24)
+
+
+@pytest.mark.parametrize("n,m,d", [(70, 40, 100), (300, 270, 602), (20_000, 64, 128), (5000, 257, 130), (4096, 2060, 600)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_products_beyond_the_range(rg, n, m, d, dtype, sign):
+    """dy and a scale that are numbers, whose product is none in 32 bits: an infinity with a code other than zero, nothing with a code of zero, and all else as it was."""
+    _, qx, sx = random_held(n, d, 1)
+    _, qw, sw = random_held(m, d, 2)
+    i, j = n // 2, m // 3
+    sx[i], sw[j] = 100.0, 100.0
+    qx[i], qw[j] = torch.arange(d, device="cuda") % 5 - 2, torch.arange(d, device="cuda") % 3 - 1
+    x, w = packed(qx, sx), packed(qw, sw)
+    dy = made(n, m, dtype, 7)
+    dy[i, j] = 0
+    clean = rg.rg_rows8_product_backward(dy, x, w, d)
+    dy[i, j] = sign * 2.0 ** 127
+    got = rg.rg_rows8_product_backward(dy, x, w, d)
+    for a, b, row, codes in ((got[0], clean[0], i, qw[j]), (got[1], clean[1], j, qx[i])):
+        keep = torch.arange(a.shape[0], device="cuda") != row
+        assert torch.equal(a[keep], b[keep])
+        none = codes == 0
+        assert torch.equal(a[row][none], b[row][none]) and bool((a[row][~none] == sign * torch.sign(codes[~none]) * float("inf")).all())
+    assert float(got[2][j]) == sign * 2.0 ** 127
