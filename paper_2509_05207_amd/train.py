@@ -102,12 +102,20 @@ class Muon:
             p.grad = None
 
 
-def held_tables(rg, W):
-    """The feature tables held in 8 bits, where they were: local rows on the device, remote ones there or in pinned host memory."""
+def held_tables(rg, W, at_once=64 << 20):
+    """The feature tables held in 8 bits, where they were: local rows on the device, remote ones there or in pinned host memory.  The latter, which may be too many for the device, by parts of `at_once` bytes."""
     tables = []
     for table in (W.local_rows, W.remote_rows):
-        held = rg.rg_quantize_rows(table[:, : W.cfg.feat_dim])
-        tables.append(held if table.is_cuda else held.cpu().pin_memory())
+        rows = table[:, : W.cfg.feat_dim]
+        if table.is_cuda:
+            tables.append(rg.rg_quantize_rows(rows))
+            continue
+        held = synth.pinned_empty((len(rows), rg.rg_rows8_bytes(W.cfg.feat_dim)), torch.uint8)
+        part = torch.empty((max(1, min(len(held), at_once // held.shape[1])), held.shape[1]), dtype=torch.uint8, device="cuda")
+        for first in range(0, len(held), len(part)):
+            n = min(len(part), len(held) - first)
+            held[first: first + n].copy_(rg.rg_quantize_rows(rows[first: first + n], out=part[:n]))      # (waits until it is there)
+        tables.append(held)
     return tables
 
 
