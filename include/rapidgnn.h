@@ -592,7 +592,8 @@ rg_status rg_rows8_product(const void *x, uint64_t x_stride, uint64_t n_rows, co
  *   dweight      dev, [n_outs][n_cols] of weight_type (RG_F32, or the same as `type`), or NULL (then x may be NULL)
  *   dbias        dev, [n_outs] of weight_type, or NULL
  *   workspace    dev, 16-byte aligned, as many bytes as rg_rows8_product_backward_workspace says for the same sizes and the same results wanted
- * n_rows, n_outs <= 2^30, either may be 0: sums of nothing are zero.  Results overlap neither the inputs nor one another.
+ * n_rows, n_outs <= 2^30, either may be 0: sums of nothing are zero.  RG_ERANGE where a launch cannot hold a result's tiles (beyond 2^37 elements), or dbias by itself (the last 63 of 2^30).
+ * Results overlap neither the inputs nor one another.
  */
 rg_status rg_rows8_product_backward_workspace(uint64_t n_rows, uint64_t n_outs, uint64_t n_cols, uint32_t type, int want_dx, int want_dweight, int want_dbias,
                                               uint64_t *bytes);

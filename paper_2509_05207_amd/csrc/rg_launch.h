@@ -333,15 +333,16 @@ inline ThinShape grad_thin_shape(uint64_t n, uint64_t d, uint64_t k, uint64_t ro
 // compute unit, or as many as the fullest has, by its start and end and its steps; splits write their sums and another launch adds them up.
 inline GradCut grad_cut(uint64_t n_i, uint64_t n_j, uint64_t n_k, int parts, int n_cu, bool along)
 {
-    struct Cost { GradWay way; uint64_t ti, tj; double alone, alone_step, start, step; };
-    static constexpr Cost COSTS[] = {{GradWay::TILES_64, 64, 64, 2.3, 0.7, 0.67, 0.25}, {GradWay::TILES_64_256, 64, 256, 3.5, 0.9, 1.5, 0.62},
-                                     {GradWay::TILES_128, 128, 128, 4, 1.05, 1.8, 0.64}, {GradWay::TILES_256, 256, 256, 8, 1.7, 10, 1.75}};
+    struct Cost { GradWay way; uint64_t ti, tj, threads; double alone, alone_step, start, step; };
+    static constexpr Cost COSTS[] = {{GradWay::TILES_64, 64, 64, 256, 2.3, 0.7, 0.67, 0.25}, {GradWay::TILES_64_256, 64, 256, 256, 3.5, 0.9, 1.5, 0.62},
+                                     {GradWay::TILES_128, 128, 128, 256, 4, 1.05, 1.8, 0.64}, {GradWay::TILES_256, 256, 256, 512, 8, 1.7, 10, 1.75}};
     const double more = 0.26 + 0.37 * parts, cu = (double)n_cu;          // measured with two and with three
     const uint64_t steps = std::max<uint64_t>(1, (n_k + GRAD_DEPTH - 1) / GRAD_DEPTH);
     GradCut best{GradWay::TILES_64, 0, 1, (int32_t)(steps * GRAD_DEPTH)};
     double least = -1;
     for (const Cost &c : COSTS) {
         const uint64_t tiles = (n_i + c.ti - 1) / c.ti * ((n_j + c.tj - 1) / c.tj);
+        if (tiles * c.threads > MAX_WORK_ITEMS && c.way != GradWay::TILES_256) continue;      // more than a launch holds (splits are for few tiles)
         // None, and as many as leave one, two or four workgroups to a compute unit, or half of them.
         for (uint64_t fill = 0; fill <= 4; ++fill) {
             const uint64_t splits = fill == 0 ? 1 : tiles ? std::min(((uint64_t)n_cu << (fill - 1)) / 2 / tiles, steps / 2) : 0;

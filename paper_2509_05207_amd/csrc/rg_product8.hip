@@ -1455,9 +1455,9 @@ extern "C" rg_status rg_rows8_product_backward(const void *dy, uint64_t dy_strid
     RG_TRY(compute_units(&n_cu));
     const GradPlan p = grad_plan(n_rows, n_outs, n_cols, n_cu, dx, dweight, dbias);
     RG_TRY(check_workspace(workspace, workspace_bytes, p.bytes));
-    RG_TRY(check_grid(p.dx.tiles * (uint64_t)p.dx.splits, 512));
-    RG_TRY(check_grid(p.dw.tiles * (uint64_t)p.dw.splits, 512));
-    RG_TRY(check_grid((n_outs + 63) / 64, 256));
+    if (p.dx.way == GradWay::TILES_256) RG_TRY(check_grid(p.dx.tiles * (uint64_t)p.dx.splits, 512));         // of the others grad_cut sees to it
+    if (p.dw.way == GradWay::TILES_256) RG_TRY(check_grid(p.dw.tiles * (uint64_t)p.dw.splits, 512));
+    if (dbias && !dweight) RG_TRY(check_grid((n_outs + 63) / 64, 256));
     const hipStream_t st = as_stream(stream);
     uint8_t *scratch = static_cast<uint8_t *>(workspace);
     float *sums = reinterpret_cast<float *>(scratch), *scales = reinterpret_cast<float *>(scratch + p.scales_at), *bias = reinterpret_cast<float *>(scratch + p.bias_at);

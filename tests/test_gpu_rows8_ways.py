@@ -63,3 +63,19 @@ def test_gradients(rg, n, m, d, dtype, weight):
     check("dbias", db, g.sum(0), (64 + n / 256) * U * g.abs().sum(0))
     out.fill_(3.0)
     assert bool((buf == 3).all())
+
+
+def test_a_thousand_million_outputs(rg):
+    """As many as there may be, in tiles of which a launch holds as many; small whole numbers, of which nothing is rounded."""
+    m = 2**30
+    held = torch.zeros((3, 16), dtype=torch.uint8, device="cuda")
+    held[:, 0] = torch.tensor([1, 2, 255], dtype=torch.uint8)
+    held.view(torch.float32)[:, -1] = 1.0
+    dy = torch.empty((3, m), dtype=torch.bfloat16, device="cuda")
+    for n in range(3):
+        for first in range(0, m, 2**28):
+            dy[n, first: first + 2**28] = (torch.arange(first, first + 2**28, device="cuda") * 7 + n) % (5 + n)
+    _, dw, db = rg.rg_rows8_product_backward(dy, held, None, 1, want_dx=False)
+    for first in range(0, m, 2**28):
+        a, b, c = dy[:, first: first + 2**28]
+        assert torch.equal(dw[first: first + 2**28, 0], a + 2 * b - c) and torch.equal(db[first: first + 2**28], a + b + c)

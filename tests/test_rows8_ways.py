@@ -38,3 +38,11 @@ def test_gradients(tmp_path):
     for (n, m, d), (way, _, splits, _, _, shares, _, _) in zip(GRADIENTS, ask(tmp_path, CUTS, [(n, d, m, 3, 256, 1) for n, m, d in GRADIENTS])):
         seen.add((way, next(k for k in (32, 64, 128, 256) if m <= k), shares > 1) if way == 4 else (way, splits > 1))
     assert seen >= tiles | {(4, k, s) for k in (32, 64, 128, 256) for s in (False, True)}, seen
+
+
+def test_launches_hold_the_tiles_of_the_largest_gradients(tmp_path):
+    """Up to 2^37 elements, as of the product: a way that a launch does not hold is not chosen."""
+    sizes = [1, 3, 64, 300, 2**20, 2**24, 2**28, 2**30]
+    cases = [(i, j, k, 3, 256, along) for i in sizes for j in (1, 16, 64, 128, 300, 4096, 131_072) for k in (0, 1, 3, 300, 100_000, 2**30) for along in (0, 1) if i * j <= 2**37]
+    for (i, j, k, _, _, _), (way, tiles, splits, *_) in zip(cases, ask(tmp_path, CUTS, cases)):
+        assert way == 4 or tiles * splits * (512 if way == 3 else 256) < 2**32, (i, j, k)
