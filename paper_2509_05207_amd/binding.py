@@ -743,7 +743,7 @@ def _place(x, rows, out):
 
 def rg_quantize_rows(x, rows=None, out=None, stream=None):
     """The rows of `x` (device or pinned matrix; rows may be padded), or those at the positions `rows` (int64; -1: a row of zeros), as
-    held rows: a uint8 matrix of rg_rows8_bytes(x.shape[1]) a row.  out: where they go."""
+    held rows: a uint8 matrix of rg_rows8_bytes(x.shape[1]) a row.  out: where they go.  Pinned memory has to stay until the call's work on the device is done."""
     device = _place(x, rows, out)
     xp, xs = _rows("x", x, x.device if not x.is_cuda else None)
     n, d = x.shape
@@ -764,7 +764,8 @@ def rg_quantize_rows(x, rows=None, out=None, stream=None):
 
 
 def rg_dequantize_rows(held, cols, dtype=torch.float32, rows=None, out=None, stream=None):
-    """What held rows of `cols` elements stand for, all of them or those at the positions `rows` (int64; -1: a row of zeros).  out: where it goes."""
+    """What held rows of `cols` elements stand for, all of them or those at the positions `rows` (int64; -1: a row of zeros).  out: where it goes.  Pinned memory
+    has to stay until the call's work on the device is done."""
     device = _place(held, rows, out)
     hp, hs, n = _held("held", held, held.device if not held.is_cuda else None, cols)
     n_out = n if rows is None else rows.shape[0]

@@ -122,7 +122,7 @@ __device__ const i32x4 ZERO_CHUNK = {0, 0, 0, 0};
 
 // Few results: 16 rows by 16 outputs to a workgroup, whose waves share out the steps of 64 codes, straight from memory into registers, and add their sums up in LDS.  Bound by w's way
 // from memory, and where that is short by a launch and what follows one another in it (bf16, 4 and 16 waves, us: 1 x 4,096 to 4,096 6.3 and 5.0, 100 x 512 to 256 3.6 and 4.9).  Up to 64 rows a
-// workgroup, w read once for all of them: 12.9 for 64 x 4,096 to 4,096, 15.8 so, but 14.6 for 11.7 with 8,192 to 1,000, and later for 300 rows than tiles.
+// workgroup, w read once for all of them: 15.8 for 64 x 4,096 to 4,096, where tiles of split codes, which the rule takes, and their join have 12.6; 11.7 for 14.6 with 8,192 to 1,000, and later for 300 rows than tiles.
 template <typename T, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64) product_few_kernel(ProductArgs a)
 {
@@ -175,8 +175,8 @@ __global__ void __launch_bounds__(WAVES * 64) product_few_kernel(ProductArgs a)
 // arrive, written into LDS by the loads themselves.  A row of a step is eight chunks of 16 bytes, stored in an order that depends on the row, so that the 16 lanes that
 // LDS serves at a time (16 rows, one chunk of each) fall on all banks once.
 // Workgroup g runs on XCD g mod 8, and every XCD has an L2 of its own: tiles that share operands, which follow one another, go to one XCD.
-// Large products are bound by the matrix operations and by what waves read of LDS: 8,192 x 8,192 to 8,192 in bf16 499 us by tiles of 256 (2,200 TOPS; the matrix units are busy for 56 %), 545 behind other
-// work.  Where that is a fraction of a tile's start and end, by these: 10,007 x 1,001 to 517 in fp32 18.5 by tiles of 128.  Workgroups that stay and take one tile after the other have no registers left for it (560).
+// Large products are bound by the matrix operations and by what waves read of LDS: 8,192 x 8,192 to 8,192 in bf16 520 us by tiles of 256 (2,110 TOPS; the matrix units are busy for 56 %), 484 on a cool card, 546 behind other
+// work.  Where that is a fraction of a tile's start and end, by these: 10,007 x 1,001 to 517 in fp32 19.4 by tiles of 128, a fifth of which are a fifth column for the last 5 outputs.  Workgroups that stay and take one tile after the other have no registers left for it (560).
 __device__ __forceinline__ uint32_t tile_of_workgroup()
 {
     constexpr uint32_t XCDS = 8;
@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) product_tiles_kernel(Product
     else finish_tile<T, Tile>(a, place, acc, scales);
 }
 
-// The splits' sums, added up, and what they stand for: four results of a row to a thread.  Bound by the sums' way through the caches; with it 300 x 8,192 to 1,000 takes 16.8 us in three splits.
+// The splits' sums, added up, and what they stand for: four results of a row to a thread.  Bound by the sums' way through the caches; 4.0 us of the 17.0 that 300 x 8,192 to 1,000 takes in three splits.
 template <typename T>
 __global__ void __launch_bounds__(256) product_join_kernel(ProductArgs a, int32_t splits)
 {
@@ -457,10 +457,10 @@ __global__ void __launch_bounds__(256) product_join_kernel(ProductArgs a, int32_
     store_four(row_at<T>(a.y, a.y_stride, n) + m, f32x4{v[0], v[1], v[2], v[3]}, count);
 }
 
-// Many rows of few codes: what bounds them is the rows' and the results' way from and to HBM, and tiles spend most of their time on it at their start and end.  Here w lies in LDS, once
+// Many rows of few codes: what bounds them is the rows' and the results' way from and to HBM and, beside it, w's way out of LDS, and tiles spend most of their time at their start and end.  Here w lies in LDS, once
 // for all rows that a workgroup does (where it has more than that holds, each workgroup has a share of the outputs), and a wave by itself takes 16 rows at a time into registers, the next
 // ones under way meanwhile: no barrier behind the first.  w lies as the matrix operations take it: of a block of 16 outputs chunk by chunk, 16 rows side by side.  150,000 x 512 to 256 in bf16: 45 us,
-// 3.4 TB/s; the matrix units are busy for 24 % of it.
+// 3.4 TB/s, where HBM would take 30 and the reads of LDS, all of w for 16 rows, 23; the matrix units are busy for 24 % of it.
 struct ThinArgs {
     ProductArgs p;
     int32_t outs;                    // of a workgroup, a multiple of 32
@@ -682,10 +682,10 @@ __device__ __forceinline__ bf16x8 codes_as_bf16(const i32x2 &c)
 // Tiles of TI x TJ by WI x WJ waves of BI x BJ blocks of 16 x 16, in steps of 32 along k.  ALONG: dy's rows run along k (dx); otherwise along i (dweight).  A step's elements of dy are read into registers
 // two steps ahead, and one step ahead are multiplied with their scales, parted, and written into LDS; the codes go there as they are.  Of operands that lie along the wrong axis LDS itself makes columns (reads
 // that transpose blocks of 16 x 8 bytes or 16 x 4 numbers).  What the lanes read at a time falls on all banks once: the order of the 16-byte chunks of a row, or of the 32-byte pieces of
-// one of dy's, depends on the row.
-// Bound by the vector units: matrix operations keep them for 41 to 56 % of the time, and what parts dy hardly overlaps with them.  In tiles of 256:
-// dweight and the sums of 199,000 x 602 to 256 in fp32, three parts, 199 us behind other work (920 TFLOP/s of bf16) and 17 for the join; 150,000 x 512 to 256 in bf16 94 and 17; 8,192 x 4,096 to 4,096
-// 450 each way (1,220).
+// one of dy's, depends on the row.  What they write of the codes, 16 bytes at steps of 32, has half of the banks at a time (0.3 to 0.4 cycles of conflicts to an instruction of LDS).
+// Bound by the vector units: matrix operations keep them for 40 to 64 % of the time, and what parts dy hardly overlaps with them.  In tiles of 256 (least of 10 passes under the profiler, us):
+// dweight and the sums of 199,000 x 602 to 256 in fp32 224 (820 TFLOP/s of bf16, a fifth of them for columns behind the last) and 17 for the join; 150,000 x 512 to 256 in bf16 117 and 17, dx 153; 8,192 x 4,096 to 4,096
+// 713 and 631 (1,160 and 1,310).
 template <typename T, bool ALONG_, bool SUMS_, int WI_, int WJ_, int BI_, int BJ_>
 struct GradTile {
     static constexpr int WI = WI_, WJ = WJ_, BI = BI_, BJ = BJ_;
@@ -979,8 +979,8 @@ __global__ void __launch_bounds__(Tile::THREADS, 2) grad_kernel(GradArgs a)
 
 // dx of many rows and few outputs, which the tiles do at the pace of their starts and ends: w's codes lie in LDS, once for all rows that a workgroup does (where there is more than that holds, each
 // has a share of the columns), and a wave by itself takes 16 rows of dy at a time, parted in registers (the next ones' elements on their way beside them spill, and so do 32 rows).  The codes lie by blocks of 16 columns, row after row: what the
-// lanes read at a time is contiguous.  Bound as the tiles are: 150,000 x 256 to 512 in bf16 97 us (810 TFLOP/s of bf16), the matrix units
-// busy for 40 %.
+// lanes read at a time is contiguous.  Bound as the tiles are, and by the codes, which every wave makes bf16 numbers of
+// anew for 16 rows: 199,000 x 256 to 602 in bf16 192 us (960 TFLOP/s of bf16), by tiles 268; 150,000 x 128 to 256 38 and 49.
 struct ThinGradArgs {
     GradArgs g;
     int32_t cols;                    // of a workgroup, a multiple of 32
@@ -1157,7 +1157,8 @@ __global__ void __launch_bounds__(256) grad_join_kernel(Join first, Join second,
     }
 }
 
-// Sums of dy's columns over a part of its rows, for calls that want no dweight, whose tiles make them on the way: 64 columns to a workgroup, four rows at a time.  Bound by HBM.
+// Sums of dy's columns over a part of its rows, for calls that want no dweight, whose tiles make them on the way: 64 columns to a workgroup, four rows at a time.  Bound by the latency of
+// loads of one element a lane: 150,000 x 256 in bf16 44 us (1.7 TB/s), 199,000 x 256 in fp32 59 (3.5).
 template <typename T>
 __global__ void __launch_bounds__(256) bias_sums_kernel(const uint8_t *dy, uint64_t dy_stride, int32_t n_rows, int32_t n_outs, int32_t each, float *partial)
 {

@@ -7,8 +7,8 @@
 //
 // Both directions are bound by HBM: a row is read once into registers and written once.  It belongs to 8 to 64 lanes of a wave, or to a workgroup, whatever holds
 // it in 40 elements a lane or fewer; rows beyond that are read twice.
-// 199,000 x 602 in fp32: written 112 us (5.4 TB/s), read back 140 (4.3 TB/s; results past the caches), where a copy reaches 5.1; 200,000 x 256 in bf16 by positions out of a million rows
-// 48 and 25; 199,000 x 602 to bf16 out of 233,000 rows 79 (4.6 TB/s).
+// 199,000 x 602 in fp32: written 111 us (5.4 TB/s), read back 137 (4.4 TB/s; results past the caches), where a copy reaches 5.1; 200,000 x 256 in bf16 by positions out of a million rows
+// 48 and 25; 199,000 x 602 to bf16 out of 233,000 rows 78 (4.6 TB/s).
 #include "rg_internal.h"
 #include "rg_elements.h"
 #include "rg_launch.h"
@@ -86,7 +86,7 @@ struct Scale {
     }
     __device__ __forceinline__ float stored() const { return finite ? s : __builtin_nanf(""); }
     // x plus ROUNDER where x / s is the whole number that the rounded quotient says, and what that leaves, x - q s.  q is off from the exact quotient's nearest whole number by one at
-    // most, and the rest, which is exact in 32 bits (a multiple of the coarser of both units, and not much more than s / 2), tells.
+    // most, and the rest, which is exact in 32 bits (x itself where q is zero; else a multiple of half of s's unit, and not much more than s / 2), tells.
     __device__ __forceinline__ float near(float x, float &rest) const
     {
         const float q = fmaf(x, inverse, ROUNDER);
