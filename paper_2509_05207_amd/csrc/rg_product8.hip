@@ -108,12 +108,15 @@ template <typename T> __device__ __forceinline__ float product_value_apart(int32
     const int power = __builtin_amdgcn_frexp_expf(sx) + __builtin_amdgcn_frexp_expf(sw);
     if constexpr (sizeof(T) == 2) {
         const int of_p = min(max(power, -100), 100);
-        return in_32_bits<T>(ldexpf(hi, power - of_p), ldexpf(p, of_p), bias);
+        return in_32_bits<T>(ldexpf(hi, min(power - of_p, 90)), ldexpf(p, of_p), bias);          // (beyond 2^90 it passes the range anyway, but is a number still)
     }
     const float lo = (float)(sum - (int32_t)hi), t = rounded(hi, p);
     const int down = fabsf(ldexpf(t, power)) >= 0x1p120f || fabsf(bias) >= 0x1p120f ? 8 : 0;
     const float at = ldexpf(t, power - down), b = ldexpf(bias, -down), v = with_bias(at, ldexpf(fmaf(hi, fmaf(mx, mw, -p), fmaf(lo, p, fmaf(hi, p, -t))), power - down), b);
-    return fabsf(at + b) < __builtin_inff() ? ldexpf(v, down) : at + b;              // (an infinity has no rest)
+    // (An infinity has no rest, and one of the bias stands against numbers of any size.)
+    const uint32_t number = (uint32_t)(fabsf(t) < __builtin_inff()) & (uint32_t)!(fabsf(bias) < __builtin_inff());
+    const float beyond = number ? bias : at + b;
+    return fabsf(at + b) < __builtin_inff() ? ldexpf(v, down) : beyond;
 }
 // A row of zeros has the least scale that there is.  Of a sum of zero the first way makes the bias whatever the scales, so rows of that scale go it too, where their codes, or all their sums, are zero.
 __device__ __forceinline__ bool least_scale(float scale) { return scale == 0x1p-126f; }

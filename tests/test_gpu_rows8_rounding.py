@@ -151,3 +151,21 @@ def test_rows_of_the_least_scale_that_are_not_zero(rg, n, m, d):
                 product = product_sum(a, b) * (s.double()[:, None] * t.double())
                 within(y, product, none.double())
                 assert bool(((y if rows else y.t())[at[1:]] != 0).any()) == bool((product.abs() if rows else product.t().abs())[at[1:]].max() > 2.0 ** -149)
+
+
+@pytest.mark.parametrize("n,m,d", [(40, 30, 50), (300, 270, 602), (20_011, 130, 300), (20_011, 517, 1300)])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_an_infinity_of_the_bias_stands_against_numbers_of_any_size(rg, n, m, d, dtype):
+    """Products of scales and codes that pass 32 bits are numbers still; a scale that is none makes a NaN."""
+    _, qx, sx = random_held(n, d, 1)
+    _, qw, sw = random_held(m, d, 2)
+    sx[:], sw[:] = 2.0 ** 120, 2.0 ** 121
+    b = torch.zeros(m, device="cuda")
+    b[0::3], b[1::3] = float("inf"), float("-inf")
+    for scale in (2.0 ** 120, 2.0 ** 90, float("nan")):
+        sx[n // 2] = scale
+        y = rg.rg_rows8_product(packed(qx, sx), packed(qw, sw), d, bias=b, dtype=dtype)
+        rows = torch.arange(n, device="cuda") != n // 2 if scale != scale else torch.ones(n, dtype=torch.bool, device="cuda")
+        assert bool(torch.isnan(y[~rows]).all())
+        assert bool((y[rows][:, 0::3] == float("inf")).all()) and bool((y[rows][:, 1::3] == float("-inf")).all())
+        assert bool((y[rows][:, 2::3] == (torch.sign(product_sum(qx, qw)) * float("inf")).nan_to_num(nan=0.0, posinf=float("inf"), neginf=float("-inf"))[rows][:, 2::3]).all())
